@@ -522,6 +522,117 @@ int q8_pool_f32(const float *x_dev, int N, int H, int W, int C, int mode, int R,
                 int stride, int pad, int Ho, int Wo, float *y_dev, int out_c_stride,
                 int out_c_off, void *stream);
 
+/* ---- a decoder's attention block in 8 and 4 bits ---------------------------------------
+ * A linear layer whose activations are quantised row by row as they come (a row is a token),
+ * a paged cache of keys and values in 4 bits, and attention over it.  Real values are of one
+ * of three types; strides are in elements, rows are dense inside.  A value that is no number
+ * counts as 0 where it is quantised, an infinite one as the largest code, and neither enters
+ * a maximum.                                                                              */
+enum { Q8_F32 = 0, Q8_F16 = 1, Q8_BF16 = 2 };
+
+/* Eq. Q (p = 7) with a factor for each row, taken from the row itself:
+ *   q_x[m] = max_k |x[m,k]| * fl(1/127) (1 if that is 0),  z[m,k] = Eq. Q(x[m,k], q_x[m]),
+ * the factor by one fp32 multiplication (at most an ulp from q8_qfactor's quotient).
+ * x_dev: M rows of K values, x_stride apart; z_dev 16-byte aligned, z_stride a multiple of 16
+ * and at least K (the bytes between K and the next multiple of 16 may be written).  M = 0 is
+ * no work.  M < 2^31 (Q8_EUNSUPPORTED).                                                    */
+int q8_quantize_rows(const void *x_dev, int type, size_t M, int K, size_t x_stride,
+                     int8_t *z_dev, size_t z_stride, float *q_x_dev, void *stream);
+
+/* Weights of the linear layer, int8 [N][K] dense (q8_quantize_weights_per_channel makes them
+ * and their factors), into the layout private to the library: packed_dev 16-byte aligned, of
+ * q8_linear_packed_bytes(N, K) bytes (0: unsupported).  1 <= K <= 131071.                   */
+size_t q8_linear_packed_bytes(int N, int K);
+int q8_linear_pack(const int8_t *z_w_dev, int N, int K, void *packed_dev, void *stream);
+
+/* The product on codes, with a factor for each row of either side (Eq. x, then Eq. D):
+ *   y[m,n] = fp32(sum_k z_x[m,k] z_w[n,k]) * (q_x[m] * q_w[n]) + bias[n]
+ * in that order of fp32 operations, rounded once to `type`; the sum is exact.
+ *   z_x_dev   int8, M rows of z_stride bytes (a multiple of 16, at least K; the bytes between K
+ *             and the next multiple of 16 are read and do not count); 16-byte aligned
+ *   q_x_dev, q_w_dev   fp32 [M], [N];   bias_dev   fp32 [N] or NULL
+ *   y_dev     M rows of N values, y_stride apart.                                          */
+int q8_linear_int8(const int8_t *z_x_dev, size_t z_stride, const float *q_x_dev, size_t M, int N,
+                   int K, const void *packed_dev, const float *q_w_dev, const float *bias_dev,
+                   void *y_dev, int type, size_t y_stride, void *stream);
+
+/* q8_quantize_rows and q8_linear_int8 as one call: bit for bit their result.  `workspace`:
+ * q8_linear_workspace_bytes(M, N, K) bytes of device memory, 256-byte aligned, for the codes
+ * and factors in between; calls that share one must not overlap in time.                   */
+size_t q8_linear_workspace_bytes(size_t M, int N, int K);
+int q8_linear(const void *x_dev, int x_type, size_t x_stride, size_t M, int N, int K,
+              const void *packed_dev, const float *q_w_dev, const float *bias_dev, void *y_dev,
+              int y_type, size_t y_stride, void *workspace, size_t workspace_bytes,
+              void *stream);
+
+/* Block tables of a step, on the GPU: request b holds lengths[b] tokens in the cache and gets
+ * added[b] more (negative counts as 0).  A page holds `page` tokens (a power of two, 16 ..
+ * 2^20); row b of the table (table_stride apart, `width` entries) names the request's pages in
+ * the order of its tokens.  Pages that the new tokens need are taken from free_pages[0 ..
+ * n_free) in request order and written behind the request's last one; nothing else of the table
+ * changes.  A request does not fit if its pages would pass `width`, its tokens would pass
+ * n_slots, or the pages that it and those before it need pass n_free: it then gets none.
+ *   slots[i], positions[i]   i < n_slots: for new token i, all requests' one after the other,
+ *             page * page size + place in the page, and the place in the request; -1 for a
+ *             token of a request that does not fit, and behind the last token
+ *   starts    [n_requests + 1]: the first new token of each request, and their number
+ *   grown     [n_requests]: lengths + added, lengths where the request does not fit
+ *   counts    [3]: pages taken, new tokens, requests that do not fit
+ * lengths, added and free_pages are only read: the caller moves on to `grown` and drops
+ * counts[0] pages from its list.  The sum of lengths and added of a request, and of all
+ * added, stays below 2^31.                                                               */
+int q8_page_tables(const int32_t *lengths_dev, const int32_t *added_dev, int n_requests, int page,
+                   const int32_t *free_pages_dev, int n_free, int32_t *table_dev, int width,
+                   size_t table_stride, int64_t *slots_dev, int32_t *positions_dev, int n_slots,
+                   int32_t *starts_dev, int32_t *grown_dev, int32_t *counts_dev, void *stream);
+
+/* The cache: uint8 [n_pages][n_heads][page / 16][18 D], 64-byte aligned, D a multiple of 32 up
+ * to 256.  32 consecutive channels of a token's head are held by Eq. Q with p = 3 (codes -8 ..
+ * 7) at the factor max|r| * fl(1/7) rounded to binary16 (at most 8188, 1 if that is 0).  With G =
+ * D / 32, sixteen consecutive tokens of a head are, one after the other,
+ *   256 G bytes   key codes      [token][j < 4][g < G][4 bytes]: byte b holds channel 32 g + 8 j + 2 b
+ *                                in its low half and the next one in its high half
+ *   256 G         value codes    [g < G][r < 16][token]: channels 32 g + r and 32 g + 16 + r
+ *   32 G          key factors    binary16 [token][g < G]
+ *   32 G          value factors  binary16 [g < G][token], each four tokens in the order 0, 2, 1, 3
+ * where a half byte holds its code plus 8.  q8_kv4_cache_bytes: its size (0: unsupported).
+ *
+ * q8_kv4_write puts T tokens' keys and values ([T][n_heads][D], strides between tokens and
+ * between heads) into their slots; q8_kv4_read writes what the slots hold (Eq. D, rounded to
+ * `type`).  A slot outside the cache is not written, and reads as zeros.  Slots of one write
+ * are distinct.                                                                           */
+size_t q8_kv4_cache_bytes(size_t n_pages, int n_heads, int page, int D);
+int q8_kv4_write(const void *k_dev, const void *v_dev, int type, size_t T, int n_heads, int D,
+                 size_t k_stride, size_t k_head_stride, size_t v_stride, size_t v_head_stride,
+                 const int64_t *slots_dev, void *cache_dev, size_t n_pages, int page,
+                 void *stream);
+int q8_kv4_read(const void *cache_dev, size_t n_pages, int page, const int64_t *slots_dev,
+                size_t T, int n_heads, int D, void *k_dev, void *v_dev, int type,
+                size_t k_stride, size_t k_head_stride, size_t v_stride, size_t v_head_stride,
+                void *stream);
+
+/* Attention over the cache: row t of q ([T][n_heads * ratio][D], Q8_F16 or Q8_BF16; query heads
+ * h * ratio .. of key head h) is a token of the request b with starts[b] <= t < starts[b + 1]
+ * (starts NULL: request t), which has lengths[b] tokens in the cache, the last of them the
+ * rows' own (written before).  A row at position i of its request sees the keys j <= i, and with
+ * window > 0 only those with j > i - window:
+ *   out[t] = sum_j softmax_j(scale q[t] . k_j) v_j,   zeros where it sees none.
+ * Lengths above width * page count as that; tokens on a page outside the cache are not seen;
+ * rows outside starts[0] .. starts[n_requests] are not written.  Sums and the softmax are fp32,
+ * products binary16 x binary16.
+ *   workspace   NULL, or device memory (16-byte aligned) with which the keys of few rows are
+ *               split over workgroups: at most q8_kv4_attend_workspace_bytes are used, `longest`
+ *               being the largest length expected (a hint; 0: nothing is split).  Calls that
+ *               share one must not overlap in time.                                        */
+size_t q8_kv4_attend_workspace_bytes(size_t T, int n_requests, int n_heads, int ratio, int D,
+                                     size_t longest);
+int q8_kv4_attend(const void *q_dev, int type, size_t T, int n_heads, int ratio, int D,
+                  size_t q_stride, size_t q_head_stride, const void *cache_dev, size_t n_pages,
+                  int page, const int32_t *table_dev, int width, size_t table_stride,
+                  const int32_t *lengths_dev, const int32_t *starts_dev, int n_requests,
+                  float scale, int window, void *out_dev, size_t o_stride,
+                  size_t o_head_stride, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Measurement only, not part of the method (no parity claim rests on it): `blocks` workgroups of four wavefronts each issue 4 * iters
  * register-resident v_mfma_i32_32x32x32_i8 (65536 int8 ops each), no memory traffic:
  * ops = blocks * 4 * 4 * iters * 65536.  The caller times the launch; the result is the

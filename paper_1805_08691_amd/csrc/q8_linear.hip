@@ -1,0 +1,231 @@
+// The 8-bit linear layer on rows of real values, one factor per row of activations (a token, known only when the
+// values are) and one per row of weights (an output channel):
+//   q_x[m] = max_k |x[m,k]| * fl(1/127),  z_x = Eq. Q(x[m,:], q_x[m])
+//   y[m,n] = fp32(sum_k z_x[m,k] z_w[n,k]) * (q_x[m] q_w[n]) + bias[n]          (Eq. x, Eq. D)
+// The sum is exact in int32 (128 * 128 * K < 2^31 for K <= 131071); the tail is three fp32 operations and the
+// rounding to y's type.
+#include "q8_common.h"
+#include "q8_conv_common.h"
+#include "q8_quant.h"
+#include "q8_value.h"
+#pragma clang fp contract(off)
+
+namespace {
+
+using namespace q8;
+
+constexpr int kMaxK = 131071;
+constexpr int kPackK = 64;                    // reduction bytes of a packed block
+constexpr int kPackN = 16;                    // and its rows
+
+inline size_t round_up(size_t a, size_t b) { return (a + b - 1) / b * b; }
+
+// ---------------------------------------------------------------- rows to codes ----------
+// One block per row: the maximum, then the codes.
+template <typename V, bool ALIGNED>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const V* __restrict__ x, int K, size_t x_stride,
+                                                            int8_t* __restrict__ z, size_t z_stride,
+                                                            float* __restrict__ q_x) {
+  const size_t row = blockIdx.x;
+  const V* __restrict__ xr = x + row * x_stride;
+  int8_t* __restrict__ zr = z + row * z_stride;
+  const int tid = threadIdx.x, body = K & ~7;
+  float m = 0.0f;
+  for (int k = tid * 8; k < body; k += 256 * 8) {
+    float v[8];
+    load_values<8, ALIGNED>(xr + k, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = fmaxf(m, finite_abs(v[e]));
+  }
+  if (tid < K - body) m = fmaxf(m, finite_abs((float)xr[body + tid]));
+  for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  __shared__ float wave_max[4];
+  if ((tid & 63) == 0) wave_max[tid >> 6] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
+  float q = __fmul_rn(m, 1.0f / 127.0f);
+  q = q > 0.0f ? q : 1.0f;
+  if (tid == 0) q_x[row] = q;
+  auto code = [&](float v) { return v == v ? quant1(v, q, -128.0f, 127.0f) : 0; };
+  for (int k = tid * 8; k < body; k += 256 * 8) {
+    float v[8];
+    load_values<8, ALIGNED>(xr + k, v);
+    uint2 w;
+    w.x = pack4(code(v[0]), code(v[1]), code(v[2]), code(v[3]));
+    w.y = pack4(code(v[4]), code(v[5]), code(v[6]), code(v[7]));
+    *reinterpret_cast<uint2*>(zr + k) = w;
+  }
+  if (tid < K - body) zr[body + tid] = (int8_t)code((float)xr[body + tid]);
+}
+
+template <typename V>
+int launch_quantize_rows(const V* x, size_t M, int K, size_t x_stride, int8_t* z, size_t z_stride, float* q_x,
+                         hipStream_t stream) {
+  const bool aligned = q8_aligned(x, 16) && x_stride * sizeof(V) % 16 == 0;
+  if (aligned)
+    quantize_rows_kernel<V, true><<<(unsigned)M, 256, 0, stream>>>(x, K, x_stride, z, z_stride, q_x);
+  else
+    quantize_rows_kernel<V, false><<<(unsigned)M, 256, 0, stream>>>(x, K, x_stride, z, z_stride, q_x);
+  return q8_launch_status();
+}
+
+// ---------------------------------------------------------------- weights ----------------
+// Packed: blocks of 16 rows x 64 reduction bytes, 1 KB each, [N / 16][K / 64]; inside a block lane l of a wavefront
+// holds 16 bytes: row l % 16, bytes 16 (l / 16) .. + 15, the operand of one 16x16x64 product.  Zeros beyond N and K.
+__global__ __launch_bounds__(256) void linear_pack_kernel(const int8_t* __restrict__ w, int N, int K, int ksteps,
+                                                          size_t chunks, int8_t* __restrict__ packed) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= chunks) return;
+  const int lane = (int)(i % 64);
+  const size_t block = i / 64;
+  const size_t n = block / ksteps * kPackN + lane % 16;
+  const int k = (int)(block % ksteps) * kPackK + lane / 16 * 16;
+  v4i v = {0, 0, 0, 0};
+  int8_t b[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) b[e] = n < (size_t)N && k + e < K ? w[n * K + k + e] : (int8_t)0;
+  __builtin_memcpy(&v, b, 16);
+  reinterpret_cast<v4i*>(packed)[i] = v;
+}
+
+// ---------------------------------------------------------------- product ----------------
+struct LinearParams {
+  const int8_t* __restrict__ z;
+  const float* __restrict__ q_x;
+  const int8_t* __restrict__ w;
+  const float* __restrict__ q_w;
+  const float* __restrict__ bias;
+  size_t z_stride, y_stride;
+  int M, N, K, ksteps;
+};
+
+// Four consecutive outputs of row m, channels n ..: the tail, and one store where the row allows it.
+template <typename Y, bool VEC>
+__device__ __forceinline__ void finish4(const LinearParams& p, Y* __restrict__ y, int m, int n, v4i acc) {
+  if (m >= p.M || n >= p.N) return;
+  const float q = p.q_x[m];
+  float v[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int c = min(n + e, p.N - 1);
+    v[e] = (float)acc[e] * (q * p.q_w[c]);
+    if (p.bias) v[e] = v[e] + p.bias[c];
+  }
+  Y* to = y + (size_t)m * p.y_stride + n;
+  if (VEC && n + 4 <= p.N) {
+    store_values<4, true>(to, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (n + e < p.N) to[e] = (Y)v[e];
+  }
+}
+
+// One wavefront per 16 channels x 16 rows, operands straight from memory.
+template <typename Y, bool VEC>
+__global__ __launch_bounds__(256) void linear_kernel(const LinearParams p, Y* __restrict__ y) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int nb = blockIdx.x * 4 + wave;
+  if (nb * kPackN >= p.N) return;
+  const int m0 = blockIdx.y * 16;
+  const int row = min(m0 + (lane & 15), p.M - 1), chunk = (lane >> 4) * 16;
+  const int8_t* __restrict__ z = p.z + (size_t)row * p.z_stride + chunk;
+  const v4i* __restrict__ w = reinterpret_cast<const v4i*>(p.w) + (size_t)nb * p.ksteps * 64 + lane;
+  v4i acc = {0, 0, 0, 0};
+  for (int s = 0; s < p.ksteps; ++s) {
+    v4i b = {0, 0, 0, 0};
+    if (s * kPackK + chunk < p.K) b = *reinterpret_cast<const v4i*>(z + s * kPackK);
+    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[(size_t)s * 64], b, acc, 0, 0, 0);
+  }
+  finish4<Y, VEC>(p, y, m0 + (lane & 15), nb * kPackN + 4 * (lane >> 4), acc);
+}
+
+template <typename Y>
+int launch_linear(const LinearParams& p, Y* y, hipStream_t stream) {
+  const dim3 grid((unsigned)((p.N + 63) / 64), (unsigned)((p.M + 15) / 16));
+  const bool vec = q8_aligned(y, 4 * sizeof(Y)) && p.y_stride % 4 == 0;
+  if (vec)
+    linear_kernel<Y, true><<<grid, 256, 0, stream>>>(p, y);
+  else
+    linear_kernel<Y, false><<<grid, 256, 0, stream>>>(p, y);
+  return q8_launch_status();
+}
+
+// Codes [M][round_up(K, 16)], then the rows' factors.
+size_t codes_bytes(size_t M, int K) { return round_up(M * round_up(K, 16), 256); }
+
+bool sizes_ok(size_t M, int N, int K) { return N >= 0 && K >= 1 && K <= kMaxK && M <= 0x7fffffffu; }
+
+}  // namespace
+
+extern "C" int q8_quantize_rows(const void* x_dev, int type, size_t M, int K, size_t x_stride, int8_t* z_dev,
+                                size_t z_stride, float* q_x_dev, void* stream) {
+  Q8_REQUIRE(type_ok(type) && K >= 1, Q8_EINVAL);
+  if (M == 0) return Q8_OK;
+  Q8_REQUIRE(M <= 0x7fffffffu, Q8_EUNSUPPORTED);
+  Q8_REQUIRE(x_dev && z_dev && q_x_dev && x_stride >= (size_t)K && z_stride >= (size_t)K, Q8_EINVAL);
+  Q8_REQUIRE(q8_aligned(x_dev, type_bytes(type)) && q8_aligned(q_x_dev, 4), Q8_EALIGN);
+  Q8_REQUIRE(q8_aligned(z_dev, 16) && z_stride % 16 == 0, Q8_EALIGN);
+  return with_type(type, [&](auto v) {
+    return launch_quantize_rows(static_cast<const decltype(v)*>(x_dev), M, K, x_stride, z_dev, z_stride, q_x_dev,
+                                (hipStream_t)stream);
+  });
+}
+
+extern "C" size_t q8_linear_packed_bytes(int N, int K) {
+  if (N < 0 || K < 1 || K > kMaxK) return 0;
+  return round_up(N, kPackN) * round_up(K, kPackK);
+}
+
+extern "C" int q8_linear_pack(const int8_t* z_w_dev, int N, int K, void* packed_dev, void* stream) {
+  Q8_REQUIRE(N >= 0 && K >= 1, Q8_EINVAL);
+  Q8_REQUIRE(K <= kMaxK, Q8_EUNSUPPORTED);
+  if (N == 0) return Q8_OK;
+  Q8_REQUIRE(z_w_dev && packed_dev, Q8_EINVAL);
+  Q8_REQUIRE(q8_aligned(packed_dev, 16), Q8_EALIGN);
+  const size_t chunks = q8_linear_packed_bytes(N, K) / 16, blocks = (chunks + 255) / 256;
+  Q8_REQUIRE(blocks <= 0x7fffffffu, Q8_EUNSUPPORTED);
+  linear_pack_kernel<<<(unsigned)blocks, 256, 0, (hipStream_t)stream>>>(
+      z_w_dev, N, K, (int)(round_up(K, kPackK) / kPackK), chunks, static_cast<int8_t*>(packed_dev));
+  return q8_launch_status();
+}
+
+extern "C" int q8_linear_int8(const int8_t* z_x_dev, size_t z_stride, const float* q_x_dev, size_t M, int N, int K,
+                              const void* packed_dev, const float* q_w_dev, const float* bias_dev, void* y_dev,
+                              int type, size_t y_stride, void* stream) {
+  Q8_REQUIRE(type_ok(type) && N >= 0 && K >= 1, Q8_EINVAL);
+  Q8_REQUIRE(sizes_ok(M, N, K), Q8_EUNSUPPORTED);
+  if (M == 0 || N == 0) return Q8_OK;
+  Q8_REQUIRE(z_x_dev && q_x_dev && packed_dev && q_w_dev && y_dev, Q8_EINVAL);
+  Q8_REQUIRE(z_stride >= (size_t)K && y_stride >= (size_t)N, Q8_EINVAL);
+  Q8_REQUIRE(q8_aligned(z_x_dev, 16) && z_stride % 16 == 0 && q8_aligned(packed_dev, 16), Q8_EALIGN);
+  Q8_REQUIRE(q8_aligned(q_x_dev, 4) && q8_aligned(q_w_dev, 4) && q8_aligned(bias_dev, 4) &&
+                 q8_aligned(y_dev, type_bytes(type)), Q8_EALIGN);
+  const LinearParams p{z_x_dev, q_x_dev, static_cast<const int8_t*>(packed_dev), q_w_dev, bias_dev, z_stride,
+                       y_stride, (int)M, N, K, (int)(round_up(K, kPackK) / kPackK)};
+  return with_type(type, [&](auto v) { return launch_linear(p, static_cast<decltype(v)*>(y_dev), (hipStream_t)stream); });
+}
+
+extern "C" size_t q8_linear_workspace_bytes(size_t M, int N, int K) {
+  if (!sizes_ok(M, N, K)) return 0;
+  return codes_bytes(M, K) + round_up(M * 4, 256);
+}
+
+extern "C" int q8_linear(const void* x_dev, int x_type, size_t x_stride, size_t M, int N, int K,
+                         const void* packed_dev, const float* q_w_dev, const float* bias_dev, void* y_dev, int y_type,
+                         size_t y_stride, void* workspace, size_t workspace_bytes, void* stream) {
+  Q8_REQUIRE(type_ok(x_type) && type_ok(y_type) && N >= 0 && K >= 1, Q8_EINVAL);
+  Q8_REQUIRE(sizes_ok(M, N, K), Q8_EUNSUPPORTED);
+  if (M == 0 || N == 0) return Q8_OK;
+  Q8_REQUIRE(x_dev && packed_dev && q_w_dev && y_dev && workspace, Q8_EINVAL);
+  Q8_REQUIRE(x_stride >= (size_t)K && y_stride >= (size_t)N, Q8_EINVAL);
+  Q8_REQUIRE(q8_aligned(workspace, 256) && q8_aligned(x_dev, type_bytes(x_type)) && q8_aligned(packed_dev, 16) &&
+                 q8_aligned(q_w_dev, 4) && q8_aligned(bias_dev, 4) && q8_aligned(y_dev, type_bytes(y_type)), Q8_EALIGN);
+  Q8_REQUIRE(workspace_bytes >= q8_linear_workspace_bytes(M, N, K), Q8_EWORKSPACE);
+  int8_t* const z = static_cast<int8_t*>(workspace);
+  float* const q_x = reinterpret_cast<float*>(z + codes_bytes(M, K));
+  const size_t z_stride = round_up(K, 16);
+  const int rc = q8_quantize_rows(x_dev, x_type, M, K, x_stride, z, z_stride, q_x, stream);
+  if (rc != Q8_OK) return rc;
+  return q8_linear_int8(z, z_stride, q_x, M, N, K, packed_dev, q_w_dev, bias_dev, y_dev, y_type, y_stride, stream);
+}

@@ -1,0 +1,60 @@
+// The value types of the operators on rows of real values and on the 4-bit cache (Q8_F32, Q8_F16, Q8_BF16): loads
+// and stores of runs of them as fp32, in 16-byte accesses where the addresses allow it.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include "q8_common.h"
+
+namespace q8 {
+
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+
+// Calls f with a value of the C++ type of a Q8_* type code.
+template <typename F>
+inline int with_type(int type, F f) {
+  switch (type) {
+    case Q8_F32: return f(float{});
+    case Q8_F16: return f(_Float16{});
+    case Q8_BF16: return f(__bf16{});
+  }
+  return Q8_EINVAL;
+}
+inline size_t type_bytes(int type) { return type == Q8_F32 ? 4 : 2; }
+inline bool type_ok(int type) { return type == Q8_F32 || type == Q8_F16 || type == Q8_BF16; }
+
+// N consecutive values at p; ALIGNED: p is 16-byte aligned (N values are a multiple of 16 bytes).
+template <int N, bool ALIGNED, typename V>
+__device__ __forceinline__ void load_values(const V* p, float (&v)[N]) {
+  if constexpr (ALIGNED) {
+    static_assert(N * sizeof(V) % 16 == 0, "whole 16-byte vectors");
+    V raw[N];
+    __builtin_memcpy(raw, __builtin_assume_aligned(p, 16), sizeof(raw));
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = (float)raw[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = (float)p[e];
+  }
+}
+template <int N, bool ALIGNED, typename V>
+__device__ __forceinline__ void store_values(V* p, const float (&v)[N]) {
+  if constexpr (ALIGNED) {
+    constexpr size_t A = N * sizeof(V) % 16 == 0 ? 16 : N * sizeof(V);
+    V raw[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) raw[e] = (V)v[e];
+    __builtin_memcpy(__builtin_assume_aligned(p, A), raw, sizeof(raw));
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) p[e] = (V)v[e];
+  }
+}
+
+// |v| where v is finite, else 0: what enters the maximum behind a factor.
+__device__ __forceinline__ float finite_abs(float v) {
+  const float a = fabsf(v);
+  return a < __builtin_inff() ? a : 0.0f;
+}
+
+}  // namespace q8

@@ -1,0 +1,447 @@
+"""The linear layer on rows, the block tables, the 4-bit cache and attention over it, against the plain references of
+decoder_plain.py: bit for bit where the result is a fixed sequence of operations, within a derived bound else."""
+import numpy as np
+import pytest
+import torch
+
+import decoder_plain as P
+
+pytestmark = pytest.mark.gpu
+TYPES = P.TYPES
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_1805_08691_amd import binding
+    return binding
+
+
+def _rng(*seed):
+    return np.random.Generator(np.random.PCG64(np.random.SeedSequence([1805, 8691, 77, *seed])))
+
+
+def _real(rng, shape, kind):
+    return torch.from_numpy((rng.standard_normal(shape) * np.exp(rng.standard_normal(shape[-1]))).astype(np.float32)).to(
+        TYPES[kind])
+
+
+# ------------------------------------------------------------------------------ rows to codes
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("M,K", [(1, 1), (3, 7), (2, 8), (5, 16), (1, 64), (4, 1000), (7, 2049), (2, 4096), (3, 16400),
+                                 (1, 131071), (300, 40)])
+def test_rows_to_codes(B, kind, M, K):
+    x = _real(_rng(M, K), (M, K), kind)
+    z, q = B.quantize_rows(x.cuda())
+    want_z, want_q = P.quantize_rows(x)
+    assert np.array_equal(q.cpu().numpy(), want_q)
+    assert np.array_equal(z.cpu().numpy(), want_z)
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("offset,pad", [(0, 8), (1, 0), (0, 3), (3, 5)])
+def test_rows_to_codes_of_strided_rows(B, kind, offset, pad):
+    M, K = 6, 200
+    whole = _real(_rng(offset, pad), (M * (K + pad) + offset,), kind).cuda()
+    x = torch.as_strided(whole, (M, K), (K + pad, 1), offset)
+    out = torch.full((M, 224), 77, dtype=torch.int8, device="cuda")
+    z, q = B.quantize_rows(x, out=out[:, :K])
+    want_z, want_q = P.quantize_rows(x.cpu())
+    assert np.array_equal(z.cpu().numpy(), want_z) and np.array_equal(q.cpu().numpy(), want_q)
+    assert bool((out[:, 208:] == 77).all())
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("K", [40, 4096, 20000])
+def test_rows_to_codes_of_special_values(B, kind, K):
+    x = torch.zeros(9, K)
+    rows = _real(_rng(1, K), (9, K), "f32")
+    x[1] = rows[1] * 1e-30
+    x[2] = rows[2] * 1e-41                                   # (denormal: 0 in binary16)
+    x[3] = rows[3] * 1e30
+    x[4] = rows[4]
+    x[4, 3] = float("nan")
+    x[5] = rows[5]
+    x[5, 1], x[5, 2] = float("inf"), float("-inf")
+    x[6] = float("nan")
+    x[7, K - 1] = float("inf")
+    x[8] = torch.arange(K) % 256 / 2.0                       # ties
+    x = x.to(TYPES[kind])
+    z, q = B.quantize_rows(x.cuda())
+    want_z, want_q = P.quantize_rows(x)
+    assert np.array_equal(q.cpu().numpy(), want_q)
+    assert np.array_equal(z.cpu().numpy(), want_z)
+
+
+# ------------------------------------------------------------------------------ the product
+def _weights(rng, N, K):
+    z_w = rng.integers(-128, 128, (N, K), dtype=np.int8)
+    return z_w, (rng.random(N) + 0.5).astype(np.float32) / 100, rng.standard_normal(N).astype(np.float32)
+
+
+SHAPES = [(1, 1, 1), (1, 16, 64), (1, 17, 65), (2, 100, 333), (15, 31, 128), (16, 64, 4096), (17, 1000, 2048), (33, 48, 16),
+          (40, 272, 130), (63, 65, 257), (64, 64, 64), (65, 129, 1000), (100, 300, 200), (128, 256, 512), (129, 257, 1024),
+          (255, 255, 255), (300, 520, 720), (513, 384, 192), (1, 5000, 80), (1000, 16, 31), (257, 1030, 2050)]
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_product(B, kind, M, N, K):
+    rng = _rng(M, N, K)
+    z_w, q_w, bias = _weights(rng, N, K)
+    z = rng.integers(-128, 128, (M, K), dtype=np.int8)
+    q_x = (rng.random(M) + 0.1).astype(np.float32)
+    packed = B.linear_pack(torch.from_numpy(z_w).cuda())
+    codes = torch.full((M, -(-K // 16) * 16), -77, dtype=torch.int8, device="cuda")
+    codes[:, :K] = torch.from_numpy(z).cuda()
+    for b in (None, bias):
+        y = B.linear_int8(codes[:, :K], torch.from_numpy(q_x).cuda(), packed, torch.from_numpy(q_w).cuda(),
+                          None if b is None else torch.from_numpy(b).cuda(), dtype=TYPES[kind])
+        want = P.linear(z, q_x, z_w, q_w, b, TYPES[kind])
+        assert torch.equal(y.cpu(), want)
+
+
+def test_product_of_the_largest_sums(B):
+    """128 * 128 * 131071 just fits the accumulator, on both sides."""
+    K = 131071
+    for a, b in ((-128, -128), (-128, 127), (127, 127)):
+        z, z_w = np.full((3, K), a, np.int8), np.full((20, K), b, np.int8)
+        one = np.ones(20, np.float32)
+        padded = torch.full((3, 131072), 100, dtype=torch.int8, device="cuda")
+        padded[:, :K] = a
+        y = B.linear_int8(padded[:, :K], torch.ones(3, device="cuda"), B.linear_pack(torch.from_numpy(z_w).cuda()),
+                          torch.ones(20, device="cuda"), dtype=torch.float32)
+        assert torch.equal(y.cpu(), P.linear(z, np.ones(3, np.float32), z_w, one, None, torch.float32))
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("M", [1, 2, 4, 16, 40, 70, 300])
+def test_product_into_strided_rows(B, kind, M):
+    """Rows inside a wider tensor, at an odd place: nothing beside them is written."""
+    N, K = 83, 96
+    rng = _rng(M, 5)
+    z_w, q_w, _ = _weights(rng, N, K)
+    z = rng.integers(-128, 128, (M, K), dtype=np.int8)
+    q_x = (rng.random(M) + 0.1).astype(np.float32)
+    wide = torch.full((M, N + 10), 3.0, dtype=TYPES[kind], device="cuda")
+    strided = torch.zeros((M, 160), dtype=torch.int8, device="cuda")
+    strided[:, 32:32 + K] = torch.from_numpy(z).cuda()
+    B.linear_int8(strided[:, 32:32 + K], torch.from_numpy(q_x).cuda(), B.linear_pack(torch.from_numpy(z_w).cuda()),
+                  torch.from_numpy(q_w).cuda(), out=wide[:, 5:5 + N])
+    want = torch.full((M, N + 10), 3.0, dtype=TYPES[kind])
+    want[:, 5:5 + N] = P.linear(z, q_x, z_w, q_w, None, TYPES[kind])
+    assert torch.equal(wide.cpu(), want)
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("M,N,K", [(1, 16, 8), (1, 4096, 4096), (2, 33, 1000), (3, 100, 4096), (4, 64, 16384), (5, 200, 77),
+                                   (8, 1000, 2048), (37, 520, 4096), (130, 300, 1000), (600, 700, 800)])
+def test_linear_is_its_two_parts(B, kind, M, N, K):
+    rng = _rng(M, N, K, 9)
+    z_w, q_w, bias = _weights(rng, N, K)
+    x = _real(rng, (M, K), kind)
+    if M > 2:
+        x[1] = 0
+        x[2, K // 2] = float("nan")
+    packed, qw, b = B.linear_pack(torch.from_numpy(z_w).cuda()), torch.from_numpy(q_w).cuda(), torch.from_numpy(bias).cuda()
+    y = B.linear(x.cuda(), packed, qw, b)
+    z, q_x = P.quantize_rows(x)
+    assert y.dtype is x.dtype
+    assert torch.equal(y.cpu(), P.linear(z, q_x, z_w, q_w, bias, TYPES[kind]))
+    y32 = B.linear(x.cuda()[:, :], packed, qw, out=torch.empty(M, N, device="cuda"))
+    assert torch.equal(y32.cpu(), P.linear(z, q_x, z_w, q_w, None, torch.float32))
+
+
+def test_linear_of_strided_rows(B):
+    rng = _rng(4, 4)
+    z_w, q_w, _ = _weights(rng, 70, 90)
+    for M, offset, pad in ((1, 1, 3), (2, 3, 1), (50, 1, 6), (200, 8, 6)):
+        whole = _real(rng, (M * (90 + pad) + offset,), "bf16").cuda()
+        x = torch.as_strided(whole, (M, 90), (90 + pad, 1), offset)
+        y = B.linear(x, B.linear_pack(torch.from_numpy(z_w).cuda()), torch.from_numpy(q_w).cuda())
+        z, q_x = P.quantize_rows(x.cpu())
+        assert torch.equal(y.cpu(), P.linear(z, q_x, z_w, q_w, None, torch.bfloat16))
+
+
+def test_linear_of_nothing(B):
+    packed, q_w = B.linear_pack(torch.ones(20, 40, dtype=torch.int8, device="cuda")), torch.ones(20, device="cuda")
+    assert B.linear(torch.zeros(0, 40, device="cuda"), packed, q_w).shape == (0, 20)
+    none = B.linear_pack(torch.ones(0, 40, dtype=torch.int8, device="cuda"))
+    assert B.linear(torch.zeros(3, 40, device="cuda"), none, q_w[:0]).shape == (3, 0)
+
+
+# ------------------------------------------------------------------------------ block tables
+def _run_tables(B, lengths, added, page, n_free, width, n_slots, pad=0, seed=0):
+    rng = _rng(len(lengths), page, n_free, seed)
+    n = len(lengths)
+    table = rng.integers(-5, 1000, (n, width + pad)).astype(np.int32)
+    free = rng.permutation(max(n_free, 1))[:n_free].astype(np.int32) + 5000
+    dev = [torch.tensor(v, dtype=torch.int32, device="cuda") for v in (lengths, added)]
+    tab = torch.from_numpy(table).cuda()
+    slots = torch.full((n_slots,), 99, dtype=torch.int64, device="cuda")
+    positions = torch.full((n_slots,), 99, dtype=torch.int32, device="cuda")
+    got = B.page_tables(*dev, page, torch.from_numpy(free).cuda(), tab[:, :width], slots, positions)
+    want = P.page_tables(lengths, added, page, free, table[:, :width], n_slots)
+    for name, w in zip(("table", "slots", "positions", "starts", "lengths", "counts"), want):
+        assert got[name].cpu().tolist() == np.asarray(w).tolist(), name
+    if pad:
+        assert np.array_equal(tab[:, width:].cpu().numpy(), table[:, width:])
+    assert dev[0].tolist() == list(lengths) and dev[1].tolist() == list(added)
+    return got
+
+
+@pytest.mark.parametrize("page", [16, 64, 256])
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 255, 1000, 1024, 1025, 3000, 9000])
+def test_tables_of_ragged_requests(B, page, n):
+    rng = _rng(n, page)
+    lengths = rng.integers(0, 2000, n)
+    added = np.where(rng.random(n) < 0.3, rng.integers(0, 40 if n > 100 else 900, n), rng.integers(0, 2, n))
+    need = int((-(-(lengths + added) // page) + (-lengths // page)).sum())
+    width = -(-3000 // page)
+    _run_tables(B, lengths.tolist(), added.tolist(), page, need + 3, width, int(added.sum()) + 11, pad=1)
+    # too few pages, too narrow a table, too few slots: what does not fit gets nothing
+    _run_tables(B, lengths.tolist(), added.tolist(), page, need // 2, width, int(added.sum()) + 11)
+    _run_tables(B, lengths.tolist(), added.tolist(), page, need, max(1, width // 3), int(added.sum()) + 11)
+    _run_tables(B, lengths.tolist(), added.tolist(), page, need, width, int(added.sum()) * 2 // 3)
+
+
+@pytest.mark.parametrize("lengths,added,page,n_free,width,n_slots", [
+    ([0], [0], 16, 0, 1, 3), ([0], [1], 16, 1, 1, 1), ([15], [1], 16, 0, 1, 1), ([16], [1], 16, 1, 2, 1),
+    ([16], [1], 16, 0, 2, 4), ([-3, 5], [4, -2], 16, 2, 3, 9), ([0, 0, 0], [0, 0, 0], 32, 4, 1, 0),
+    ([0, 7], [100000, 3], 16, 7000, 7000, 100010), ([5], [2000000], 64, 40000, 40000, 2000001), ([3], [4], 1024, 0, 1, 9),
+    ([1], [50], 16, 10, 0, 60)])
+def test_tables_at_the_edges(B, lengths, added, page, n_free, width, n_slots):
+    _run_tables(B, lengths, added, page, n_free, width, n_slots)
+
+
+def test_tables_of_no_request(B):
+    e = torch.empty(0, dtype=torch.int32, device="cuda")
+    slots, positions = torch.ones(5, dtype=torch.int64, device="cuda"), torch.ones(5, dtype=torch.int32, device="cuda")
+    got = B.page_tables(e, e, 16, e, e.reshape(0, 4), slots, positions)
+    assert got["starts"].tolist() == [0] and got["counts"].tolist() == [0, 0, 0]
+    assert got["slots"].tolist() == [-1] * 5 == got["positions"].tolist()
+
+
+# ------------------------------------------------------------------------------ tokens in and out
+def _slots(rng, T, places):
+    """Runs of consecutive slots, some alone, some outside the cache."""
+    order = []
+    while len(order) < T:
+        a = int(rng.integers(0, places))
+        order += [s for s in range(a, min(places, a + int(rng.integers(1, 40)))) if s not in order]
+    order = order[:T]
+    for i in range(0, T, 7):
+        order[i] = [-1, places, -(1 << 40), 1 << 40][i // 7 % 4] if i % 2 else order[i]
+    return np.array(order, np.int64)
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("T,H,D,page", [(1, 1, 32, 16), (5, 2, 64, 16), (40, 3, 96, 32), (70, 1, 128, 64), (33, 2, 160, 16),
+                                        (20, 1, 224, 128), (17, 2, 256, 64), (150, 1, 192, 16)])
+def test_tokens_in_and_out(B, kind, T, H, D, page):
+    rng = _rng(T, H, D)
+    pages = -(-3 * T // page) + 1
+    k, v = _real(rng, (T, H, D), kind), _real(rng, (T, H, D), kind)
+    k[0, 0, :32] = 0
+    v[T // 2, H - 1, 3], k[T // 2, 0, 5], v[T // 2, 0, 6] = float("nan"), float("inf"), float("-inf")
+    slots = _slots(rng, T, pages * page)
+    before = rng.integers(0, 256, (pages, H, page // 16, 18 * D)).astype(np.uint8)
+    cache = torch.from_numpy(before.copy()).cuda()
+    # keys and values as slices of a joint projection's rows, at an odd place for fp32 and the 16-bit types alike
+    joint = torch.zeros((T, 3, H, D + 8), dtype=TYPES[kind], device="cuda")
+    joint[:, 1, :, 8:] = k.cuda()
+    joint[:, 2, :, 8:] = v.cuda()
+    dev = torch.from_numpy(slots).cuda()
+    B.kv4_write(cache, joint[:, 1, :, 8:], joint[:, 2, :, 8:], dev)
+    want = before.copy()
+    P.kv4_write(want, k.float().numpy(), v.float().numpy(), slots, page)
+    assert np.array_equal(cache.cpu().numpy(), want)
+    # the same through unaligned rows
+    odd = torch.zeros((T, H, D + 1), dtype=TYPES[kind], device="cuda")[:, :, 1:]
+    other = torch.from_numpy(before.copy()).cuda()
+    B.kv4_write(other, odd.copy_(k), v.cuda(), dev)
+    assert torch.equal(other, cache)
+    inside = (slots >= 0) & (slots < pages * page)
+    for out_kind in sorted(TYPES):
+        got = B.kv4_read(cache, dev, dtype=TYPES[out_kind])
+        for g, x in zip(got, (k, v)):
+            held = torch.from_numpy(P.kv4_values(x.float().numpy()) * inside[:, None, None])
+            assert torch.equal(g.cpu(), held.to(torch.float32).to(TYPES[out_kind]))
+    out = [torch.full((T, H, D + 3), 5.0, dtype=TYPES[kind], device="cuda") for _ in range(2)]
+    B.kv4_read(cache, dev, out[0][:, :, 1:-2], out[1][:, :, 1:-2])
+    same = B.kv4_read(cache, dev, dtype=TYPES[kind])
+    for o, s in zip(out, same):
+        assert torch.equal(o[:, :, 1:-2], s) and bool((o[:, :, :1] == 5).all()) and bool((o[:, :, -2:] == 5).all())
+
+
+@pytest.mark.parametrize("size", [0.0, 1e-9, 1e-6, 1e-3, 100.0, 6e4, 1e6])
+def test_sizes_that_the_cache_holds(B, size):
+    """Factors down to binary16's smallest number and up to the largest that 8 of still fit."""
+    k = _real(_rng(3), (16, 1, 64), "f32") * size
+    cache = B.kv4_cache(1, 1, 16, 64)
+    slots = torch.arange(16, device="cuda")
+    B.kv4_write(cache, k.cuda(), -k.cuda(), slots)
+    got = B.kv4_read(cache, slots, dtype=torch.float32)
+    assert np.array_equal(got[0].cpu().numpy(), P.kv4_values(k.numpy()).astype(np.float32))
+    assert np.array_equal(got[1].cpu().numpy(), P.kv4_values(-k.numpy()).astype(np.float32))
+
+
+# ------------------------------------------------------------------------------ attention
+def _filled(B, rng, lengths, H, D, page, spare=2, kv=None):
+    """A cache of requests of these lengths on shuffled pages; unwritten places hold bytes that are no numbers."""
+    held = [-(-n // page) for n in lengths]
+    pool = sum(held) + spare
+    width = max(max(held), 1) + 1
+    order = rng.permutation(pool)
+    table = np.full((len(lengths), width), -1, np.int32)
+    at = 0
+    for b, n in enumerate(held):
+        table[b, :n] = order[at:at + n]
+        at += n
+    cache = torch.full((pool, H, page // 16, 18 * D), 255, dtype=torch.uint8, device="cuda")   # binary16 NaN factors
+    keys, values, ks, vs, slots = [], [], [], [], []
+    for b, n in enumerate(lengths):
+        k, v = kv(b, n) if kv else (_real(rng, (n, H, D), "f32"), _real(rng, (n, H, D), "f32"))
+        ks.append(k)
+        vs.append(v)
+        slots += [int(table[b, i // page]) * page + i % page for i in range(n)]
+        keys.append(P.kv4_values(k.numpy()))
+        values.append(P.kv4_values(v.numpy()))
+    if slots:
+        B.kv4_write(cache, torch.cat(ks).cuda(), torch.cat(vs).cuda(), torch.tensor(slots, device="cuda"))
+    return cache, torch.from_numpy(table).cuda(), keys, values
+
+
+def _check_attend(B, rng, lengths, added, H, ratio, D, page, kind, window=0, scale=None, workspace=True, peak=1.0):
+    cache, table, keys, values = _filled(B, rng, lengths, H, D, page)
+    T = sum(added)
+    q = (_real(rng, (T, H * ratio, D), "f32") * peak).to(TYPES[kind])
+    starts = np.concatenate([[0], np.cumsum(added)]).tolist()
+    scale = D ** -0.5 if scale is None else scale
+    lens = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    first = None if all(a == 1 for a in added) else torch.tensor(starts, dtype=torch.int32, device="cuda")
+    ws = B.kv4_attend_workspace(q, cache, len(lengths), max(lengths + [1])) if workspace else None
+    out = torch.full((T, H * ratio, D), 9.0, dtype=TYPES[kind], device="cuda")
+    got = B.kv4_attend(q.cuda(), cache, table, lens, first, scale, window=window, out=out, workspace=ws)
+    want, most = P.attend(q.double().numpy(), keys, values, lengths, starts, scale, window)
+    off = np.abs(got.double().cpu().numpy() - want)
+    bound = P.attend_tolerance(want, values, most, TYPES[kind])
+    assert np.all(off <= bound), (float(np.nanmax(off / bound)), bool(np.isnan(off).any()))
+    return q, cache, table, lens, first, got
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("D", range(32, 257, 32))
+def test_attention_of_single_tokens(B, kind, D):
+    _check_attend(B, _rng(D), [1, 0, 70, 16, 200, 64, 65], [1] * 7, 2, 3, D, 16, kind)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("D", range(32, 257, 32))
+def test_attention_of_several_tokens(B, kind, D):
+    _check_attend(B, _rng(D, 1), [130, 20, 3, 0, 50], [70, 20, 0, 0, 1], 2, 3, D, 32, kind)
+
+
+@pytest.mark.parametrize("ratio", [1, 2, 4, 5, 8, 16, 17, 40])
+@pytest.mark.parametrize("page", [16, 64, 256])
+def test_attention_by_heads_and_pages(B, ratio, page):
+    _check_attend(B, _rng(ratio, page), [40, 129, 1, 300], [1] * 4, 2, ratio, 64, page, "bf16")
+    _check_attend(B, _rng(ratio, page, 1), [40, 129, 2, 300], [3, 40, 2, 33], 1, ratio, 64, page, "bf16")
+
+
+@pytest.mark.parametrize("lengths", [[5000], [4097, 1, 900], [513, 512, 511, 0], [20000]])
+@pytest.mark.parametrize("workspace", [True, False])
+def test_attention_over_long_contexts(B, lengths, workspace):
+    _check_attend(B, _rng(*lengths), lengths, [1] * len(lengths), 2, 4, 64, 64, "bf16", workspace=workspace)
+    _check_attend(B, _rng(*lengths), lengths, [min(n, 5) for n in lengths], 1, 2, 128, 32, "f16", workspace=workspace)
+
+
+@pytest.mark.parametrize("window", [1, 2, 15, 16, 63, 64, 65, 100, 5000])
+def test_attention_in_a_window(B, window):
+    lengths = [300, 64, 1, 700, 0]
+    _check_attend(B, _rng(window), lengths, [1] * 5, 2, 2, 64, 16, "bf16", window=window)
+    _check_attend(B, _rng(window, 1), lengths, [90, 64, 1, 37, 0], 1, 3, 96, 32, "bf16", window=window)
+
+
+def test_attention_of_more_rows_than_tokens(B):
+    """A request with more rows than tokens in the cache: the first rows stand in front of its first key."""
+    _check_attend(B, _rng(8), [3, 0, 20], [5, 4, 30], 2, 2, 64, 16, "bf16")
+
+
+@pytest.mark.parametrize("peak,scale", [(0.0, None), (1e-6, None), (30.0, None), (1.0, -0.3), (1.0, 0.0), (3000.0, 1e-4)])
+def test_attention_of_flat_and_peaked_rows(B, peak, scale):
+    for kind in ("bf16", "f16"):
+        _check_attend(B, _rng(5), [200, 33], [1, 1], 2, 4, 64, 16, kind, peak=peak, scale=scale)
+
+
+def test_attention_reads_no_page_that_a_request_has_not(B):
+    """Pages outside the cache inside a request's length: their tokens are not seen, whatever the table says."""
+    rng = _rng(12)
+    H, D, page = 2, 64, 16
+    cache, table, keys, values = _filled(B, rng, [100, 50], H, D, page)
+    table[0, 2], table[1, 0] = 1 << 30, -7
+    q = _real(rng, (2, 4, D), "bf16")
+    got = B.kv4_attend(q.cuda(), cache, table, torch.tensor([100, 50], dtype=torch.int32, device="cuda"))
+    for k in (keys, values):
+        k[0] = np.delete(k[0], range(32, 48), 0)
+        k[1] = k[1][16:]
+    want, most = P.attend(q.double().numpy(), keys, values, [84, 34], [0, 1, 2], D ** -0.5, 0)
+    bound = P.attend_tolerance(want, values, most, torch.bfloat16)
+    assert np.all(np.abs(got.double().cpu().numpy() - want) <= bound)
+    # a window whose first pages have been given away
+    whole = int(table[0, 1])                                     # (a page that the first request has filled)
+    table[:] = -1
+    table[0, 3] = whole
+    lens = torch.tensor([64, 0], dtype=torch.int32, device="cuda")
+    got = B.kv4_attend(q.cuda(), cache, table, lens, window=16)
+    assert bool(torch.isfinite(got).all()) and not bool(got[1].any())
+
+
+def test_attention_leaves_other_rows_alone(B):
+    """Strided queries and outputs; rows in front of the first request's and behind the last one's stay as they are."""
+    rng = _rng(13)
+    H, ratio, D = 2, 2, 64
+    lengths, starts = [40, 20], [2, 5, 6]
+    cache, table, keys, values = _filled(B, rng, lengths, H, D, 16)
+    q = torch.zeros((9, H * ratio + 1, D + 1), dtype=torch.bfloat16, device="cuda")
+    out = torch.full((9, H * ratio + 2, D + 3), 7.0, dtype=torch.bfloat16, device="cuda")
+    rows = _real(rng, (9, H * ratio, D), "bf16")
+    q[:, 1:, 1:] = rows.cuda()
+    B.kv4_attend(q[:, 1:, 1:], cache, table, torch.tensor(lengths, dtype=torch.int32, device="cuda"),
+                 torch.tensor(starts, dtype=torch.int32, device="cuda"), out=out[:, 1:-1, 1:-2])
+    want, most = P.attend(rows[2:6].double().numpy(), keys, values, lengths, [0, 3, 4], D ** -0.5, 0)
+    got = out[2:6, 1:-1, 1:-2].double().cpu().numpy()
+    assert np.all(np.abs(got - want) <= P.attend_tolerance(want, values, most, torch.bfloat16))
+    out[2:6, 1:-1, 1:-2] = 7.0
+    assert bool((out == 7).all())
+
+
+def test_the_last_pages_of_a_large_cache(B):
+    """Byte offsets beyond 32 bits."""
+    H, D, page = 8, 256, 16
+    pages = (9 << 29) // (H * 18 * D) + 1                       # 4.5 GiB
+    cache = torch.empty((pages, H, 1, 18 * D), dtype=torch.uint8, device="cuda")
+    rng = _rng(14)
+    n = 45
+    k, v = _real(rng, (n, H, D), "bf16"), _real(rng, (n, H, D), "bf16")
+    table = torch.tensor([[pages - 1, pages - 4, pages // 2]], dtype=torch.int32, device="cuda")
+    at = torch.arange(n, device="cuda")
+    slots = table[0].long()[at // page] * page + at % page
+    B.kv4_write(cache, k.cuda(), v.cuda(), slots)
+    got = B.kv4_read(cache, slots, dtype=torch.float32)
+    keys, values = P.kv4_values(k.float().numpy()), P.kv4_values(v.float().numpy())
+    assert np.array_equal(got[0].cpu().numpy(), keys.astype(np.float32))
+    assert np.array_equal(got[1].cpu().numpy(), values.astype(np.float32))
+    q = _real(rng, (1, 2 * H, D), "bf16")
+    out = B.kv4_attend(q.cuda(), cache, table, torch.tensor([n], dtype=torch.int32, device="cuda"))
+    want, most = P.attend(q.double().numpy(), [keys], [values], [n], [0, 1], D ** -0.5, 0)
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= P.attend_tolerance(want, [values], most, torch.bfloat16))
+
+
+def test_attention_is_the_same_every_time(B):
+    rng = _rng(15)
+    q, cache, table, lens, first, got = _check_attend(B, rng, [3000, 2000], [1, 1], 2, 4, 128, 64, "bf16")
+    ws = B.kv4_attend_workspace(q, cache, 2, 3000)
+    for _ in range(5):
+        again = B.kv4_attend(q.cuda(), cache, table, lens, first, workspace=ws.fill_(255) if ws.numel() else ws)
+        ws = B.kv4_attend_workspace(q, cache, 2, 3000)
+        assert torch.equal(got, again)
