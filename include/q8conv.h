@@ -556,6 +556,15 @@ int q8_linear_int8(const int8_t *z_x_dev, size_t z_stride, const float *q_x_dev,
                    int K, const void *packed_dev, const float *q_w_dev, const float *bias_dev,
                    void *y_dev, int type, size_t y_stride, void *stream);
 
+/* Tests and tuning only: q8_linear_int8 with the build of its kernel given by the caller (0 ..
+ * q8_linear_num_variants() - 1; -1: the library's choice).  The results are the same bits.   */
+int q8_linear_num_variants(void);
+const char *q8_linear_variant_name(int variant);
+int q8_linear_int8_variant(const int8_t *z_x_dev, size_t z_stride, const float *q_x_dev, size_t M,
+                           int N, int K, const void *packed_dev, const float *q_w_dev,
+                           const float *bias_dev, void *y_dev, int type, size_t y_stride,
+                           int variant, void *stream);
+
 /* q8_quantize_rows and q8_linear_int8 as one call: bit for bit their result.  `workspace`:
  * q8_linear_workspace_bytes(M, N, K) bytes of device memory, 256-byte aligned, for the codes
  * and factors in between; calls that share one must not overlap in time.                   */

@@ -39,7 +39,8 @@ EXPORTS = [
     "q8_probe_mfma_i8", "q8_run_ops", "q8_group_variant",
     "q8_block_variant", "q8_block_pays", "q8_num_bottleneck_builds", "q8_bottleneck_build_name", "q8_run_bottleneck", "q8_joined_op", "q8_conv_estimate_us",
     "q8_conv_f32_ref", "q8_conv_f32_observed", "q8_conv_f32_observed_spread", "q8_calibrate_fold", "q8_conv_f32_variant", "q8_maxpool_i8", "q8_maxpool_f32", "q8_pool_i8", "q8_pool_f32",
-    "q8_quantize_rows", "q8_linear_packed_bytes", "q8_linear_pack", "q8_linear_int8", "q8_linear_workspace_bytes",
+    "q8_quantize_rows", "q8_linear_packed_bytes", "q8_linear_pack", "q8_linear_int8", "q8_linear_num_variants",
+    "q8_linear_variant_name", "q8_linear_int8_variant", "q8_linear_workspace_bytes",
     "q8_linear", "q8_page_tables", "q8_kv4_cache_bytes", "q8_kv4_write", "q8_kv4_read",
     "q8_kv4_attend_workspace_bytes", "q8_kv4_attend",
 ]
@@ -190,6 +191,10 @@ lib.q8_linear_packed_bytes.restype = _sz
 lib.q8_linear_packed_bytes.argtypes = [_i, _i]
 lib.q8_linear_pack.argtypes = [_vp, _i, _i, _vp, _vp]
 lib.q8_linear_int8.argtypes = [_vp, _sz, _vp, _sz, _i, _i, _vp, _vp, _vp, _vp, _i, _sz, _vp]
+lib.q8_linear_num_variants.argtypes = []
+lib.q8_linear_variant_name.restype = C.c_char_p
+lib.q8_linear_variant_name.argtypes = [_i]
+lib.q8_linear_int8_variant.argtypes = [_vp, _sz, _vp, _sz, _i, _i, _vp, _vp, _vp, _vp, _i, _sz, _i, _vp]
 lib.q8_linear_workspace_bytes.restype = _sz
 lib.q8_linear_workspace_bytes.argtypes = [_sz, _i, _i]
 lib.q8_linear.argtypes = [_vp, _i, _sz, _sz, _i, _i, _vp, _vp, _vp, _vp, _i, _sz, _vp, _sz, _vp]
@@ -714,8 +719,9 @@ def _linear_args(K, packed, q_w, bias, out):
             _value_type(out), _rows(out)[1])
 
 
-def linear_int8(z_x, q_x, packed, q_w, bias=None, out=None, dtype=torch.bfloat16):
-    """Codes [M, K] and their rows' factors (quantize_rows) times packed weights: [M, N] real values."""
+def linear_int8(z_x, q_x, packed, q_w, bias=None, out=None, dtype=torch.bfloat16, variant=-1):
+    """Codes [M, K] and their rows' factors (quantize_rows) times packed weights: [M, N] real values.  ``variant`` >= 0
+    (tests, tuning): that build of the kernel."""
     M, K = z_x.shape
     assert z_x.dtype is torch.int8 and q_x.numel() == M
     if out is None:
@@ -723,7 +729,8 @@ def linear_int8(z_x, q_x, packed, q_w, bias=None, out=None, dtype=torch.bfloat16
     assert out.shape[0] == M
     zp, zs = _codes(z_x)
     w, qw, b, y, ytype, ys = _linear_args(K, packed, q_w, bias, out)
-    _check(lib.q8_linear_int8(zp, zs, _ptr(q_x, torch.float32), M, q_w.numel(), K, w, qw, b, y, ytype, ys, _stream()))
+    _check(lib.q8_linear_int8_variant(zp, zs, _ptr(q_x, torch.float32), M, q_w.numel(), K, w, qw, b, y, ytype, ys, variant,
+                                      _stream()))
     return out
 
 

@@ -5,9 +5,9 @@
 // The sum is exact in int32 (128 * 128 * K < 2^31 for K <= 131071); the tail is three fp32 operations and the
 // rounding to y's type.
 #include "q8_common.h"
-#include "q8_conv_common.h"
+#include "q8_linear.h"
 #include "q8_quant.h"
-#include "q8_value.h"
+#include <math.h>
 #pragma clang fp contract(off)
 
 namespace {
@@ -15,8 +15,6 @@ namespace {
 using namespace q8;
 
 constexpr int kMaxK = 131071;
-constexpr int kPackK = 64;                    // reduction bytes of a packed block
-constexpr int kPackN = 16;                    // and its rows
 
 inline size_t round_up(size_t a, size_t b) { return (a + b - 1) / b * b; }
 
@@ -31,11 +29,11 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const V* __restrict_
   int8_t* __restrict__ zr = z + row * z_stride;
   const int tid = threadIdx.x, body = K & ~7;
   float m = 0.0f;
+  bool finite = true;
   for (int k = tid * 8; k < body; k += 256 * 8) {
     float v[8];
     load_values<8, ALIGNED>(xr + k, v);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) m = fmaxf(m, finite_abs(v[e]));
+    m = row_max8(v, m, &finite);
   }
   if (tid < K - body) m = fmaxf(m, finite_abs((float)xr[body + tid]));
   for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
@@ -46,16 +44,16 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const V* __restrict_
   float q = __fmul_rn(m, 1.0f / 127.0f);
   q = q > 0.0f ? q : 1.0f;
   if (tid == 0) q_x[row] = q;
-  auto code = [&](float v) { return v == v ? quant1(v, q, -128.0f, 127.0f) : 0; };
+  const float inv_q = __fdiv_rn(1.0f, q);
   for (int k = tid * 8; k < body; k += 256 * 8) {
     float v[8];
     load_values<8, ALIGNED>(xr + k, v);
-    uint2 w;
-    w.x = pack4(code(v[0]), code(v[1]), code(v[2]), code(v[3]));
-    w.y = pack4(code(v[4]), code(v[5]), code(v[6]), code(v[7]));
-    *reinterpret_cast<uint2*>(zr + k) = w;
+    *reinterpret_cast<uint2*>(zr + k) = row_codes(v, q, inv_q, finite);
   }
-  if (tid < K - body) zr[body + tid] = (int8_t)code((float)xr[body + tid]);
+  if (tid < K - body) {
+    const float v = (float)xr[body + tid];
+    zr[body + tid] = (int8_t)(v == v ? quant1(v, q, -128.0f, 127.0f) : 0);
+  }
 }
 
 template <typename V>
@@ -89,41 +87,9 @@ __global__ __launch_bounds__(256) void linear_pack_kernel(const int8_t* __restri
 }
 
 // ---------------------------------------------------------------- product ----------------
-struct LinearParams {
-  const int8_t* __restrict__ z;
-  const float* __restrict__ q_x;
-  const int8_t* __restrict__ w;
-  const float* __restrict__ q_w;
-  const float* __restrict__ bias;
-  size_t z_stride, y_stride;
-  int M, N, K, ksteps;
-};
-
-// Four consecutive outputs of row m, channels n ..: the tail, and one store where the row allows it.
+// Rows at any distance: one wavefront per 16 channels x 16 rows, operands straight from memory.
 template <typename Y, bool VEC>
-__device__ __forceinline__ void finish4(const LinearParams& p, Y* __restrict__ y, int m, int n, v4i acc) {
-  if (m >= p.M || n >= p.N) return;
-  const float q = p.q_x[m];
-  float v[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int c = min(n + e, p.N - 1);
-    v[e] = (float)acc[e] * (q * p.q_w[c]);
-    if (p.bias) v[e] = v[e] + p.bias[c];
-  }
-  Y* to = y + (size_t)m * p.y_stride + n;
-  if (VEC && n + 4 <= p.N) {
-    store_values<4, true>(to, v);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (n + e < p.N) to[e] = (Y)v[e];
-  }
-}
-
-// One wavefront per 16 channels x 16 rows, operands straight from memory.
-template <typename Y, bool VEC>
-__global__ __launch_bounds__(256) void linear_kernel(const LinearParams p, Y* __restrict__ y) {
+__global__ __launch_bounds__(256) void linear_any_kernel(const LinearParams p, Y* __restrict__ y) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int nb = blockIdx.x * 4 + wave;
   if (nb * kPackN >= p.N) return;
@@ -137,18 +103,63 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinearParams p, Y* __
     if (s * kPackK + chunk < p.K) b = *reinterpret_cast<const v4i*>(z + s * kPackK);
     acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[(size_t)s * 64], b, acc, 0, 0, 0);
   }
-  finish4<Y, VEC>(p, y, m0 + (lane & 15), nb * kPackN + 4 * (lane >> 4), acc);
+  const int m = m0 + (lane & 15), n = nb * kPackN + 4 * (lane >> 4);
+  if (m >= p.M || n >= p.N) return;
+  const int v[4] = {acc[0], acc[1], acc[2], acc[3]};
+  finish_outputs<4, VEC>(p, y, m, n, p.q_x[m], v);
 }
 
 template <typename Y>
-int launch_linear(const LinearParams& p, Y* y, hipStream_t stream) {
+int launch_any_rows(const LinearParams& p, Y* y, hipStream_t stream) {
   const dim3 grid((unsigned)((p.N + 63) / 64), (unsigned)((p.M + 15) / 16));
   const bool vec = q8_aligned(y, 4 * sizeof(Y)) && p.y_stride % 4 == 0;
   if (vec)
-    linear_kernel<Y, true><<<grid, 256, 0, stream>>>(p, y);
+    linear_any_kernel<Y, true><<<grid, 256, 0, stream>>>(p, y);
   else
-    linear_kernel<Y, false><<<grid, 256, 0, stream>>>(p, y);
+    linear_any_kernel<Y, false><<<grid, 256, 0, stream>>>(p, y);
   return q8_launch_status();
+}
+
+// The builds of the product, and what the choice between them goes by: a launch of `tiles` tiles takes
+//   base + (share * tiles / 256 + (1 - share) * ceil(tiles / 256)) * (round + per_k * K / 1024)
+// us (256 compute units; a round costs its steps along K and a constant; `share` of a round that is not full is saved),
+// and no less than its operands' way from memory, m = 2.2 us + bytes at 5.4 TB/s; the lesser of the two counts a
+// fifth.  The constants are fitted to every build on 128 sizes (1 .. 4096 rows, 512 .. 16384 channels and values a
+// row); there the pick is 1.3 % longer than the best build in the mean and 24 % at most.
+struct Variant {
+  const char* name;
+  int bn, bm;                  // channels and rows of a tile
+  int columns, squares;        // rows build: packed columns and squares of 16 rows
+  int tile;                    // tile build, or -1
+  float base, round, per_k, share;
+};
+constexpr Variant kVariants[] = {
+    {"rows_16x16", 16, 16, 1, 1, -1, 1.92f, 0.91f, 0.45f, 0.30f},
+    {"rows_32x16", 32, 16, 2, 1, -1, 1.00f, 1.79f, 0.61f, 0.30f},
+    {"rows_64x16", 64, 16, 4, 1, -1, 1.00f, 2.11f, 1.00f, 0.00f},
+    {"rows_64x32", 64, 32, 4, 2, -1, 1.00f, 1.90f, 1.47f, 0.04f},
+    {"tile_64x64", 64, 64, 0, 0, 0, 2.71f, 1.12f, 1.79f, 0.46f},
+    {"tile_128x64", 128, 64, 0, 0, 1, 2.45f, 2.21f, 2.66f, 0.17f},
+    {"tile_128x128", 128, 128, 0, 0, 2, 1.00f, 6.12f, 3.49f, 0.24f},
+    {"tile_128x128_8", 128, 128, 0, 0, 3, 1.00f, 5.40f, 3.77f, 0.00f},
+    {"tile_256x256", 256, 256, 0, 0, 4, 1.00f, 17.15f, 8.95f, 0.80f},
+    {"rows_any", 16, 16, 0, 0, -1, 0.0f, 0.0f, 0.0f, 0.0f}};      // rows so far apart that a tile passes 2^31 bytes
+constexpr int kNumVariants = sizeof(kVariants) / sizeof(kVariants[0]);
+constexpr size_t kTileStride = 1 << 22;      // 256 rows of a tile stay below 2^31 bytes
+
+int pick(const LinearParams& p) {
+  int best = 0;
+  float least = 0.0f;
+  const float memory = 2.2f + ((float)p.N + (float)p.M) * (float)p.K / 5.4e6f;
+  for (int i = 0; i + 1 < kNumVariants; ++i) {
+    const Variant& v = kVariants[i];
+    const float tiles = (float)((p.N + v.bn - 1) / v.bn) * (float)((p.M + v.bm - 1) / v.bm), rounds = tiles / 256.0f;
+    const float passes = fmaxf(1.0f, v.share * rounds + (1.0f - v.share) * ceilf(rounds));
+    const float time = v.base + passes * (v.round + v.per_k * (float)p.K / 1024.0f);
+    const float cost = fmaxf(time, memory) + 0.2f * fminf(time, memory);
+    if (i == 0 || cost < least) best = i, least = cost;
+  }
+  return best;
 }
 
 // Codes [M][round_up(K, 16)], then the rows' factors.
@@ -190,9 +201,16 @@ extern "C" int q8_linear_pack(const int8_t* z_w_dev, int N, int K, void* packed_
   return q8_launch_status();
 }
 
-extern "C" int q8_linear_int8(const int8_t* z_x_dev, size_t z_stride, const float* q_x_dev, size_t M, int N, int K,
-                              const void* packed_dev, const float* q_w_dev, const float* bias_dev, void* y_dev,
-                              int type, size_t y_stride, void* stream) {
+extern "C" int q8_linear_num_variants(void) { return kNumVariants; }
+
+extern "C" const char* q8_linear_variant_name(int variant) {
+  return variant >= 0 && variant < kNumVariants ? kVariants[variant].name : "unsupported";
+}
+
+extern "C" int q8_linear_int8_variant(const int8_t* z_x_dev, size_t z_stride, const float* q_x_dev, size_t M, int N,
+                                      int K, const void* packed_dev, const float* q_w_dev, const float* bias_dev,
+                                      void* y_dev, int type, size_t y_stride, int variant, void* stream) {
+  Q8_REQUIRE(variant < kNumVariants, Q8_EINVAL);
   Q8_REQUIRE(type_ok(type) && N >= 0 && K >= 1, Q8_EINVAL);
   Q8_REQUIRE(sizes_ok(M, N, K), Q8_EUNSUPPORTED);
   if (M == 0 || N == 0) return Q8_OK;
@@ -203,7 +221,19 @@ extern "C" int q8_linear_int8(const int8_t* z_x_dev, size_t z_stride, const floa
                  q8_aligned(y_dev, type_bytes(type)), Q8_EALIGN);
   const LinearParams p{z_x_dev, q_x_dev, static_cast<const int8_t*>(packed_dev), q_w_dev, bias_dev, z_stride,
                        y_stride, (int)M, N, K, (int)(round_up(K, kPackK) / kPackK)};
-  return with_type(type, [&](auto v) { return launch_linear(p, static_cast<decltype(v)*>(y_dev), (hipStream_t)stream); });
+  if (variant < 0) variant = z_stride <= kTileStride ? pick(p) : kNumVariants - 1;
+  const Variant& v = kVariants[variant];
+  if (v.columns) return linear_rows(p, y_dev, type, v.columns, v.squares, (hipStream_t)stream);
+  if (v.tile >= 0 && z_stride > kTileStride) return Q8_EUNSUPPORTED;
+  if (v.tile >= 0) return linear_tile(p, y_dev, type, v.tile, (hipStream_t)stream);
+  return with_type(type, [&](auto v) { return launch_any_rows(p, static_cast<decltype(v)*>(y_dev), (hipStream_t)stream); });
+}
+
+extern "C" int q8_linear_int8(const int8_t* z_x_dev, size_t z_stride, const float* q_x_dev, size_t M, int N, int K,
+                              const void* packed_dev, const float* q_w_dev, const float* bias_dev, void* y_dev,
+                              int type, size_t y_stride, void* stream) {
+  return q8_linear_int8_variant(z_x_dev, z_stride, q_x_dev, M, N, K, packed_dev, q_w_dev, bias_dev, y_dev, type, y_stride,
+                                -1, stream);
 }
 
 extern "C" size_t q8_linear_workspace_bytes(size_t M, int N, int K) {
@@ -222,6 +252,11 @@ extern "C" int q8_linear(const void* x_dev, int x_type, size_t x_stride, size_t 
   Q8_REQUIRE(q8_aligned(workspace, 256) && q8_aligned(x_dev, type_bytes(x_type)) && q8_aligned(packed_dev, 16) &&
                  q8_aligned(q_w_dev, 4) && q8_aligned(bias_dev, 4) && q8_aligned(y_dev, type_bytes(y_type)), Q8_EALIGN);
   Q8_REQUIRE(workspace_bytes >= q8_linear_workspace_bytes(M, N, K), Q8_EWORKSPACE);
+  if (linear_rows_take_real((int)M, K)) {
+    const LinearParams p{nullptr, nullptr, static_cast<const int8_t*>(packed_dev), q_w_dev, bias_dev, 0, y_stride, (int)M,
+                         N, K, (int)(round_up(K, kPackK) / kPackK)};
+    return linear_rows_real(p, x_dev, x_type, x_stride, y_dev, y_type, (hipStream_t)stream);
+  }
   int8_t* const z = static_cast<int8_t*>(workspace);
   float* const q_x = reinterpret_cast<float*>(z + codes_bytes(M, K));
   const size_t z_stride = round_up(K, 16);

@@ -1,0 +1,214 @@
+// The 8-bit linear layer's product where rows are many: y[m][n] = tail(sum_k z_x[m][k] z_w[n][k]).
+//
+// A workgroup owns a tile of BN channels x BM rows and walks over K in steps of 64 bytes: both operands go from memory
+// to LDS without registers in between (a ring of STAGES steps, one bare barrier a step), and a wavefront multiplies its
+// TN x TM squares of 32 x 32 on v_mfma_i32_32x32x32_i8.  Packed weights lie in the order in which a wavefront reads
+// them; rows of activations are 64 bytes in LDS with their 16-byte chunks swapped (swz) so that neither meets a
+// bank twice.
+#include "q8_linear.h"
+#include <type_traits>
+
+namespace {
+
+using namespace q8;
+
+constexpr int kXcds = 8;
+
+template <int WN_, int WM_, int TN_, int TM_, int STAGES_>
+struct Shape {
+  static constexpr int WN = WN_, WM = WM_, TN = TN_, TM = TM_, STAGES = STAGES_;
+  static constexpr int NW = WN * WM, BN = WN * TN * 32, BM = WM * TM * 32;
+  static constexpr int A_BYTES = BN * kPackK, B_BYTES = BM * kPackK, STAGE_BYTES = A_BYTES + B_BYTES;
+  static constexpr int LDS_BYTES = STAGES * STAGE_BYTES;
+  static constexpr int A_LOADS = BN / 16 / NW, B_LOADS = BM / 16 / NW, LOADS = A_LOADS + B_LOADS;
+  static_assert(A_LOADS * NW * 16 == BN && B_LOADS * NW * 16 == BM, "every wavefront issues the same loads");
+  static_assert((STAGES - 2) * LOADS < 64, "vmcnt is 6 bits");
+};
+
+template <typename Sh, typename Y, bool VEC>
+__global__ __launch_bounds__(Sh::NW * 64) void linear_tile_kernel(const LinearParams p, Y* __restrict__ y, int tiles_n,
+                                                                  int tiles_m) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int TN = Sh::TN, TM = Sh::TM, NW = Sh::NW, STAGES = Sh::STAGES, LOADS = Sh::LOADS;
+  extern __shared__ __attribute__((aligned(1024))) int8_t lds[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave_n = wave % Sh::WN, wave_m = wave / Sh::WN;
+
+  // ---- the tile: an XCD takes a contiguous run of them, eight rows of tiles at a time
+  const int total = tiles_n * tiles_m, per = (total + kXcds - 1) / kXcds;
+  const int id = blockIdx.x % kXcds * per + blockIdx.x / kXcds;
+  if (blockIdx.x / kXcds >= per || id >= total) return;
+  constexpr int GROUP = 8;
+  const int group = id / (GROUP * tiles_n), in = id - group * (GROUP * tiles_n);
+  const int rows = min(GROUP, tiles_m - group * GROUP);
+  const int n0 = in / rows * Sh::BN, m0 = (group * GROUP + in % rows) * Sh::BM;
+
+  // ---- loaders.  Weights: blocks of 16 rows as they lie.  Activations: lane l takes row l / 4, slot l % 4.
+  const int nk = p.ksteps;
+  const int8_t* a_base = p.w + (size_t)(n0 / kPackN) * nk * 1024;
+  const int8_t* b_base = p.z + (size_t)m0 * p.z_stride;
+  const size_t a_all = ((size_t)((p.N + kPackN - 1) / kPackN) - n0 / kPackN) * nk * 1024;
+  int a_bytes = (int)(a_all < 0x7fffffffu ? a_all : 0x7fffffffu);
+  const size_t b_all = (size_t)(p.M - m0 - 1) * p.z_stride + ((p.K + 15) & ~15);
+  int b_bytes = (int)(b_all < 0x7fffffffu ? b_all : 0x7fffffffu);
+  int a_off[Sh::A_LOADS], b_off[Sh::B_LOADS];
+#pragma unroll
+  for (int i = 0; i < Sh::A_LOADS; ++i) a_off[i] = (wave + NW * i) * nk * 1024 + lane * 16;
+#pragma unroll
+  for (int i = 0; i < Sh::B_LOADS; ++i) {
+    const int row = (wave + NW * i) * 16 + (lane >> 2);
+    b_off[i] = row * (int)p.z_stride + swz<4>(row, lane & 3) * 16;
+  }
+  int issued = 0;
+  auto issue = [&](int stage) __attribute__((always_inline)) {
+    const bool in_k = issued < nk;
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void*)a_base, 0, in_k ? a_bytes : 0, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc((void*)b_base, 0, in_k ? b_bytes : 0, 0x00020000);
+    int8_t* to = lds + stage * Sh::STAGE_BYTES;
+#pragma unroll
+    for (int i = 0; i < Sh::A_LOADS; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          ra, (__attribute__((address_space(3))) void*)(to + (wave + NW * i) * 1024), 16, a_off[i], 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < Sh::B_LOADS; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rb, (__attribute__((address_space(3))) void*)(to + Sh::A_BYTES + (wave + NW * i) * 1024), 16, b_off[i], 0, 0, 0);
+    // (a row's last step may end behind its last byte: only as far as the next row, or it reads as zeros)
+    ++issued;
+    a_base += 1024;
+    a_bytes -= 1024;
+    b_base += kPackK;
+    b_bytes -= kPackK;
+  };
+
+  v16i acc[TN][TM];
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+
+  // ---- operand fragments: half h of a step is the chunks 2 h and 2 h + 1 of its rows
+  const int half = lane >> 5, ch = row_to_channel(lane & 31), row = lane & 31;
+  const int a_frag = wave_n * TN * 2048 + (ch >> 4) * 1024 + (ch & 15) * 16 + half * 256;
+  const int b_frag = Sh::A_BYTES + (wave_m * TM * 32 + row) * kPackK + swz<4>(row, half) * 16;
+  v4i af[2][TN], bf[2][TM];
+#pragma unroll
+  for (int i = 0; i < TN; ++i) af[1][i] = v4i{0, 0, 0, 0};
+#pragma unroll
+  for (int j = 0; j < TM; ++j) bf[1][j] = v4i{0, 0, 0, 0};
+  auto load_half = [&](const int8_t* stage, auto h_c) __attribute__((always_inline)) {
+    constexpr int h = decltype(h_c)::value;
+#pragma unroll
+    for (int i = 0; i < TN; ++i) af[h][i] = *reinterpret_cast<const v4i*>(stage + a_frag + i * 2048 + h * 512);
+#pragma unroll
+    for (int j = 0; j < TM; ++j) bf[h][j] = *reinterpret_cast<const v4i*>(stage + (b_frag ^ (h * 32)) + j * 2048);
+  };
+  auto multiply = [&](auto h_c) __attribute__((always_inline)) {
+    constexpr int h = decltype(h_c)::value;
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+      for (int j = 0; j < TM; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(af[h][i], bf[h][j], acc[i][j], 0, 0, 0);
+  };
+  using std::integral_constant;
+  constexpr integral_constant<int, 0> first{};
+  constexpr integral_constant<int, 1> second{};
+
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s) issue(s);
+  __builtin_amdgcn_s_waitcnt(0xc07f);                // scalar loads are settled before the loop
+  int stage = 0;
+  for (int k = 0; k < nk; ++k) {
+    wait_vmcnt<(STAGES - 2) * LOADS>();
+    __builtin_amdgcn_s_waitcnt(0xc07f);              // this wavefront's reads of the step before have returned
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const int8_t* at = lds + stage * Sh::STAGE_BYTES;
+    load_half(at, first);
+    issue(stage == 0 ? STAGES - 1 : stage - 1);
+    multiply(second);                                // of the step before (zeros at first)
+    load_half(at, second);
+    multiply(first);
+    // reads of the first half; then products with a load to LDS behind each, and the second half's reads between them
+    __builtin_amdgcn_sched_group_barrier(0x100, TN + TM, 0);
+    int loads = LOADS, reads = TN + TM;
+#pragma unroll
+    for (int g = 0; g < 2 * TN * TM; ++g) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if (loads > 0) {
+        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        --loads;
+      }
+      if (reads > 0) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        --reads;
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+  }
+  multiply(second);
+  wait_vmcnt<0>();                                   // (loads behind the last step write zeros into this LDS)
+
+  // ---- tail: a lane holds 16 consecutive channels of a row
+#pragma unroll
+  for (int j = 0; j < TM; ++j) {
+    const int m = m0 + (wave_m * TM + j) * 32 + row;
+    if (m >= p.M) continue;
+    const float q = p.q_x[m];
+#pragma unroll
+    for (int i = 0; i < TN; ++i) {
+      int v[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = acc[i][j][e];
+      const int n = n0 + (wave_n * TN + i) * 32 + 16 * half;
+      if (n < p.N) finish_outputs<16, VEC>(p, y, m, n, q, v);
+    }
+  }
+#endif
+}
+
+template <typename Sh, typename Y, bool VEC>
+int launch(const LinearParams& p, Y* y, hipStream_t stream) {
+  if constexpr (Sh::LDS_BYTES > 65536) {
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&linear_tile_kernel<Sh, Y, VEC>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, Sh::LDS_BYTES);
+    if (attr != hipSuccess) return Q8_EHIP;
+  }
+  const long tn = (p.N + Sh::BN - 1) / Sh::BN, tm = (p.M + Sh::BM - 1) / Sh::BM;
+  Q8_REQUIRE(tn * tm <= 0x7ffffff0l, Q8_EUNSUPPORTED);
+  const unsigned blocks = (unsigned)((tn * tm + kXcds - 1) / kXcds * kXcds);
+  linear_tile_kernel<Sh, Y, VEC><<<blocks, Sh::NW * 64, Sh::LDS_BYTES, stream>>>(p, y, (int)tn, (int)tm);
+  return q8_launch_status();
+}
+
+template <typename Sh>
+int launch_any(const LinearParams& p, void* y, int type, hipStream_t stream) {
+  return with_type(type, [&](auto one) {
+    using Y = decltype(one);
+    const bool vec = q8_aligned(y, 16) && p.y_stride * sizeof(Y) % 16 == 0;
+    return vec ? launch<Sh, Y, true>(p, static_cast<Y*>(y), stream) : launch<Sh, Y, false>(p, static_cast<Y*>(y), stream);
+  });
+}
+
+}  // namespace
+
+namespace q8 {
+
+int linear_tile(const LinearParams& p, void* y, int type, int variant, hipStream_t stream) {
+  switch (variant) {
+    case 0: return launch_any<Shape<2, 2, 1, 1, 6>>(p, y, type, stream);      // 64 channels x 64 rows
+    case 1: return launch_any<Shape<2, 2, 2, 1, 4>>(p, y, type, stream);      // 128 x 64
+    case 2: return launch_any<Shape<2, 2, 2, 2, 4>>(p, y, type, stream);      // 128 x 128
+    case 3: return launch_any<Shape<2, 4, 2, 1, 6>>(p, y, type, stream);      // 128 x 128, eight wavefronts
+    case 4: return launch_any<Shape<2, 4, 4, 2, 4>>(p, y, type, stream);      // 256 x 256
+  }
+  return Q8_EUNSUPPORTED;
+}
+
+}  // namespace q8

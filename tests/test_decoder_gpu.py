@@ -100,6 +100,43 @@ def test_product(B, kind, M, N, K):
         assert torch.equal(y.cpu(), want)
 
 
+@pytest.mark.parametrize("M,N,K", [(1, 3, 5), (40, 70, 64), (16, 16, 128), (65, 257, 200), (130, 100, 1100), (300, 520, 720),
+                                   (513, 384, 449)])
+def test_every_build_of_the_product(B, M, N, K):
+    rng = _rng(M, N, K, 3)
+    z_w, q_w, bias = _weights(rng, N, K)
+    z = rng.integers(-128, 128, (M, K), dtype=np.int8)
+    q_x = (rng.random(M) + 0.1).astype(np.float32)
+    packed = B.linear_pack(torch.from_numpy(z_w).cuda())
+    codes = torch.full((M, -(-K // 16) * 16), -77, dtype=torch.int8, device="cuda")
+    codes[:, :K] = torch.from_numpy(z).cuda()
+    dev = [torch.from_numpy(v).cuda() for v in (q_x, q_w, bias)]
+    names = [B.lib.q8_linear_variant_name(v).decode() for v in range(B.lib.q8_linear_num_variants())]
+    assert len(set(names)) == len(names) >= 2
+    for kind in sorted(TYPES):
+        want = P.linear(z, q_x, z_w, q_w, bias, TYPES[kind])
+        for v in range(len(names)):
+            out = torch.full((M + 2, N), 3.0, dtype=TYPES[kind], device="cuda")
+            B.linear_int8(codes[:, :K], dev[0], packed, dev[1], dev[2], out=out[1:-1], variant=v)
+            assert torch.equal(out[1:-1].cpu(), want), names[v]
+            assert bool((out[0] == 3).all()) and bool((out[-1] == 3).all()), names[v]
+
+
+def test_product_of_rows_far_apart(B):
+    """Rows more than 4 MiB apart: a tile's offsets would pass 32 bits."""
+    M, N, K = 40, 50, 100
+    rng = _rng(21)
+    z_w, q_w, _ = _weights(rng, N, K)
+    z = rng.integers(-128, 128, (M, K), dtype=np.int8)
+    stride = (1 << 26) + 16
+    whole = torch.empty((M - 1) * stride + 112, dtype=torch.int8, device="cuda")
+    codes = torch.as_strided(whole, (M, K), (stride, 1), 0)
+    codes.copy_(torch.from_numpy(z))
+    y = B.linear_int8(codes, torch.ones(M, device="cuda"), B.linear_pack(torch.from_numpy(z_w).cuda()),
+                      torch.from_numpy(q_w).cuda(), dtype=torch.float32)
+    assert torch.equal(y.cpu(), P.linear(z, np.ones(M, np.float32), z_w, q_w, None, torch.float32))
+
+
 def test_product_of_the_largest_sums(B):
     """128 * 128 * 131071 just fits the accumulator, on both sides."""
     K = 131071

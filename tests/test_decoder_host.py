@@ -53,6 +53,8 @@ def _linear(x=A, kind=0, xs=64, M=4, N=8, K=64, w=A, q_w=A, bias=None, y=A, yk=0
 
 
 def test_products_refused():
+    assert L.q8_linear_int8_variant(A, 64, A, 4, 8, 64, A, A, None, A, 0, 8, L.q8_linear_num_variants(), None) == EINVAL
+    assert L.q8_linear_variant_name(-1) == L.q8_linear_variant_name(10 ** 6) == b"unsupported"
     for f in (_product, _linear):
         assert f(M=0) == OK == f(N=0)
         for bad in (dict(w=None), dict(q_w=None), dict(y=None), dict(K=0), dict(N=-1), dict(ys=7), dict(kind=5)):
