@@ -239,6 +239,9 @@ _q8call.bind(_ptr, _device, _raw_stream, ConvDesc, torch.int8, torch.int32, torc
                  lib.q8_conv_int8, lib.q8_conv_u8, lib.q8_conv_int8_per_channel,
                  lib.q8_conv_int8_real_output, lib.q8_conv_f32_observed_spread, lib.q8_calibrate_maxabs,
                  lib.q8_quantize, lib.q8_dequantize)))
+_q8call.bind_rows(*(C.cast(f, C.c_void_p).value for f in (
+    lib.q8_quantize_rows, lib.q8_linear_int8_variant, lib.q8_linear, lib.q8_linear_packed_bytes, lib.q8_page_tables,
+    lib.q8_kv4_write, lib.q8_kv4_read, lib.q8_kv4_attend)))
 
 
 def calibrate_maxabs(x, maxabs):
@@ -647,28 +650,6 @@ def pool_f32(x, mode, R, S, stride, pad, Ho, Wo, out=None, out_c_off=0):
 
 
 # ------------------------------------------------------- a decoder's attention block in 8 and 4 bits
-_VALUE_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
-
-
-def _value_type(t):
-    assert t.dtype in _VALUE_TYPES, t.dtype
-    return _VALUE_TYPES[t.dtype]
-
-
-def _rows(t, cols=None):
-    """A device tensor of two dimensions with dense rows -> (address, elements between rows)."""
-    assert t.is_cuda and t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1), "device tensor, dense rows"
-    assert cols is None or t.shape[1] == cols, (t.shape, cols)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
-
-
-def _heads(t):
-    """A device tensor [tokens, heads, D] with dense heads -> (address, elements between tokens, between heads)."""
-    assert t.is_cuda and t.dim() == 3 and (t.shape[2] <= 1 or t.stride(2) == 1), "device tensor, dense heads"
-    return (t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2],
-            t.stride(1) if t.shape[1] > 1 else t.shape[2])
-
-
 def quantize_rows(x, out=None, factors=None):
     """x [M, K] (fp32, fp16 or bf16) -> (int8 codes [M, K], fp32 factors [M]): Eq. Q with p = 7 and a factor for
     each row, from the row itself.  ``out``: rows a multiple of 16 apart, as made here."""
@@ -677,22 +658,8 @@ def quantize_rows(x, out=None, factors=None):
         out = torch.empty((M, -(-K // 16) * 16), dtype=torch.int8, device=x.device)[:, :K]
     if factors is None:
         factors = torch.empty(M, dtype=torch.float32, device=x.device)
-    assert out.dtype is torch.int8 and out.shape == x.shape and factors.numel() == M
-    xp, xs = _rows(x)
-    zp, zs = _codes(out)
-    _check(lib.q8_quantize_rows(xp, _value_type(x), M, K, xs, zp, zs, _ptr(factors, torch.float32), _stream()))
+    _check(_q8call.quantize_rows(x, out, factors))
     return out, factors
-
-
-def _codes(z):
-    """Codes [M, K]: as _rows, and the storage holds the last row up to a multiple of 16 bytes."""
-    p, stride = _rows(z)
-    K16 = -(-z.shape[1] // 16) * 16
-    if z.shape[0] == 1:
-        stride = max(z.stride(0), K16)
-    end = z.storage_offset() + (z.shape[0] - 1) * stride + K16
-    assert z.shape[0] == 0 or end <= z.untyped_storage().nbytes(), "codes: rows to a multiple of 16 bytes"
-    return p, stride if z.shape[0] > 1 else K16
 
 
 def linear_pack(z_w):
@@ -711,43 +678,23 @@ def linear_workspace(M, N, K, device="cuda"):
     return torch.empty(lib.q8_linear_workspace_bytes(M, N, K), dtype=torch.uint8, device=device)
 
 
-def _linear_args(K, packed, q_w, bias, out):
-    N = q_w.numel()
-    assert packed.numel() >= lib.q8_linear_packed_bytes(N, K), "weights packed for other sizes"
-    assert bias is None or bias.numel() == N
-    return (_ptr(packed, torch.int8), _ptr(q_w, torch.float32), _ptr(bias, torch.float32), _rows(out, N)[0],
-            _value_type(out), _rows(out)[1])
-
-
 def linear_int8(z_x, q_x, packed, q_w, bias=None, out=None, dtype=torch.bfloat16, variant=-1):
     """Codes [M, K] and their rows' factors (quantize_rows) times packed weights: [M, N] real values.  ``variant`` >= 0
     (tests, tuning): that build of the kernel."""
-    M, K = z_x.shape
-    assert z_x.dtype is torch.int8 and q_x.numel() == M
     if out is None:
-        out = torch.empty((M, q_w.numel()), dtype=dtype, device=z_x.device)
-    assert out.shape[0] == M
-    zp, zs = _codes(z_x)
-    w, qw, b, y, ytype, ys = _linear_args(K, packed, q_w, bias, out)
-    _check(lib.q8_linear_int8_variant(zp, zs, _ptr(q_x, torch.float32), M, q_w.numel(), K, w, qw, b, y, ytype, ys, variant,
-                                      _stream()))
+        out = torch.empty((z_x.shape[0], q_w.numel()), dtype=dtype, device=z_x.device)
+    _check(_q8call.linear_int8(z_x, q_x, packed, q_w, bias, out, variant))
     return out
 
 
 def linear(x, packed, q_w, bias=None, out=None, workspace=None):
     """The 8-bit linear layer on real rows x [M, K]: quantize_rows, then linear_int8.  ``out``: [M, N], x's type
     unless given."""
-    M, K = x.shape
-    N = q_w.numel()
     if out is None:
-        out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+        out = torch.empty((x.shape[0], q_w.numel()), dtype=x.dtype, device=x.device)
     if workspace is None:
-        workspace = linear_workspace(M, N, K, x.device)
-    assert out.shape[0] == M
-    xp, xs = _rows(x)
-    w, qw, b, y, ytype, ys = _linear_args(K, packed, q_w, bias, out)
-    _check(lib.q8_linear(xp, _value_type(x), xs, M, N, K, w, qw, b, y, ytype, ys, _ptr(workspace, torch.uint8),
-                         workspace.numel(), _stream()))
+        workspace = linear_workspace(x.shape[0], q_w.numel(), x.shape[1], x.device)
+    _check(_q8call.linear(x, packed, q_w, bias, out, workspace))
     return out
 
 
@@ -760,12 +707,7 @@ def page_tables(lengths, added, page, free_pages, table, slots, positions, start
     starts = torch.empty(n + 1, dtype=i32, device=lengths.device) if starts is None else starts
     grown = torch.empty(n, dtype=i32, device=lengths.device) if grown is None else grown
     counts = torch.empty(3, dtype=i32, device=lengths.device) if counts is None else counts
-    assert added.numel() == n and table.dtype is i32 and table.shape[0] == n and slots.numel() == positions.numel()
-    assert starts.numel() == n + 1 and grown.numel() == n and counts.numel() == 3
-    tp, ts = _rows(table)
-    _check(lib.q8_page_tables(_ptr(lengths, i32), _ptr(added, i32), n, page, _ptr(free_pages, i32), free_pages.numel(),
-                              tp, table.shape[1], ts, _ptr(slots, torch.int64), _ptr(positions, i32), slots.numel(),
-                              _ptr(starts, i32), _ptr(grown, i32), _ptr(counts, i32), _stream()))
+    _check(_q8call.page_tables(lengths, added, page, free_pages, table, slots, positions, starts, grown, counts))
     return dict(table=table, slots=slots, positions=positions, starts=starts, lengths=grown, counts=counts)
 
 
@@ -776,35 +718,21 @@ def kv4_cache(n_pages, heads, page, D, device="cuda"):
     return torch.zeros((n_pages, heads, page // 16, 18 * D), dtype=torch.uint8, device=device)
 
 
-def _cache(cache):
-    """-> (address, pages, heads, tokens of a page, D)."""
-    assert cache.dim() == 4 and cache.shape[3] % 18 == 0, cache.shape
-    return _ptr(cache, torch.uint8), cache.shape[0], cache.shape[1], cache.shape[2] * 16, cache.shape[3] // 18
-
-
-def _tokens(k, v, slots, heads, D):
-    assert k.shape == v.shape == (slots.numel(), heads, D) and k.dtype is v.dtype, (k.shape, v.shape, heads, D)
-    (kp, ks, kh), (vp, vs, vh) = _heads(k), _heads(v)
-    return kp, vp, _value_type(k), k.shape[0], (ks, kh, vs, vh)
-
-
 def kv4_write(cache, k, v, slots):
     """Keys and values [T, heads, D] of T tokens into their slots (int64; -1: nowhere)."""
-    cp, n, heads, page, D = _cache(cache)
-    kp, vp, kind, T, strides = _tokens(k, v, slots, heads, D)
-    _check(lib.q8_kv4_write(kp, vp, kind, T, heads, D, *strides, _ptr(slots, torch.int64), cp, n, page, _stream()))
+    _check(_q8call.kv4_write(cache, k, v, slots))
     return cache
 
 
 def kv4_read(cache, slots, k_out=None, v_out=None, dtype=torch.bfloat16):
     """What the cache holds in these slots (zeros outside it): keys and values [T, heads, D]."""
-    cp, n, heads, page, D = _cache(cache)
+    assert cache.dim() == 4, cache.shape
+    shape = (slots.numel(), cache.shape[1], cache.shape[3] // 18)
     if k_out is None:
-        k_out = torch.empty((slots.numel(), heads, D), dtype=dtype, device=cache.device)
+        k_out = torch.empty(shape, dtype=dtype if v_out is None else v_out.dtype, device=cache.device)
     if v_out is None:
-        v_out = torch.empty((slots.numel(), heads, D), dtype=k_out.dtype, device=cache.device)
-    kp, vp, kind, T, strides = _tokens(k_out, v_out, slots, heads, D)
-    _check(lib.q8_kv4_read(cp, n, page, _ptr(slots, torch.int64), T, heads, D, kp, vp, kind, *strides, _stream()))
+        v_out = torch.empty(shape, dtype=k_out.dtype, device=cache.device)
+    _check(_q8call.kv4_read(cache, slots, k_out, v_out))
     return k_out, v_out
 
 
@@ -820,20 +748,8 @@ def kv4_attend(q, cache, table, lengths, starts=None, scale=None, window=0, out=
     """Attention of the new tokens' queries q [T, query heads, D] over the cache: rows starts[b] .. starts[b + 1] are
     the last of the lengths[b] tokens of request b (``starts`` None: one row per request).  Row at position i sees
     the keys up to i, with ``window`` the last ``window`` of them."""
-    cp, n, heads, page, D = _cache(cache)
-    T, q_heads, _ = q.shape
-    assert q.shape[2] == D and q_heads % heads == 0, (q.shape, cache.shape)
     if out is None:
-        out = torch.empty((T, q_heads, D), dtype=q.dtype, device=q.device)
-    assert out.shape == q.shape and out.dtype is q.dtype
-    requests = lengths.numel()
-    assert table.dtype is torch.int32 and table.shape[0] == requests
-    assert T == requests if starts is None else starts.numel() == requests + 1
-    qp, qs, qh = _heads(q)
-    op, os_, oh = _heads(out)
-    tp, ts = _rows(table)
-    _check(lib.q8_kv4_attend(qp, _value_type(q), T, heads, q_heads // heads, D, qs, qh, cp, n, page, tp,
-                             table.shape[1], ts, _ptr(lengths, torch.int32), _ptr(starts, torch.int32), requests,
-                             D ** -0.5 if scale is None else scale, window, op, os_, oh,
-                             _ptr(workspace, torch.uint8), 0 if workspace is None else workspace.numel(), _stream()))
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _check(_q8call.kv4_attend(q, cache, table, lengths, starts, q.shape[2] ** -0.5 if scale is None else scale, window,
+                              out, workspace))
     return out
