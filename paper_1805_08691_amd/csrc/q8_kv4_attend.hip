@@ -12,7 +12,9 @@
 // so that a lane's 16 probabilities belong to the 16 tokens whose value codes it loads: nothing is exchanged
 // between lanes but the maximum.
 // The key axis is split over workgroups where columns are few; kv4_join_kernel adds the parts.
+#include "q8_conv_common.h"
 #include "q8_kv4.h"
+#include <type_traits>
 #pragma clang fp contract(fast)
 
 namespace {
@@ -20,21 +22,26 @@ namespace {
 using namespace q8;
 
 typedef float f4 __attribute__((ext_vector_type(4)));
+typedef short s2 __attribute__((ext_vector_type(2)));
 
 constexpr int kCols = 16;              // columns of a tile
 constexpr int kStep = 64;              // keys of a wavefront's step
 constexpr int kWaves = 4;
+constexpr int kTarget = 512;           // parts that the keys are cut into where tiles are few
+constexpr int kMinSteps = 8;           // steps of a part, at least
+constexpr int kMaxTiles = 256;         // beyond them nothing is cut: a thread each
 
 struct AttendParams {
   const uint8_t* __restrict__ cache;
   const int* __restrict__ table;
   const int* __restrict__ lengths;
   const int* __restrict__ starts;      // null: request b is row b
-  float* __restrict__ parts;           // workspace of the split, null: one part
+  float* __restrict__ parts;           // workspace of the split, null: none is split
+  int4* __restrict__ cuts;             // kTarget lines (tile, head, first part's place, parts), and their number
   size_t q_stride, q_head, o_stride, o_head, table_stride;
   long n_pages;
   int T, B, H, ratio, width, shift;    // shift: page = 16 << shift tokens
-  int tiles, splits, window;
+  int tiles, window;
   float scale_log2;                    // scale * log2(e)
 };
 
@@ -81,215 +88,364 @@ __device__ __forceinline__ bool find_tile(const AttendParams& p, int w, Tile* t)
   return true;
 }
 
-// Steps of a part, and how many parts hold any (at least one: it writes the zeros of empty rows).
-__device__ __forceinline__ int steps_per_part(const Tile& t, int splits) {
-  return max((t.steps + splits - 1) / splits, kWaves);
+// The split of the key axis.  The steps of all tiles and heads over kTarget are what a part should hold (kMinSteps at
+// least); a tile of more steps is cut into equal parts of no more.  Every workgroup works this out for itself from the
+// lengths, a tile to a thread.  Parts of cut tiles have a place in the workspace, no more than 2 kTarget of them (a cut
+// tile has more than `per` steps), and the cut tiles' heads, no more than kTarget, a line in the list that the
+// joining launch goes by.
+struct Part {
+  int tile, head, part, parts, slot;   // slot: of the tile's first part, in units of H places
+  int step0, step1;
+};
+
+__device__ __forceinline__ void set_part(Part* a, const Tile& t) {
+  const int each = (t.steps + a->parts - 1) / a->parts;
+  a->step0 = a->part * each;
+  a->step1 = min(a->step0 + each, t.steps);
 }
 
-// Four half bytes of each half of w, in the order 0 4 2 6 (from = the low half bytes) or 1 5 3 7, as binary16 codes.
-__device__ __forceinline__ h2 codes_low(unsigned w) {
-  const unsigned b = (w & 0x000f000fu) | 0x64006400u;              // 1024 + u
-  return __builtin_bit_cast(h2, b) - h2{1032.0f16, 1032.0f16};
-}
-__device__ __forceinline__ h2 codes_high(unsigned w) {
-  const unsigned b = (w & 0x00f000f0u) | 0x64006400u;              // 1024 + 16 u
-  return __builtin_elementwise_fma(__builtin_bit_cast(h2, b), h2{0.0625f16, 0.0625f16}, h2{-72.0f16, -72.0f16});
+// The part of workgroup `id`; false: there is none.
+__device__ bool find_part(const AttendParams& p, int id, Part* a) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int at = id / p.H, head = id - at * p.H;
+  *a = Part{at, head, 0, 1, 0, 0, 0};
+  if (!p.parts) return at < p.tiles;
+  __shared__ long sums[2][kWaves];
+  __shared__ int found[5];
+  Tile t;
+  const int steps = tid < p.tiles && find_tile(p, tid, &t) ? max(t.steps, 1) : 0;
+  long total = steps;
+  for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off, 64);
+  if (lane == 0) sums[0][wave] = total;
+  if (tid == 0) found[4] = 0;
+  __syncthreads();
+  total = ((sums[0][0] + sums[0][1]) + (sums[0][2] + sums[0][3])) * p.H;
+  const int per = (int)max((total + kTarget - 1) / kTarget, (long)kMinSteps);
+  // the sums before each tile: parts; those of cut tiles (16 bits up); cut tiles (40 bits up)
+  const long n = steps ? (steps + per - 1) / per : 0, own = n > 1 ? n | n << 20 | 1l << 40 : n;
+  long v = own;
+  for (int off = 1; off < 64; off <<= 1) {
+    const long o = __shfl_up(v, off, 64);
+    if (lane >= off) v += o;
+  }
+  if (lane == 63) sums[1][wave] = v;
+  __syncthreads();
+  for (int u = 0; u < wave; ++u) v += sums[1][u];
+  const long before = v - own;
+  const int first = (int)(before & 0xfffff), slot = (int)(before >> 20 & 0xfffff), rank = (int)(before >> 40);
+  if (at >= first && at < first + n) {
+    found[0] = tid, found[1] = at - first, found[2] = (int)n, found[3] = slot, found[4] = 1;
+    if (n > 1 && at == first) p.cuts[rank * p.H + head] = int4{tid, head, slot, (int)n};
+  }
+  if (id == 0 && tid == kMaxTiles - 1) p.cuts[kTarget] = int4{(int)(v >> 40) * p.H, 0, 0, 0};
+  __syncthreads();
+  a->tile = found[0], a->part = found[1], a->parts = found[2], a->slot = found[3];
+  return found[4] != 0;
 }
 
+// Half bytes u as binary16: the low ones of w's bytes 0 and 2 as 1024 + u, the high ones as 1024 + 16 u, one instruction
+// for two (mask and pattern in registers: one instruction takes them, not two literals).
+struct Unpack {
+  unsigned low_mask = 0x000f000fu, high_mask = 0x00f000f0u, one = 0x64006400u;
+  __device__ __forceinline__ Unpack() { asm volatile("" : "+s"(low_mask), "+s"(high_mask), "+v"(one)); }
+  __device__ __forceinline__ h2 low(unsigned w) const { return __builtin_bit_cast(h2, (w & low_mask) | one); }
+  __device__ __forceinline__ h2 high(unsigned w) const { return __builtin_bit_cast(h2, (w & high_mask) | one); }
+};
 __device__ __forceinline__ h8 join4(h2 a, h2 b, h2 c, h2 d) {
   return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// The largest of the four lanes that hold a column (lane % 16).
+__device__ __forceinline__ float column_max(float v) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// A wavefront's step in LDS, 64 keys: the codes of its four sixteens' keys (32 bytes between them: the four rows that one
+// LDS access serves then meet different banks), of their values, and their factors.
+template <int G>
+struct Stage {
+  static constexpr int SIXTEEN = 576 * G, CODES = 256 * G, FACTORS = 64 * G;
+  static constexpr int K_PITCH = CODES + 32, V_AT = 4 * K_PITCH, F_AT = V_AT + 4 * CODES, SIZE = F_AT + 4 * FACTORS;
+  static constexpr int LOADS = 4 * (2 * ((CODES + 1023) / 1024) + 1);                      // of 16 bytes a lane
+};
+
+[[maybe_unused]] constexpr float kLift = 10.0f;      // probabilities times 2^10 / (a power of two above the values' factors)
+
 template <int G, typename V>
-__global__ __launch_bounds__(256) void kv4_attend_kernel(const AttendParams p, const V* __restrict__ q,
-                                                         V* __restrict__ out) {
+__global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const AttendParams p, const V* __restrict__ q,
+                                                                         V* __restrict__ out) {
+#if defined(__HIP_DEVICE_COMPILE__)
   constexpr int D = 32 * G, CT = 2 * G;                 // channels, tiles of 16 of them
-  extern __shared__ float shared[];                     // [4 waves][16 columns][D], then maxima and sums
+  using St = Stage<G>;
+  extern __shared__ __attribute__((aligned(16))) char shared[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, j = lane >> 4;
-  const int head = blockIdx.x % p.H, w = blockIdx.x / p.H % p.tiles, split = blockIdx.x / p.H / p.tiles;
+  const Unpack un;
+  Part a;
   Tile t;
-  if (!find_tile(p, w, &t)) return;
-  const int per = steps_per_part(t, p.splits);
-  const int step0 = split * per, step1 = min(step0 + per, t.steps);
-  if (split > 0 && step0 >= t.steps) return;
+  if (!find_part(p, blockIdx.x, &a)) return;
+  a.tile = __builtin_amdgcn_readfirstlane(a.tile);
+  if (!find_tile(p, a.tile, &t)) return;
+  set_part(&a, t);
+  const int head = a.head, step0 = __builtin_amdgcn_readfirstlane(a.step0), step1 = __builtin_amdgcn_readfirstlane(a.step1);
+  const int last = min(t.lo + t.steps * kStep, t.len);         // keys of the tile end here
+  const int iterations = step0 + wave < step1 ? (step1 - step0 - wave + kWaves - 1) / kWaves : 0;
 
-  // ---- the column of this lane: its queries as the right operand, scaled to [1, 2) by a power of two
+  // ---- loads: lane l holds where sixteen l % 4 of iteration l / 4 (of 16) lies, bit l of `held` whether it is there
+  const int* __restrict__ table = p.table + t.b * p.table_stride;
+  long where = 0;
+  unsigned long held = 0;
+  auto find_sixteens = [&](int it0) {
+    const int s = step0 + wave + (it0 + (lane >> 2)) * kWaves, at = (t.lo >> 4) + s * 4 + (lane & 3);
+    int page = -1;
+    if (s < step1 && at * 16 < last) page = table[at >> p.shift];
+    const bool in = page >= 0 && page < p.n_pages;
+    where = in ? (((((long)page * p.H + head) << p.shift) + (at & ((1 << p.shift) - 1))) * St::SIXTEEN) : 0;
+    held = __ballot(in);
+  };
+  find_sixteens(0);
+  char* const stage = shared + wave * St::SIZE;
+  auto load = [&](__amdgpu_buffer_rsrc_t from, int at, int bytes, char* to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int l = 0; l < (bytes + 1023) / 1024; ++l)
+      if (l * 1024 + 1024 <= bytes || lane * 16 < bytes - l * 1024)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + l * 1024), 16,
+                                                 lane * 16 + at + l * 1024, 0, 0, 0);
+  };
+  unsigned there = 0;                                          // the iteration's sixteens that there are
+  auto issue = [&](int it) __attribute__((always_inline)) {
+    if (it > 0 && (it & 15) == 0) find_sixteens(it);
+    there = (unsigned)(held >> ((it & 15) * 4)) & 15u;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int l = (it & 15) * 4 + c;
+      const unsigned lo = __builtin_amdgcn_readlane((int)where, l), hi = __builtin_amdgcn_readlane((int)(where >> 32), l);
+      const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(
+          (void*)(p.cache + ((size_t)hi << 32 | lo)), 0, there >> c & 1u ? St::SIXTEEN : 0, 0x00020000);
+      load(from, 0, St::CODES, stage + c * St::K_PITCH);
+      load(from, 2 * St::CODES, St::FACTORS, stage + St::F_AT + c * St::FACTORS);
+      load(from, St::CODES, St::CODES, stage + St::V_AT + c * St::CODES);
+    }
+  };
+
+  // ---- the column of this lane: its queries as the right operand, scaled to [1, 2) by a power of two and turned so
+  // that scores grow with the products.  The high half bytes come 16 times as large: their queries are a 16th.
   const int col = t.first + r;
   const bool given = col < t.cols;
   const int tok = min(col, t.cols - 1) / p.ratio, qh = min(col, t.cols - 1) % p.ratio;
   const int pos = given ? t.len - t.n + tok : -1;       // (no key is at or before -1)
   const int from = p.window > 0 ? pos - p.window : -1;  // keys behind this one
-  const size_t q_head = (size_t)head * p.ratio + qh;
   h8 qf[G];
-  float col_scale;
+  float scale;
   {
-    const V* qr = q + (size_t)(t.row + tok) * p.q_stride + q_head * p.q_head + 8 * j;
+    const V* qr = q + (size_t)(t.row + tok) * p.q_stride + ((size_t)head * p.ratio + qh) * p.q_head + 8 * j;
     float v[G][8], top = 0.0f;
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      load_values<8, false>(qr + 32 * g, v[g]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[g][e]));
-    }
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const unsigned e2 = min(max(__float_as_uint(top) >> 23, 1u), 253u);
-    const float down = __uint_as_float((254u - e2) << 23);
-    col_scale = p.scale_log2 * __uint_as_float(e2 << 23);
-    constexpr int kOrder[8] = {0, 4, 2, 6, 1, 5, 3, 7};
+    for (int g = 0; g < G; ++g) load_values<8, false>(qr + 32 * g, v[g]);
+    if (iterations > 0) issue(0);
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) qf[g][e] = (_Float16)(v[g][kOrder[e]] * down);
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[g][e]));
+    top = column_max(top);
+    const unsigned e2 = min(max(__float_as_uint(top) >> 23, 1u), 253u);
+    const float down = copysignf(__uint_as_float((254u - e2) << 23), p.scale_log2);
+    scale = fmaxf(fabsf(p.scale_log2) * __uint_as_float(e2 << 23), 1e-30f);    // (no 0 times infinity)
+    constexpr int kKeyOrder[8] = {0, 4, 2, 6, 1, 5, 3, 7};
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) qf[g][e] = (_Float16)(v[g][kKeyOrder[e]] * (e < 4 ? down : down * 0.0625f));
   }
+  // steps whose every key is seen by every column: behind `clear0`, up to `clear1`
+  const int pos0 = t.len - t.n + t.first / p.ratio, pos1 = t.len - t.n + (min(t.first + kCols, t.cols) - 1) / p.ratio;
+  const int clear0 = p.window > 0 ? pos1 - p.window : -1, clear1 = pos0;
 
   f4 o[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c) o[c] = f4{0, 0, 0, 0};
-  float top = -__builtin_inff(), sum = 0.0f;
+  float top = -__builtin_inff(), ref = -__builtin_inff(), sum = 0.0f;     // ref: what sum and o are relative to, as a power of 2
+  float lift = kLift, limit = 0.0f;                     // kLift - log2 of the factors' power, and where it has to grow
+  constexpr _Float16 kLow = -1032.0f16, kHigh = -1152.0f16;
+  const h8 low_off = {kLow, kLow, kLow, kLow, kLow, kLow, kLow, kLow};
+  const h8 high_off = {kHigh, kHigh, kHigh, kHigh, kHigh, kHigh, kHigh, kHigh};
+  const h8 key_off = {kLow, kLow, kLow, kLow, kHigh, kHigh, kHigh, kHigh};
 
-  const int* __restrict__ table = p.table + t.b * p.table_stride;
-  const int last = min(t.lo + t.steps * kStep, t.len);         // keys of the tile end here
-  for (int s = step0 + wave; s < step1; s += kWaves) {
-    const int key0 = t.lo + s * kStep;
-    // ---- the sixteens: lane (r, j) loads keys of sixteen r / 4 and values of sixteen j
-    const int mine = (key0 >> 4) + (r >> 2);
-    int page = -1;
-    if (mine * 16 < last) page = table[mine >> p.shift];
-    const bool held = page >= 0 && page < p.n_pages;
-    const size_t at = (((size_t)(held ? page : 0) * p.H + head) << p.shift) + (mine & ((1 << p.shift) - 1));
-    const uint8_t* kb = p.cache + at * (576 * G);
-    const int other = j * 4;                                   // a lane whose sixteen is j
-    const bool v_held = __shfl((int)held, other, 64) != 0;
-    const size_t v_at = (size_t)__shfl((long)at, other, 64);
-    const uint8_t* vb = p.cache + v_at * (576 * G);
+  for (int it = 0; it < iterations; ++it) {
+    const int key0 = t.lo + (step0 + wave + it * kWaves) * kStep;
+    const bool more = it + 1 < iterations;
+    wait_vmcnt<0>();
+    asm volatile("" ::: "memory");
+    const bool clear = key0 > clear0 && key0 + kStep - 1 <= clear1 && there == 15u;
+    const char* const factors = stage + St::F_AT + j * St::FACTORS;
 
     // ---- S^T, keys 16 j + 4 tile + i in register i of tile `tile`
     float x[4][4];
 #pragma unroll
     for (int tile = 0; tile < 4; ++tile) {
-      const int tk = 4 * tile + (r & 3);
       unsigned kc[G];
-      _Float16 kf[G];
-      __builtin_memcpy(kc, __builtin_assume_aligned(kb + tk * 16 * G + j * 4 * G, 4), 4 * G);
-      __builtin_memcpy(kf, __builtin_assume_aligned(kb + 512 * G + tk * 2 * G, 2), 2 * G);
-      f4 acc = {0, 0, 0, 0};
+      _Float16 kf[4][G];
+      __builtin_memcpy(kc, __builtin_assume_aligned(stage + (r >> 2) * St::K_PITCH + (4 * tile + (r & 3)) * 16 * G + j * 4 * G, 4), 4 * G);
+      __builtin_memcpy(kf, __builtin_assume_aligned(factors + tile * 8 * G, 8), 8 * G);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[tile][i] = 0.0f;
 #pragma unroll
       for (int g = 0; g < G; ++g) {
-        const h2 f = {kf[g], kf[g]};
         const unsigned w8 = kc[g] >> 8;
-        const h8 a = join4(codes_low(kc[g]) * f, codes_low(w8) * f, codes_high(kc[g]) * f, codes_high(w8) * f);
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, qf[g], acc, 0, 0, 0);
-      }
+        f4 s = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_off, qf[g], f4{0, 0, 0, 0}, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_16x16x32_f16(join4(un.low(kc[g]), un.low(w8), un.high(kc[g]), un.high(w8)), qf[g], s, 0, 0, 0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int key = key0 + 16 * j + 4 * tile + i;
-        const bool seen = v_held && key <= pos && key > from;
-        x[tile][i] = seen ? acc[i] * col_scale : -__builtin_inff();
+        for (int i = 0; i < 4; ++i) x[tile][i] = __builtin_fmaf(s[i], (float)kf[i][g], x[tile][i]);
       }
     }
+    if (!clear) {
+      int upto = (there >> j & 1u) ? pos : -1, behind = from;
+      asm volatile("" : "+v"(upto), "+v"(behind));      // (a branch, not selects in every step)
+#pragma unroll
+      for (int tile = 0; tile < 4; ++tile)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = key0 + 16 * j + 4 * tile + i;
+          x[tile][i] = key <= upto && key > behind ? x[tile][i] : -__builtin_inff();
+        }
+    }
+    // ---- the values' factors.  What lies outside the keys that the rows see may be no number: it counts as zero.
+    // (Read twice, for their largest and for use: they would not fit the registers of three wavefronts a SIMD.)
+    const bool edge = key0 < t.seen || key0 + kStep > last;
+    auto value_factors = [&](int g, h2 (&vf)[8]) __attribute__((always_inline)) {
+      __builtin_memcpy(vf, __builtin_assume_aligned(factors + 32 * G + g * 32, 16), 32);
+      if (edge) {
+        int before = t.seen - (key0 + 16 * j), behind = last - (key0 + 16 * j);
+        asm volatile("" : "+v"(before), "+v"(behind));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int t0 = 4 * (e >> 1) + (e & 1), t2 = t0 + 2;
+          vf[e] = h2{t0 >= before && t0 < behind ? vf[e][0] : 0.0f16, t2 >= before && t2 < behind ? vf[e][1] : 0.0f16};
+        }
+      }
+    };
+    s2 most = {0, 0};                                   // (none is negative: their patterns order as numbers)
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      h2 vf[8];
+      value_factors(g, vf);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(s2, vf[e]));
+    }
+    asm volatile("" ::: "memory");
+    const h2 both = __builtin_bit_cast(h2, most);
+    const float big = fmaxf((float)both[0], (float)both[1]);
+    if (__any(big > limit)) {                           // (the first step, and where factors grow beyond 32 times)
+      const float all = column_max(big);
+      const int e = (int)(__float_as_uint(all) >> 23) - 126;                  // all < 2^e
+      lift = kLift - (float)e;
+      limit = __uint_as_float((unsigned)(min(e + 5, 126) + 127) << 23);
+    }
     // ---- running maximum and sum
-    float m = top;
+    float m = x[0][0];
 #pragma unroll
     for (int tile = 0; tile < 4; ++tile)
 #pragma unroll
       for (int i = 0; i < 4; ++i) m = fmaxf(m, x[tile][i]);
-    m = fmaxf(m, __shfl_xor(m, 16, 64));
-    m = fmaxf(m, __shfl_xor(m, 32, 64));
-    const float base = m == -__builtin_inff() ? 0.0f : m;
-    const float shrink = __builtin_amdgcn_exp2f(top - base);
-    top = m;
+    top = fmaxf(top, column_max(m));
+    const float now = top == -__builtin_inff() ? 0.0f : __builtin_fmaf(top, scale, -lift);
+    const float shrink = __builtin_amdgcn_exp2f(ref - now);
+    ref = top == -__builtin_inff() ? top : now;
     sum *= shrink;
-    h2 pr[4][2];
+    if (__any(shrink != 1.0f)) {
 #pragma unroll
-    for (int tile = 0; tile < 4; ++tile) {
+      for (int c = 0; c < CT; ++c) o[c] *= shrink;
+    }
+#pragma unroll
+    for (int tile = 0; tile < 4; ++tile)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        x[tile][i] = __builtin_amdgcn_exp2f(x[tile][i] - base);
+        x[tile][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tile][i], scale, -now));
         sum += x[tile][i];
       }
-      pr[tile][0] = h2{(_Float16)x[tile][0], (_Float16)x[tile][2]};
-      pr[tile][1] = h2{(_Float16)x[tile][1], (_Float16)x[tile][3]};
-    }
-#pragma unroll
-    for (int c = 0; c < CT; ++c) o[c] *= shrink;
-    // ---- O^T.  What lies outside the keys that the rows see, or in a page that the request has not, may be no
-    // number: its factors count as zeros.
-    const h8 p0 = join4(pr[0][0], pr[0][1], pr[1][0], pr[1][1]), p1 = join4(pr[2][0], pr[2][1], pr[3][0], pr[3][1]);
-    const int before = t.seen - (key0 + 16 * j), behind = v_held ? last - (key0 + 16 * j) : 0;   // of 16 tokens
-    const bool edge = key0 < t.seen || key0 + kStep > last || !__all(v_held);
+    // ---- O^T: a probability times its token's factor is the right operand.  What the codes have too much goes first,
+    // as a product with the same operand: the sum of both is exact to a unit of the larger.
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      unsigned vc[4];
       h2 vf[8];
-      __builtin_memcpy(vc, __builtin_assume_aligned(vb + 256 * G + (g * 16 + r) * 16, 16), 16);
-      __builtin_memcpy(vf, __builtin_assume_aligned(vb + 544 * G + g * 32, 16), 32);
-      if (edge) {
+      value_factors(g, vf);
+      unsigned vc[4];
+      __builtin_memcpy(vc, __builtin_assume_aligned(stage + St::V_AT + j * St::CODES + (g * 16 + r) * 16, 16), 16);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int t0 = 4 * (e >> 1) + (e & 1), t2 = t0 + 2;  // tokens t0 and t0 + 2
-          vf[e] = h2{t0 >= before && t0 < behind ? vf[e][0] : 0.0f16, t2 >= before && t2 < behind ? vf[e][1] : 0.0f16};
+      for (int h = 0; h < 2; ++h) {
+        h8 pr;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int tile = 2 * h + (e >> 1), i = e & 1;
+          if constexpr (std::is_same<V, _Float16>::value) {                   // rounded once: fp16 outputs show it
+            pr[2 * e] = (_Float16)__builtin_fmaf(x[tile][i], (float)vf[2 * tile + i][0], 0.0f);
+            pr[2 * e + 1] = (_Float16)__builtin_fmaf(x[tile][i + 2], (float)vf[2 * tile + i][1], 0.0f);
+          } else {
+            const h2 two = h2{(_Float16)x[tile][i], (_Float16)x[tile][i + 2]} * vf[2 * tile + i];
+            pr[2 * e] = two[0], pr[2 * e + 1] = two[1];
+          }
         }
+        const unsigned c = vc[2 * h], d = vc[2 * h + 1];
+        f4 lo = __builtin_amdgcn_mfma_f32_16x16x32_f16(low_off, pr, o[2 * g], 0, 0, 0);
+        f4 hi = __builtin_amdgcn_mfma_f32_16x16x32_f16(high_off, pr, o[2 * g + 1], 0, 0, 0);
+        o[2 * g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join4(un.low(c), un.low(c >> 8), un.low(d), un.low(d >> 8)), pr,
+                                                          lo, 0, 0, 0);
+        o[2 * g + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+            join4(un.high(c), un.high(c >> 8), un.high(d), un.high(d >> 8)), pr, hi, 0, 0, 0);
       }
-      h2 low[8], high[8];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        low[2 * e] = codes_low(vc[e]) * vf[2 * e];
-        low[2 * e + 1] = codes_low(vc[e] >> 8) * vf[2 * e + 1];
-        high[2 * e] = codes_high(vc[e]) * vf[2 * e];
-        high[2 * e + 1] = codes_high(vc[e] >> 8) * vf[2 * e + 1];
-      }
-      o[2 * g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join4(low[0], low[1], low[2], low[3]), p0, o[2 * g], 0, 0, 0);
-      o[2 * g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join4(low[4], low[5], low[6], low[7]), p1, o[2 * g], 0, 0, 0);
-      o[2 * g + 1] =
-          __builtin_amdgcn_mfma_f32_16x16x32_f16(join4(high[0], high[1], high[2], high[3]), p0, o[2 * g + 1], 0, 0, 0);
-      o[2 * g + 1] =
-          __builtin_amdgcn_mfma_f32_16x16x32_f16(join4(high[4], high[5], high[6], high[7]), p1, o[2 * g + 1], 0, 0, 0);
     }
+    __builtin_amdgcn_s_waitcnt(0xc07f);                 // the stage has been read
+    asm volatile("" ::: "memory");
+    if (more) issue(it + 1);
   }
+#pragma unroll
+  for (int g = 0; g < G; ++g) o[2 * g + 1] *= 0.0625f;
   sum += __shfl_xor(sum, 16, 64);
   sum += __shfl_xor(sum, 32, 64);
+  __syncthreads();                                      // the stages have been read: the columns take their place
 
   // ---- the four wavefronts' columns together
-  float* const tops = shared + kWaves * kCols * D;
-  float* const sums = tops + kWaves * kCols;
+  float* const cols = reinterpret_cast<float*>(shared);
+  float* const refs = cols + kWaves * kCols * D;
+  float* const sums = refs + kWaves * kCols;
   if (j == 0) {
-    tops[wave * kCols + r] = top;
+    refs[wave * kCols + r] = ref;
     sums[wave * kCols + r] = sum;
   }
   __syncthreads();
   float all = -__builtin_inff();
 #pragma unroll
-  for (int v = 0; v < kWaves; ++v) all = fmaxf(all, tops[v * kCols + r]);
-  const float mine = top == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top - all);
-  float* const to = shared + (wave * kCols + r) * D + 4 * j;
+  for (int v = 0; v < kWaves; ++v) all = fmaxf(all, refs[v * kCols + r]);
+  const float mine = ref == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ref - all);
+  float* const to = cols + (wave * kCols + r) * D + 4 * j;
 #pragma unroll
   for (int c = 0; c < CT; ++c) *reinterpret_cast<f4*>(to + 16 * c) = o[c] * mine;
   __syncthreads();
-  const bool whole = p.splits == 1 || per >= t.steps;
-  for (int i = tid; i < kCols * D / 4; i += 256) {
+  const bool whole = a.parts == 1;
+  const int valid = min(kCols, t.cols - t.first);
+  for (int i = tid; i < valid * D / 4; i += 256) {
     const int c = i / (D / 4), d = i % (D / 4) * 4;
     f4 v = {0, 0, 0, 0};
     float m = -__builtin_inff(), l = 0.0f;
 #pragma unroll
-    for (int u = 0; u < kWaves; ++u) m = fmaxf(m, tops[u * kCols + c]);
+    for (int u = 0; u < kWaves; ++u) m = fmaxf(m, refs[u * kCols + c]);
 #pragma unroll
     for (int u = 0; u < kWaves; ++u) {
-      v += *reinterpret_cast<const f4*>(shared + (u * kCols + c) * D + d);
-      const float tu = tops[u * kCols + c];
-      l += tu == -__builtin_inff() ? 0.0f : sums[u * kCols + c] * __builtin_amdgcn_exp2f(tu - m);
+      v += *reinterpret_cast<const f4*>(cols + (u * kCols + c) * D + d);
+      const float ru = refs[u * kCols + c];
+      l += ru == -__builtin_inff() ? 0.0f : sums[u * kCols + c] * __builtin_amdgcn_exp2f(ru - m);
     }
     if (whole) {
       const int oc = t.first + c;
-      if (oc < t.cols) {
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-        const float y[4] = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
-        store_values<4, false>(out + (size_t)(t.row + oc / p.ratio) * p.o_stride +
-                                   ((size_t)head * p.ratio + oc % p.ratio) * p.o_head + d, y);
-      }
+      const float inv = l > 0.0f ? 1.0f / l : l;        // (no key: zeros; no number: none)
+      const float y[4] = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+      store_values<4, false>(out + (size_t)(t.row + oc / p.ratio) * p.o_stride +
+                                 ((size_t)head * p.ratio + oc % p.ratio) * p.o_head + d, y);
     } else {
-      float* part = p.parts + (((size_t)w * p.H + head) * p.splits + split) * (kCols * (D + 2));
+      float* part = p.parts + ((size_t)(a.slot + a.part) * p.H + head) * (size_t)(kCols * (D + 2));
       *reinterpret_cast<f4*>(part + c * D + d) = v;
       if (d == 0) {
         part[kCols * D + c] = m;
@@ -297,45 +453,86 @@ __global__ __launch_bounds__(256) void kv4_attend_kernel(const AttendParams p, c
       }
     }
   }
+#endif
 }
 
-// The parts of a tile and head, one after the other in their order.
+// The parts of a cut tile and head: a block for each `cols` columns.  A thread takes four channels of a column and every so manieth part; where
+// columns are few, `groups` threads share them and meet in LDS.  The order of the sums is fixed by the sizes.
 template <typename V>
-__global__ __launch_bounds__(256) void kv4_join_kernel(const AttendParams p, int D, V* __restrict__ out) {
-  const int head = blockIdx.x % p.H, w = blockIdx.x / p.H;
+__global__ __launch_bounds__(512) void kv4_join_kernel(const AttendParams p, int D, int cols, int groups,
+                                                       V* __restrict__ out) {
+  __shared__ f4 sums[512];
+  __shared__ float tops[kCols], totals[kCols];
+  const int line = blockIdx.x / (kCols / cols), c0 = blockIdx.x % (kCols / cols) * cols;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (line >= p.cuts[kTarget].x) return;
+  const int4 cut = p.cuts[line];
   Tile t;
-  if (!find_tile(p, w, &t)) return;
-  const int per = steps_per_part(t, p.splits);
-  if (per >= t.steps) return;                            // (one part: it has written the output)
-  const int n = (t.steps + per - 1) / per;
-  const float* part = p.parts + ((size_t)w * p.H + head) * p.splits * (kCols * (D + 2));
-  const size_t stride = kCols * (D + 2);
-  for (int i = threadIdx.x; i < kCols * D; i += 256) {
-    const int c = i / D, d = i % D, oc = t.first + c;
-    if (oc >= t.cols) return;
-    float m = -__builtin_inff(), l = 0.0f, v = 0.0f;
-    for (int s = 0; s < n; ++s) m = fmaxf(m, part[s * stride + kCols * D + c]);
-    for (int s = 0; s < n; ++s) {
-      const float ms = part[s * stride + kCols * D + c];
-      const float f = ms == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ms - m);
-      l += f * part[s * stride + kCols * D + kCols + c];
-      v += f * part[s * stride + c * D + d];
+  if (!find_tile(p, cut.x, &t) || t.first + c0 >= t.cols) return;
+  t.first += c0;
+  const int n = cut.w, head = cut.y, valid = min(cols, t.cols - t.first);
+  const size_t stride = (size_t)p.H * (kCols * (D + 2));
+  const float* part = p.parts + ((size_t)cut.z * p.H + head) * (kCols * (D + 2));
+  const float* refs = part + kCols * D + c0;            // of this block's columns; their sums are kCols behind
+  part += c0 * D;
+  // maxima and sums of the columns: a wavefront each
+  for (int c = wave; c < valid; c += 8) {
+    float top = -__builtin_inff(), l = 0.0f;
+    for (int s = lane; s < n; s += 64) top = fmaxf(top, refs[s * stride + c]);
+    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    for (int s = lane; s < n; s += 64) {
+      const float ref = refs[s * stride + c];
+      l += ref == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ref - top) * refs[s * stride + kCols + c];
     }
-    out[(size_t)(t.row + oc / p.ratio) * p.o_stride + ((size_t)head * p.ratio + oc % p.ratio) * p.o_head + d] =
-        (V)(l > 0.0f ? v / l : 0.0f);
+    for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off, 64);
+    if (lane == 0) tops[c] = top, totals[c] = l;
+  }
+  __syncthreads();
+  const int quads = D / 4, items = valid * quads, each = 512 / groups, group = tid / each;
+  for (int i0 = 0; i0 < items; i0 += each) {
+    const int i = i0 + tid % each, c = min(i / quads, valid - 1), d = i % quads * 4;
+    f4 v = {0, 0, 0, 0};
+    if (i < items && group < groups)
+      for (int s = group; s < n; s += groups) {
+        const float ref = refs[s * stride + c];
+        const float weight = ref == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ref - tops[c]);
+        v += weight * *reinterpret_cast<const f4*>(part + s * stride + c * D + d);
+      }
+    if (groups > 1) {
+      sums[tid] = v;
+      __syncthreads();
+      if (group == 0)
+        for (int g = 1; g < groups; ++g) v += sums[g * each + tid];
+      __syncthreads();
+    }
+    if (group == 0 && i < items) {
+      const int oc = t.first + c;
+      const float l = totals[c], inv = l > 0.0f ? 1.0f / l : l;
+      const float y[4] = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+      store_values<4, false>(out + (size_t)(t.row + oc / p.ratio) * p.o_stride +
+                                 ((size_t)head * p.ratio + oc % p.ratio) * p.o_head + d, y);
+    }
   }
 }
 
 template <int G, typename V>
 int launch(const AttendParams& p, const V* q, V* out, hipStream_t stream) {
-  const size_t lds = (size_t)kWaves * kCols * (32 * G + 2) * 4;
+  const size_t stages = (size_t)kWaves * Stage<G>::SIZE, columns = (size_t)kWaves * kCols * (32 * G + 2) * 4;
+  const size_t lds = stages > columns ? stages : columns;
   if (lds > 65536) {
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_attend_kernel<G, V>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (attr != hipSuccess) return Q8_EHIP;
   }
-  kv4_attend_kernel<G, V><<<(unsigned)(p.tiles * p.H * p.splits), 256, lds, stream>>>(p, q, out);
-  if (p.splits > 1) kv4_join_kernel<V><<<(unsigned)(p.tiles * p.H), 256, 0, stream>>>(p, 32 * G, out);
+  const unsigned blocks = (unsigned)(p.tiles * p.H) + (p.parts ? kTarget : 0);
+  kv4_attend_kernel<G, V><<<blocks, 256, lds, stream>>>(p, q, out);
+  if (p.parts) {
+    const unsigned lines = p.tiles * p.H < kTarget ? p.tiles * p.H : kTarget;
+    const int cols = lines <= 64 ? 1 : kCols;              // columns of a block: one where there are few blocks
+    int groups = 1;                                        // threads to a column's four channels
+    while (groups < 16 && (cols == 1 ? 1 : kCols) * 8 * G * groups * 2 <= 512) groups *= 2;
+    kv4_join_kernel<V><<<lines * (kCols / cols), 512, 0, stream>>>(p, 32 * G, cols, groups, out);
+  }
   return q8_launch_status();
 }
 
@@ -354,28 +551,22 @@ int launch_any(int G, const AttendParams& p, const V* q, V* out, hipStream_t str
   return Q8_EUNSUPPORTED;
 }
 
-// Tiles of 16 columns that T rows of B requests can have (find_tile), and the parts that they are split into for
-// keys of at most `longest`: four workgroups for a compute unit, a part of 512 keys at least.
+// Tiles of 16 columns that T rows of B requests can have (find_tile).
 size_t tiles_of(size_t T, int B, int ratio, bool starts) {
   return starts ? T * ratio / kCols + B : (size_t)B * ((ratio + kCols - 1) / kCols);
 }
-size_t splits_of(size_t tiles, int H, size_t longest) {
-  const size_t want = 1024 / (tiles * H ? tiles * H : 1), most = longest / 512;
-  const size_t s = want < most ? want : most;
-  return s < 1 ? 1 : s;
-}
-size_t part_bytes(size_t tiles, int H, int D) { return tiles * H * kCols * (D + 2) * 4; }
+// Whether keys of at most `longest` are cut: where parts of kMinSteps could be made, and tiles are so few that a part of
+// the longest could keep compute units waiting.
+bool cut(size_t tiles, size_t longest) { return tiles <= kMaxTiles && longest > (size_t)kMinSteps * kStep; }
+size_t parts_bytes(int D) { return (size_t)2 * kTarget * kCols * (D + 2) * 4; }
+size_t split_bytes(int D) { return parts_bytes(D) + (kTarget + 1) * sizeof(int4); }
 
 }  // namespace
 
 extern "C" size_t q8_kv4_attend_workspace_bytes(size_t T, int n_requests, int n_heads, int ratio, int D,
                                                 size_t longest) {
   if (n_requests < 1 || n_heads < 1 || ratio < 1 || D < 32 || D > kMaxHead || T > 0x7fffffffu) return 0;
-  // (whether the rows' starts are given is not known here: the more tiles, the fewer splits)
-  const size_t a = tiles_of(T, n_requests, ratio, false), b = tiles_of(T, n_requests, ratio, true);
-  const size_t sa = splits_of(a, n_heads, longest), sb = splits_of(b, n_heads, longest);
-  const size_t na = sa > 1 ? sa * part_bytes(a, n_heads, D) : 0, nb = sb > 1 ? sb * part_bytes(b, n_heads, D) : 0;
-  return na > nb ? na : nb;
+  return cut(tiles_of(T, n_requests, ratio, false), longest) ? split_bytes(D) : 0;
 }
 
 extern "C" int q8_kv4_attend(const void* q_dev, int type, size_t T, int n_heads, int ratio, int D, size_t q_stride,
@@ -396,23 +587,21 @@ extern "C" int q8_kv4_attend(const void* q_dev, int type, size_t T, int n_heads,
   Q8_REQUIRE(q8_aligned(q_dev, 2) && q8_aligned(out_dev, 2) && q8_aligned(cache_dev, 64) && q8_aligned(table_dev, 4) &&
                  q8_aligned(lengths_dev, 4) && q8_aligned(starts_dev, 4) && q8_aligned(workspace, 16), Q8_EALIGN);
   const size_t tiles = tiles_of(T, n_requests, ratio, starts_dev != nullptr);
-  size_t splits = splits_of(tiles, n_heads, (size_t)width * page);
-  const size_t part = part_bytes(tiles, n_heads, D);
-  if (!workspace || workspace_bytes / part < 2) splits = 1;
-  else if (workspace_bytes / part < splits) splits = workspace_bytes / part;
-  Q8_REQUIRE(tiles * n_heads * splits <= 0x7fffffffu && T * ratio <= 0x7fffffffu, Q8_EUNSUPPORTED);
+  const bool split = workspace && workspace_bytes >= split_bytes(D) && cut(tiles, (size_t)width * page);
+  Q8_REQUIRE((tiles * n_heads + kTarget) * kCols <= 0x7fffffffu && T * ratio <= 0x7fffffffu, Q8_EUNSUPPORTED);
   AttendParams p{};
   p.cache = static_cast<const uint8_t*>(cache_dev);
   p.table = table_dev;
   p.lengths = lengths_dev;
   p.starts = starts_dev;
-  p.parts = static_cast<float*>(workspace);
+  p.parts = split ? static_cast<float*>(workspace) : nullptr;
+  p.cuts = split ? reinterpret_cast<int4*>(static_cast<char*>(workspace) + parts_bytes(D)) : nullptr;
   p.q_stride = q_stride, p.q_head = q_head_stride, p.o_stride = o_stride, p.o_head = o_head_stride;
   p.table_stride = table_stride;
   p.n_pages = (long)n_pages;
   p.T = (int)T, p.B = n_requests, p.H = n_heads, p.ratio = ratio, p.width = width;
   p.shift = __builtin_ctz(page) - 4;
-  p.tiles = (int)tiles, p.splits = (int)splits, p.window = window;
+  p.tiles = (int)tiles, p.window = window;
   p.scale_log2 = scale * 1.4426950408889634f;
   if (type == Q8_F16)
     return launch_any(D / 32, p, static_cast<const _Float16*>(q_dev), static_cast<_Float16*>(out_dev),
