@@ -11,7 +11,7 @@
 // bytes as they lie), times their factor exact to half a unit of binary16.  Which 16 keys a tile of S takes is chosen
 // so that a lane's 16 probabilities belong to the 16 tokens whose value codes it loads: nothing is exchanged
 // between lanes but the maximum.
-// The key axis is split over workgroups where columns are few; kv4_join_kernel adds the parts.
+// The key axis is split over workgroups where columns are few; the last of them to finish adds the parts, in their order.
 #include "q8_conv_common.h"
 #include "q8_kv4.h"
 #include <type_traits>
@@ -37,7 +37,7 @@ struct AttendParams {
   const int* __restrict__ lengths;
   const int* __restrict__ starts;      // null: request b is row b
   float* __restrict__ parts;           // workspace of the split, null: none is split
-  int4* __restrict__ cuts;             // kTarget lines (tile, head, first part's place, parts), and their number
+  int* __restrict__ counters;          // kTarget: parts of a cut tile and head that are done; zero between calls
   size_t q_stride, q_head, o_stride, o_head, table_stride;
   long n_pages;
   int T, B, H, ratio, width, shift;    // shift: page = 16 << shift tokens
@@ -91,10 +91,10 @@ __device__ __forceinline__ bool find_tile(const AttendParams& p, int w, Tile* t)
 // The split of the key axis.  The steps of all tiles and heads over kTarget are what a part should hold (kMinSteps at
 // least); a tile of more steps is cut into equal parts of no more.  Every workgroup works this out for itself from the
 // lengths, a tile to a thread.  Parts of cut tiles have a place in the workspace, no more than 2 kTarget of them (a cut
-// tile has more than `per` steps), and the cut tiles' heads, no more than kTarget, a line in the list that the
-// joining launch goes by.
+// tile has more than `per` steps), and the cut tiles' heads, no more than kTarget, a counter.
 struct Part {
-  int tile, head, part, parts, slot;   // slot: of the tile's first part, in units of H places
+  int tile, head, part, parts;
+  int slot, rank;                      // of a cut tile: its first part's place and its number, in units of H
   int step0, step1;
 };
 
@@ -108,16 +108,16 @@ __device__ __forceinline__ void set_part(Part* a, const Tile& t) {
 __device__ bool find_part(const AttendParams& p, int id, Part* a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int at = id / p.H, head = id - at * p.H;
-  *a = Part{at, head, 0, 1, 0, 0, 0};
+  *a = Part{at, head, 0, 1, 0, 0, 0, 0};
   if (!p.parts) return at < p.tiles;
   __shared__ long sums[2][kWaves];
-  __shared__ int found[5];
+  __shared__ int found[6];
   Tile t;
   const int steps = tid < p.tiles && find_tile(p, tid, &t) ? max(t.steps, 1) : 0;
   long total = steps;
   for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off, 64);
   if (lane == 0) sums[0][wave] = total;
-  if (tid == 0) found[4] = 0;
+  if (tid == 0) found[5] = 0;
   __syncthreads();
   total = ((sums[0][0] + sums[0][1]) + (sums[0][2] + sums[0][3])) * p.H;
   const int per = (int)max((total + kTarget - 1) / kTarget, (long)kMinSteps);
@@ -134,13 +134,11 @@ __device__ bool find_part(const AttendParams& p, int id, Part* a) {
   const long before = v - own;
   const int first = (int)(before & 0xfffff), slot = (int)(before >> 20 & 0xfffff), rank = (int)(before >> 40);
   if (at >= first && at < first + n) {
-    found[0] = tid, found[1] = at - first, found[2] = (int)n, found[3] = slot, found[4] = 1;
-    if (n > 1 && at == first) p.cuts[rank * p.H + head] = int4{tid, head, slot, (int)n};
+    found[0] = tid, found[1] = at - first, found[2] = (int)n, found[3] = slot, found[4] = rank, found[5] = 1;
   }
-  if (id == 0 && tid == kMaxTiles - 1) p.cuts[kTarget] = int4{(int)(v >> 40) * p.H, 0, 0, 0};
   __syncthreads();
-  a->tile = found[0], a->part = found[1], a->parts = found[2], a->slot = found[3];
-  return found[4] != 0;
+  a->tile = found[0], a->part = found[1], a->parts = found[2], a->slot = found[3], a->rank = found[4];
+  return found[5] != 0;
 }
 
 // Half bytes u as binary16: the low ones of w's bytes 0 and 2 as 1024 + u, the high ones as 1024 + 16 u, one instruction
@@ -153,6 +151,17 @@ struct Unpack {
 };
 __device__ __forceinline__ h8 join4(h2 a, h2 b, h2 c, h2 d) {
   return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Two numbers of the workspace, between workgroups of different XCDs: written through and read past their caches.
+typedef unsigned long word;
+typedef float f2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void put(word* to, float a, float b) {
+  __hip_atomic_store(to, (word)__float_as_uint(a) | (word)__float_as_uint(b) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+}
+__device__ __forceinline__ f2 get(const word* from) {
+  const word v = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+  return f2{__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32))};
 }
 
 // The largest of the four lanes that hold a column (lane % 16).
@@ -179,6 +188,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
                                                                          V* __restrict__ out) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int D = 32 * G, CT = 2 * G;                 // channels, tiles of 16 of them
+  constexpr size_t kPartWords = kCols * (D + 2) / 2;    // of a part: sums [16][D], then a maximum and a sum for each column
   using St = Stage<G>;
   extern __shared__ __attribute__((aligned(16))) char shared[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -445,65 +455,79 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
       store_values<4, false>(out + (size_t)(t.row + oc / p.ratio) * p.o_stride +
                                  ((size_t)head * p.ratio + oc % p.ratio) * p.o_head + d, y);
     } else {
-      float* part = p.parts + ((size_t)(a.slot + a.part) * p.H + head) * (size_t)(kCols * (D + 2));
-      *reinterpret_cast<f4*>(part + c * D + d) = v;
-      if (d == 0) {
-        part[kCols * D + c] = m;
-        part[kCols * D + kCols + c] = l;
-      }
+      // past this XCD's cache, for the workgroup that adds the parts
+      word* part = reinterpret_cast<word*>(p.parts) + ((size_t)(a.slot + a.part) * p.H + head) * kPartWords;
+      put(part + (c * D + d) / 2, v[0], v[1]);
+      put(part + (c * D + d) / 2 + 1, v[2], v[3]);
+      if (d == 0) put(part + kCols * D / 2 + c, m, l);
     }
   }
-#endif
-}
+  if (whole) return;
 
-// The parts of a cut tile and head: a block for each `cols` columns.  A thread takes four channels of a column and every so manieth part; where
-// columns are few, `groups` threads share them and meet in LDS.  The order of the sums is fixed by the sizes.
-template <typename V>
-__global__ __launch_bounds__(512) void kv4_join_kernel(const AttendParams p, int D, int cols, int groups,
-                                                       V* __restrict__ out) {
-  __shared__ f4 sums[512];
-  __shared__ float tops[kCols], totals[kCols];
-  const int line = blockIdx.x / (kCols / cols), c0 = blockIdx.x % (kCols / cols) * cols;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (line >= p.cuts[kTarget].x) return;
-  const int4 cut = p.cuts[line];
-  Tile t;
-  if (!find_tile(p, cut.x, &t) || t.first + c0 >= t.cols) return;
-  t.first += c0;
-  const int n = cut.w, head = cut.y, valid = min(cols, t.cols - t.first);
-  const size_t stride = (size_t)p.H * (kCols * (D + 2));
-  const float* part = p.parts + ((size_t)cut.z * p.H + head) * (kCols * (D + 2));
-  const float* refs = part + kCols * D + c0;            // of this block's columns; their sums are kCols behind
-  part += c0 * D;
-  // maxima and sums of the columns: a wavefront each
-  for (int c = wave; c < valid; c += 8) {
-    float top = -__builtin_inff(), l = 0.0f;
-    for (int s = lane; s < n; s += 64) top = fmaxf(top, refs[s * stride + c]);
-    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-    for (int s = lane; s < n; s += 64) {
-      const float ref = refs[s * stride + c];
-      l += ref == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ref - top) * refs[s * stride + kCols + c];
+  // ---- the parts of the tile and head: the workgroup that finishes last adds them, whichever it is in their order
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this wavefront's words have arrived
+  __syncthreads();                                      // and the others'; LDS is free
+  int* const flag = reinterpret_cast<int*>(shared);
+  int* const counter = p.counters + a.rank * p.H + head;
+  if (tid == 0) flag[0] = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+  __syncthreads();
+  if (flag[0] != a.parts - 1) return;
+  __syncthreads();
+  if (tid == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+  const word* const parts = reinterpret_cast<const word*>(p.parts) + ((size_t)a.slot * p.H + head) * kPartWords;
+  const size_t stride = (size_t)p.H * kPartWords;
+  const int n = a.parts;
+  f4* const quads = reinterpret_cast<f4*>(shared);      // 256
+  float* const weights = reinterpret_cast<float*>(quads + 256);               // [n][16], then the columns' sums
+  float* const totals = weights + (size_t)kTarget * kCols;
+  for (int c = wave; c < valid; c += kWaves) {
+    float most = -__builtin_inff(), l = 0.0f;
+    f2 rs[kTarget / 64];
+#pragma unroll
+    for (int u = 0; u < kTarget / 64; ++u) {
+      rs[u] = f2{-__builtin_inff(), 0.0f};
+      if (u * 64 < n && u * 64 + lane < n) rs[u] = get(parts + (u * 64 + lane) * stride + kCols * D / 2 + c);
     }
+#pragma unroll
+    for (int u = 0; u < kTarget / 64; ++u) most = fmaxf(most, rs[u][0]);
+    for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, 64));
+#pragma unroll
+    for (int u = 0; u < kTarget / 64; ++u)
+      if (u * 64 + lane < n) {
+        const float weight = rs[u][0] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(rs[u][0] - most);
+        weights[(u * 64 + lane) * kCols + c] = weight;
+        l += weight * rs[u][1];
+      }
     for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off, 64);
-    if (lane == 0) tops[c] = top, totals[c] = l;
+    if (lane == 0) totals[c] = l;
   }
   __syncthreads();
-  const int quads = D / 4, items = valid * quads, each = 512 / groups, group = tid / each;
-  for (int i0 = 0; i0 < items; i0 += each) {
-    const int i = i0 + tid % each, c = min(i / quads, valid - 1), d = i % quads * 4;
+  // a thread takes four channels of a column, and where these are few, every so manieth part
+  const int items = valid * (D / 4), groups = items >= 256 ? 1 : 256 / items, each = groups > 1 ? items : 256;
+  for (int i0 = 0; i0 < items; i0 += 256) {
+    const int group = groups > 1 ? tid / each : 0, i = i0 + (groups > 1 ? tid - group * each : tid);
+    const int c = i / (D / 4), d = i % (D / 4) * 4;
     f4 v = {0, 0, 0, 0};
-    if (i < items && group < groups)
-      for (int s = group; s < n; s += groups) {
-        const float ref = refs[s * stride + c];
-        const float weight = ref == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ref - tops[c]);
-        v += weight * *reinterpret_cast<const f4*>(part + s * stride + c * D + d);
+    if (i < items && group < groups) {
+      const word* from = parts + (c * D + d) / 2;
+      constexpr int kBatch = 16;                        // parts on their way at a time
+      for (int s0 = group; s0 < n; s0 += groups * kBatch) {
+        f2 x[kBatch], y[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const int s = min(s0 + u * groups, n - 1);
+          x[u] = get(from + s * stride), y[u] = get(from + s * stride + 1);
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+          if (s0 + u * groups < n) v += weights[(s0 + u * groups) * kCols + c] * f4{x[u][0], x[u][1], y[u][0], y[u][1]};
       }
+    }
     if (groups > 1) {
-      sums[tid] = v;
+      quads[tid] = v;
       __syncthreads();
       if (group == 0)
-        for (int g = 1; g < groups; ++g) v += sums[g * each + tid];
-      __syncthreads();
+        for (int g = 1; g < groups; ++g) v += quads[g * each + tid];
     }
     if (group == 0 && i < items) {
       const int oc = t.first + c;
@@ -513,12 +537,15 @@ __global__ __launch_bounds__(512) void kv4_join_kernel(const AttendParams p, int
                                  ((size_t)head * p.ratio + oc % p.ratio) * p.o_head + d, y);
     }
   }
+#endif
 }
 
 template <int G, typename V>
 int launch(const AttendParams& p, const V* q, V* out, hipStream_t stream) {
   const size_t stages = (size_t)kWaves * Stage<G>::SIZE, columns = (size_t)kWaves * kCols * (32 * G + 2) * 4;
-  const size_t lds = stages > columns ? stages : columns;
+  const size_t adding = 256 * sizeof(f4) + (kTarget + 1) * kCols * sizeof(float);
+  size_t lds = stages > columns ? stages : columns;
+  if (p.parts && lds < adding) lds = adding;
   if (lds > 65536) {
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_attend_kernel<G, V>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -526,13 +553,6 @@ int launch(const AttendParams& p, const V* q, V* out, hipStream_t stream) {
   }
   const unsigned blocks = (unsigned)(p.tiles * p.H) + (p.parts ? kTarget : 0);
   kv4_attend_kernel<G, V><<<blocks, 256, lds, stream>>>(p, q, out);
-  if (p.parts) {
-    const unsigned lines = p.tiles * p.H < kTarget ? p.tiles * p.H : kTarget;
-    const int cols = lines <= 64 ? 1 : kCols;              // columns of a block: one where there are few blocks
-    int groups = 1;                                        // threads to a column's four channels
-    while (groups < 16 && (cols == 1 ? 1 : kCols) * 8 * G * groups * 2 <= 512) groups *= 2;
-    kv4_join_kernel<V><<<lines * (kCols / cols), 512, 0, stream>>>(p, 32 * G, cols, groups, out);
-  }
   return q8_launch_status();
 }
 
@@ -559,7 +579,7 @@ size_t tiles_of(size_t T, int B, int ratio, bool starts) {
 // the longest could keep compute units waiting.
 bool cut(size_t tiles, size_t longest) { return tiles <= kMaxTiles && longest > (size_t)kMinSteps * kStep; }
 size_t parts_bytes(int D) { return (size_t)2 * kTarget * kCols * (D + 2) * 4; }
-size_t split_bytes(int D) { return parts_bytes(D) + (kTarget + 1) * sizeof(int4); }
+size_t split_bytes(int D) { return parts_bytes(D) + kTarget * sizeof(int); }
 
 }  // namespace
 
@@ -595,7 +615,7 @@ extern "C" int q8_kv4_attend(const void* q_dev, int type, size_t T, int n_heads,
   p.lengths = lengths_dev;
   p.starts = starts_dev;
   p.parts = split ? static_cast<float*>(workspace) : nullptr;
-  p.cuts = split ? reinterpret_cast<int4*>(static_cast<char*>(workspace) + parts_bytes(D)) : nullptr;
+  p.counters = split ? reinterpret_cast<int*>(static_cast<char*>(workspace) + parts_bytes(D)) : nullptr;
   p.q_stride = q_stride, p.q_head = q_head_stride, p.o_stride = o_stride, p.o_head = o_head_stride;
   p.table_stride = table_stride;
   p.n_pages = (long)n_pages;
