@@ -23,7 +23,7 @@ SOURCES = ["q8_conv_ring.hip", "q8_conv_ring_ext.hip", "q8_conv_ring_pair.hip", 
            "q8_conv_f32.hip", "q8_conv_f32_lds.hip", "q8_conv_f32_split.hip", "q8_conv_direct.hip",
            "q8_program.hip", "q8_conv_ext.hip",
            "q8_conv.hip", "q8_conv_reg.hip", "q8_elementwise.hip", "q8_helpers.hip",
-           "q8_linear.hip", "q8_linear_tile.hip", "q8_linear_rows.hip", "q8_kv4.hip", "q8_kv4_attend.hip"]
+           "q8_linear.hip", "q8_linear_tile.hip", "q8_linear_rows.hip", "q8_kv4.hip", "q8_kv4_attend.hip", "q8_kv4_wide.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 EXTRA = os.environ.get("Q8_EXTRA_FLAGS", "").split()

@@ -12,81 +12,16 @@
 // so that a lane's 16 probabilities belong to the 16 tokens whose value codes it loads: nothing is exchanged
 // between lanes but the maximum.
 // The key axis is split over workgroups where columns are few; the last of them to finish adds the parts, in their order.
-#include "q8_conv_common.h"
-#include "q8_kv4.h"
-#include <type_traits>
+#include "q8_kv4_attend.h"
 #pragma clang fp contract(fast)
 
 namespace {
 
 using namespace q8;
 
-typedef float f4 __attribute__((ext_vector_type(4)));
-typedef short s2 __attribute__((ext_vector_type(2)));
-
-constexpr int kCols = 16;              // columns of a tile
-constexpr int kStep = 64;              // keys of a wavefront's step
-constexpr int kWaves = 4;
 constexpr int kTarget = 512;           // parts that the keys are cut into where tiles are few
 constexpr int kMinSteps = 8;           // steps of a part, at least
 constexpr int kMaxTiles = 256;         // beyond them nothing is cut: a thread each
-
-struct AttendParams {
-  const uint8_t* __restrict__ cache;
-  const int* __restrict__ table;
-  const int* __restrict__ lengths;
-  const int* __restrict__ starts;      // null: request b is row b
-  float* __restrict__ parts;           // workspace of the split, null: none is split
-  int* __restrict__ counters;          // kTarget: parts of a cut tile and head that are done; zero between calls
-  size_t q_stride, q_head, o_stride, o_head, table_stride;
-  long n_pages;
-  int T, B, H, ratio, width, shift;    // shift: page = 16 << shift tokens
-  int tiles, window;
-  float scale_log2;                    // scale * log2(e)
-};
-
-// What a workgroup works on: the 16 columns of tile `tile` of request b, whose row 0 is q row `row`.
-struct Tile {
-  int b, row, first, cols, len, n;     // first column, columns of the request, keys, new tokens
-  int seen, lo, steps;                 // first key that a row sees, that key's step's first one, and steps of kStep keys
-};
-
-__device__ __forceinline__ bool find_tile(const AttendParams& p, int w, Tile* t) {
-  int b = 0, base = 0;
-  if (!p.starts) {
-    const int per = (p.ratio + kCols - 1) / kCols;
-    b = w / per;
-    base = b * per;
-    t->row = b;
-    t->n = 1;
-  } else {
-    // request b's tiles begin at floor(starts[b] ratio / 16) + b: none overlap, and those behind its last are empty
-    auto start = [&](int i) { return min(max(p.starts[i], 0), p.T); };
-    auto first = [&](int i) { return (int)((long)start(i) * p.ratio / kCols) + i; };
-    int lo = 0, hi = p.B - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (first(mid) <= w) lo = mid; else hi = mid - 1;
-    }
-    b = lo;
-    base = first(b);
-    t->row = start(b);
-    t->n = start(b + 1) - t->row;
-  }
-  if (b >= p.B) return false;
-  t->b = b;
-  t->first = (w - base) * kCols;
-  t->cols = t->n * p.ratio;
-  if (t->first < 0 || t->first >= t->cols) return false;
-  const long longest = (long)p.width << (p.shift + 4);
-  t->len = (int)min((long)max(p.lengths[b], 0), longest);
-  const int tok0 = t->first / p.ratio, tok1 = (min(t->first + kCols, t->cols) - 1) / p.ratio;
-  const int pos0 = t->len - t->n + tok0, pos1 = t->len - t->n + tok1;
-  t->seen = p.window > 0 ? max(0, pos0 - p.window + 1) : 0;
-  t->lo = t->seen & ~(kStep - 1);
-  t->steps = pos1 < t->lo ? 0 : (pos1 - t->lo) / kStep + 1;
-  return true;
-}
 
 // The split of the key axis.  The steps of all tiles and heads over kTarget are what a part should hold (kMinSteps at
 // least); a tile of more steps is cut into equal parts of no more.  Every workgroup works this out for itself from the
@@ -113,7 +48,7 @@ __device__ bool find_part(const AttendParams& p, int id, Part* a) {
   __shared__ long sums[2][kWaves];
   __shared__ int found[6];
   Tile t;
-  const int steps = tid < p.tiles && find_tile(p, tid, &t) ? max(t.steps, 1) : 0;
+  const int steps = tid < p.tiles && find_tile<kCols>(p, tid, &t) ? max(t.steps, 1) : 0;
   long total = steps;
   for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off, 64);
   if (lane == 0) sums[0][wave] = total;
@@ -141,18 +76,6 @@ __device__ bool find_part(const AttendParams& p, int id, Part* a) {
   return found[5] != 0;
 }
 
-// Half bytes u as binary16: the low ones of w's bytes 0 and 2 as 1024 + u, the high ones as 1024 + 16 u, one instruction
-// for two (mask and pattern in registers: one instruction takes them, not two literals).
-struct Unpack {
-  unsigned low_mask = 0x000f000fu, high_mask = 0x00f000f0u, one = 0x64006400u;
-  __device__ __forceinline__ Unpack() { asm volatile("" : "+s"(low_mask), "+s"(high_mask), "+v"(one)); }
-  __device__ __forceinline__ h2 low(unsigned w) const { return __builtin_bit_cast(h2, (w & low_mask) | one); }
-  __device__ __forceinline__ h2 high(unsigned w) const { return __builtin_bit_cast(h2, (w & high_mask) | one); }
-};
-__device__ __forceinline__ h8 join4(h2 a, h2 b, h2 c, h2 d) {
-  return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-
 // Two numbers of the workspace, between workgroups of different XCDs: written through and read past their caches.
 typedef unsigned long word;
 typedef float f2 __attribute__((ext_vector_type(2)));
@@ -162,14 +85,6 @@ __device__ __forceinline__ void put(word* to, float a, float b) {
 __device__ __forceinline__ f2 get(const word* from) {
   const word v = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
   return f2{__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32))};
-}
-
-// The largest of the four lanes that hold a column (lane % 16).
-__device__ __forceinline__ float column_max(float v) {
-  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 // A wavefront's step in LDS, 64 keys: the codes of its four sixteens' keys (32 bytes between them: the four rows that one
@@ -198,7 +113,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
   Tile t;
   if (!find_part(p, blockIdx.x, &a)) return;
   a.tile = __builtin_amdgcn_readfirstlane(a.tile);
-  if (!find_tile(p, a.tile, &t)) return;
+  if (!find_tile<kCols>(p, a.tile, &t)) return;
   set_part(&a, t);
   const int head = a.head, step0 = __builtin_amdgcn_readfirstlane(a.step0), step1 = __builtin_amdgcn_readfirstlane(a.step1);
   const int last = min(t.lo + t.steps * kStep, t.len);         // keys of the tile end here
@@ -571,9 +486,9 @@ int launch_any(int G, const AttendParams& p, const V* q, V* out, hipStream_t str
   return Q8_EUNSUPPORTED;
 }
 
-// Tiles of 16 columns that T rows of B requests can have (find_tile).
-size_t tiles_of(size_t T, int B, int ratio, bool starts) {
-  return starts ? T * ratio / kCols + B : (size_t)B * ((ratio + kCols - 1) / kCols);
+// Tiles of `cols` columns that T rows of B requests can have (find_tile).
+size_t tiles_of(size_t T, int B, int ratio, bool starts, int cols = kCols) {
+  return starts ? T * ratio / cols + B : (size_t)B * ((ratio + cols - 1) / cols);
 }
 // Whether keys of at most `longest` are cut: where parts of kMinSteps could be made, and tiles are so few that a part of
 // the longest could keep compute units waiting.
@@ -609,6 +524,11 @@ extern "C" int q8_kv4_attend(const void* q_dev, int type, size_t T, int n_heads,
   const size_t tiles = tiles_of(T, n_requests, ratio, starts_dev != nullptr);
   const bool split = workspace && workspace_bytes >= split_bytes(D) && cut(tiles, (size_t)width * page);
   Q8_REQUIRE((tiles * n_heads + kTarget) * kCols <= 0x7fffffffu && T * ratio <= 0x7fffffffu, Q8_EUNSUPPORTED);
+  const size_t wide_tiles = tiles_of(T, n_requests, ratio, starts_dev != nullptr, kWideCols);
+  // Many columns of a request, and enough tiles of them for the compute units: those of 128 columns unpack a key once for
+  // all.  (Pieces of 2048 tokens over 8192 keys, 8 query heads to a key head: 752 us in tiles of 16 columns, 458 so;
+  // 64 tokens of 4 requests, 72 tiles: 60 and 314.)
+  const bool wide = starts_dev && T * ratio >= (size_t)n_requests * (kWideCols / 2) && wide_tiles * n_heads >= 256;
   AttendParams p{};
   p.cache = static_cast<const uint8_t*>(cache_dev);
   p.table = table_dev;
@@ -623,6 +543,10 @@ extern "C" int q8_kv4_attend(const void* q_dev, int type, size_t T, int n_heads,
   p.shift = __builtin_ctz(page) - 4;
   p.tiles = (int)tiles, p.window = window;
   p.scale_log2 = scale * 1.4426950408889634f;
+  if (wide) {
+    p.tiles = (int)wide_tiles;
+    return kv4_attend_wide(D / 32, p, q_dev, out_dev, type, (hipStream_t)stream);
+  }
   if (type == Q8_F16)
     return launch_any(D / 32, p, static_cast<const _Float16*>(q_dev), static_cast<_Float16*>(out_dev),
                       (hipStream_t)stream);

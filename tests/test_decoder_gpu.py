@@ -399,6 +399,37 @@ def test_attention_in_a_window(B, window):
     _check_attend(B, _rng(window, 1), lengths, [90, 64, 1, 37, 0], 1, 3, 96, 32, "bf16", window=window)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("D,H,ratio", [(32, 16, 8), (64, 16, 7), (96, 16, 4), (128, 16, 8), (160, 16, 8), (192, 16, 5), (224, 16, 8),
+                                       (256, 16, 8)])
+def test_attention_of_prompts(B, kind, D, H, ratio):
+    """Columns enough for the wide tiles: ragged prompts, in part over what the cache holds, some empty."""
+    lengths, added = [330, 0, 200, 70, 129], [150, 0, 200, 70, 1]
+    _check_attend(B, _rng(D, 3), lengths, added, H, ratio, D, 32, kind)
+
+
+@pytest.mark.parametrize("window", [1, 17, 64, 130, 1000])
+def test_attention_of_prompts_in_a_window(B, window):
+    _check_attend(B, _rng(window, 2), [400, 150, 90], [300, 150, 100], 16, 4, 64, 16, "bf16", window=window)
+    _check_attend(B, _rng(window, 3), [400, 150, 90], [300, 150, 100], 16, 4, 64, 16, "f16", window=window, scale=-0.2)
+
+
+def test_attention_of_prompts_reads_no_page_that_a_request_has_not(B):
+    rng = _rng(16)
+    H, ratio, D, page = 16, 8, 64, 16
+    cache, table, keys, values = _filled(B, rng, [200, 130], H, D, page)
+    table[0, 2], table[1, 0] = 1 << 30, -7
+    q = _real(rng, (330, H * ratio, D), "bf16")
+    lens, starts = [torch.tensor(v, dtype=torch.int32, device="cuda") for v in ([200, 130], [0, 200, 330])]
+    got = B.kv4_attend(q.cuda(), cache, table, lens, starts).double().cpu().numpy()
+    for rows, b, gone in ((range(48, 200, 19), 0, slice(32, 48)), (range(216, 330, 23), 1, slice(0, 16))):
+        for t in rows:
+            n = t + 1 - starts[b].item()
+            k, v = [np.delete(x[b][:n], gone, 0) for x in (keys, values)]
+            want, most = P.attend(q[t:t + 1].double().numpy(), [k], [v], [len(k)], [0, 1], D ** -0.5, 0)
+            assert np.all(np.abs(got[t:t + 1] - want) <= P.attend_tolerance(want, [v], most, torch.bfloat16)), t
+
+
 def test_attention_of_more_rows_than_tokens(B):
     """A request with more rows than tokens in the cache: the first rows stand in front of its first key."""
     _check_attend(B, _rng(8), [3, 0, 20], [5, 4, 30], 2, 2, 64, 16, "bf16")
