@@ -119,87 +119,286 @@ struct Kv4Params {
   int T, H, G, shift;                           // shift: page = 1 << shift tokens
 };
 
-// Sixteen of a slot and head, and the token's place in it.
-__device__ __forceinline__ uint8_t* sixteen_of(const Kv4Params& p, long slot, int head, int* t) {
-  const long page = slot >> p.shift;
-  const int in = (int)(slot & ((1 << p.shift) - 1));
-  *t = in & 15;
-  return p.cache + ((((size_t)page * p.H + head) << (p.shift - 4)) + (in >> 4)) * (size_t)(576 * p.G);
+// A block takes 16 tokens and four groups of 32 channels (of the H G of a token); four lanes share a group, eight
+// channels each, so that a wavefront reads and writes whole rows of the tokens' values.  Key codes are a word a lane as
+// they lie in the cache.  Value codes lie by channel: they pass through LDS, where 16 tokens make rows of 16 bytes, and
+// leave as words where four tokens' slots are neighbours (bytes elsewhere).  The floor is memory; what bounds it is
+// vector instructions, so places are worked out once for a block.
+constexpr int kTok = 16, kGroups = 4;
+
+// The block's tokens, in LDS.
+struct Places {
+  long base[kTok];                 // where the token's sixteen of head 0 lies, -1: nowhere
+  int t[kTok];                     // its place there
+  // A row's bytes of the tokens, four to a lane: the first of them, whether they are one aligned word of the cache, and
+  // how many of them are not first .. but the last tokens.  (In a run of neighbours that begins `off` places into a word,
+  // three of the four lanes have whole words, and the first what is left in front of them and behind.)
+  int first[4], word[4], tail[4];
+};
+__device__ __forceinline__ int place_of(const Places& s, int w, int e) {
+  return e < 4 - s.tail[w] ? s.first[w] + e : kTok - 4 + e;
 }
 
-// A thread per group of 32 channels of a token's head, keys and values.
+__device__ __forceinline__ void find_places(const Kv4Params& p, size_t token0, Places* s) {
+  const int tid = threadIdx.x;
+  if (tid < 64) {
+    const size_t i = token0 + tid;
+    const long slot = tid < kTok && i < (size_t)p.T ? p.slots[i] : -1;
+    const bool in = slot >= 0 && slot < p.n_slots;
+    const int place = (int)(slot & ((1 << p.shift) - 1));
+    if (tid < kTok) {
+      s->base[tid] = in ? ((((slot >> p.shift) * p.H) << (p.shift - 4)) + (place >> 4)) * (576 * p.G) : -1;
+      s->t[tid] = place & 15;
+    }
+    const long first = __shfl(slot, 0, 64), before = __shfl_up(slot, 1, 64);
+    const bool next = in && slot == before + 1;                 // one behind the token before
+    const unsigned long chain = __ballot(next), held = __ballot(in);
+    const bool run = (chain & 0xfffe) == 0xfffe && (held & 1);
+    if (tid < 4) {
+      const int off = run ? (int)(first & 3) : 0;
+      s->first[tid] = 4 * tid - (tid ? off : 0);
+      s->tail[tid] = tid == 0 ? off : 0;
+      s->word[tid] = run ? tid > 0 || off == 0 : 0;
+    }
+    // outside a run: tokens 4 w .. + 3 are neighbours, and the first begins a word
+    if (!run && tid < kTok && (tid & 3) == 0) s->word[tid >> 2] = in && (slot & 3) == 0 && (chain >> (tid + 1) & 7) == 7;
+  }
+  __syncthreads();
+}
+
+// Group `group` of the four that begin at group g0 of head0.
+struct Group {
+  int head, g;
+  bool in;                         // there is such a group
+  __device__ __forceinline__ Group(const Kv4Params& p, int head0, int g0, int group) {
+    head = head0, g = g0 + group;
+#pragma unroll
+    for (int e = 1; e < kGroups; ++e)
+      if (g >= p.G) g -= p.G, ++head;
+    in = head < p.H;
+  }
+};
+
+// The codes plus 8 of a lane's eight values, a byte each, and the factor f of its group, whose other 24 the three lanes
+// beside it hold: Round(r / f) of each, on the correctly rounded quotient (a 16-bit r is often exactly between two codes:
+// max / 7 is a binary16 number for one maximum in seven).  r * inv is off by a few units; a step t + (r - f t) inv, its
+// remainder exact, ends within a unit of r / f, and on it where r / f is a number.  A 16-bit r (11 bits at most, as f) is
+// either that at a tie or 2^-12 away from one, so a step and any inv near 1 / f will do; for fp32 two steps on the
+// rounded 1 / f end on the rounded quotient (Markstein 1990; f is none of that theorem's exceptions).  A value that is not
+// finite takes the division.
+template <bool WIDE>
+__device__ __forceinline__ void quad_codes(const float (&r)[8], _Float16* factor, unsigned (&u)[2]) {
+  float m = 0.0f;
+  bool none = false;               // one is no number
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    m = fmaxf(m, fmaxf(fabsf(r[e]), fabsf(r[e + 1])));
+    none |= __builtin_isunordered(r[e], r[e + 1]);
+  }
+  const bool finite = !none && m < __builtin_inff();
+  if (!finite) {
+    m = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = fmaxf(m, finite_abs(r[e]));
+  }
+  m = fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0xb1, 0xf, 0xf, true)));        // lanes 1 0 3 2
+  m = fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0x4e, 0xf, 0xf, true)));        // lanes 2 3 0 1
+  *factor = kv4_factor(m);
+  const float f = (float)*factor, inv = WIDE ? __fdiv_rn(1.0f, f) : __builtin_amdgcn_rcpf(f), low = -8.0f * f, high = 7.0f * f;
+  constexpr float kRound = 12582912.0f + 8.0f;            // 1.5 * 2^23: rounds half to even, the code plus 8 in the low byte
+  unsigned z[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float x = __builtin_amdgcn_fmed3f(r[e], low, high);
+    float t = __fmul_rn(x, inv);
+    t = __builtin_fmaf(__builtin_fmaf(-f, t, x), inv, t);
+    if constexpr (WIDE) t = __builtin_fmaf(__builtin_fmaf(-f, t, x), inv, t);
+    z[e] = __float_as_uint(__fadd_rn(t, kRound));
+  }
+  if (!finite) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = (unsigned)((r[e] == r[e] ? quant1(r[e], f, -8.0f, 7.0f) : 0) + 8);
+  }
+  u[0] = __builtin_amdgcn_perm(z[1], z[0], 0x0c0c0400u) | __builtin_amdgcn_perm(z[3], z[2], 0x04000c0cu);
+  u[1] = __builtin_amdgcn_perm(z[5], z[4], 0x0c0c0400u) | __builtin_amdgcn_perm(z[7], z[6], 0x04000c0cu);
+}
+
+// `per` fours of groups one after the other, so that the tokens' places are worked out once; the next four's values are
+// on their way meanwhile.
 template <typename V, bool ALIGNED>
 __global__ __launch_bounds__(256) void kv4_write_kernel(const Kv4Params p, const V* __restrict__ k,
-                                                        const V* __restrict__ v, size_t n_groups) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n_groups) return;
-  const int g = (int)(i % p.G), head = (int)(i / p.G % p.H);
-  const size_t token = i / p.G / p.H;
-  const long slot = p.slots[token];
-  if (slot < 0 || slot >= p.n_slots) return;
-  int t;
-  uint8_t* to = sixteen_of(p, slot, head, &t);
-  const int G = p.G;
-#pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    const V* from = which ? v + token * p.v_stride + head * p.v_head : k + token * p.k_stride + head * p.k_head;
-    float r[32];
-    load_values<32, ALIGNED>(from + 32 * g, r);
-    float m = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 32; ++e) m = fmaxf(m, finite_abs(r[e]));
-    const _Float16 factor = kv4_factor(m);
-    const float q = (float)factor;
-    unsigned u[32];
-#pragma unroll
-    for (int e = 0; e < 32; ++e) u[e] = (unsigned)(r[e] == r[e] ? quant1(r[e], q, -8.0f, 7.0f) : 0) + 8u;
-    if (which == 0) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        unsigned w = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w |= u[8 * j + e] << (4 * e);
-        *reinterpret_cast<unsigned*>(to + t * 16 * G + j * 4 * G + 4 * g) = w;
-      }
-      *reinterpret_cast<_Float16*>(to + 512 * G + 2 * (t * G + g)) = factor;
+                                                        const V* __restrict__ v, int group_blocks, int per) {
+  __shared__ Places places;
+  __shared__ __attribute__((aligned(4))) unsigned char rows[2][kGroups][16][kTok + 4];            // [group][channel pair][token]
+  const int blocks = (group_blocks + per - 1) / per, first = (int)(blockIdx.x % blocks) * per, G = p.G;
+  const size_t token0 = (size_t)(blockIdx.x / blocks) * kTok;
+  const int end = min(first + per, group_blocks);
+  int g0 = first * kGroups, head0 = g0 / G;
+  g0 -= head0 * G;
+  const int tid = threadIdx.x, q = tid & 3, group = tid >> 2 & 3, ti = tid >> 4;
+  const size_t token = token0 + ti, in_k = token * p.k_stride, in_v = token * p.v_stride;
+  const bool there = token < (size_t)p.T;
+  V rk[8], rv[8];
+  auto fetch = [&](const Group& a) __attribute__((always_inline)) {       // (of no group: any values, which go nowhere)
+    const bool in = a.in && there;
+    const V *fk = k + (in ? in_k + a.head * p.k_head + 32 * a.g + 8 * q : 0),
+            *fv = v + (in ? in_v + a.head * p.v_head + 32 * a.g + 8 * q : 0);
+    if constexpr (ALIGNED) {
+      __builtin_memcpy(rk, __builtin_assume_aligned(fk, 16), sizeof(rk));
+      __builtin_memcpy(rv, __builtin_assume_aligned(fv, 16), sizeof(rv));
     } else {
 #pragma unroll
-      for (int c = 0; c < 16; ++c) to[256 * G + (g * 16 + c) * 16 + t] = (uint8_t)(u[c] | u[16 + c] << 4);
-      *reinterpret_cast<_Float16*>(to + 544 * G + 2 * (g * 16 + kv4_place(t))) = factor;
+      for (int e = 0; e < 8; ++e) rk[e] = fk[e], rv[e] = fv[e];
+    }
+  };
+  Group a(p, head0, g0, group);
+  fetch(a);                                               // (its way does not depend on the slots)
+  find_places(p, token0, &places);
+  const size_t head_bytes = (size_t)(576 * G) << (p.shift - 4);
+  const long base = places.base[ti];
+  const int t = places.t[ti];
+  uint8_t* const mine = p.cache + base;
+  // rows out: four tokens of a channel pair
+  const int out_group = tid >> 6, r = tid >> 2 & 15, w = tid & 3, i0 = places.first[w];
+  const bool word = places.word[w] != 0;
+  int byte_of[4];
+  long byte_at[4];                                        // -1: nowhere
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    byte_of[e] = word ? i0 + e : place_of(places, w, e);
+    const long at = places.base[byte_of[e]];
+    byte_at[e] = at >= 0 ? at + places.t[byte_of[e]] + 256 * G + r * 16 : -1;
+  }
+
+  for (int block = first; block < end; ++block) {
+    float nk[8], nv[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) nk[e] = (float)rk[e], nv[e] = (float)rv[e];
+    const Group now = a, leave(p, head0, g0, out_group);
+    g0 += kGroups;
+    while (g0 >= G) g0 -= G, ++head0;
+    a = Group(p, head0, g0, group);
+    if (block + 1 < end) fetch(a);
+    unsigned char (*const to)[16][kTok + 4] = rows[block & 1];
+    const bool held = now.in && base >= 0;
+    uint8_t* const at = mine + now.head * head_bytes;
+    _Float16 factor;
+    unsigned u[2];
+    quad_codes<sizeof(V) == 4>(nk, &factor, u);
+    if (held) {
+      // half byte e of the word is byte e of u
+      const unsigned x = u[0] | u[0] >> 4, y = u[1] | u[1] >> 4;
+      *reinterpret_cast<unsigned*>(at + t * 16 * G + q * 4 * G + 4 * now.g) = __builtin_amdgcn_perm(y, x, 0x06040200u);
+      if (q == 0) *reinterpret_cast<_Float16*>(at + 512 * G + 2 * (t * G + now.g)) = factor;
+    }
+    quad_codes<sizeof(V) == 4>(nv, &factor, u);
+    // lanes q and q + 2 hold the low and the high halves of the same eight bytes: each makes four of them
+    const unsigned give = q < 2 ? u[1] : u[0];                       // what the other one needs
+    const unsigned other = (unsigned)__builtin_amdgcn_mov_dpp((int)give, 0x4e, 0xf, 0xf, true);
+    const unsigned bytes = q < 2 ? u[0] | other << 4 : other | u[1] << 4;
+    const int r0 = 8 * (q & 1) + 4 * (q >> 1);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) to[group][r0 + e][ti] = (unsigned char)(bytes >> (8 * e));
+    if (held && q == 0) *reinterpret_cast<_Float16*>(at + 544 * G + 2 * (now.g * 16 + kv4_place(t))) = factor;
+    lds_barrier();
+    if (leave.in) {
+      const unsigned char* const b = to[out_group][r];
+      const size_t beyond = leave.head * head_bytes + leave.g * 256;
+      if (word) {
+        *reinterpret_cast<unsigned*>(p.cache + byte_at[0] + beyond) =
+            (unsigned)b[i0] | (unsigned)b[i0 + 1] << 8 | (unsigned)b[i0 + 2] << 16 | (unsigned)b[i0 + 3] << 24;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (byte_at[e] >= 0) p.cache[byte_at[e] + beyond] = b[byte_of[e]];
+      }
     }
   }
 }
 
 template <typename V, bool ALIGNED>
 __global__ __launch_bounds__(256) void kv4_read_kernel(const Kv4Params p, V* __restrict__ k, V* __restrict__ v,
-                                                       size_t n_groups) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n_groups) return;
-  const int g = (int)(i % p.G), head = (int)(i / p.G % p.H);
-  const size_t token = i / p.G / p.H;
-  const long slot = p.slots[token];
-  const bool in = slot >= 0 && slot < p.n_slots;
-  int t;
-  const uint8_t* from = sixteen_of(p, in ? slot : 0, head, &t);
-  const int G = p.G;
-  float r[32];
-  const float qk = in ? (float)*reinterpret_cast<const _Float16*>(from + 512 * G + 2 * (t * G + g)) : 0.0f;
+                                                       int group_blocks, int per) {
+  __shared__ Places places;
+  __shared__ __attribute__((aligned(16))) unsigned char rows[2][kGroups][kTok][16];               // [group][token][channel pair]
+  const int blocks = (group_blocks + per - 1) / per, first = (int)(blockIdx.x % blocks) * per, G = p.G;
+  const size_t token0 = (size_t)(blockIdx.x / blocks) * kTok;
+  const int end = min(first + per, group_blocks);
+  int g0 = first * kGroups, head0 = g0 / G;
+  g0 -= head0 * G;
+  const size_t head_bytes = (size_t)(576 * G) << (p.shift - 4);
+  find_places(p, token0, &places);
+  const int tid = threadIdx.x, q = tid & 3, group = tid >> 2 & 3, ti = tid >> 4;
+  const size_t token = token0 + ti, out_k = token * p.k_stride, out_v = token * p.v_stride;
+  const bool there = token < (size_t)p.T;
+  const long base = places.base[ti];
+  const int t = places.t[ti];
+  const uint8_t* const mine = p.cache + base;
+  const int in_group = tid >> 6, r = tid >> 2 & 15, w = tid & 3, i0 = places.first[w];
+  const bool word = places.word[w] != 0;
+  int byte_of[4];
+  long byte_at[4];                                        // -1: nowhere
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const unsigned w = in ? *reinterpret_cast<const unsigned*>(from + t * 16 * G + j * 4 * G + 4 * g) : 0x88888888u;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r[8 * j + e] = (float)((int)(w >> (4 * e) & 15u) - 8) * qk;
+  for (int e = 0; e < 4; ++e) {
+    byte_of[e] = word ? i0 + e : place_of(places, w, e);
+    const long at = places.base[byte_of[e]];
+    byte_at[e] = at >= 0 ? at + places.t[byte_of[e]] + 256 * G + r * 16 : -1;
   }
-  store_values<32, ALIGNED>(k + token * p.k_stride + head * p.k_head + 32 * g, r);
-  const float qv = in ? (float)*reinterpret_cast<const _Float16*>(from + 544 * G + 2 * (g * 16 + kv4_place(t))) : 0.0f;
+
+  // a four's bytes on their way: a row's word (or bytes), a key word and two factors
+  unsigned row4 = 0, kc = 0;
+  _Float16 kf = 0, vf = 0;
+  auto fetch = [&](int head, int g) __attribute__((always_inline)) {
+    const Group arrive(p, head, g, in_group), a(p, head, g, group);
+    row4 = 0x88888888u, kc = 0x88888888u;
+    kf = vf = 0;
+    if (arrive.in) {
+      const size_t beyond = arrive.head * head_bytes + arrive.g * 256;
+      if (word) {
+        row4 = *reinterpret_cast<const unsigned*>(p.cache + byte_at[0] + beyond);
+      } else {
+        row4 = 0;
 #pragma unroll
-  for (int c = 0; c < 16; ++c) {
-    const unsigned b = in ? from[256 * G + (g * 16 + c) * 16 + t] : 0x88u;
-    r[c] = (float)((int)(b & 15u) - 8) * qv;
-    r[16 + c] = (float)((int)(b >> 4) - 8) * qv;
+        for (int e = 0; e < 4; ++e) row4 |= (byte_at[e] >= 0 ? (unsigned)p.cache[byte_at[e] + beyond] : 0x88u) << (8 * e);
+      }
+    }
+    if (a.in && base >= 0) {
+      const uint8_t* const at = mine + a.head * head_bytes;
+      kc = *reinterpret_cast<const unsigned*>(at + t * 16 * G + q * 4 * G + 4 * a.g);
+      kf = *reinterpret_cast<const _Float16*>(at + 512 * G + 2 * (t * G + a.g));
+      vf = *reinterpret_cast<const _Float16*>(at + 544 * G + 2 * (a.g * 16 + kv4_place(t)));
+    }
+  };
+  fetch(head0, g0);
+  for (int block = first; block < end; ++block) {
+    const unsigned bytes = row4, codes = kc;
+    const float fk = (float)kf, fv = (float)vf;
+    const Group a(p, head0, g0, group);
+    g0 += kGroups;
+    while (g0 >= G) g0 -= G, ++head0;
+    if (block + 1 < end) fetch(head0, g0);
+    unsigned char (*const to)[kTok][16] = rows[block & 1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) to[in_group][byte_of[e]][r] = (unsigned char)(bytes >> (8 * e));
+    lds_barrier();
+    if (there && a.in) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = (float)((int)(codes >> (4 * e) & 15u) - 8) * fk;
+      store_values<8, ALIGNED>(k + out_k + a.head * p.k_head + 32 * a.g + 8 * q, x);
+      // (the low half bytes of eight channel pairs, or their high ones)
+      uint2 vc;
+      __builtin_memcpy(&vc, __builtin_assume_aligned(&to[group][ti][8 * (q & 1)], 8), 8);
+      const int high = 4 * (q >> 1);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = (float)((int)((e < 4 ? vc.x : vc.y) >> (8 * (e & 3) + high) & 15u) - 8) * fv;
+      store_values<8, ALIGNED>(v + out_v + a.head * p.v_head + 32 * a.g + 8 * q, x);
+    }
   }
-  store_values<32, ALIGNED>(v + token * p.v_stride + head * p.v_head + 32 * g, r);
 }
+
+// Fours of groups that a block takes one after the other: as many as leave the compute units eight blocks each.
+inline int fours_per_block(size_t blocks) { return (int)(blocks / 2048 < 1 ? 1 : blocks / 2048 > 8 ? 8 : blocks / 2048); }
 
 int check_tokens(const void* k, const void* v, int type, size_t T, int H, int D, size_t k_stride, size_t k_head,
                  size_t v_stride, size_t v_head, const int64_t* slots, const void* cache, size_t n_pages, int page) {
@@ -248,15 +447,17 @@ extern "C" int q8_kv4_write(const void* k_dev, const void* v_dev, int type, size
   if (rc != Q8_OK || T == 0) return rc;
   const Kv4Params p{reinterpret_cast<const long*>(slots_dev), static_cast<uint8_t*>(cache_dev), k_stride, k_head_stride,
                     v_stride, v_head_stride, (long)n_pages * page, (int)T, n_heads, D / 32, __builtin_ctz(page)};
-  const size_t groups = T * n_heads * (D / 32), blocks = (groups + 255) / 256;
+  const size_t group_blocks = ((size_t)n_heads * (D / 32) + kGroups - 1) / kGroups, blocks = (T + kTok - 1) / kTok * group_blocks;
+  const int per = fours_per_block(blocks);
+  const size_t grid = (T + kTok - 1) / kTok * ((group_blocks + per - 1) / per);
   Q8_REQUIRE(blocks <= 0x7fffffffu, Q8_EUNSUPPORTED);
   return with_type(type, [&](auto one) {
     using V = decltype(one);
     const V *k = static_cast<const V*>(k_dev), *v = static_cast<const V*>(v_dev);
     if (kv4_rows_aligned<V>(k_dev, v_dev, k_stride, k_head_stride, v_stride, v_head_stride))
-      kv4_write_kernel<V, true><<<(unsigned)blocks, 256, 0, (hipStream_t)stream>>>(p, k, v, groups);
+      kv4_write_kernel<V, true><<<(unsigned)grid, 256, 0, (hipStream_t)stream>>>(p, k, v, (int)group_blocks, per);
     else
-      kv4_write_kernel<V, false><<<(unsigned)blocks, 256, 0, (hipStream_t)stream>>>(p, k, v, groups);
+      kv4_write_kernel<V, false><<<(unsigned)grid, 256, 0, (hipStream_t)stream>>>(p, k, v, (int)group_blocks, per);
     return q8_launch_status();
   });
 }
@@ -270,15 +471,17 @@ extern "C" int q8_kv4_read(const void* cache_dev, size_t n_pages, int page, cons
   const Kv4Params p{reinterpret_cast<const long*>(slots_dev), static_cast<uint8_t*>(const_cast<void*>(cache_dev)),
                     k_stride, k_head_stride, v_stride, v_head_stride, (long)n_pages * page, (int)T, n_heads, D / 32,
                     __builtin_ctz(page)};
-  const size_t groups = T * n_heads * (D / 32), blocks = (groups + 255) / 256;
+  const size_t group_blocks = ((size_t)n_heads * (D / 32) + kGroups - 1) / kGroups, blocks = (T + kTok - 1) / kTok * group_blocks;
+  const int per = fours_per_block(blocks);
+  const size_t grid = (T + kTok - 1) / kTok * ((group_blocks + per - 1) / per);
   Q8_REQUIRE(blocks <= 0x7fffffffu, Q8_EUNSUPPORTED);
   return with_type(type, [&](auto one) {
     using V = decltype(one);
     V *k = static_cast<V*>(k_dev), *v = static_cast<V*>(v_dev);
     if (kv4_rows_aligned<V>(k_dev, v_dev, k_stride, k_head_stride, v_stride, v_head_stride))
-      kv4_read_kernel<V, true><<<(unsigned)blocks, 256, 0, (hipStream_t)stream>>>(p, k, v, groups);
+      kv4_read_kernel<V, true><<<(unsigned)grid, 256, 0, (hipStream_t)stream>>>(p, k, v, (int)group_blocks, per);
     else
-      kv4_read_kernel<V, false><<<(unsigned)blocks, 256, 0, (hipStream_t)stream>>>(p, k, v, groups);
+      kv4_read_kernel<V, false><<<(unsigned)grid, 256, 0, (hipStream_t)stream>>>(p, k, v, (int)group_blocks, per);
     return q8_launch_status();
   });
 }

@@ -18,14 +18,6 @@ constexpr int kWavesK = 8;                    // wavefronts, which share K
 constexpr int kThreads8 = kWavesK * 64;
 constexpr int kRealVectors = 4;               // of 8 values each, that a lane holds of x
 
-// A barrier that waits for LDS only: loads of weights stay in flight.
-__device__ __forceinline__ void lds_barrier() {
-  __builtin_amdgcn_s_waitcnt(0xc07f);
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-
 // The largest of a wavefront's values (none is negative or no number), in lane 63.
 __device__ __forceinline__ float wave_max(float v) {
   auto step = [&](auto ctrl_c) {

@@ -51,6 +51,14 @@ __device__ __forceinline__ void store_values(V* p, const float (&v)[N]) {
   }
 }
 
+// A barrier that waits for LDS only: loads and stores of memory stay in flight.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // |v| where v is finite, else 0: what enters the maximum behind a factor.
 __device__ __forceinline__ float finite_abs(float v) {
   const float a = fabsf(v);
