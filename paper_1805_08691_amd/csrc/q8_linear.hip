@@ -125,7 +125,7 @@ int launch_any_rows(const LinearParams& p, Y* y, hipStream_t stream) {
 // us (256 compute units; a round costs its steps along K and a constant; `share` of a round that is not full is saved),
 // and no less than its operands' way from memory, m = 2.2 us + bytes at 5.4 TB/s; the lesser of the two counts a
 // fifth.  The constants are fitted to every build on 128 sizes (1 .. 4096 rows, 512 .. 16384 channels and values a
-// row); there the pick is 1.3 % longer than the best build in the mean and 24 % at most.
+// row); there the pick is 1.0 % longer than the best build in the mean and 23 % at most.
 struct Variant {
   const char* name;
   int bn, bm;                  // channels and rows of a tile
@@ -134,15 +134,15 @@ struct Variant {
   float base, round, per_k, share;
 };
 constexpr Variant kVariants[] = {
-    {"rows_16x16", 16, 16, 1, 1, -1, 1.92f, 0.91f, 0.45f, 0.30f},
-    {"rows_32x16", 32, 16, 2, 1, -1, 1.00f, 1.79f, 0.61f, 0.30f},
-    {"rows_64x16", 64, 16, 4, 1, -1, 1.00f, 2.11f, 1.00f, 0.00f},
-    {"rows_64x32", 64, 32, 4, 2, -1, 1.00f, 1.90f, 1.47f, 0.04f},
-    {"tile_64x64", 64, 64, 0, 0, 0, 2.71f, 1.12f, 1.79f, 0.46f},
-    {"tile_128x64", 128, 64, 0, 0, 1, 2.45f, 2.21f, 2.66f, 0.17f},
-    {"tile_128x128", 128, 128, 0, 0, 2, 1.00f, 6.12f, 3.49f, 0.24f},
-    {"tile_128x128_8", 128, 128, 0, 0, 3, 1.00f, 5.40f, 3.77f, 0.00f},
-    {"tile_256x256", 256, 256, 0, 0, 4, 1.00f, 17.15f, 8.95f, 0.80f},
+    {"rows_16x16", 16, 16, 1, 1, -1, 1.88f, 0.92f, 0.46f, 0.80f},
+    {"rows_32x16", 32, 16, 2, 1, -1, 1.00f, 1.84f, 0.61f, 0.36f},
+    {"rows_64x16", 64, 16, 4, 1, -1, 1.00f, 2.40f, 1.01f, 0.00f},
+    {"rows_64x32", 64, 32, 4, 2, -1, 1.00f, 1.89f, 1.48f, 0.03f},
+    {"tile_64x64", 64, 64, 0, 0, 0, 2.11f, 1.52f, 1.61f, 0.37f},
+    {"tile_128x64", 128, 64, 0, 0, 1, 2.22f, 2.59f, 2.64f, 0.33f},
+    {"tile_128x128", 128, 128, 0, 0, 2, 1.00f, 6.05f, 3.47f, 0.19f},
+    {"tile_128x128_8", 128, 128, 0, 0, 3, 1.00f, 5.32f, 3.74f, 0.00f},
+    {"tile_256x256", 256, 256, 0, 0, 4, 1.00f, 16.53f, 9.56f, 0.30f},
     {"rows_any", 16, 16, 0, 0, -1, 0.0f, 0.0f, 0.0f, 0.0f}};      // rows so far apart that a tile passes 2^31 bytes
 constexpr int kNumVariants = sizeof(kVariants) / sizeof(kVariants[0]);
 constexpr size_t kTileStride = 1 << 22;      // 256 rows of a tile stay below 2^31 bytes

@@ -1,6 +1,6 @@
 // The 8-bit linear layer's product where rows are many: y[m][n] = tail(sum_k z_x[m][k] z_w[n][k]).
 //
-// A workgroup owns a tile of BN channels x BM rows and walks over K in steps of 64 bytes: both operands go from memory
+// A workgroup owns a tile of BN channels x BM rows and walks over K in steps of KB times 64 bytes: both operands go from memory
 // to LDS without registers in between (a ring of STAGES steps, one bare barrier a step), and a wavefront multiplies its
 // TN x TM squares of 32 x 32 on v_mfma_i32_32x32x32_i8.  Packed weights lie in the order in which a wavefront reads
 // them; rows of activations are 64 bytes in LDS with their 16-byte chunks swapped (swz) so that neither meets a
@@ -14,13 +14,13 @@ using namespace q8;
 
 constexpr int kXcds = 8;
 
-template <int WN_, int WM_, int TN_, int TM_, int STAGES_>
+template <int WN_, int WM_, int TN_, int TM_, int STAGES_, int KB_ = 1>
 struct Shape {
-  static constexpr int WN = WN_, WM = WM_, TN = TN_, TM = TM_, STAGES = STAGES_;
+  static constexpr int WN = WN_, WM = WM_, TN = TN_, TM = TM_, STAGES = STAGES_, KB = KB_;      // KB: 64 bytes of K each, of a step
   static constexpr int NW = WN * WM, BN = WN * TN * 32, BM = WM * TM * 32;
-  static constexpr int A_BYTES = BN * kPackK, B_BYTES = BM * kPackK, STAGE_BYTES = A_BYTES + B_BYTES;
+  static constexpr int A_BYTES = BN * kPackK, B_BYTES = BM * kPackK, BLOCK = A_BYTES + B_BYTES, STAGE_BYTES = KB * BLOCK;
   static constexpr int LDS_BYTES = STAGES * STAGE_BYTES;
-  static constexpr int A_LOADS = BN / 16 / NW, B_LOADS = BM / 16 / NW, LOADS = A_LOADS + B_LOADS;
+  static constexpr int A_LOADS = BN / 16 / NW, B_LOADS = BM / 16 / NW, LOADS = KB * (A_LOADS + B_LOADS);
   static_assert(A_LOADS * NW * 16 == BN && B_LOADS * NW * 16 == BM, "every wavefront issues the same loads");
   static_assert((STAGES - 2) * LOADS < 64, "vmcnt is 6 bits");
 };
@@ -62,24 +62,27 @@ __global__ __launch_bounds__(Sh::NW * 64) void linear_tile_kernel(const LinearPa
   }
   int issued = 0;
   auto issue = [&](int stage) __attribute__((always_inline)) {
-    const bool in_k = issued < nk;
-    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void*)a_base, 0, in_k ? a_bytes : 0, 0x00020000);
-    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc((void*)b_base, 0, in_k ? b_bytes : 0, 0x00020000);
-    int8_t* to = lds + stage * Sh::STAGE_BYTES;
 #pragma unroll
-    for (int i = 0; i < Sh::A_LOADS; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          ra, (__attribute__((address_space(3))) void*)(to + (wave + NW * i) * 1024), 16, a_off[i], 0, 0, 0);
+    for (int kb = 0; kb < Sh::KB; ++kb) {
+      const bool in_k = issued < nk;
+      const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void*)a_base, 0, in_k ? a_bytes : 0, 0x00020000);
+      const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc((void*)b_base, 0, in_k ? b_bytes : 0, 0x00020000);
+      int8_t* to = lds + stage * Sh::STAGE_BYTES + kb * Sh::BLOCK;
 #pragma unroll
-    for (int i = 0; i < Sh::B_LOADS; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rb, (__attribute__((address_space(3))) void*)(to + Sh::A_BYTES + (wave + NW * i) * 1024), 16, b_off[i], 0, 0, 0);
-    // (a row's last step may end behind its last byte: only as far as the next row, or it reads as zeros)
-    ++issued;
-    a_base += 1024;
-    a_bytes -= 1024;
-    b_base += kPackK;
-    b_bytes -= kPackK;
+      for (int i = 0; i < Sh::A_LOADS; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            ra, (__attribute__((address_space(3))) void*)(to + (wave + NW * i) * 1024), 16, a_off[i], 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < Sh::B_LOADS; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            rb, (__attribute__((address_space(3))) void*)(to + Sh::A_BYTES + (wave + NW * i) * 1024), 16, b_off[i], 0, 0, 0);
+      // (a row's last step may end behind its last byte: only as far as the next row, or it reads as zeros)
+      ++issued;
+      a_base += 1024;
+      a_bytes -= 1024;
+      b_base += kPackK;
+      b_bytes -= kPackK;
+    }
   };
 
   v16i acc[TN][TM];
@@ -100,14 +103,16 @@ __global__ __launch_bounds__(Sh::NW * 64) void linear_tile_kernel(const LinearPa
 #pragma unroll
   for (int j = 0; j < TM; ++j) bf[1][j] = v4i{0, 0, 0, 0};
   auto load_half = [&](const int8_t* stage, auto h_c) __attribute__((always_inline)) {
-    constexpr int h = decltype(h_c)::value;
+    constexpr int h = decltype(h_c)::value, kb = h >> 1, half_of = h & 1;
 #pragma unroll
-    for (int i = 0; i < TN; ++i) af[h][i] = *reinterpret_cast<const v4i*>(stage + a_frag + i * 2048 + h * 512);
+    for (int i = 0; i < TN; ++i)
+      af[h & 1][i] = *reinterpret_cast<const v4i*>(stage + kb * Sh::BLOCK + a_frag + i * 2048 + half_of * 512);
 #pragma unroll
-    for (int j = 0; j < TM; ++j) bf[h][j] = *reinterpret_cast<const v4i*>(stage + (b_frag ^ (h * 32)) + j * 2048);
+    for (int j = 0; j < TM; ++j)
+      bf[h & 1][j] = *reinterpret_cast<const v4i*>(stage + kb * Sh::BLOCK + (b_frag ^ (half_of * 32)) + j * 2048);
   };
   auto multiply = [&](auto h_c) __attribute__((always_inline)) {
-    constexpr int h = decltype(h_c)::value;
+    constexpr int h = decltype(h_c)::value & 1;
 #pragma unroll
     for (int i = 0; i < TN; ++i)
 #pragma unroll
@@ -115,44 +120,55 @@ __global__ __launch_bounds__(Sh::NW * 64) void linear_tile_kernel(const LinearPa
         acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(af[h][i], bf[h][j], acc[i][j], 0, 0, 0);
   };
   using std::integral_constant;
-  constexpr integral_constant<int, 0> first{};
-  constexpr integral_constant<int, 1> second{};
+  constexpr int HALVES = 2 * Sh::KB;
+  constexpr integral_constant<int, HALVES - 1> last{};
 
 #pragma unroll
   for (int s = 0; s < STAGES - 1; ++s) issue(s);
   __builtin_amdgcn_s_waitcnt(0xc07f);                // scalar loads are settled before the loop
   int stage = 0;
-  for (int k = 0; k < nk; ++k) {
+  const int steps = (nk + Sh::KB - 1) / Sh::KB;
+  for (int k = 0; k < steps; ++k) {
     wait_vmcnt<(STAGES - 2) * LOADS>();
     __builtin_amdgcn_s_waitcnt(0xc07f);              // this wavefront's reads of the step before have returned
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     const int8_t* at = lds + stage * Sh::STAGE_BYTES;
-    load_half(at, first);
+    load_half(at, integral_constant<int, 0>{});
     issue(stage == 0 ? STAGES - 1 : stage - 1);
-    multiply(second);                                // of the step before (zeros at first)
-    load_half(at, second);
-    multiply(first);
-    // reads of the first half; then products with a load to LDS behind each, and the second half's reads between them
+    multiply(last);                                  // of the step before (zeros at first)
+    auto rest = [&](auto self, auto h_c) __attribute__((always_inline)) -> void {
+      constexpr int h = decltype(h_c)::value;
+      if constexpr (h < HALVES) {
+        load_half(at, h_c);
+        multiply(integral_constant<int, h - 1>{});
+        self(self, integral_constant<int, h + 1>{});
+      }
+    };
+    rest(rest, integral_constant<int, 1>{});
+    // reads of the first half; then products with a load to LDS behind each, and the next half's reads between them
     __builtin_amdgcn_sched_group_barrier(0x100, TN + TM, 0);
-    int loads = LOADS, reads = TN + TM;
+    int loads = LOADS;
 #pragma unroll
-    for (int g = 0; g < 2 * TN * TM; ++g) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      if (loads > 0) {
-        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
-        --loads;
+    for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+      for (int g = 0; g < TN * TM; ++g) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (loads > 0) {
+          __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+          --loads;
+        }
+        if (h + 1 < HALVES) {
+          const int reads = (TN + TM) * (g + 1) / (TN * TM) - (TN + TM) * g / (TN * TM);
+          for (int i = 0; i < 4; ++i)
+            if (i < reads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
       }
-      if (reads > 0) {
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        --reads;
-      }
-    }
     __builtin_amdgcn_sched_barrier(0);
     stage = stage + 1 == STAGES ? 0 : stage + 1;
   }
-  multiply(second);
+  multiply(last);
   wait_vmcnt<0>();                                   // (loads behind the last step write zeros into this LDS)
 
   // ---- tail: a lane holds 16 consecutive channels of a row
@@ -202,11 +218,11 @@ namespace q8 {
 
 int linear_tile(const LinearParams& p, void* y, int type, int variant, hipStream_t stream) {
   switch (variant) {
-    case 0: return launch_any<Shape<2, 2, 1, 1, 6>>(p, y, type, stream);      // 64 channels x 64 rows
-    case 1: return launch_any<Shape<2, 2, 2, 1, 4>>(p, y, type, stream);      // 128 x 64
+    case 0: return launch_any<Shape<2, 2, 1, 1, 4, 2>>(p, y, type, stream);      // 64 channels x 64 rows
+    case 1: return launch_any<Shape<2, 2, 2, 1, 3, 2>>(p, y, type, stream);      // 128 x 64
     case 2: return launch_any<Shape<2, 2, 2, 2, 4>>(p, y, type, stream);      // 128 x 128
-    case 3: return launch_any<Shape<2, 4, 2, 1, 6>>(p, y, type, stream);      // 128 x 128, eight wavefronts
-    case 4: return launch_any<Shape<2, 4, 4, 2, 4>>(p, y, type, stream);      // 256 x 256
+    case 3: return launch_any<Shape<2, 4, 2, 1, 3, 2>>(p, y, type, stream);      // 128 x 128, eight wavefronts
+    case 4: return launch_any<Shape<2, 4, 4, 2, 2, 2>>(p, y, type, stream);      // 256 x 256
   }
   return Q8_EUNSUPPORTED;
 }
