@@ -516,3 +516,139 @@ def test_attention_is_the_same_every_time(B):
     for q, cache, table, lens, first, got in more:
         for _ in range(20):
             assert torch.equal(got, B.kv4_attend(q.cuda(), cache, table, lens, first, workspace=ws))
+
+
+# ------------------------------------------------------------------------------ together
+def _block(rng, requests=4, n_pages=60, most=400, **kw):
+    from paper_1805_08691_amd.decoder import AttentionBlock
+    E, H, ratio, D = 160, 2, 3, 64
+    w_qkv = torch.from_numpy(rng.standard_normal((H * (ratio + 2) * D, E)).astype(np.float32) / E ** 0.5).cuda()
+    w_out = torch.from_numpy(rng.standard_normal((E, H * ratio * D)).astype(np.float32) / 20).cuda()
+    return E, w_qkv, w_out, AttentionBlock(w_qkv, w_out, H, ratio, D, n_pages, 16, requests, 400, most, **kw)
+
+
+def test_a_block_serves_requests(B):
+    """Prompts in pieces, decoding, a request that ends and another in its place: every output within what 8 and 4 bits
+    cost of the block in fp32, and the pages add up."""
+    from paper_1805_08691_amd.decoder import _plain
+    rng = _rng(30)
+    E, w_qkv, w_out, block = _block(rng)
+    xs = [torch.from_numpy(rng.standard_normal((n, E)).astype(np.float32)).cuda() for n in (120, 70, 33, 200)]
+    want = _plain(w_qkv, w_out, xs, 2, 3, 64)
+    at, got = [0] * 4, [[] for _ in range(4)]
+    for added in ([50, 0, 33, 90], [1, 70, 0, 60], [60, 0, 0, 1], [1, 0, 0, 1], [8, 0, 0, 48]):
+        x = torch.cat([v[a:a + n] for v, a, n in zip(xs, at, added)]).bfloat16()
+        y = block.step(x, added).float()
+        for b, part in enumerate(y.split(added)):
+            got[b].append(part)
+        at = [a + n for a, n in zip(at, added)]
+        assert block.lengths == at == block._lengths.tolist()
+        assert block.taken == sum(-(-n // 16) for n in at)
+    assert at == [120, 70, 33, 200]
+    for g, w in zip(got, want):
+        # 4-bit values: a code is off by a third of its factor in the mean, max / 7 / sqrt(12), against values of max / 2.5
+        off = (torch.cat(g) - w).norm() / w.norm()
+        assert off < 0.25, off
+    block.release(1)
+    taken = block.taken
+    assert taken == sum(-(-n // 16) for n in (120, 33, 200))
+    again = block.step(xs[1].bfloat16(), [0, 70, 0, 0]).float()
+    assert block.taken == taken + 5 and torch.equal(again, torch.cat(got[1]))
+    block.step(torch.zeros(400, E, dtype=torch.bfloat16, device="cuda"), [200, 0, 200, 0])       # 24 of 31 pages left
+    state = block.table.clone(), list(block.lengths), block.taken
+    with pytest.raises(MemoryError):                                     # 9 pages of 7 that are left
+        block.step(torch.zeros(150, E, dtype=torch.bfloat16, device="cuda"), [0, 0, 150, 0])
+    with pytest.raises(MemoryError):                                     # 6 pages, but 401 tokens of 400
+        block.step(torch.zeros(81, E, dtype=torch.bfloat16, device="cuda"), [81, 0, 0, 0])
+    assert torch.equal(state[0], block.table) and state[1:] == (block.lengths, block.taken)
+    rows = [block.table[b, :-(-n // 16)] for b, n in enumerate(block.lengths)]
+    used = torch.cat(rows).tolist()
+    assert len(set(used)) == len(used) == block.taken
+
+
+def test_a_step_is_its_calls(B):
+    rng = _rng(31)
+    E, _, _, block = _block(rng, b_out=torch.from_numpy(rng.standard_normal(160).astype(np.float32)).cuda())
+    x = torch.from_numpy(rng.standard_normal((57, E)).astype(np.float32)).cuda().half()
+    y = block.step(x, [30, 0, 20, 7])
+    joint = block.qkv(x).view(57, -1, 64)
+    slots = torch.cat([block.table[b].long()[torch.arange(n, device="cuda") // 16] * 16 + torch.arange(n, device="cuda") % 16
+                       for b, n in enumerate(block.lengths)])
+    other = torch.zeros_like(block.cache)
+    B.kv4_write(other, joint[:, 6:8], joint[:, 8:], slots)
+    assert torch.equal(other, block.cache)
+    starts = torch.tensor([0, 30, 30, 50, 57], dtype=torch.int32, device="cuda")
+    o = B.kv4_attend(joint[:, :6], other, block.table, block._lengths, starts)
+    assert torch.equal(y, block.out(o.view(57, -1)))
+
+
+def test_recorded_steps(B):
+    """A decoding step recorded once and replayed with other values, between eager work and synchronizations."""
+    rng = _rng(32)
+    E, _, _, block = _block(rng, window=50)
+    block.step(torch.from_numpy(rng.standard_normal((150, E)).astype(np.float32)).cuda().bfloat16(), [70, 30, 49, 1])
+    one, dev = torch.ones(4, dtype=torch.int32, device="cuda"), torch.device("cuda")
+    x = torch.zeros(4, E, dtype=torch.bfloat16, device=dev)
+    slots, positions = torch.empty(4, dtype=torch.int64, device=dev), torch.empty(4, dtype=torch.int32, device=dev)
+    free, out = torch.empty(4, dtype=torch.int32, device=dev), torch.empty_like(x)
+    free.copy_(block.free[block.taken:block.taken + 4])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    keep = [t.clone() for t in (block.cache, block.table)]
+    with torch.cuda.stream(side):
+        block.launch(x, one, free, slots, positions, out=out)            # (a first call outside of the recording)
+    torch.cuda.current_stream().wait_stream(side)
+    for t, k in zip((block.cache, block.table), keep):
+        t.copy_(k)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        block.launch(x, one, free, slots, positions, out=out)
+    for i in range(6):
+        new = torch.from_numpy(rng.standard_normal((4, E)).astype(np.float32)).cuda().bfloat16()
+        x.copy_(new)
+        free.copy_(block.free[block.taken:block.taken + 4])
+        if i % 2:
+            torch.cuda.synchronize()
+        graph.replay()
+        replayed = out.clone()
+        cache = block.cache.clone()
+        # the same step by eager launches, on another stream than the default one
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            y = block.launch(x, one, free, slots, positions)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(replayed, y) and torch.equal(cache, block.cache), i
+        assert positions.tolist() == block.lengths
+        block._lengths.copy_(block._grown)                               # (the recording's buffers stay in place)
+        need = block.pages_needed([1] * 4)
+        assert block._counts.tolist() == [need, 4, 0]
+        block.lengths = [n + 1 for n in block.lengths]
+        block.taken += need
+
+
+def test_steps_on_two_streams(B):
+    """Two blocks, each on a stream of its own, with buffers and workspaces of their own."""
+    rng = _rng(33)
+    blocks = [_block(rng)[3] for _ in range(2)]
+    xs = [torch.from_numpy(rng.standard_normal((200, 160)).astype(np.float32)).cuda().bfloat16() for _ in range(2)]
+    want = []
+    for b, x in zip(blocks, xs):
+        want.append([b.step(x, [100, 60, 0, 40]), b.step(x[:4], [1] * 4)])
+        for r in range(4):
+            b.release(r)
+        b.cache.zero_()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        got = [[], []]
+        for added, n in (([100, 60, 0, 40], 200), ([1] * 4, 4)):
+            for g, b, x, s in zip(got, blocks, xs, streams):
+                with torch.cuda.stream(s):
+                    g.append(b.step(x[:n], added))
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert all(torch.equal(p, q) for p, q in zip(g, w))
+        for b in blocks:
+            for r in range(4):
+                b.release(r)
+        torch.cuda.synchronize()
