@@ -19,51 +19,75 @@ constexpr int kMaxK = 131071;
 inline size_t round_up(size_t a, size_t b) { return (a + b - 1) / b * b; }
 
 // ---------------------------------------------------------------- rows to codes ----------
-// One block per row: the maximum, then the codes.
-template <typename V, bool ALIGNED>
-__global__ __launch_bounds__(256) void quantize_rows_kernel(const V* __restrict__ x, int K, size_t x_stride,
+// A row belongs to WAVES wavefronts of a block of four: the maximum, then the codes.  The first HELD chunks of 8 values
+// of a lane stay in registers between the two; what a longer row has beyond them is read again.
+template <typename V, bool ALIGNED, int WAVES, int HELD>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const V* __restrict__ x, size_t M, int K, size_t x_stride,
                                                             int8_t* __restrict__ z, size_t z_stride,
                                                             float* __restrict__ q_x) {
-  const size_t row = blockIdx.x;
+  constexpr int THREADS = WAVES * 64, STEP = THREADS * 8;
+  const size_t row = WAVES == 4 ? blockIdx.x : (size_t)blockIdx.x * 4 + threadIdx.x / 64;
+  if (row >= M) return;
   const V* __restrict__ xr = x + row * x_stride;
   int8_t* __restrict__ zr = z + row * z_stride;
-  const int tid = threadIdx.x, body = K & ~7;
-  float m = 0.0f;
+  const int tid = threadIdx.x % THREADS, body = K & ~7;
+  V held[HELD][8];
+#pragma unroll
+  for (int i = 0; i < HELD; ++i)
+    if (tid * 8 + i * STEP < body)
+      __builtin_memcpy(held[i], __builtin_assume_aligned(xr + tid * 8 + i * STEP, ALIGNED ? 16 : sizeof(V)), sizeof(held[i]));
+  const float tail = tid < K - body ? (float)xr[body + tid] : 0.0f;
+  float m = finite_abs(tail);
   bool finite = true;
-  for (int k = tid * 8; k < body; k += 256 * 8) {
+#pragma unroll
+  for (int i = 0; i < HELD; ++i)
+    if (tid * 8 + i * STEP < body) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = (float)held[i][e];
+      m = row_max8(v, m, &finite);
+    }
+  for (int k = tid * 8 + HELD * STEP; k < body; k += STEP) {
     float v[8];
     load_values<8, ALIGNED>(xr + k, v);
     m = row_max8(v, m, &finite);
   }
-  if (tid < K - body) m = fmaxf(m, finite_abs((float)xr[body + tid]));
   for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-  __shared__ float wave_max[4];
-  if ((tid & 63) == 0) wave_max[tid >> 6] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
+  if constexpr (WAVES == 4) {
+    __shared__ float wave_max[4];
+    if ((tid & 63) == 0) wave_max[tid >> 6] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
+  }
   float q = __fmul_rn(m, 1.0f / 127.0f);
   q = q > 0.0f ? q : 1.0f;
   if (tid == 0) q_x[row] = q;
   const float inv_q = __fdiv_rn(1.0f, q);
-  for (int k = tid * 8; k < body; k += 256 * 8) {
+#pragma unroll
+  for (int i = 0; i < HELD; ++i)
+    if (tid * 8 + i * STEP < body) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = (float)held[i][e];
+      *reinterpret_cast<uint2*>(zr + tid * 8 + i * STEP) = row_codes(v, q, inv_q, finite);
+    }
+  for (int k = tid * 8 + HELD * STEP; k < body; k += STEP) {
     float v[8];
     load_values<8, ALIGNED>(xr + k, v);
     *reinterpret_cast<uint2*>(zr + k) = row_codes(v, q, inv_q, finite);
   }
-  if (tid < K - body) {
-    const float v = (float)xr[body + tid];
-    zr[body + tid] = (int8_t)(v == v ? quant1(v, q, -128.0f, 127.0f) : 0);
-  }
+  if (tid < K - body) zr[body + tid] = (int8_t)(tail == tail ? quant1(tail, q, -128.0f, 127.0f) : 0);
 }
 
-template <typename V>
+template <typename V, bool ALIGNED>
 int launch_quantize_rows(const V* x, size_t M, int K, size_t x_stride, int8_t* z, size_t z_stride, float* q_x,
                          hipStream_t stream) {
-  const bool aligned = q8_aligned(x, 16) && x_stride * sizeof(V) % 16 == 0;
-  if (aligned)
-    quantize_rows_kernel<V, true><<<(unsigned)M, 256, 0, stream>>>(x, K, x_stride, z, z_stride, q_x);
+  if (K <= 1024)
+    quantize_rows_kernel<V, ALIGNED, 1, 2><<<(unsigned)((M + 3) / 4), 256, 0, stream>>>(x, M, K, x_stride, z, z_stride, q_x);
+  else if (K <= 4096)
+    quantize_rows_kernel<V, ALIGNED, 4, 2><<<(unsigned)M, 256, 0, stream>>>(x, M, K, x_stride, z, z_stride, q_x);
   else
-    quantize_rows_kernel<V, false><<<(unsigned)M, 256, 0, stream>>>(x, K, x_stride, z, z_stride, q_x);
+    quantize_rows_kernel<V, ALIGNED, 4, 4><<<(unsigned)M, 256, 0, stream>>>(x, M, K, x_stride, z, z_stride, q_x);
   return q8_launch_status();
 }
 
@@ -125,7 +149,7 @@ int launch_any_rows(const LinearParams& p, Y* y, hipStream_t stream) {
 // us (256 compute units; a round costs its steps along K and a constant; `share` of a round that is not full is saved),
 // and no less than its operands' way from memory, m = 2.2 us + bytes at 5.4 TB/s; the lesser of the two counts a
 // fifth.  The constants are fitted to every build on 128 sizes (1 .. 4096 rows, 512 .. 16384 channels and values a
-// row); there the pick is 1.0 % longer than the best build in the mean and 23 % at most.
+// row); there the pick is 1.1 % longer than the best build in the mean and 25 % at most.
 struct Variant {
   const char* name;
   int bn, bm;                  // channels and rows of a tile
@@ -134,15 +158,15 @@ struct Variant {
   float base, round, per_k, share;
 };
 constexpr Variant kVariants[] = {
-    {"rows_16x16", 16, 16, 1, 1, -1, 1.88f, 0.92f, 0.46f, 0.80f},
-    {"rows_32x16", 32, 16, 2, 1, -1, 1.00f, 1.84f, 0.61f, 0.36f},
-    {"rows_64x16", 64, 16, 4, 1, -1, 1.00f, 2.40f, 1.01f, 0.00f},
-    {"rows_64x32", 64, 32, 4, 2, -1, 1.00f, 1.89f, 1.48f, 0.03f},
-    {"tile_64x64", 64, 64, 0, 0, 0, 2.11f, 1.52f, 1.61f, 0.37f},
-    {"tile_128x64", 128, 64, 0, 0, 1, 2.22f, 2.59f, 2.64f, 0.33f},
-    {"tile_128x128", 128, 128, 0, 0, 2, 1.00f, 6.05f, 3.47f, 0.19f},
-    {"tile_128x128_8", 128, 128, 0, 0, 3, 1.00f, 5.32f, 3.74f, 0.00f},
-    {"tile_256x256", 256, 256, 0, 0, 4, 1.00f, 16.53f, 9.56f, 0.30f},
+    {"rows_16x16", 16, 16, 1, 1, -1, 1.89f, 0.92f, 0.46f, 0.30f},
+    {"rows_32x16", 32, 16, 2, 1, -1, 1.00f, 1.84f, 0.61f, 0.34f},
+    {"rows_64x16", 64, 16, 4, 1, -1, 1.00f, 2.40f, 1.00f, 0.00f},
+    {"rows_64x32", 64, 32, 4, 2, -1, 1.00f, 1.91f, 1.48f, 0.09f},
+    {"tile_64x64", 64, 64, 0, 0, 0, 2.10f, 1.09f, 1.58f, 0.29f},
+    {"tile_128x64", 128, 64, 0, 0, 1, 2.01f, 1.53f, 2.49f, 0.21f},
+    {"tile_128x128", 128, 128, 0, 0, 2, 1.00f, 3.35f, 3.40f, 0.08f},
+    {"tile_128x128_8", 128, 128, 0, 0, 3, 1.00f, 3.30f, 3.63f, 0.00f},
+    {"tile_256x256", 256, 256, 0, 0, 4, 1.00f, 7.29f, 9.55f, 0.80f},
     {"rows_any", 16, 16, 0, 0, -1, 0.0f, 0.0f, 0.0f, 0.0f}};      // rows so far apart that a tile passes 2^31 bytes
 constexpr int kNumVariants = sizeof(kVariants) / sizeof(kVariants[0]);
 constexpr size_t kTileStride = 1 << 22;      // 256 rows of a tile stay below 2^31 bytes
@@ -178,8 +202,11 @@ extern "C" int q8_quantize_rows(const void* x_dev, int type, size_t M, int K, si
   Q8_REQUIRE(q8_aligned(x_dev, type_bytes(type)) && q8_aligned(q_x_dev, 4), Q8_EALIGN);
   Q8_REQUIRE(q8_aligned(z_dev, 16) && z_stride % 16 == 0, Q8_EALIGN);
   return with_type(type, [&](auto v) {
-    return launch_quantize_rows(static_cast<const decltype(v)*>(x_dev), M, K, x_stride, z_dev, z_stride, q_x_dev,
-                                (hipStream_t)stream);
+    using V = decltype(v);
+    const V* const x = static_cast<const V*>(x_dev);
+    if (q8_aligned(x, 16) && x_stride * sizeof(V) % 16 == 0)
+      return launch_quantize_rows<V, true>(x, M, K, x_stride, z_dev, z_stride, q_x_dev, (hipStream_t)stream);
+    return launch_quantize_rows<V, false>(x, M, K, x_stride, z_dev, z_stride, q_x_dev, (hipStream_t)stream);
   });
 }
 

@@ -7,6 +7,7 @@
 // bank twice.
 #include "q8_linear.h"
 #include <type_traits>
+#pragma clang fp contract(off)
 
 namespace {
 
@@ -25,7 +26,10 @@ struct Shape {
   static_assert((STAGES - 2) * LOADS < 64, "vmcnt is 6 bits");
 };
 
-template <typename Sh, typename Y, bool VEC>
+// Value e of a lane in a square of 32 x 32: its row.
+__device__ __forceinline__ constexpr int square_row(int e, int half) { return (e & 3) + 8 * (e >> 2) + 4 * half; }
+
+template <typename Sh, typename Y, bool PAIRS>
 __global__ __launch_bounds__(Sh::NW * 64) void linear_tile_kernel(const LinearParams p, Y* __restrict__ y, int tiles_n,
                                                                   int tiles_m) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -60,6 +64,17 @@ __global__ __launch_bounds__(Sh::NW * 64) void linear_tile_kernel(const LinearPa
     const int row = (wave + NW * i) * 16 + (lane >> 2);
     b_off[i] = row * (int)p.z_stride + swz<4>(row, lane & 3) * 16;
   }
+  // ---- factors and bias of this lane's rows and channels
+  float q_x[TM], q_w[TN], bias[TN];
+#pragma unroll
+  for (int j = 0; j < TM; ++j) q_x[j] = p.q_x[min(m0 + (wave_m * TM + j) * 32 + (lane & 31), p.M - 1)];
+#pragma unroll
+  for (int i = 0; i < TN; ++i) {
+    const int n = min(n0 + (wave_n * TN + i) * 32 + (lane & 31), p.N - 1);
+    q_w[i] = p.q_w[n];
+    bias[i] = p.bias ? p.bias[n] : 0.0f;
+  }
+
   int issued = 0;
   auto issue = [&](int stage) __attribute__((always_inline)) {
 #pragma unroll
@@ -94,8 +109,8 @@ __global__ __launch_bounds__(Sh::NW * 64) void linear_tile_kernel(const LinearPa
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
 
   // ---- operand fragments: half h of a step is the chunks 2 h and 2 h + 1 of its rows
-  const int half = lane >> 5, ch = row_to_channel(lane & 31), row = lane & 31;
-  const int a_frag = wave_n * TN * 2048 + (ch >> 4) * 1024 + (ch & 15) * 16 + half * 256;
+  const int half = lane >> 5, row = lane & 31;
+  const int a_frag = wave_n * TN * 2048 + (row >> 4) * 1024 + (row & 15) * 16 + half * 256;
   const int b_frag = Sh::A_BYTES + (wave_m * TM * 32 + row) * kPackK + swz<4>(row, half) * 16;
   v4i af[2][TN], bf[2][TM];
 #pragma unroll
@@ -117,7 +132,7 @@ __global__ __launch_bounds__(Sh::NW * 64) void linear_tile_kernel(const LinearPa
     for (int i = 0; i < TN; ++i)
 #pragma unroll
       for (int j = 0; j < TM; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(af[h][i], bf[h][j], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bf[h][j], af[h][i], acc[i][j], 0, 0, 0);
   };
   using std::integral_constant;
   constexpr int HALVES = 2 * Sh::KB;
@@ -171,35 +186,59 @@ __global__ __launch_bounds__(Sh::NW * 64) void linear_tile_kernel(const LinearPa
   multiply(last);
   wait_vmcnt<0>();                                   // (loads behind the last step write zeros into this LDS)
 
-  // ---- tail: a lane holds 16 consecutive channels of a row
+  // ---- tail: a lane holds 16 rows of one channel, so that 32 lanes store neighbours; 16-bit values change places
+  // between two lanes first (PAIRS), which makes them two neighbours of one row each
+  const unsigned sel = lane & 1 ? 0x03020706u : 0x05040100u;
 #pragma unroll
   for (int j = 0; j < TM; ++j) {
-    const int m = m0 + (wave_m * TM + j) * 32 + row;
-    if (m >= p.M) continue;
-    const float q = p.q_x[m];
+    float q[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) q[e] = __shfl(q_x[j], square_row(e, half), 64);
 #pragma unroll
     for (int i = 0; i < TN; ++i) {
-      int v[16];
+      const int m = m0 + (wave_m * TM + j) * 32, n = n0 + (wave_n * TN + i) * 32 + row;
+      float v[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) v[e] = acc[i][j][e];
-      const int n = n0 + (wave_n * TN + i) * 32 + 16 * half;
-      if (n < p.N) finish_outputs<16, VEC>(p, y, m, n, q, v);
+      for (int e = 0; e < 16; ++e) {
+        v[e] = (float)acc[i][j][e] * (q[e] * q_w[i]);
+        if (p.bias) v[e] = v[e] + bias[i];
+      }
+      if constexpr (PAIRS) {
+        Y* const to = y + (size_t)m * p.y_stride + (n & ~1);
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          const Y two[2] = {(Y)v[e], (Y)v[e + 1]};
+          unsigned own;
+          __builtin_memcpy(&own, two, 4);
+          const unsigned other = __builtin_amdgcn_update_dpp(0u, own, 0xb1, 0xf, 0xf, true);      // of lane ^ 1
+          const unsigned out = __builtin_amdgcn_perm(other, own, sel);
+          const int r = square_row(e, half) + (lane & 1);
+          if (m + r < p.M && n < p.N) __builtin_memcpy(__builtin_assume_aligned(to + (size_t)r * p.y_stride, 4), &out, 4);
+        }
+      } else {
+        Y* const to = y + (size_t)m * p.y_stride + n;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int r = square_row(e, half);
+          if (m + r < p.M && n < p.N) to[(size_t)r * p.y_stride] = (Y)v[e];
+        }
+      }
     }
   }
 #endif
 }
 
-template <typename Sh, typename Y, bool VEC>
+template <typename Sh, typename Y, bool PAIRS>
 int launch(const LinearParams& p, Y* y, hipStream_t stream) {
   if constexpr (Sh::LDS_BYTES > 65536) {
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&linear_tile_kernel<Sh, Y, VEC>),
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&linear_tile_kernel<Sh, Y, PAIRS>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, Sh::LDS_BYTES);
     if (attr != hipSuccess) return Q8_EHIP;
   }
   const long tn = (p.N + Sh::BN - 1) / Sh::BN, tm = (p.M + Sh::BM - 1) / Sh::BM;
   Q8_REQUIRE(tn * tm <= 0x7ffffff0l, Q8_EUNSUPPORTED);
   const unsigned blocks = (unsigned)((tn * tm + kXcds - 1) / kXcds * kXcds);
-  linear_tile_kernel<Sh, Y, VEC><<<blocks, Sh::NW * 64, Sh::LDS_BYTES, stream>>>(p, y, (int)tn, (int)tm);
+  linear_tile_kernel<Sh, Y, PAIRS><<<blocks, Sh::NW * 64, Sh::LDS_BYTES, stream>>>(p, y, (int)tn, (int)tm);
   return q8_launch_status();
 }
 
@@ -207,8 +246,10 @@ template <typename Sh>
 int launch_any(const LinearParams& p, void* y, int type, hipStream_t stream) {
   return with_type(type, [&](auto one) {
     using Y = decltype(one);
-    const bool vec = q8_aligned(y, 16) && p.y_stride * sizeof(Y) % 16 == 0;
-    return vec ? launch<Sh, Y, true>(p, static_cast<Y*>(y), stream) : launch<Sh, Y, false>(p, static_cast<Y*>(y), stream);
+    if constexpr (sizeof(Y) == 2) {
+      if (q8_aligned(y, 4) && p.y_stride % 2 == 0 && p.N % 2 == 0) return launch<Sh, Y, true>(p, static_cast<Y*>(y), stream);
+    }
+    return launch<Sh, Y, false>(p, static_cast<Y*>(y), stream);
   });
 }
 

@@ -23,32 +23,23 @@ inline int with_type(int type, F f) {
 inline size_t type_bytes(int type) { return type == Q8_F32 ? 4 : 2; }
 inline bool type_ok(int type) { return type == Q8_F32 || type == Q8_F16 || type == Q8_BF16; }
 
-// N consecutive values at p; ALIGNED: p is 16-byte aligned (N values are a multiple of 16 bytes).
+// N consecutive values at p.  ALIGNED: p is 16-byte aligned, or a multiple of the N values' bytes where these are fewer
+// (told to the compiler; the accesses are as wide without it, and take longer where they cross a line).
 template <int N, bool ALIGNED, typename V>
 __device__ __forceinline__ void load_values(const V* p, float (&v)[N]) {
-  if constexpr (ALIGNED) {
-    static_assert(N * sizeof(V) % 16 == 0, "whole 16-byte vectors");
-    V raw[N];
-    __builtin_memcpy(raw, __builtin_assume_aligned(p, 16), sizeof(raw));
+  constexpr size_t A = ALIGNED ? (N * sizeof(V) % 16 == 0 ? 16 : N * sizeof(V)) : sizeof(V);
+  V raw[N];
+  __builtin_memcpy(raw, __builtin_assume_aligned(p, A), sizeof(raw));
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = (float)raw[e];
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = (float)p[e];
-  }
+  for (int e = 0; e < N; ++e) v[e] = (float)raw[e];
 }
 template <int N, bool ALIGNED, typename V>
 __device__ __forceinline__ void store_values(V* p, const float (&v)[N]) {
-  if constexpr (ALIGNED) {
-    constexpr size_t A = N * sizeof(V) % 16 == 0 ? 16 : N * sizeof(V);
-    V raw[N];
+  constexpr size_t A = ALIGNED ? (N * sizeof(V) % 16 == 0 ? 16 : N * sizeof(V)) : sizeof(V);
+  V raw[N];
 #pragma unroll
-    for (int e = 0; e < N; ++e) raw[e] = (V)v[e];
-    __builtin_memcpy(__builtin_assume_aligned(p, A), raw, sizeof(raw));
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e) p[e] = (V)v[e];
-  }
+  for (int e = 0; e < N; ++e) raw[e] = (V)v[e];
+  __builtin_memcpy(__builtin_assume_aligned(p, A), raw, sizeof(raw));
 }
 
 // A barrier that waits for LDS only: loads and stores of memory stay in flight.
