@@ -36,42 +36,56 @@ struct Tile {
   int seen, lo, steps;                 // first key that a row sees, that key's step's first one, and steps of kStep keys
 };
 
+// Request i's tiles begin at floor(starts[i] ratio / COLS) + i: none overlap, and those behind its last are empty.
+__device__ __forceinline__ int request_start(const AttendParams& p, int i) { return min(max(p.starts[i], 0), p.T); }
 template <int COLS>
-__device__ __forceinline__ bool find_tile(const AttendParams& p, int w, Tile* t) {
-  int b = 0, base = 0;
-  if (!p.starts) {
-    const int per = (p.ratio + COLS - 1) / COLS;
-    b = w / per;
-    base = b * per;
-    t->row = b;
-    t->n = 1;
-  } else {
-    // request b's tiles begin at floor(starts[b] ratio / COLS) + b: none overlap, and those behind its last are empty
-    auto start = [&](int i) { return min(max(p.starts[i], 0), p.T); };
-    auto first = [&](int i) { return (int)((long)start(i) * p.ratio / COLS) + i; };
-    int lo = 0, hi = p.B - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (first(mid) <= w) lo = mid; else hi = mid - 1;
-    }
-    b = lo;
-    base = first(b);
-    t->row = start(b);
-    t->n = start(b + 1) - t->row;
-  }
-  if (b >= p.B) return false;
+__device__ __forceinline__ int first_tile(const AttendParams& p, int start, int i) {
+  return (int)((long)start * p.ratio / COLS) + i;
+}
+
+// Tile w, of request b whose tiles begin at `base`, whose rows are row .. next - 1 and whose keys are `length`.
+template <int COLS>
+__device__ __forceinline__ bool set_tile(const AttendParams& p, int w, int b, int base, int row, int next, int length, Tile* t) {
   t->b = b;
+  t->row = row;
+  t->n = next - row;
   t->first = (w - base) * COLS;
   t->cols = t->n * p.ratio;
   if (t->first < 0 || t->first >= t->cols) return false;
   const long longest = (long)p.width << (p.shift + 4);
-  t->len = (int)min((long)max(p.lengths[b], 0), longest);
+  t->len = (int)min((long)max(length, 0), longest);
   const int tok0 = t->first / p.ratio, tok1 = (min(t->first + COLS, t->cols) - 1) / p.ratio;
   const int pos0 = t->len - t->n + tok0, pos1 = t->len - t->n + tok1;
   t->seen = p.window > 0 ? max(0, pos0 - p.window + 1) : 0;
   t->lo = t->seen & ~(kStep - 1);
   t->steps = pos1 < t->lo ? 0 : (pos1 - t->lo) / kStep + 1;
   return true;
+}
+
+// Tile w, which a whole wavefront looks for: 64 requests at a time, one trip to memory for most launches.
+template <int COLS>
+__device__ __forceinline__ bool find_tile(const AttendParams& p, int w, Tile* t) {
+  if (!p.starts) {
+    const int per = (p.ratio + COLS - 1) / COLS, b = w / per;
+    return b < p.B && set_tile<COLS>(p, w, b, b * per, b, b + 1, p.lengths[b], t);
+  }
+  int lo = 0, hi = p.B - 1;
+  while (hi - lo >= 64) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (first_tile<COLS>(p, request_start(p, mid), mid) <= w) lo = mid; else hi = mid - 1;
+  }
+  const int lane = threadIdx.x & 63, i = min(lo + lane, hi);
+  const int row = request_start(p, i), next = request_start(p, i + 1), length = p.lengths[i], base = first_tile<COLS>(p, row, i);
+  const unsigned long begun = __ballot(lo + lane <= hi && base <= w);
+  if (begun == 0) return false;
+  const int k = 63 - __builtin_clzl(begun);
+  return set_tile<COLS>(p, w, lo + k, __builtin_amdgcn_readlane(base, k), __builtin_amdgcn_readlane(row, k),
+                        __builtin_amdgcn_readlane(next, k), __builtin_amdgcn_readlane(length, k), t);
+}
+
+// Bits t0 .. 15 of those below t1, each end within 0 .. 16: which of a sixteen's tokens count.
+__device__ __forceinline__ unsigned token_bits(int t0, int t1) {
+  return ((1u << min(max(t1, 0), 16)) - 1u) & ~((1u << min(max(t0, 0), 16)) - 1u);
 }
 
 // Half bytes u as binary16: the low ones of w's bytes 0 and 2 as 1024 + u, the high ones as 1024 + 16 u, one instruction

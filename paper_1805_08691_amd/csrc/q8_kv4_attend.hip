@@ -28,33 +28,51 @@ constexpr int kMaxTiles = 256;         // beyond them nothing is cut: a thread e
 // lengths, a tile to a thread.  Parts of cut tiles have a place in the workspace, no more than 2 kTarget of them (a cut
 // tile has more than `per` steps), and the cut tiles' heads, no more than kTarget, a counter.
 struct Part {
-  int tile, head, part, parts;
+  int head, part, parts;
   int slot, rank;                      // of a cut tile: its first part's place and its number, in units of H
   int step0, step1;
 };
 
-__device__ __forceinline__ void set_part(Part* a, const Tile& t) {
-  const int each = (t.steps + a->parts - 1) / a->parts;
-  a->step0 = a->part * each;
-  a->step1 = min(a->step0 + each, t.steps);
-}
-
-// The part of workgroup `id`; false: there is none.
-__device__ bool find_part(const AttendParams& p, int id, Part* a) {
+// The part of workgroup `id`, and its tile; false: there is none.  `shared`: LDS that is free until then.
+__device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* shared, Part* a, Tile* out) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int at = id / p.H, head = id - at * p.H;
-  *a = Part{at, head, 0, 1, 0, 0, 0, 0};
-  if (!p.parts) return at < p.tiles;
-  __shared__ long sums[2][kWaves];
-  __shared__ int found[6];
+  const int at = id / p.H;
+  *a = Part{id - at * p.H, 0, 1, 0, 0, 0, 0};
+  if (!p.parts) {
+    if (at >= p.tiles || !find_tile<kCols>(p, at, out)) return false;
+    a->step1 = out->steps;
+    return true;
+  }
+  long* const sums = reinterpret_cast<long*>(shared);          // [2][kWaves]
+  int* const found = reinterpret_cast<int*>(sums + 2 * kWaves);
+  int* const bases = found + 16;                               // of the requests: first tiles
+  int* const rows = bases + kMaxTiles;                         // and rows, with the last one's end
   Tile t;
-  const int steps = tid < p.tiles && find_tile<kCols>(p, tid, &t) ? max(t.steps, 1) : 0;
+  bool is = false;
+  if (!p.starts) {
+    const int per = (p.ratio + kCols - 1) / kCols, b = tid / per;
+    if (tid < p.tiles) is = set_tile<kCols>(p, tid, b, b * per, b, b + 1, p.lengths[b], &t);
+  } else {
+    for (int i = tid; i <= p.B; i += 256) {                    // (no more requests than tiles)
+      const int start = request_start(p, i);
+      rows[i] = start;
+      if (i < p.B) bases[i] = first_tile<kCols>(p, start, i);
+    }
+    __syncthreads();
+    int b = 0, hi = p.B - 1;
+    while (b < hi) {
+      const int mid = (b + hi + 1) >> 1;
+      if (bases[mid] <= tid) b = mid; else hi = mid - 1;
+    }
+    if (tid < p.tiles) is = set_tile<kCols>(p, tid, b, bases[b], rows[b], rows[b + 1], p.lengths[b], &t);
+  }
+  const int steps = is ? max(t.steps, 1) : 0;
   long total = steps;
   for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off, 64);
-  if (lane == 0) sums[0][wave] = total;
-  if (tid == 0) found[5] = 0;
+  if (lane == 0) sums[wave] = total;
+  if (tid == 0) found[0] = 0;
   __syncthreads();
-  total = ((sums[0][0] + sums[0][1]) + (sums[0][2] + sums[0][3])) * p.H;
+  total = ((sums[0] + sums[1]) + (sums[2] + sums[3])) * p.H;
   const int per = (int)max((total + kTarget - 1) / kTarget, (long)kMinSteps);
   // the sums before each tile: parts; those of cut tiles (16 bits up); cut tiles (40 bits up)
   const long n = steps ? (steps + per - 1) / per : 0, own = n > 1 ? n | n << 20 | 1l << 40 : n;
@@ -63,17 +81,25 @@ __device__ bool find_part(const AttendParams& p, int id, Part* a) {
     const long o = __shfl_up(v, off, 64);
     if (lane >= off) v += o;
   }
-  if (lane == 63) sums[1][wave] = v;
+  if (lane == 63) sums[kWaves + wave] = v;
   __syncthreads();
-  for (int u = 0; u < wave; ++u) v += sums[1][u];
+  for (int u = 0; u < wave; ++u) v += sums[kWaves + u];
   const long before = v - own;
   const int first = (int)(before & 0xfffff), slot = (int)(before >> 20 & 0xfffff), rank = (int)(before >> 40);
   if (at >= first && at < first + n) {
-    found[0] = tid, found[1] = at - first, found[2] = (int)n, found[3] = slot, found[4] = rank, found[5] = 1;
+    const int each = (t.steps + (int)n - 1) / (int)n, step0 = (at - first) * each;
+    found[0] = 1, found[1] = at - first, found[2] = (int)n, found[3] = slot, found[4] = rank;
+    found[5] = step0, found[6] = min(step0 + each, t.steps);
+    found[7] = t.b, found[8] = t.row, found[9] = t.first, found[10] = t.cols, found[11] = t.len, found[12] = t.n;
+    found[13] = t.seen, found[14] = t.lo, found[15] = t.steps;
   }
   __syncthreads();
-  a->tile = found[0], a->part = found[1], a->parts = found[2], a->slot = found[3], a->rank = found[4];
-  return found[5] != 0;
+  auto get = [&](int i) { return __builtin_amdgcn_readfirstlane(found[i]); };
+  const bool there = get(0) != 0;
+  *a = Part{a->head, get(1), get(2), get(3), get(4), get(5), get(6)};
+  *out = Tile{get(7), get(8), get(9), get(10), get(11), get(12), get(13), get(14), get(15)};
+  __syncthreads();                     // (LDS is free)
+  return there;
 }
 
 // Two numbers of the workspace, between workgroups of different XCDs: written through and read past their caches.
@@ -103,21 +129,32 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
                                                                          V* __restrict__ out) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int D = 32 * G, CT = 2 * G;                 // channels, tiles of 16 of them
+  constexpr int PITCH = D + 4;                          // of a column in LDS: eight lanes' quads meet different banks
   constexpr size_t kPartWords = kCols * (D + 2) / 2;    // of a part: sums [16][D], then a maximum and a sum for each column
   using St = Stage<G>;
   extern __shared__ __attribute__((aligned(16))) char shared[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, j = lane >> 4;
-  const Unpack un;
   Part a;
   Tile t;
-  if (!find_part(p, blockIdx.x, &a)) return;
-  a.tile = __builtin_amdgcn_readfirstlane(a.tile);
-  if (!find_tile<kCols>(p, a.tile, &t)) return;
-  set_part(&a, t);
-  const int head = a.head, step0 = __builtin_amdgcn_readfirstlane(a.step0), step1 = __builtin_amdgcn_readfirstlane(a.step1);
+  if (!find_part(p, blockIdx.x, shared, &a, &t)) return;
+  const int head = a.head, step0 = a.step0, step1 = a.step1;
+  const Unpack un;
   const int last = min(t.lo + t.steps * kStep, t.len);         // keys of the tile end here
   const int iterations = step0 + wave < step1 ? (step1 - step0 - wave + kWaves - 1) / kWaves : 0;
+
+  // ---- the column of this lane
+  const int col = t.first + r;
+  const bool given = col < t.cols;
+  const int tok = min(col, t.cols - 1) / p.ratio, qh = min(col, t.cols - 1) % p.ratio;
+  const int pos = given ? t.len - t.n + tok : -1;       // (no key is at or before -1)
+  const int from = p.window > 0 ? pos - p.window : -1;  // keys behind this one
+  float v[G][8];
+  {
+    const V* qr = q + (size_t)(t.row + tok) * p.q_stride + ((size_t)head * p.ratio + qh) * p.q_head + 8 * j;
+#pragma unroll
+    for (int g = 0; g < G; ++g) load_values<8, false>(qr + 32 * g, v[g]);
+  }
 
   // ---- loads: lane l holds where sixteen l % 4 of iteration l / 4 (of 16) lies, bit l of `held` whether it is there
   const int* __restrict__ table = p.table + t.b * p.table_stride;
@@ -131,7 +168,6 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
     where = in ? (((((long)page * p.H + head) << p.shift) + (at & ((1 << p.shift) - 1))) * St::SIXTEEN) : 0;
     held = __ballot(in);
   };
-  find_sixteens(0);
   char* const stage = shared + wave * St::SIZE;
   auto load = [&](__amdgpu_buffer_rsrc_t from, int at, int bytes, char* to) __attribute__((always_inline)) {
 #pragma unroll
@@ -156,21 +192,15 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
     }
   };
 
-  // ---- the column of this lane: its queries as the right operand, scaled to [1, 2) by a power of two and turned so
-  // that scores grow with the products.  The high half bytes come 16 times as large: their queries are a 16th.
-  const int col = t.first + r;
-  const bool given = col < t.cols;
-  const int tok = min(col, t.cols - 1) / p.ratio, qh = min(col, t.cols - 1) % p.ratio;
-  const int pos = given ? t.len - t.n + tok : -1;       // (no key is at or before -1)
-  const int from = p.window > 0 ? pos - p.window : -1;  // keys behind this one
+  find_sixteens(0);
+  if (iterations > 0) issue(0);
+
+  // ---- its queries as the right operand, scaled to [1, 2) by a power of two and turned so that scores grow with the
+  // products.  The high half bytes come 16 times as large: their queries are a 16th.
   h8 qf[G];
   float scale;
   {
-    const V* qr = q + (size_t)(t.row + tok) * p.q_stride + ((size_t)head * p.ratio + qh) * p.q_head + 8 * j;
-    float v[G][8], top = 0.0f;
-#pragma unroll
-    for (int g = 0; g < G; ++g) load_values<8, false>(qr + 32 * g, v[g]);
-    if (iterations > 0) issue(0);
+    float top = 0.0f;
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
@@ -227,29 +257,32 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
       }
     }
     if (!clear) {
-      int upto = (there >> j & 1u) ? pos : -1, behind = from;
-      asm volatile("" : "+v"(upto), "+v"(behind));      // (a branch, not selects in every step)
+      const int base = key0 + 16 * j;
+      unsigned see = token_bits(from + 1 - base, (there >> j & 1u) ? pos + 1 - base : 0);
+      asm volatile("" : "+v"(see));                     // (a branch, not selects in every step)
 #pragma unroll
       for (int tile = 0; tile < 4; ++tile)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = key0 + 16 * j + 4 * tile + i;
-          x[tile][i] = key <= upto && key > behind ? x[tile][i] : -__builtin_inff();
-        }
+        for (int i = 0; i < 4; ++i) x[tile][i] = see >> (4 * tile + i) & 1u ? x[tile][i] : -__builtin_inff();
     }
     // ---- the values' factors.  What lies outside the keys that the rows see may be no number: it counts as zero.
     // (Read twice, for their largest and for use: they would not fit the registers of three wavefronts a SIMD.)
     const bool edge = key0 < t.seen || key0 + kStep > last;
+    unsigned keep[8] = {};                              // of the factors as they lie, two each
+    if (edge) {
+      unsigned in = token_bits(t.seen - (key0 + 16 * j), last - (key0 + 16 * j));
+      asm volatile("" : "+v"(in));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int t0 = 4 * (e >> 1) + (e & 1);
+        keep[e] = (in >> t0 & 1u) * 0xffffu | (in >> (t0 + 2) & 1u) * 0xffff0000u;
+      }
+    }
     auto value_factors = [&](int g, h2 (&vf)[8]) __attribute__((always_inline)) {
       __builtin_memcpy(vf, __builtin_assume_aligned(factors + 32 * G + g * 32, 16), 32);
       if (edge) {
-        int before = t.seen - (key0 + 16 * j), behind = last - (key0 + 16 * j);
-        asm volatile("" : "+v"(before), "+v"(behind));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int t0 = 4 * (e >> 1) + (e & 1), t2 = t0 + 2;
-          vf[e] = h2{t0 >= before && t0 < behind ? vf[e][0] : 0.0f16, t2 >= before && t2 < behind ? vf[e][1] : 0.0f16};
-        }
+        for (int e = 0; e < 8; ++e) vf[e] = __builtin_bit_cast(h2, __builtin_bit_cast(unsigned, vf[e]) & keep[e]);
       }
     };
     s2 most = {0, 0};                                   // (none is negative: their patterns order as numbers)
@@ -334,7 +367,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
 
   // ---- the four wavefronts' columns together
   float* const cols = reinterpret_cast<float*>(shared);
-  float* const refs = cols + kWaves * kCols * D;
+  float* const refs = cols + kWaves * kCols * PITCH;
   float* const sums = refs + kWaves * kCols;
   if (j == 0) {
     refs[wave * kCols + r] = ref;
@@ -345,7 +378,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
 #pragma unroll
   for (int v = 0; v < kWaves; ++v) all = fmaxf(all, refs[v * kCols + r]);
   const float mine = ref == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ref - all);
-  float* const to = cols + (wave * kCols + r) * D + 4 * j;
+  float* const to = cols + (wave * kCols + r) * PITCH + 4 * j;
 #pragma unroll
   for (int c = 0; c < CT; ++c) *reinterpret_cast<f4*>(to + 16 * c) = o[c] * mine;
   __syncthreads();
@@ -359,7 +392,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
     for (int u = 0; u < kWaves; ++u) m = fmaxf(m, refs[u * kCols + c]);
 #pragma unroll
     for (int u = 0; u < kWaves; ++u) {
-      v += *reinterpret_cast<const f4*>(cols + (u * kCols + c) * D + d);
+      v += *reinterpret_cast<const f4*>(cols + (u * kCols + c) * PITCH + d);
       const float ru = refs[u * kCols + c];
       l += ru == -__builtin_inff() ? 0.0f : sums[u * kCols + c] * __builtin_amdgcn_exp2f(ru - m);
     }
@@ -457,7 +490,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
 
 template <int G, typename V>
 int launch(const AttendParams& p, const V* q, V* out, hipStream_t stream) {
-  const size_t stages = (size_t)kWaves * Stage<G>::SIZE, columns = (size_t)kWaves * kCols * (32 * G + 2) * 4;
+  const size_t stages = (size_t)kWaves * Stage<G>::SIZE, columns = (size_t)kWaves * kCols * (32 * G + 6) * 4;
   const size_t adding = 256 * sizeof(f4) + (kTarget + 1) * kCols * sizeof(float);
   size_t lds = stages > columns ? stages : columns;
   if (p.parts && lds < adding) lds = adding;
