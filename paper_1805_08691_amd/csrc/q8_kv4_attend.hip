@@ -33,6 +33,17 @@ struct Part {
   int step0, step1;
 };
 
+// Sums over the lanes up to this one (16 at a time, then over the rows of 16).
+__device__ __forceinline__ unsigned scan64(unsigned v) {
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x111, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x142, 0xa, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+
 // The part of workgroup `id`, and its tile; false: there is none.  `shared`: LDS that is free until then.
 __device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* shared, Part* a, Tile* out) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -43,10 +54,13 @@ __device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* s
     a->step1 = out->steps;
     return true;
   }
-  long* const sums = reinterpret_cast<long*>(shared);          // [2][kWaves]
-  int* const found = reinterpret_cast<int*>(sums + 2 * kWaves);
-  int* const bases = found + 16;                               // of the requests: first tiles
-  int* const rows = bases + kMaxTiles;                         // and rows, with the last one's end
+  int* const found = reinterpret_cast<int*>(shared);
+  unsigned* const low = reinterpret_cast<unsigned*>(found + 16);               // [kWaves], three times
+  unsigned* const high = low + kWaves;
+  unsigned* const sums = high + kWaves;
+  int* const bases = reinterpret_cast<int*>(sums + kWaves);    // of the requests: first tiles,
+  int* const lengths = bases + kMaxTiles;
+  int* const rows = lengths + kMaxTiles;                       // rows, with the last one's end
   Tile t;
   bool is = false;
   if (!p.starts) {
@@ -54,9 +68,9 @@ __device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* s
     if (tid < p.tiles) is = set_tile<kCols>(p, tid, b, b * per, b, b + 1, p.lengths[b], &t);
   } else {
     for (int i = tid; i <= p.B; i += 256) {                    // (no more requests than tiles)
-      const int start = request_start(p, i);
+      const int start = request_start(p, i), length = i < p.B ? p.lengths[i] : 0;
       rows[i] = start;
-      if (i < p.B) bases[i] = first_tile<kCols>(p, start, i);
+      if (i < p.B) bases[i] = first_tile<kCols>(p, start, i), lengths[i] = length;
     }
     __syncthreads();
     int b = 0, hi = p.B - 1;
@@ -64,29 +78,25 @@ __device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* s
       const int mid = (b + hi + 1) >> 1;
       if (bases[mid] <= tid) b = mid; else hi = mid - 1;
     }
-    if (tid < p.tiles) is = set_tile<kCols>(p, tid, b, bases[b], rows[b], rows[b + 1], p.lengths[b], &t);
+    if (tid < p.tiles) is = set_tile<kCols>(p, tid, b, bases[b], rows[b], rows[b + 1], lengths[b], &t);
   }
-  const int steps = is ? max(t.steps, 1) : 0;
-  long total = steps;
-  for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off, 64);
-  if (lane == 0) sums[wave] = total;
+  // all tiles' steps, in two halves: less than 2^25 of each, 2^8 tiles
+  const unsigned steps = is ? max(t.steps, 1) : 0;
+  const unsigned lo = scan64(steps & 0xffffu), hi = scan64(steps >> 16);
+  if (lane == 63) low[wave] = lo, high[wave] = hi;
   if (tid == 0) found[0] = 0;
   __syncthreads();
-  total = ((sums[0] + sums[1]) + (sums[2] + sums[3])) * p.H;
-  const int per = (int)max((total + kTarget - 1) / kTarget, (long)kMinSteps);
-  // the sums before each tile: parts; those of cut tiles (16 bits up); cut tiles (40 bits up)
-  const long n = steps ? (steps + per - 1) / per : 0, own = n > 1 ? n | n << 20 | 1l << 40 : n;
-  long v = own;
-  for (int off = 1; off < 64; off <<= 1) {
-    const long o = __shfl_up(v, off, 64);
-    if (lane >= off) v += o;
-  }
-  if (lane == 63) sums[kWaves + wave] = v;
+  const long total = ((long)((low[0] + low[1]) + (low[2] + low[3])) + ((long)((high[0] + high[1]) + (high[2] + high[3])) << 16)) * p.H;
+  const unsigned per = (unsigned)max((total + kTarget - 1) / kTarget, (long)kMinSteps);
+  // the sums before each tile: parts (kTarget + kMaxTiles at most); those of cut tiles (10 bits up); cut tiles (20 bits up)
+  const unsigned n = steps ? (steps + per - 1) / per : 0, own = n > 1 ? n | n << 10 | 1u << 20 : n;
+  unsigned v = scan64(own);
+  if (lane == 63) sums[wave] = v;
   __syncthreads();
-  for (int u = 0; u < wave; ++u) v += sums[kWaves + u];
-  const long before = v - own;
-  const int first = (int)(before & 0xfffff), slot = (int)(before >> 20 & 0xfffff), rank = (int)(before >> 40);
-  if (at >= first && at < first + n) {
+  for (int u = 0; u < wave; ++u) v += sums[u];
+  const unsigned before = v - own;
+  const int first = (int)(before & 0x3ffu), slot = (int)(before >> 10 & 0x3ffu), rank = (int)(before >> 20);
+  if (at >= first && at < first + (int)n) {
     const int each = (t.steps + (int)n - 1) / (int)n, step0 = (at - first) * each;
     found[0] = 1, found[1] = at - first, found[2] = (int)n, found[3] = slot, found[4] = rank;
     found[5] = step0, found[6] = min(step0 + each, t.steps);
