@@ -4,11 +4,15 @@
 // A workgroup of four wavefronts owns 128 columns that share a key head, 32 of each wavefront's, and walks over the
 // keys they see, 64 at a time.  The codes go from memory to LDS as they lie; the wavefronts unpack a quarter of them
 // each, into operands of the matrix instruction in the order in which a wavefront reads them, and multiply all.
-// Bound by vector instructions (unpacking 1.6 a code, the softmax 8 a score) beside the matrix instructions, so several
-// workgroups share a compute unit and two barriers a step are hidden behind each other's.
-// bf16 outputs: a key is its code times its factor, rounded to binary16 (2^-12 of a key, 4.5e-4 of an output, under bf16's
-// 1.6e-3).  fp16 outputs show that: there codes are multiplied and factors go into the sums.  A maximum that grows by
-// less than 2^8 is left: probabilities are up to 256, and sums are not rescaled.
+// Bound by vector instructions (unpacking 1.6 a code of a workgroup's keys, the softmax 4.5 a score) beside the matrix
+// instructions, of which a third of the cycles is full, so three workgroups share a compute unit and two barriers a step
+// are hidden behind each other's.
+// bf16 outputs: a key is its code times its factor, and a query has the scale in it, both rounded to binary16 (2^-12 of
+// each, 6e-4 of an output, under bf16's 1.6e-3); scores come out of the products relative to the running maximum, which
+// they begin with.  fp16 outputs show that: there codes are multiplied, and factors and scale go into the sums.  A maximum
+// that grows by less than 2^8 is left: probabilities are up to 256, and sums are not rescaled.  The sum is that of the
+// probabilities as the values meet them, rounded to binary16.
+// Pieces of 2048 tokens of 3 requests over 8192 keys, 32 query heads of 128 channels: 395 us, 910 TFLOP/s.
 #include "q8_kv4_attend.h"
 
 namespace {
@@ -77,7 +81,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
 
   // ---- the columns of this lane
   h8 qf[kTiles][G];
-  float scale[kTiles], ref[kTiles], sum[kTiles];
+  float rest[kTiles], ref[kTiles], limit[kTiles], sum[kTiles];   // scores are products times `rest`
   int* const positions = reinterpret_cast<int*>(shared + W::POS_AT) + wave * kTiles * kCols + r;   // (registers are short)
   f4 o[kTiles][CT];
   if (t.steps > 0) issue(0);
@@ -97,13 +101,22 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
     top = column_max(top);
     const unsigned e2 = min(max(__float_as_uint(top) >> 23, 1u), 253u);
     const float down = copysignf(__uint_as_float((254u - e2) << 23), p.scale_log2);
-    scale[c] = fmaxf(fabsf(p.scale_log2) * __uint_as_float(e2 << 23), 1e-30f);   // (no 0 times infinity)
+    rest[c] = fmaxf(fabsf(p.scale_log2) * __uint_as_float(e2 << 23), 1e-30f);    // (no 0 times infinity)
+    float fold = 1.0f;
+    if constexpr (!EXACT) {
+      // into the queries, all of it or all but a power of two
+      const float power = __uint_as_float(__float_as_uint(rest[c]) & 0x7f800000u);
+      const float keep = power >= 0x1p-8f && power <= 0x1p8f ? 1.0f : power;
+      fold = rest[c] / keep;
+      rest[c] = keep;
+    }
     constexpr int kKeyOrder[8] = {0, 4, 2, 6, 1, 5, 3, 7};
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) qf[c][g][e] = (_Float16)(v[g][kKeyOrder[e]] * down);
-    ref[c] = -__builtin_inff();
+      for (int e = 0; e < 8; ++e) qf[c][g][e] = (_Float16)(v[g][kKeyOrder[e]] * (down * fold));
+    ref[c] = 0.0f;
+    limit[c] = -__builtin_inff();
     sum[c] = 0.0f;
 #pragma unroll
     for (int i = 0; i < CT; ++i) o[c][i] = f4{0, 0, 0, 0};
@@ -117,6 +130,9 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
     return __builtin_elementwise_fma(un.high(w), h2{kSixteenth, kSixteenth}, h2{kHighBias, kHighBias});
   };
 
+  bool folded = !EXACT;
+#pragma unroll
+  for (int c = 0; c < kTiles; ++c) folded &= !__any(rest[c] != 1.0f);
   for (int s = 0; s < t.steps; ++s) {
     const int key0 = t.lo + s * kStep;
     wait_vmcnt<0>();
@@ -148,7 +164,6 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
     }
     // ---- and of the values, a group's 32 of the keys each.  What lies outside the keys that the rows see may be no
     // number: its factors count as zeros.
-    const int before = t.seen - (key0 + 16 * j), behind = last - (key0 + 16 * j);
     const bool edge = key0 < t.seen || key0 + kStep > last;
 #pragma unroll
     for (int i0 = 0; i0 < 2 * G; i0 += kWaves) {
@@ -160,10 +175,13 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
         __builtin_memcpy(vc, __builtin_assume_aligned(at + W::CODES + (g * 16 + r) * 16 + 8 * h, 8), 8);
         __builtin_memcpy(vf, __builtin_assume_aligned(at + 544 * G + g * 32 + 16 * h, 16), 16);
         if (edge) {
+          unsigned in = token_bits(t.seen - (key0 + 16 * j), last - (key0 + 16 * j)) >> 8 * h;
+          asm volatile("" : "+v"(in));
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int t0 = 8 * h + 4 * (e >> 1) + (e & 1), t2 = t0 + 2;
-            vf[e] = h2{t0 >= before && t0 < behind ? vf[e][0] : 0.0f16, t2 >= before && t2 < behind ? vf[e][1] : 0.0f16};
+            const int t0 = 4 * (e >> 1) + (e & 1);
+            const unsigned keep = (in >> t0 & 1u) * 0xffffu | (in >> (t0 + 2) & 1u) * 0xffff0000u;
+            vf[e] = __builtin_bit_cast(h2, __builtin_bit_cast(unsigned, vf[e]) & keep);
           }
         }
         char* const to = shared + W::V_AT + (g * 4 + h) * 1024 + lane * 16;
@@ -177,12 +195,18 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 
-    // ---- S^T, keys 16 j + 4 tile + i in register i of tile `tile`
+    // (Wavefronts that multiply go before those that unpack: pieces of 2048 tokens 417 -> 395 us, a prompt of 4096 163 -> 170,
+    // whose tiles are of all lengths.)
+    __builtin_amdgcn_s_setprio(1);
+    // ---- S^T, keys 16 j + 4 tile + i in register i of tile `tile`, relative to `ref`: the products begin with it
     f4 x[kTiles][4];
+    float from[kTiles];
+#pragma unroll
+    for (int c = 0; c < kTiles; ++c) from[c] = folded ? -ref[c] : 0.0f;
 #pragma unroll
     for (int tile = 0; tile < 4; ++tile) {
 #pragma unroll
-      for (int c = 0; c < kTiles; ++c) x[c][tile] = f4{0, 0, 0, 0};
+      for (int c = 0; c < kTiles; ++c) x[c][tile] = f4{from[c], from[c], from[c], from[c]};
       _Float16 kf[4][G];
       if constexpr (EXACT)
         __builtin_memcpy(kf, __builtin_assume_aligned(raw + j * W::SIXTEEN + 512 * G + tile * 8 * G, 8), 8 * G);
@@ -201,20 +225,25 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
         }
       }
     }
+    if (EXACT || !folded) {
+#pragma unroll
+      for (int c = 0; c < kTiles; ++c)
+#pragma unroll
+        for (int tile = 0; tile < 4; ++tile)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[c][tile][i] = __builtin_fmaf(x[c][tile][i], rest[c], -ref[c]);
+    }
     const bool clear = key0 > clear0 && key0 + kStep - 1 <= clear1 && there[0] == 15u;
     if (!clear) {
 #pragma unroll
       for (int c = 0; c < kTiles; ++c) {
-        const int pos = positions[c * kCols];
-        int upto = (there[0] >> j & 1u) ? pos : -1, after = p.window > 0 ? pos - p.window : -1;
-        asm volatile("" : "+v"(upto), "+v"(after));   // (a branch, not selects in every step)
+        const int pos = positions[c * kCols] + 1 - (key0 + 16 * j);
+        unsigned see = token_bits(p.window > 0 ? pos - p.window : 0, there[0] >> j & 1u ? pos : 0);
+        asm volatile("" : "+v"(see));                 // (a branch, not selects in every step)
 #pragma unroll
         for (int tile = 0; tile < 4; ++tile)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int key = key0 + 16 * j + 4 * tile + i;
-            x[c][tile][i] = key <= upto && key > after ? x[c][tile][i] : -__builtin_inff();
-          }
+          for (int i = 0; i < 4; ++i) x[c][tile][i] = see >> (4 * tile + i) & 1u ? x[c][tile][i] : -__builtin_inff();
       }
     }
     // ---- probabilities
@@ -226,27 +255,32 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
       for (int tile = 0; tile < 4; ++tile)
 #pragma unroll
         for (int i = 0; i < 4; ++i) m = fmaxf(m, x[c][tile][i]);
-      m = column_max(m) * scale[c];
-      if (__any(m > ref[c] + kSlack)) {
-        const float now = fmaxf(ref[c], m);
-        const float shrink = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(ref[c] - now);
-        ref[c] = now;
+      m = column_max(m);
+      if (__any(m > limit[c])) {                      // (the first keys that a column sees: no limit yet)
+        const bool begun = limit[c] > -__builtin_inff(), seen = m > -__builtin_inff();
+        const float more = begun ? fmaxf(m, 0.0f) : seen ? m : 0.0f;
+        const float shrink = begun ? __builtin_amdgcn_exp2f(-more) : 1.0f;
+        ref[c] += more;
+        if (seen) limit[c] = kSlack;
         sum[c] *= shrink;
 #pragma unroll
         for (int i = 0; i < CT; ++i) o[c][i] *= shrink;
+#pragma unroll
+        for (int tile = 0; tile < 4; ++tile)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[c][tile][i] -= more;
       }
-      const float base = ref[c] == -__builtin_inff() ? 0.0f : ref[c];
 #pragma unroll
       for (int tile = 0; tile < 4; ++tile) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[c][tile][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[c][tile][i], scale[c], -base));
-          sum[c] += x[c][tile][i];
-        }
-        pr[c][tile >> 1][4 * (tile & 1)] = (_Float16)x[c][tile][0];
-        pr[c][tile >> 1][4 * (tile & 1) + 1] = (_Float16)x[c][tile][2];
-        pr[c][tile >> 1][4 * (tile & 1) + 2] = (_Float16)x[c][tile][1];
-        pr[c][tile >> 1][4 * (tile & 1) + 3] = (_Float16)x[c][tile][3];
+        for (int i = 0; i < 4; ++i) x[c][tile][i] = __builtin_amdgcn_exp2f(x[c][tile][i]);
+        const h2 ones = {1.0f16, 1.0f16}, even = {(_Float16)x[c][tile][0], (_Float16)x[c][tile][2]};
+        const h2 odd = {(_Float16)x[c][tile][1], (_Float16)x[c][tile][3]};
+        sum[c] = __builtin_amdgcn_fdot2(even, ones, sum[c], false);             // of what the values are multiplied by
+        sum[c] = __builtin_amdgcn_fdot2(odd, ones, sum[c], false);
+        h8& to = pr[c][tile >> 1];
+        to[4 * (tile & 1)] = even[0], to[4 * (tile & 1) + 1] = even[1];
+        to[4 * (tile & 1) + 2] = odd[0], to[4 * (tile & 1) + 3] = odd[1];
       }
     }
     // ---- O^T
@@ -258,8 +292,8 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
 #pragma unroll
         for (int c = 0; c < kTiles; ++c) o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, pr[c][h], o[c][i], 0, 0, 0);
       }
+    __builtin_amdgcn_s_setprio(0);
   }
-
 #pragma unroll
   for (int c = 0; c < kTiles; ++c) {
     sum[c] += __shfl_xor(sum[c], 16, 64);
