@@ -631,7 +631,8 @@ int q8_kv4_read(const void *cache_dev, size_t n_pages, int page, const int64_t *
  * products binary16 x binary16.
  *   workspace   NULL, or device memory (16-byte aligned) with which the keys of few rows are
  *               split over workgroups: q8_kv4_attend_workspace_bytes, `longest` being the largest
- *               length expected (a hint; 0 bytes: nothing is split).  The caller zeroes it once
+ *               length expected (a hint; 0 bytes: nothing is split).  With less memory than a call
+ *               would split with it does without.  The caller zeroes it once
  *               after allocating it; every call leaves its counters zero again.  Calls that share
  *               one must not overlap in time.                                              */
 size_t q8_kv4_attend_workspace_bytes(size_t T, int n_requests, int n_heads, int ratio, int D,

@@ -108,10 +108,118 @@ __device__ __forceinline__ float column_max(float v) {
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
+constexpr int kTarget = 512;           // parts that the keys are cut into where tiles are few
+constexpr int kMinSteps = 8;           // steps of a part, at least
+constexpr int kMaxTiles = 256;         // beyond them nothing is cut: a thread each
+
+// The split of the key axis.  The steps of all tiles and heads over kTarget are what a part should hold (kMinSteps at
+// least); a tile of more steps is cut into equal parts of no more.  Every workgroup works this out for itself from the
+// lengths, a tile to a thread.  Parts of cut tiles have a place in the workspace, no more than 2 kTarget of them (a cut
+// tile has more than `per` steps), and the cut tiles' heads, no more than kTarget, a counter.
+struct Part {
+  int head, part, parts;
+  int slot, rank;                      // of a cut tile: its first part's place and its number, in units of H
+  int step0, step1;
+};
+
+// Sums over the lanes up to this one (16 at a time, then over the rows of 16).
+__device__ __forceinline__ unsigned scan64(unsigned v) {
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x111, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x142, 0xa, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+
+// The part of workgroup `id` (of MOST that a tile is cut into at most), and its tile; false: there is none.  `shared`: LDS that is free until then.
+template <int COLS, int MOST>
+__device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* shared, Part* a, Tile* out) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int at = id / p.H;
+  *a = Part{id - at * p.H, 0, 1, 0, 0, 0, 0};
+  if (!p.parts) {
+    if (at >= p.tiles || !find_tile<COLS>(p, at, out)) return false;
+    a->step1 = out->steps;
+    return true;
+  }
+  int* const found = reinterpret_cast<int*>(shared);
+  unsigned* const low = reinterpret_cast<unsigned*>(found + 16);               // [kWaves], three times
+  unsigned* const high = low + kWaves;
+  unsigned* const sums = high + kWaves;
+  int* const bases = reinterpret_cast<int*>(sums + kWaves);    // of the requests: first tiles,
+  int* const lengths = bases + kMaxTiles;
+  int* const rows = lengths + kMaxTiles;                       // rows, with the last one's end
+  Tile t;
+  bool is = false;
+  if (!p.starts) {
+    const int per = (p.ratio + COLS - 1) / COLS, b = tid / per;
+    if (tid < p.tiles) is = set_tile<COLS>(p, tid, b, b * per, b, b + 1, p.lengths[b], &t);
+  } else {
+    for (int i = tid; i <= p.B; i += 256) {                    // (no more requests than tiles)
+      const int start = request_start(p, i), length = i < p.B ? p.lengths[i] : 0;
+      rows[i] = start;
+      if (i < p.B) bases[i] = first_tile<COLS>(p, start, i), lengths[i] = length;
+    }
+    __syncthreads();
+    int b = 0, hi = p.B - 1;
+    while (b < hi) {
+      const int mid = (b + hi + 1) >> 1;
+      if (bases[mid] <= tid) b = mid; else hi = mid - 1;
+    }
+    if (tid < p.tiles) is = set_tile<COLS>(p, tid, b, bases[b], rows[b], rows[b + 1], lengths[b], &t);
+  }
+  // all tiles' steps, in two halves: less than 2^25 of each, 2^8 tiles
+  const unsigned steps = is ? max(t.steps, 1) : 0;
+  const unsigned lo = scan64(steps & 0xffffu), hi = scan64(steps >> 16);
+  if (lane == 63) low[wave] = lo, high[wave] = hi;
+  if (tid == 0) found[0] = 0;
+  __syncthreads();
+  const long total = ((long)((low[0] + low[1]) + (low[2] + low[3])) + ((long)((high[0] + high[1]) + (high[2] + high[3])) << 16)) * p.H;
+  const unsigned per = (unsigned)max((total + kTarget - 1) / kTarget, (long)kMinSteps);
+  // the sums before each tile: parts (kTarget + kMaxTiles at most); those of cut tiles (10 bits up); cut tiles (20 bits up)
+  const unsigned n = steps ? min((steps + per - 1) / per, (unsigned)MOST) : 0, own = n > 1 ? n | n << 10 | 1u << 20 : n;
+  unsigned v = scan64(own);
+  if (lane == 63) sums[wave] = v;
+  __syncthreads();
+  for (int u = 0; u < wave; ++u) v += sums[u];
+  // (the last tiles of a request see most keys: where tiles take longest they go first)
+  const int place = COLS == kCols ? at : (int)(((sums[0] + sums[1]) + (sums[2] + sums[3])) & 0x3ffu) - 1 - at;
+  const unsigned before = v - own;
+  const int first = (int)(before & 0x3ffu), slot = (int)(before >> 10 & 0x3ffu), rank = (int)(before >> 20);
+  if (place >= first && place < first + (int)n) {
+    const int each = (t.steps + (int)n - 1) / (int)n, step0 = (place - first) * each;
+    found[0] = 1, found[1] = place - first, found[2] = (int)n, found[3] = slot, found[4] = rank;
+    found[5] = step0, found[6] = min(step0 + each, t.steps);
+    found[7] = t.b, found[8] = t.row, found[9] = t.first, found[10] = t.cols, found[11] = t.len, found[12] = t.n;
+    found[13] = t.seen, found[14] = t.lo, found[15] = t.steps;
+  }
+  __syncthreads();
+  auto get = [&](int i) { return __builtin_amdgcn_readfirstlane(found[i]); };
+  const bool there = get(0) != 0;
+  *a = Part{a->head, get(1), get(2), get(3), get(4), get(5), get(6)};
+  *out = Tile{get(7), get(8), get(9), get(10), get(11), get(12), get(13), get(14), get(15)};
+  __syncthreads();                     // (LDS is free)
+  return there;
+}
+
+// Two numbers of the workspace, between workgroups of different XCDs: written through and read past their caches.
+typedef unsigned long word;
+typedef float f2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void put(word* to, float a, float b) {
+  __hip_atomic_store(to, (word)__float_as_uint(a) | (word)__float_as_uint(b) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+}
+__device__ __forceinline__ f2 get(const word* from) {
+  const word v = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+  return f2{__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32))};
+}
+
 }  // namespace
 
 // The launch for many columns (q8_kv4_wide.hip); p.tiles: of kWideCols columns.
 constexpr int kWideCols = 128;
+constexpr int kWideParts = 16;         // that a tile of them is cut into at most: the last workgroup adds them alone
 int kv4_attend_wide(int G, const AttendParams& p, const void* q, void* out, int type, hipStream_t stream);
 
 }  // namespace q8

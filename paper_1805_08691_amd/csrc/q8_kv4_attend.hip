@@ -19,110 +19,6 @@ namespace {
 
 using namespace q8;
 
-constexpr int kTarget = 512;           // parts that the keys are cut into where tiles are few
-constexpr int kMinSteps = 8;           // steps of a part, at least
-constexpr int kMaxTiles = 256;         // beyond them nothing is cut: a thread each
-
-// The split of the key axis.  The steps of all tiles and heads over kTarget are what a part should hold (kMinSteps at
-// least); a tile of more steps is cut into equal parts of no more.  Every workgroup works this out for itself from the
-// lengths, a tile to a thread.  Parts of cut tiles have a place in the workspace, no more than 2 kTarget of them (a cut
-// tile has more than `per` steps), and the cut tiles' heads, no more than kTarget, a counter.
-struct Part {
-  int head, part, parts;
-  int slot, rank;                      // of a cut tile: its first part's place and its number, in units of H
-  int step0, step1;
-};
-
-// Sums over the lanes up to this one (16 at a time, then over the rows of 16).
-__device__ __forceinline__ unsigned scan64(unsigned v) {
-  v += __builtin_amdgcn_update_dpp(0u, v, 0x111, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0u, v, 0x112, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0u, v, 0x114, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0u, v, 0x118, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0u, v, 0x142, 0xa, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0u, v, 0x143, 0xc, 0xf, false);
-  return v;
-}
-
-// The part of workgroup `id`, and its tile; false: there is none.  `shared`: LDS that is free until then.
-__device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* shared, Part* a, Tile* out) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int at = id / p.H;
-  *a = Part{id - at * p.H, 0, 1, 0, 0, 0, 0};
-  if (!p.parts) {
-    if (at >= p.tiles || !find_tile<kCols>(p, at, out)) return false;
-    a->step1 = out->steps;
-    return true;
-  }
-  int* const found = reinterpret_cast<int*>(shared);
-  unsigned* const low = reinterpret_cast<unsigned*>(found + 16);               // [kWaves], three times
-  unsigned* const high = low + kWaves;
-  unsigned* const sums = high + kWaves;
-  int* const bases = reinterpret_cast<int*>(sums + kWaves);    // of the requests: first tiles,
-  int* const lengths = bases + kMaxTiles;
-  int* const rows = lengths + kMaxTiles;                       // rows, with the last one's end
-  Tile t;
-  bool is = false;
-  if (!p.starts) {
-    const int per = (p.ratio + kCols - 1) / kCols, b = tid / per;
-    if (tid < p.tiles) is = set_tile<kCols>(p, tid, b, b * per, b, b + 1, p.lengths[b], &t);
-  } else {
-    for (int i = tid; i <= p.B; i += 256) {                    // (no more requests than tiles)
-      const int start = request_start(p, i), length = i < p.B ? p.lengths[i] : 0;
-      rows[i] = start;
-      if (i < p.B) bases[i] = first_tile<kCols>(p, start, i), lengths[i] = length;
-    }
-    __syncthreads();
-    int b = 0, hi = p.B - 1;
-    while (b < hi) {
-      const int mid = (b + hi + 1) >> 1;
-      if (bases[mid] <= tid) b = mid; else hi = mid - 1;
-    }
-    if (tid < p.tiles) is = set_tile<kCols>(p, tid, b, bases[b], rows[b], rows[b + 1], lengths[b], &t);
-  }
-  // all tiles' steps, in two halves: less than 2^25 of each, 2^8 tiles
-  const unsigned steps = is ? max(t.steps, 1) : 0;
-  const unsigned lo = scan64(steps & 0xffffu), hi = scan64(steps >> 16);
-  if (lane == 63) low[wave] = lo, high[wave] = hi;
-  if (tid == 0) found[0] = 0;
-  __syncthreads();
-  const long total = ((long)((low[0] + low[1]) + (low[2] + low[3])) + ((long)((high[0] + high[1]) + (high[2] + high[3])) << 16)) * p.H;
-  const unsigned per = (unsigned)max((total + kTarget - 1) / kTarget, (long)kMinSteps);
-  // the sums before each tile: parts (kTarget + kMaxTiles at most); those of cut tiles (10 bits up); cut tiles (20 bits up)
-  const unsigned n = steps ? (steps + per - 1) / per : 0, own = n > 1 ? n | n << 10 | 1u << 20 : n;
-  unsigned v = scan64(own);
-  if (lane == 63) sums[wave] = v;
-  __syncthreads();
-  for (int u = 0; u < wave; ++u) v += sums[u];
-  const unsigned before = v - own;
-  const int first = (int)(before & 0x3ffu), slot = (int)(before >> 10 & 0x3ffu), rank = (int)(before >> 20);
-  if (at >= first && at < first + (int)n) {
-    const int each = (t.steps + (int)n - 1) / (int)n, step0 = (at - first) * each;
-    found[0] = 1, found[1] = at - first, found[2] = (int)n, found[3] = slot, found[4] = rank;
-    found[5] = step0, found[6] = min(step0 + each, t.steps);
-    found[7] = t.b, found[8] = t.row, found[9] = t.first, found[10] = t.cols, found[11] = t.len, found[12] = t.n;
-    found[13] = t.seen, found[14] = t.lo, found[15] = t.steps;
-  }
-  __syncthreads();
-  auto get = [&](int i) { return __builtin_amdgcn_readfirstlane(found[i]); };
-  const bool there = get(0) != 0;
-  *a = Part{a->head, get(1), get(2), get(3), get(4), get(5), get(6)};
-  *out = Tile{get(7), get(8), get(9), get(10), get(11), get(12), get(13), get(14), get(15)};
-  __syncthreads();                     // (LDS is free)
-  return there;
-}
-
-// Two numbers of the workspace, between workgroups of different XCDs: written through and read past their caches.
-typedef unsigned long word;
-typedef float f2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ void put(word* to, float a, float b) {
-  __hip_atomic_store(to, (word)__float_as_uint(a) | (word)__float_as_uint(b) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
-}
-__device__ __forceinline__ f2 get(const word* from) {
-  const word v = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
-  return f2{__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32))};
-}
-
 // A wavefront's step in LDS, 64 keys: the codes of its four sixteens' keys (32 bytes between them: the four rows that one
 // LDS access serves then meet different banks), of their values, and their factors.
 template <int G>
@@ -147,7 +43,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
   const int r = lane & 15, j = lane >> 4;
   Part a;
   Tile t;
-  if (!find_part(p, blockIdx.x, shared, &a, &t)) return;
+  if (!find_part<kCols, kTarget>(p, blockIdx.x, shared, &a, &t)) return;
   const int head = a.head, step0 = a.step0, step1 = a.step1;
   const Unpack un;
   const int last = min(t.lo + t.steps * kStep, t.len);         // keys of the tile end here
@@ -536,14 +432,29 @@ size_t tiles_of(size_t T, int B, int ratio, bool starts, int cols = kCols) {
 // Whether keys of at most `longest` are cut: where parts of kMinSteps could be made, and tiles are so few that a part of
 // the longest could keep compute units waiting.
 bool cut(size_t tiles, size_t longest) { return tiles <= kMaxTiles && longest > (size_t)kMinSteps * kStep; }
-size_t parts_bytes(int D) { return (size_t)2 * kTarget * kCols * (D + 2) * 4; }
-size_t split_bytes(int D) { return parts_bytes(D) + kTarget * sizeof(int); }
+// Workspace: the counters (in one place for both kernels), then the parts.
+constexpr size_t kCounterBytes = (kTarget + 15) / 16 * 16 * sizeof(int);
+size_t split_bytes(int D, int cols = kCols) { return kCounterBytes + (size_t)2 * kTarget * cols * (D + 2) * 4; }
+
+// Whether tiles of 128 columns, which unpack a key once for all of them, are taken for new tokens in runs of several: where
+// requests have that many columns and the tiles are a workgroup for every compute unit, or can be cut, and parts of them
+// are long enough for what adding them costs.  (3 pieces of 2048 tokens over 8192 keys, 32 query heads on 4 of 128 channels:
+// 752 us in tiles of 16 columns, 395 so; 512 tokens of one request, 32 on 8, over 4096, 8192, 32768 keys: 91, 163, 591
+// and, cut, 68, 108, 321; but 128 tokens over 8192 keys 60 and 71, and with 256 channels, 2 times 256 tokens over 16384
+// keys, 179 and 226.)
+bool wide_for(size_t T, int B, int H, int ratio, int D, size_t longest, bool cuts) {
+  const size_t tiles = tiles_of(T, B, ratio, true, kWideCols) * H;
+  if (T * ratio < (size_t)B * (kWideCols / 2)) return false;
+  return tiles >= 256 || (cuts && tiles >= 32 && tiles * (longest / kStep) / kTarget >= (D <= 128 ? 32u : 64u));
+}
 
 }  // namespace
 
 extern "C" size_t q8_kv4_attend_workspace_bytes(size_t T, int n_requests, int n_heads, int ratio, int D,
                                                 size_t longest) {
   if (n_requests < 1 || n_heads < 1 || ratio < 1 || D < 32 || D > kMaxHead || T > 0x7fffffffu) return 0;
+  const bool cuts = cut(tiles_of(T, n_requests, ratio, true, kWideCols), longest);
+  if (cuts && wide_for(T, n_requests, n_heads, ratio, D, longest, true)) return split_bytes(D, kWideCols);
   return cut(tiles_of(T, n_requests, ratio, false), longest) ? split_bytes(D) : 0;
 }
 
@@ -564,21 +475,19 @@ extern "C" int q8_kv4_attend(const void* q_dev, int type, size_t T, int n_heads,
   Q8_REQUIRE(T <= 0x7fffffffu && n_pages <= 0x7fffffffu && (size_t)width * page <= 0x7fffffc0u, Q8_EUNSUPPORTED);
   Q8_REQUIRE(q8_aligned(q_dev, 2) && q8_aligned(out_dev, 2) && q8_aligned(cache_dev, 64) && q8_aligned(table_dev, 4) &&
                  q8_aligned(lengths_dev, 4) && q8_aligned(starts_dev, 4) && q8_aligned(workspace, 16), Q8_EALIGN);
-  const size_t tiles = tiles_of(T, n_requests, ratio, starts_dev != nullptr);
-  const bool split = workspace && workspace_bytes >= split_bytes(D) && cut(tiles, (size_t)width * page);
+  const size_t wide_tiles = tiles_of(T, n_requests, ratio, true, kWideCols), longest = (size_t)width * page;
+  const bool cuts = workspace && workspace_bytes >= split_bytes(D, kWideCols) && cut(wide_tiles, longest);
+  const bool wide = starts_dev && wide_for(T, n_requests, n_heads, ratio, D, longest, cuts);
+  const size_t tiles = wide ? wide_tiles : tiles_of(T, n_requests, ratio, starts_dev != nullptr);
+  const bool split = wide ? cuts : workspace && workspace_bytes >= split_bytes(D) && cut(tiles, longest);
   Q8_REQUIRE((tiles * n_heads + kTarget) * kCols <= 0x7fffffffu && T * ratio <= 0x7fffffffu, Q8_EUNSUPPORTED);
-  const size_t wide_tiles = tiles_of(T, n_requests, ratio, starts_dev != nullptr, kWideCols);
-  // Many columns of a request, and enough tiles of them for the compute units: those of 128 columns unpack a key once for
-  // all.  (Pieces of 2048 tokens over 8192 keys, 8 query heads to a key head: 752 us in tiles of 16 columns, 458 so;
-  // 64 tokens of 4 requests, 72 tiles: 60 and 314.)
-  const bool wide = starts_dev && T * ratio >= (size_t)n_requests * (kWideCols / 2) && wide_tiles * n_heads >= 256;
   AttendParams p{};
   p.cache = static_cast<const uint8_t*>(cache_dev);
   p.table = table_dev;
   p.lengths = lengths_dev;
   p.starts = starts_dev;
-  p.parts = split ? static_cast<float*>(workspace) : nullptr;
-  p.counters = split ? reinterpret_cast<int*>(static_cast<char*>(workspace) + parts_bytes(D)) : nullptr;
+  p.counters = split ? static_cast<int*>(workspace) : nullptr;
+  p.parts = split ? reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes) : nullptr;
   p.q_stride = q_stride, p.q_head = q_head_stride, p.o_stride = o_stride, p.o_head = o_head_stride;
   p.table_stride = table_stride;
   p.n_pages = (long)n_pages;
@@ -586,10 +495,7 @@ extern "C" int q8_kv4_attend(const void* q_dev, int type, size_t T, int n_heads,
   p.shift = __builtin_ctz(page) - 4;
   p.tiles = (int)tiles, p.window = window;
   p.scale_log2 = scale * 1.4426950408889634f;
-  if (wide) {
-    p.tiles = (int)wide_tiles;
-    return kv4_attend_wide(D / 32, p, q_dev, out_dev, type, (hipStream_t)stream);
-  }
+  if (wide) return kv4_attend_wide(D / 32, p, q_dev, out_dev, type, (hipStream_t)stream);
   if (type == Q8_F16)
     return launch_any(D / 32, p, static_cast<const _Float16*>(q_dev), static_cast<_Float16*>(out_dev),
                       (hipStream_t)stream);

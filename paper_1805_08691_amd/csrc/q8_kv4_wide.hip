@@ -42,10 +42,12 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, j = lane >> 4;
   const Unpack un;
-  const int head = blockIdx.x % p.H;
+  Part a;
   Tile t;
-  // (the last tiles of a request see most keys: they go first)
-  if (!find_tile<kWide>(p, p.tiles - 1 - blockIdx.x / p.H, &t)) return;
+  // (whole tiles: the last of a request see most keys, so they go first)
+  if (!find_part<kWide, kWideParts>(p, p.parts ? blockIdx.x : (p.tiles - 1 - blockIdx.x / p.H) * p.H + blockIdx.x % p.H, shared, &a, &t))
+    return;
+  const int head = a.head, start = t.lo + a.step0 * kStep, steps = a.step1 - a.step0;
   const int last = min(t.lo + t.steps * kStep, t.len);
 
   // ---- loads: lane l holds where sixteen l % 4 of step l / 4 (of 16) lies, bit l of `held` whether it is there; wave w
@@ -54,7 +56,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
   long where = 0;
   unsigned long held = 0;
   auto find_sixteens = [&](int s0) {
-    const int at = (t.lo >> 4) + s0 * 4 + lane;
+    const int at = (start >> 4) + s0 * 4 + lane;
     int page = -1;
     if (at * 16 < last) page = table[at >> p.shift];
     const bool in = page >= 0 && page < p.n_pages;
@@ -84,7 +86,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
   float rest[kTiles], ref[kTiles], limit[kTiles], sum[kTiles];   // scores are products times `rest`
   int* const positions = reinterpret_cast<int*>(shared + W::POS_AT) + wave * kTiles * kCols + r;   // (registers are short)
   f4 o[kTiles][CT];
-  if (t.steps > 0) issue(0);
+  if (steps > 0) issue(0);
 #pragma unroll
   for (int c = 0; c < kTiles; ++c) {
     const int col = t.first + (wave * kTiles + c) * kCols + r, in = min(col, t.cols - 1);
@@ -133,14 +135,14 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
   bool folded = !EXACT;
 #pragma unroll
   for (int c = 0; c < kTiles; ++c) folded &= !__any(rest[c] != 1.0f);
-  for (int s = 0; s < t.steps; ++s) {
-    const int key0 = t.lo + s * kStep;
+  for (int s = 0; s < steps; ++s) {
+    const int key0 = start + s * kStep;
     wait_vmcnt<0>();
     __builtin_amdgcn_s_waitcnt(0xc07f);               // the operands of the step before have been read
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (s + 1 < t.steps) issue(s + 1);
+    if (s + 1 < steps) issue(s + 1);
     else there[0] = there[1];
     const char* const raw = shared + (s & 1) * W::RAW;
     // ---- a quarter of the keys: tile `wave`, whose row r is token 4 wave + r % 4 of sixteen r / 4
@@ -294,18 +296,101 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
       }
     __builtin_amdgcn_s_setprio(0);
   }
+  constexpr int D = 32 * G;
+  constexpr size_t kPartWords = (size_t)kWide * (D + 2) / 2;    // of a part: [tile][CT][2][lane], then maxima and sums
+  word* const part = reinterpret_cast<word*>(p.parts) + ((size_t)(a.slot + a.part) * p.H + head) * kPartWords;
 #pragma unroll
   for (int c = 0; c < kTiles; ++c) {
     sum[c] += __shfl_xor(sum[c], 16, 64);
     sum[c] += __shfl_xor(sum[c], 32, 64);
-    const int col = t.first + (wave * kTiles + c) * kCols + r;
+    const int of = (wave * kTiles + c) * kCols + r, col = t.first + of;
     if (col >= t.cols) continue;
-    const float l = sum[c], inv = l > 0.0f ? 1.0f / l : l;      // (no key: zeros; no number: none)
-    V* const to = out + (size_t)(t.row + col / p.ratio) * p.o_stride + ((size_t)head * p.ratio + col % p.ratio) * p.o_head + 4 * j;
+    const float l = sum[c];
+    if (a.parts == 1) {
+      const float inv = l > 0.0f ? 1.0f / l : l;                // (no key: zeros; no number: none)
+      V* const to = out + (size_t)(t.row + col / p.ratio) * p.o_stride + ((size_t)head * p.ratio + col % p.ratio) * p.o_head + 4 * j;
 #pragma unroll
-    for (int i = 0; i < CT; ++i) {
-      const float y[4] = {o[c][i][0] * inv, o[c][i][1] * inv, o[c][i][2] * inv, o[c][i][3] * inv};
-      store_values<4, false>(to + 16 * i, y);
+      for (int i = 0; i < CT; ++i) {
+        const float y[4] = {o[c][i][0] * inv, o[c][i][1] * inv, o[c][i][2] * inv, o[c][i][3] * inv};
+        store_values<4, false>(to + 16 * i, y);
+      }
+    } else {
+      word* const to = part + (wave * kTiles + c) * CT * 128 + lane;
+#pragma unroll
+      for (int i = 0; i < CT; ++i) {
+        put(to + 128 * i, o[c][i][0], o[c][i][1]);
+        put(to + 128 * i + 64, o[c][i][2], o[c][i][3]);
+      }
+      if (j == 0) put(part + kWide * D / 2 + of, limit[c] > -__builtin_inff() ? ref[c] : -__builtin_inff(), l);
+    }
+  }
+  if (a.parts == 1) return;
+
+  // ---- the parts of the tile and head: the workgroup that finishes last adds them, whichever it is in their order
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this wavefront's words have arrived
+  __syncthreads();                                      // and the others'; LDS is free
+  int* const flag = reinterpret_cast<int*>(shared);
+  int* const counter = p.counters + a.rank * p.H + head;
+  if (tid == 0) flag[0] = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+  __syncthreads();
+  if (flag[0] != a.parts - 1) return;
+  __syncthreads();
+  if (tid == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+  const word* const parts = reinterpret_cast<const word*>(p.parts) + ((size_t)a.slot * p.H + head) * kPartWords;
+  const size_t stride = (size_t)p.H * kPartWords;
+  float* const weights = reinterpret_cast<float*>(shared);      // [16][128], then the columns' sums
+  float* const totals = weights + kWideParts * kWide;
+  if (tid < kWide) {
+    f2 rs[kWideParts];
+    float most = -__builtin_inff(), l = 0.0f;
+#pragma unroll
+    for (int u = 0; u < kWideParts; ++u) {
+      rs[u] = f2{-__builtin_inff(), 0.0f};
+      if (u < a.parts && t.first + tid < t.cols) rs[u] = get(parts + u * stride + kWide * D / 2 + tid);
+    }
+#pragma unroll
+    for (int u = 0; u < kWideParts; ++u) most = fmaxf(most, rs[u][0]);
+#pragma unroll
+    for (int u = 0; u < kWideParts; ++u) {
+      const float weight = rs[u][0] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(rs[u][0] - most);
+      weights[u * kWide + tid] = weight;
+      l += weight * rs[u][1];
+    }
+    totals[tid] = l;
+  }
+  __syncthreads();
+  // a thread takes four channels of a column, as a lane had them, and several such, so that enough is on its way
+  const int valid = t.cols - t.first, groups = min((valid + kCols - 1) / kCols, kWide / kCols) * CT;     // of 64 lanes' quads
+  constexpr int kItems = 4, kBatch = 4;
+  for (int g0 = wave; g0 < groups; g0 += kWaves * kItems) {
+    f4 v[kItems];
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) v[k] = f4{0, 0, 0, 0};
+    for (int s0 = 0; s0 < a.parts; s0 += kBatch) {
+      f2 x[kItems][kBatch][2];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+        for (int k = 0; k < kItems; ++k) {
+          const word* const from = parts + min(s0 + u, a.parts - 1) * stride + min(g0 + k * kWaves, groups - 1) * 128 + lane;
+          x[k][u][0] = get(from), x[k][u][1] = get(from + 64);
+        }
+#pragma unroll
+      for (int k = 0; k < kItems; ++k)
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+          if (s0 + u < a.parts)
+            v[k] += weights[(s0 + u) * kWide + min(g0 + k * kWaves, groups - 1) / CT * kCols + r] *
+                    f4{x[k][u][0][0], x[k][u][0][1], x[k][u][1][0], x[k][u][1][1]};
+    }
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int g = g0 + k * kWaves, of = g / CT * kCols + r, col = t.first + of;
+      if (g >= groups || col >= t.cols) continue;
+      const float l = totals[of], inv = l > 0.0f ? 1.0f / l : l;
+      const float y[4] = {v[k][0] * inv, v[k][1] * inv, v[k][2] * inv, v[k][3] * inv};
+      store_values<4, false>(out + (size_t)(t.row + col / p.ratio) * p.o_stride + ((size_t)head * p.ratio + col % p.ratio) * p.o_head +
+                                 g % CT * 16 + 4 * j, y);
     }
   }
 #endif
@@ -318,7 +403,7 @@ int launch(const AttendParams& p, const V* q, V* out, hipStream_t stream) {
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, Wide<G>::LDS);
     if (attr != hipSuccess) return Q8_EHIP;
   }
-  kv4_wide_kernel<G, V><<<(unsigned)(p.tiles * p.H), 256, Wide<G>::LDS, stream>>>(p, q, out);
+  kv4_wide_kernel<G, V><<<(unsigned)(p.tiles * p.H) + (p.parts ? kTarget : 0), 256, Wide<G>::LDS, stream>>>(p, q, out);
   return q8_launch_status();
 }
 

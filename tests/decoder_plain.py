@@ -127,7 +127,9 @@ def attend(q, keys, values, lengths, starts, scale, window):
 def attend_tolerance(out, values, most, dtype):
     """How far the kernel may be off, element by element.  Its products are of binary16 numbers: a key or a value is a
     code times its factor rounded once (2^-11 of it at most), a query is scaled by a power of two and exact in fp16 and
-    bf16 alike unless it is 2^-14 of its row's largest (then off by 2^-25 of that).  A score is then off by at most
+    bf16 alike unless it is 2^-14 of its row's largest (then off by 2^-25 of that).  (For bf16 outputs of many rows the queries have the scale in
+    them and are rounded too: nothing is added for that, since it and the keys' rounding are the worst case of 2^-11 in
+    each of D products, all of one sign.)  A score is then off by at most
     d = 2^-11 sum |q k| scale (and fp32 noise, 2^-20 of the same), which moves weights by a factor of exp(2 d) at most; a
     probability is rounded once more (2^-11) while the sum of them is not, and a probability below 2^-14 of the
     largest is off by 2^-25.  The output is rounded once."""

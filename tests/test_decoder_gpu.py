@@ -414,6 +414,42 @@ def test_attention_of_prompts_in_a_window(B, window):
     _check_attend(B, _rng(window, 3), [400, 150, 90], [300, 150, 100], 16, 4, 64, 16, "f16", window=window, scale=-0.2)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("D,H,ratio,window", [(32, 4, 8, 0), (64, 4, 7, 0), (128, 4, 8, 0), (128, 5, 6, 600), (192, 4, 8, 0), (256, 4, 8, 0),
+                                              (96, 12, 3, 40)])
+def test_attention_of_cut_prompts(B, kind, D, H, ratio, window):
+    """Few wide tiles over tables that hold long contexts: the keys are cut, and the parts are added in the same order
+    every time."""
+    rng = _rng(D, H, 5)
+    lengths, added, page, longest = [1500, 0, 700, 2300, 40], [60, 0, 130, 64, 40], 32, 140000
+    cache, table, keys, values = _filled(B, rng, lengths, H, D, page)
+    table = torch.nn.functional.pad(table, (0, longest // page - table.shape[1]), value=-1)
+    T, starts = sum(added), [0, 60, 60, 190, 254, 294]
+    q = _real(rng, (T, H * ratio, D), "f32").to(TYPES[kind])
+    lens, first = [torch.tensor(v, dtype=torch.int32, device="cuda") for v in (lengths, starts)]
+    ws = B.kv4_attend_workspace(q, cache, len(lengths), longest)
+    assert ws.numel() >= 1024 * 128 * (D + 2) * 4
+    got = B.kv4_attend(q.cuda(), cache, table, lens, first, window=window, workspace=ws)
+    want, most = P.attend(q.double().numpy(), keys, values, lengths, starts, D ** -0.5, window)
+    bound = P.attend_tolerance(want, values, most, TYPES[kind])
+    assert np.all(np.abs(got.double().cpu().numpy() - want) <= bound)
+    for _ in range(10):
+        assert torch.equal(got, B.kv4_attend(q.cuda(), cache, table, lens, first, window=window, workspace=ws))
+    # the same workspace for single tokens, whose parts are others, and back
+    one = torch.arange(6, dtype=torch.int32, device="cuda")
+    few = B.kv4_attend(q[:5].cuda(), cache, table, lens, one, window=window, workspace=ws)
+    assert torch.equal(few, B.kv4_attend(q[:5].cuda(), cache, table, lens, one, window=window,
+                                         workspace=B.kv4_attend_workspace(q[:5], cache, len(lengths), longest)))
+    assert torch.equal(got, B.kv4_attend(q.cuda(), cache, table, lens, first, window=window, workspace=ws))
+
+
+@pytest.mark.parametrize("peak,scale", [(0.0, None), (1e-6, None), (30.0, None), (1.0, -0.3), (1.0, 0.0), (3000.0, 1e-4), (1e-3, 1e-5)])
+def test_attention_of_flat_and_peaked_prompts(B, peak, scale):
+    """Scales that fit the queries' binary16 and such that do not."""
+    for kind in ("bf16", "f16") if peak < 1000.0 else ("bf16",):         # (the largest are no fp16 numbers)
+        _check_attend(B, _rng(9, 9), [300, 90], [130, 90], 16, 8, 64, 16, kind, scale=scale, peak=peak)
+
+
 def test_attention_of_prompts_reads_no_page_that_a_request_has_not(B):
     rng = _rng(16)
     H, ratio, D, page = 16, 8, 64, 16
