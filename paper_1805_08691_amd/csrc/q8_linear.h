@@ -45,14 +45,17 @@ __device__ __forceinline__ uint2 row_codes(const float (&r)[8], float q, float i
   return uint2{lo0 | hi0, lo1 | hi1};
 }
 
-// The largest finite magnitude of eight values beside m, and whether all are finite.
-__device__ __forceinline__ float row_max8(const float (&r)[8], float m, bool* finite) {
+// The largest of eight magnitudes and m as bit patterns, whose order is that of the numbers: at least kNotFinite where one
+// is infinite or no number, and then the lane takes its maximum again, of the finite ones (row_max8).
+constexpr unsigned kNotFinite = 0x7f800000u;
+__device__ __forceinline__ unsigned row_bits8(const float (&r)[8], unsigned m) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const bool in = fabsf(r[e]) < __builtin_inff();
-    *finite &= in;
-    m = fmaxf(m, in ? fabsf(r[e]) : 0.0f);
-  }
+  for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(r[e]) & 0x7fffffffu);
+  return m;
+}
+__device__ __forceinline__ float row_max8(const float (&r)[8], float m) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = fmaxf(m, finite_abs(r[e]));
   return m;
 }
 
@@ -86,7 +89,7 @@ int linear_tile(const LinearParams& p, void* y, int type, int variant, hipStream
 
 // The build for few rows (q8_linear_rows.hip), on codes, and on real values where it takes that many.
 int linear_rows(const LinearParams& p, void* y, int type, int columns, int squares, hipStream_t stream);
-bool linear_rows_take_real(int M, int K);
+bool linear_rows_take_real(int M, int N, int K);
 int linear_rows_real(const LinearParams& p, const void* x, int x_type, size_t x_stride, void* y, int type,
                      hipStream_t stream);
 

@@ -37,21 +37,31 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const V* __restrict_
     if (tid * 8 + i * STEP < body)
       __builtin_memcpy(held[i], __builtin_assume_aligned(xr + tid * 8 + i * STEP, ALIGNED ? 16 : sizeof(V)), sizeof(held[i]));
   const float tail = tid < K - body ? (float)xr[body + tid] : 0.0f;
-  float m = finite_abs(tail);
-  bool finite = true;
+  // all of a lane's values one after the other
+  auto each = [&](auto use) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < HELD; ++i)
-    if (tid * 8 + i * STEP < body) {
+    for (int i = 0; i < HELD; ++i)
+      if (tid * 8 + i * STEP < body) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (float)held[i][e];
+        use(v, tid * 8 + i * STEP);
+      }
+    for (int k = tid * 8 + HELD * STEP; k < body; k += STEP) {
       float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (float)held[i][e];
-      m = row_max8(v, m, &finite);
+      load_values<8, ALIGNED>(xr + k, v);
+      use(v, k);
     }
-  for (int k = tid * 8 + HELD * STEP; k < body; k += STEP) {
-    float v[8];
-    load_values<8, ALIGNED>(xr + k, v);
-    m = row_max8(v, m, &finite);
+  };
+  unsigned all = 0;
+  each([&](const float (&v)[8], int) { all = row_bits8(v, all); });
+  const bool finite = all < kNotFinite;
+  float m = __uint_as_float(all);
+  if (!finite) {
+    m = 0.0f;
+    each([&](const float (&v)[8], int) { m = row_max8(v, m); });
   }
+  m = fmaxf(m, finite_abs(tail));
   for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
   if constexpr (WAVES == 4) {
     __shared__ float wave_max[4];
@@ -63,19 +73,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const V* __restrict_
   q = q > 0.0f ? q : 1.0f;
   if (tid == 0) q_x[row] = q;
   const float inv_q = __fdiv_rn(1.0f, q);
-#pragma unroll
-  for (int i = 0; i < HELD; ++i)
-    if (tid * 8 + i * STEP < body) {
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (float)held[i][e];
-      *reinterpret_cast<uint2*>(zr + tid * 8 + i * STEP) = row_codes(v, q, inv_q, finite);
-    }
-  for (int k = tid * 8 + HELD * STEP; k < body; k += STEP) {
-    float v[8];
-    load_values<8, ALIGNED>(xr + k, v);
-    *reinterpret_cast<uint2*>(zr + k) = row_codes(v, q, inv_q, finite);
-  }
+  each([&](const float (&v)[8], int k) { *reinterpret_cast<uint2*>(zr + k) = row_codes(v, q, inv_q, finite); });
   if (tid < K - body) zr[body + tid] = (int8_t)(tail == tail ? quant1(tail, q, -128.0f, 127.0f) : 0);
 }
 
@@ -279,7 +277,7 @@ extern "C" int q8_linear(const void* x_dev, int x_type, size_t x_stride, size_t 
   Q8_REQUIRE(q8_aligned(workspace, 256) && q8_aligned(x_dev, type_bytes(x_type)) && q8_aligned(packed_dev, 16) &&
                  q8_aligned(q_w_dev, 4) && q8_aligned(bias_dev, 4) && q8_aligned(y_dev, type_bytes(y_type)), Q8_EALIGN);
   Q8_REQUIRE(workspace_bytes >= q8_linear_workspace_bytes(M, N, K), Q8_EWORKSPACE);
-  if (linear_rows_take_real((int)M, K)) {
+  if (linear_rows_take_real((int)M, N, K)) {
     const LinearParams p{nullptr, nullptr, static_cast<const int8_t*>(packed_dev), q_w_dev, bias_dev, 0, y_stride, (int)M,
                          N, K, (int)(round_up(K, kPackK) / kPackK)};
     return linear_rows_real(p, x_dev, x_type, x_stride, y_dev, y_type, (hipStream_t)stream);

@@ -16,7 +16,9 @@ using namespace q8;
 
 constexpr int kWavesK = 8;                    // wavefronts, which share K
 constexpr int kThreads8 = kWavesK * 64;
-constexpr int kRealVectors = 4;               // of 8 values each, that a lane holds of x
+// Real values, of which a lane holds 4 vectors of 8: one or two rows that the workgroup takes together, or two rows of a
+// wavefront (WAVE), SPAN vectors of each.
+constexpr int kRealVectors = 4, kSpan = 2, kWaveRows = kWavesK * (kRealVectors / kSpan);
 
 // The largest of a wavefront's values (none is negative or no number), in lane 63.
 __device__ __forceinline__ float wave_max(float v) {
@@ -34,13 +36,13 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
-template <int NB, int MT, typename X, typename Y, bool VEC, bool REAL, bool ALIGNED>
+template <int NB, int MT, typename X, typename Y, bool VEC, bool REAL, bool WAVE>
 __global__ __launch_bounds__(kThreads8) void linear_rows_kernel(const LinearParams p, const X* __restrict__ x,
                                                                 size_t x_stride, Y* __restrict__ y) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int kAhead = NB + MT <= 5 ? 4 : 2;                // steps of a wavefront in flight
   extern __shared__ __attribute__((aligned(16))) int8_t lds[];
-  __shared__ unsigned row_max[kRealVectors];
+  __shared__ unsigned row_max[kWaveRows];                     // (bits of a number that is none negative)
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int nb = blockIdx.x * NB, nk = p.ksteps;              // first packed column, of NB
@@ -48,22 +50,28 @@ __global__ __launch_bounds__(kThreads8) void linear_rows_kernel(const LinearPara
   const int pitch = nk * kPackK + 16;                         // of a row of codes in LDS
   const int m_grid = blockIdx.y * (16 * MT);
 
-  // ---- real values: vector u of a lane is one of row u / turns, 512 vectors of which are a turn
+  // ---- real values: vector u of a lane is one of row u / turns, 512 vectors of which are a turn; or of the wavefront's
+  // row u / kSpan
   float r[kRealVectors][8];
   const int turns = (p.K + kThreads8 * 8 - 1) / (kThreads8 * 8), vectors = p.M * turns;
+  auto row_of = [&](int u) { return WAVE ? wave + u / kSpan * kWavesK : u / turns; };
+  auto first_of = [&](int u) { return WAVE ? (lane + u % kSpan * 64) * 8 : (tid + (u - u / turns * turns) * kThreads8) * 8; };
+  auto given = [&](int u) { return WAVE ? row_of(u) < p.M && u % kSpan * 512 < p.K : u < vectors; };
   if constexpr (REAL) {
-    if (tid < kRealVectors) row_max[tid] = 0;
+    if (!WAVE && tid < kWaveRows) row_max[tid] = 0;
 #pragma unroll
     for (int u = 0; u < kRealVectors; ++u) {
-      const int row = u / turns, k = (tid + (u - row * turns) * kThreads8) * 8;
 #pragma unroll
       for (int e = 0; e < 8; ++e) r[u][e] = 0.0f;
-      if (u < vectors) {
-        const X* from = x + row * x_stride + k;
+      if (given(u)) {
+        const int k = first_of(u);
+        const X* from = x + row_of(u) * x_stride + k;
         if (k + 8 <= p.K) {
-          load_values<8, ALIGNED>(from, r[u]);
+          load_values<8, false>(from, r[u]);
         } else {
-          for (int e = 0; e < p.K - k; ++e) r[u][e] = (float)from[e];
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (k + e < p.K) r[u][e] = (float)from[e];
         }
       }
     }
@@ -102,22 +110,49 @@ __global__ __launch_bounds__(kThreads8) void linear_rows_kernel(const LinearPara
       for (int t = 0; t < MT; ++t) b[u][t] = load_row(t, wave + u * kWavesK);
     }
   }
-  if constexpr (REAL) {
+  auto factor = [&](unsigned most) {
+    const float q = __fmul_rn(__uint_as_float(most), 1.0f / 127.0f);
+    return q > 0.0f ? q : 1.0f;
+  };
+  if constexpr (REAL && WAVE) {
+#pragma unroll
+    for (int i = 0; i < kRealVectors; i += kSpan)
+      if (row_of(i) < p.M) {
+        unsigned all = 0;
+#pragma unroll
+        for (int u = i; u < i + kSpan; ++u) all = row_bits8(r[u], all);
+        const bool finite = all < kNotFinite;
+        float most = __uint_as_float(all);
+        if (!finite) {
+          most = 0.0f;
+#pragma unroll
+          for (int u = i; u < i + kSpan; ++u) most = row_max8(r[u], most);
+        }
+        const unsigned bits = __builtin_amdgcn_readlane(__float_as_uint(wave_max(most)), 63);
+        const float q = factor(bits), inv_q = __fdiv_rn(1.0f, q);
+        if (lane == 0) row_max[row_of(i)] = bits;
+#pragma unroll
+        for (int u = i; u < i + kSpan; ++u)
+          if (first_of(u) < p.K) *reinterpret_cast<uint2*>(lds + row_of(u) * pitch + first_of(u)) = row_codes(r[u], q, inv_q, finite);
+      }
+    lds_barrier();
+  } else if constexpr (REAL) {
     lds_barrier();                                            // row_max is zero
     bool finite = true;
 #pragma unroll
     for (int u = 0; u < kRealVectors; ++u)
-      if (u < vectors) {
-        const float m = wave_max(row_max8(r[u], 0.0f, &finite));
-        if (lane == 63) atomicMax(&row_max[u / turns], __float_as_uint(m));
+      if (given(u)) {
+        const unsigned all = row_bits8(r[u], 0);
+        finite &= all < kNotFinite;
+        const float m = wave_max(all < kNotFinite ? __uint_as_float(all) : row_max8(r[u], 0.0f));
+        if (lane == 63) atomicMax(&row_max[row_of(u)], __float_as_uint(m));
       }
     lds_barrier();
 #pragma unroll
     for (int u = 0; u < kRealVectors; ++u)
-      if (u < vectors) {
-        const int row = u / turns, k = (tid + (u - row * turns) * kThreads8) * 8;
-        float q = __fmul_rn(__uint_as_float(row_max[row]), 1.0f / 127.0f);
-        q = q > 0.0f ? q : 1.0f;
+      if (given(u)) {
+        const int row = row_of(u), k = first_of(u);
+        const float q = factor(row_max[row]);
         if (k < p.K) *reinterpret_cast<uint2*>(lds + row * pitch + k) = row_codes(r[u], q, __fdiv_rn(1.0f, q), finite);
       }
     lds_barrier();
@@ -173,12 +208,8 @@ __global__ __launch_bounds__(kThreads8) void linear_rows_kernel(const LinearPara
       const int m = m_grid + t * 16 + (lane & 15), n = (nb + c) * kPackN + 4 * (lane >> 4);
       if (m < p.M && n < p.N) {
         float q;
-        if constexpr (REAL) {
-          q = __fmul_rn(__uint_as_float(row_max[m]), 1.0f / 127.0f);
-          q = q > 0.0f ? q : 1.0f;
-        } else {
-          q = p.q_x[m];
-        }
+        if constexpr (REAL) q = factor(row_max[m]);
+        else q = p.q_x[m];
         const int v[4] = {total[0], total[1], total[2], total[3]};
         finish_outputs<4, VEC>(p, y, m, n, q, v);
       }
@@ -198,21 +229,29 @@ int launch_codes(const LinearParams& p, Y* y, hipStream_t stream) {
   return q8_launch_status();
 }
 
+// Whether real values are taken, a row to a wavefront, or as one or two rows by the workgroup together.  Every workgroup
+// makes the rows' codes again; the launch that this saves takes 3 us.  us of the layer in one launch and in two, a row to a
+// wavefront: 1024 -> 4096 3 rows 4.7 / 6.5, 8 4.8 / 7.4, 16 7.0 / 8.0; 884 -> 2439 3 rows 5.1 / 6.6, 16 6.9 / 7.7; but
+// 512 -> 16384 16 rows 10.8 / 8.4, 2048 -> 2048 16 rows 9.1 / 7.5.  Together, 1.1 us a row: 4096 -> 4096 1 row 5.5 / 8.2,
+// 2 6.7 / 8.3, 3 7.8 / 8.4, 4 8.9 / 8.5; 4096 -> 16384 14.2 / 16.9, 16.4 / 17.1, 18.8 / 17.4; 16384 -> 4096 1 row 18.4 / 23.
+bool real_rows_of_waves(int M, int N, int K) { return M > 1 && M <= kWaveRows && K <= kSpan * 512 && (M <= kWavesK || N <= 8192); }
+bool real_rows_together(int M, int K) { return M <= 2 && M * ((K + kThreads8 * 8 - 1) / (kThreads8 * 8)) <= kRealVectors; }
+
 template <int NB, typename X, typename Y>
 int launch_real(const LinearParams& p, const X* x, size_t x_stride, Y* y, hipStream_t stream) {
   const dim3 grid((unsigned)((p.N + kPackN * NB - 1) / (kPackN * NB)));
   const size_t bytes = (size_t)p.M * (p.ksteps * kPackK + 16);
   const bool vec = q8_aligned(y, 4 * sizeof(Y)) && p.y_stride % 4 == 0;
-  const bool aligned = q8_aligned(x, 16) && x_stride * sizeof(X) % 16 == 0;
-  auto go = [&](auto vec_c, auto aligned_c) {
-    linear_rows_kernel<NB, 1, X, Y, decltype(vec_c)::value, true, decltype(aligned_c)::value>
+  auto go = [&](auto vec_c, auto wave_c) {
+    linear_rows_kernel<NB, 1, X, Y, decltype(vec_c)::value, true, decltype(wave_c)::value>
         <<<grid, kThreads8, bytes, stream>>>(p, x, x_stride, y);
   };
   using T = std::true_type;
   using F = std::false_type;
-  if (aligned && vec) go(T{}, T{});
+  const bool wave = real_rows_of_waves(p.M, p.N, p.K);
+  if (vec && wave) go(T{}, T{});
   else if (vec) go(T{}, F{});
-  else if (aligned) go(F{}, T{});
+  else if (wave) go(F{}, T{});
   else go(F{}, F{});
   return q8_launch_status();
 }
@@ -235,10 +274,7 @@ int linear_rows(const LinearParams& p, void* y, int type, int columns, int squar
   });
 }
 
-// Every workgroup makes the rows' codes again, 1.1 us a row; the launch that this saves takes 3.  us of the layer in one
-// launch and in two: 4096 -> 4096 1 row 5.5 / 8.2, 2 6.7 / 8.3, 3 7.8 / 8.4, 4 8.9 / 8.5; 4096 -> 16384 14.2 / 16.9, 16.4 /
-// 17.1, 18.8 / 17.4; 16384 -> 4096 1 row 18.4 / 23.  Values are kept in registers: no more than 4 vectors a lane.
-bool linear_rows_take_real(int M, int K) { return M <= 2 && M * ((K + kThreads8 * 8 - 1) / (kThreads8 * 8)) <= kRealVectors; }
+bool linear_rows_take_real(int M, int N, int K) { return real_rows_of_waves(M, N, K) || real_rows_together(M, K); }
 
 int linear_rows_real(const LinearParams& p, const void* x, int x_type, size_t x_stride, void* y, int type,
                      hipStream_t stream) {

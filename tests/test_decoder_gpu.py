@@ -188,6 +188,24 @@ def test_linear_is_its_two_parts(B, kind, M, N, K):
     assert torch.equal(y32.cpu(), P.linear(z, q_x, z_w, q_w, None, torch.float32))
 
 
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("M", [2, 3, 8, 9, 15, 16, 17])
+def test_linear_of_a_few_short_rows(B, kind, M):
+    """Rows that a wavefront takes: odd lengths and distances, rows of zeros, infinities and no numbers."""
+    rng = _rng(M, 51)
+    for K, N, pad in ((1, 5, 0), (7, 16, 1), (64, 40, 3), (511, 33, 0), (512, 100, 8), (513, 17, 2), (1000, 2439, 0), (1024, 64, 1),
+                      (1025, 64, 0), (40, 9000, 0)):
+        z_w, q_w, bias = _weights(rng, N, K)
+        x = _real(rng, (M, K + pad), kind)
+        x[0] = 0.0
+        x[1, 0] = float("nan")
+        x[M - 1, K - 1] = float("inf")
+        qw, b = torch.from_numpy(q_w).cuda(), torch.from_numpy(bias).cuda()
+        got = B.linear(x.cuda()[:, :K], B.linear_pack(torch.from_numpy(z_w).cuda()), qw, b)
+        z, q_x = P.quantize_rows(x[:, :K])
+        assert torch.equal(got.cpu(), P.linear(z, q_x, z_w, q_w, bias, TYPES[kind])), (K, N)
+
+
 def test_linear_of_strided_rows(B):
     rng = _rng(4, 4)
     z_w, q_w, _ = _weights(rng, 70, 90)
