@@ -168,18 +168,20 @@ constexpr Variant kVariants[] = {
     {"rows_any", 16, 16, 0, 0, -1, 0.0f, 0.0f, 0.0f, 0.0f}};      // rows so far apart that a tile passes 2^31 bytes
 constexpr int kNumVariants = sizeof(kVariants) / sizeof(kVariants[0]);
 constexpr size_t kTileStride = 1 << 22;      // 256 rows of a tile stay below 2^31 bytes
+constexpr int kMostRows = 16 * 65535;        // of the rows builds: a launch's second dimension
 
 int pick(const LinearParams& p) {
-  int best = 0;
+  int best = -1;
   float least = 0.0f;
   const float memory = 2.2f + ((float)p.N + (float)p.M) * (float)p.K / 5.4e6f;
   for (int i = 0; i + 1 < kNumVariants; ++i) {
     const Variant& v = kVariants[i];
+    if (v.columns && p.M > kMostRows) continue;
     const float tiles = (float)((p.N + v.bn - 1) / v.bn) * (float)((p.M + v.bm - 1) / v.bm), rounds = tiles / 256.0f;
     const float passes = fmaxf(1.0f, v.share * rounds + (1.0f - v.share) * ceilf(rounds));
     const float time = v.base + passes * (v.round + v.per_k * (float)p.K / 1024.0f);
     const float cost = fmaxf(time, memory) + 0.2f * fminf(time, memory);
-    if (i == 0 || cost < least) best = i, least = cost;
+    if (best < 0 || cost < least) best = i, least = cost;
   }
   return best;
 }
@@ -248,6 +250,7 @@ extern "C" int q8_linear_int8_variant(const int8_t* z_x_dev, size_t z_stride, co
                        y_stride, (int)M, N, K, (int)(round_up(K, kPackK) / kPackK)};
   if (variant < 0) variant = z_stride <= kTileStride ? pick(p) : kNumVariants - 1;
   const Variant& v = kVariants[variant];
+  Q8_REQUIRE(v.tile >= 0 || (int)M <= kMostRows, Q8_EUNSUPPORTED);
   if (v.columns) return linear_rows(p, y_dev, type, v.columns, v.squares, (hipStream_t)stream);
   if (v.tile >= 0 && z_stride > kTileStride) return Q8_EUNSUPPORTED;
   if (v.tile >= 0) return linear_tile(p, y_dev, type, v.tile, (hipStream_t)stream);

@@ -137,6 +137,18 @@ def test_product_of_rows_far_apart(B):
     assert torch.equal(y.cpu(), P.linear(z, np.ones(M, np.float32), z_w, q_w, None, torch.float32))
 
 
+def test_product_of_very_many_rows(B):
+    """More rows than a launch's second dimension has sixteens."""
+    M, N, K = 16 * 65535 + 33, 20, 16
+    rng = _rng(6, 6)
+    z_w, q_w, bias = _weights(rng, N, K)
+    z = torch.from_numpy(rng.integers(-128, 128, (M, K), dtype=np.int8))
+    q_x = torch.from_numpy(rng.random(M).astype(np.float32) + 0.5)
+    y = B.linear_int8(z.cuda(), q_x.cuda(), B.linear_pack(torch.from_numpy(z_w).cuda()), torch.from_numpy(q_w).cuda(),
+                      torch.from_numpy(bias).cuda(), dtype=torch.float16)
+    assert torch.equal(y.cpu(), P.linear(z.numpy(), q_x.numpy(), z_w, q_w, bias, torch.float16))
+
+
 def test_product_of_the_largest_sums(B):
     """128 * 128 * 131071 just fits the accumulator, on both sides."""
     K = 131071
