@@ -108,11 +108,15 @@ __device__ __forceinline__ float column_max(float v) {
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-constexpr int kTarget = 512;           // parts that the keys are cut into where tiles are few
-constexpr int kMinSteps = 8;           // steps of a part, at least
+// Parts that the keys are cut into where tiles are few: two for a compute unit.  (48 requests of up to 16384 tokens, 64 query
+// heads on 8 of 128 channels, 107 us; for 384 parts 125, 640 114, 768 115.  One of 131071, 32 heads on 8: 44, 51, 49, 47.)
+constexpr int kTarget = 512;
+// A part is not shorter than a step for each wavefront, and than two of them where that makes kTarget / 2 parts.  (One
+// request of 2000 tokens 11.6 us, never shorter than 8 or 16 steps 13.2 and 16.9; 8 of 4096, 64 channels, 14.0, with 4 14.8.)
+constexpr int kShortest = 4;
 constexpr int kMaxTiles = 256;         // beyond them nothing is cut: a thread each
 
-// The split of the key axis.  The steps of all tiles and heads over kTarget are what a part should hold (kMinSteps at
+// The split of the key axis.  The steps of all tiles and heads over kTarget are what a part should hold (`least` at
 // least); a tile of more steps is cut into equal parts of no more.  Every workgroup works this out for itself from the
 // lengths, a tile to a thread.  Parts of cut tiles have a place in the workspace, no more than 2 kTarget of them (a cut
 // tile has more than `per` steps), and the cut tiles' heads, no more than kTarget, a counter.
@@ -133,7 +137,8 @@ __device__ __forceinline__ unsigned scan64(unsigned v) {
   return v;
 }
 
-// The part of workgroup `id` (of MOST that a tile is cut into at most), and its tile; false: there is none.  `shared`: LDS that is free until then.
+// The part of workgroup `id` (of MOST that a tile is cut into at most), and its tile; false: there is none.  `shared`: LDS
+// that is free until then.
 template <int COLS, int MOST>
 __device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* shared, Part* a, Tile* out) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -177,7 +182,8 @@ __device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* s
   if (tid == 0) found[0] = 0;
   __syncthreads();
   const long total = ((long)((low[0] + low[1]) + (low[2] + low[3])) + ((long)((high[0] + high[1]) + (high[2] + high[3])) << 16)) * p.H;
-  const unsigned per = (unsigned)max((total + kTarget - 1) / kTarget, (long)kMinSteps);
+  const long least = min(max((2 * total + kTarget - 1) / kTarget, (long)kShortest), 2l * kShortest);
+  const unsigned per = (unsigned)max((total + kTarget - 1) / kTarget, least);
   // the sums before each tile: parts (kTarget + kMaxTiles at most); those of cut tiles (10 bits up); cut tiles (20 bits up)
   const unsigned n = steps ? min((steps + per - 1) / per, (unsigned)MOST) : 0, own = n > 1 ? n | n << 10 | 1u << 20 : n;
   unsigned v = scan64(own);

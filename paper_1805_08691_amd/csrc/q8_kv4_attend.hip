@@ -12,6 +12,11 @@
 // so that a lane's 16 probabilities belong to the 16 tokens whose value codes it loads: nothing is exchanged
 // between lanes but the maximum.
 // The key axis is split over workgroups where columns are few; the last of them to finish adds the parts, in their order.
+// Bound by memory while it loops (48 requests of up to 16384 tokens, 64 query heads on 8 of 128 channels: 415 MB in 102 us,
+// 70 to 80 of them in the loop at 5 to 5.5 TB/s; 2000 cycles of vector instructions a step beside 1000 of the matrix
+// cores) and by dependent trips to memory at both ends (5 us in front of the first keys' products of a split, 4 to 7 behind:
+// one request of 131071 tokens, 151 MB, 41 us; 5 short ones 6.7).  One step in LDS a wavefront: with three workgroups a
+// compute unit that is 110 KB on their way, and a second would leave room for fewer of them.
 #include "q8_kv4_attend.h"
 #pragma clang fp contract(fast)
 
@@ -429,9 +434,9 @@ int launch_any(int G, const AttendParams& p, const V* q, V* out, hipStream_t str
 size_t tiles_of(size_t T, int B, int ratio, bool starts, int cols = kCols) {
   return starts ? T * ratio / cols + B : (size_t)B * ((ratio + cols - 1) / cols);
 }
-// Whether keys of at most `longest` are cut: where parts of kMinSteps could be made, and tiles are so few that a part of
-// the longest could keep compute units waiting.
-bool cut(size_t tiles, size_t longest) { return tiles <= kMaxTiles && longest > (size_t)kMinSteps * kStep; }
+// Whether keys of at most `longest` are cut: where tiles are so few that a part of the longest could keep compute units
+// waiting, and two parts of 2 kShortest steps could be made.  (5 requests of up to 300 tokens: 7.3 us, and cut 10.4.)
+bool cut(size_t tiles, size_t longest) { return tiles <= kMaxTiles && longest > (size_t)2 * kShortest * kStep; }
 // Workspace: the counters (in one place for both kernels), then the parts.
 constexpr size_t kCounterBytes = (kTarget + 15) / 16 * 16 * sizeof(int);
 size_t split_bytes(int D, int cols = kCols) { return kCounterBytes + (size_t)2 * kTarget * cols * (D + 2) * 4; }

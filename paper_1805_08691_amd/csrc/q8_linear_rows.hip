@@ -5,7 +5,8 @@
 // wavefronts take the blocks of K in turn, straight from memory to registers, and multiply them on
 // v_mfma_i32_16x16x64_i8: no operand is shared inside a workgroup, so nothing goes through LDS and no wavefront waits
 // for another.  Their sums meet in LDS at the end (integers: any order gives the same bits).  With real values as input (REAL) the workgroup makes the rows' codes
-// itself, in LDS, while its first weights are on their way: one launch instead of two.
+// itself, in LDS, while its first weights are on their way: one launch instead of two.  1 x 4096 -> 4096 takes 4.5 us (16.8 MB of
+// weights: 3.7 TB/s with the launch), 16 x 4096 -> 16384 15 (4.5 TB/s).
 #include "q8_linear.h"
 #include "q8_quant.h"
 #pragma clang fp contract(off)
