@@ -42,9 +42,10 @@ template <int THREADS, int PER>
 __global__ __launch_bounds__(THREADS) void page_tables_kernel(const PageParams p) {
   constexpr int kPerThread = PER, kMost = THREADS * PER, kWaves = THREADS / 64;
   __shared__ int starts[kMost + 1], from[kMost];           // first new token; where free_pages[from + page number] is its page
-  __shared__ long sums[2][kWaves];
+  __shared__ int lengths[kMost];
+  __shared__ unsigned sums[2][2][kWaves];
   __shared__ int took[kWaves], out[kWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, each = (p.n + THREADS - 1) / THREADS;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), each = (p.n + THREADS - 1) / THREADS;
   int len[kPerThread], add[kPerThread];
   long tokens = 0;
 #pragma unroll
@@ -55,16 +56,23 @@ __global__ __launch_bounds__(THREADS) void page_tables_kernel(const PageParams p
     add[e] = in ? max(p.added[b], 0) : 0;
     tokens += add[e];
   }
-  auto before = [&](long v, long* sums) {                 // the sum of the threads before
-    const long own = v;
-    for (int off = 1; off < 64; off <<= 1) {
-      const long o = __shfl_up(v, off, 64);
-      if (lane >= off) v += o;
+  // The sum of the threads before, v < 2^33: its low 20 bits and the others by themselves, which 1024 threads' sums leave
+  // in 32 bits each.
+  auto before = [&](long v, unsigned (*sums)[kWaves]) {
+    const unsigned own[2] = {(unsigned)v & 0xfffffu, (unsigned)(v >> 20)};
+    unsigned upto[2], waves[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      upto[h] = scan64(own[h]);
+      if (lane == 63) sums[h][wave] = upto[h];
     }
-    if (lane == 63) sums[wave] = v;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) v += sums[w];
-    return v - own;
+    lds_barrier();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      waves[h] = scan64(lane < kWaves ? sums[h][lane] : 0u);
+      waves[h] = wave ? __builtin_amdgcn_readlane(waves[h], wave - 1) : 0u;
+    }
+    return (long)(waves[0] + upto[0] - own[0]) + ((long)(waves[1] + upto[1] - own[1]) << 20);
   };
   long at = before(tokens, sums[0]), need_all = 0;
   long begin[kPerThread], need[kPerThread];
@@ -87,6 +95,7 @@ __global__ __launch_bounds__(THREADS) void page_tables_kernel(const PageParams p
     fits[e] = fits[e] && (need[e] == 0 || upto <= p.n_free);
     if (e < each && b < p.n) {
       starts[b] = (int)begin[e];
+      lengths[b] = len[e];
       from[b] = fits[e] ? (int)(upto - need[e]) - pages_of(len[e], p.shift) : INT_MIN;
       taken += fits[e] ? (int)need[e] : 0;
       refused += !fits[e];
@@ -101,15 +110,15 @@ __global__ __launch_bounds__(THREADS) void page_tables_kernel(const PageParams p
     for (int off = 32; off > 0; off >>= 1) taken += __shfl_xor(taken, off, 64), refused += __shfl_xor(refused, off, 64);
     if (lane == 0) took[wave] = taken, out[wave] = refused;
   }
-  __syncthreads();
+  lds_barrier();
   if (blockIdx.x == 0 && tid == 0) {
     int t = 0, r = 0;
     for (int w = 0; w < kWaves; ++w) t += took[w], r += out[w];
     p.starts[p.n] = starts[p.n];
     p.counts[0] = t, p.counts[1] = starts[p.n], p.counts[2] = r;
   }
-  const int end = min((int)(blockIdx.x + 1) * 2 * THREADS, p.n_slots);
-  for (int i = blockIdx.x * 2 * THREADS + tid; i < end; i += THREADS) {
+  const int i = blockIdx.x * THREADS + tid;
+  if (i < p.n_slots) {
     long slot = -1;
     int position = -1;
     if (i < starts[p.n]) {
@@ -119,7 +128,7 @@ __global__ __launch_bounds__(THREADS) void page_tables_kernel(const PageParams p
         if (starts[mid] <= i) lo = mid; else hi = mid - 1;
       }
       if (from[lo] != INT_MIN && i < starts[lo + 1]) {
-        const int held = max(p.lengths[lo], 0);
+        const int held = lengths[lo];
         position = held + i - starts[lo];
         const int number = position >> p.shift, in = position & ((1 << p.shift) - 1);
         int* const entry = p.table + lo * p.table_stride + number;
@@ -539,7 +548,7 @@ extern "C" int q8_page_tables(const int32_t* lengths_dev, const int32_t* added_d
                      positions_dev, starts_dev, grown_dev, counts_dev, n_requests, __builtin_ctz(page), n_free, width,
                      n_slots, table_stride};
   if (n_requests <= kFew) {
-    const int threads = n_requests <= kFewest ? 256 : 1024, blocks = n_slots > 0 ? (n_slots - 1) / (2 * threads) + 1 : 1;
+    const int threads = n_requests <= kFewest ? 256 : 1024, blocks = n_slots > 0 ? (n_slots - 1) / threads + 1 : 1;
     if (threads == 256)
       page_tables_kernel<256, 1><<<blocks, 256, 0, (hipStream_t)stream>>>(p);
     else

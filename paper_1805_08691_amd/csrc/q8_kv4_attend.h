@@ -126,17 +126,6 @@ struct Part {
   int step0, step1;
 };
 
-// Sums over the lanes up to this one (16 at a time, then over the rows of 16).
-__device__ __forceinline__ unsigned scan64(unsigned v) {
-  v += __builtin_amdgcn_update_dpp(0u, v, 0x111, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0u, v, 0x112, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0u, v, 0x114, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0u, v, 0x118, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0u, v, 0x142, 0xa, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0u, v, 0x143, 0xc, 0xf, false);
-  return v;
-}
-
 // The part of workgroup `id` (of MOST that a tile is cut into at most), and its tile; false: there is none.  `shared`: LDS
 // that is free until then.
 template <int COLS, int MOST>

@@ -50,6 +50,17 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("" ::: "memory");
 }
 
+// Sums over the lanes up to this one (16 at a time, then over the rows of 16).
+__device__ __forceinline__ unsigned scan64(unsigned v) {
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x111, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x142, 0xa, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0u, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+
 // |v| where v is finite, else 0: what enters the maximum behind a factor.
 __device__ __forceinline__ float finite_abs(float v) {
   const float a = fabsf(v);
