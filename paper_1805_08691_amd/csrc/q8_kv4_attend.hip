@@ -367,9 +367,10 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
     const int group = groups > 1 ? tid / each : 0, i = i0 + (groups > 1 ? tid - group * each : tid);
     const int c = i / (D / 4), d = i % (D / 4) * 4;
     f4 v = {0, 0, 0, 0};
-    if (i < items && group < groups) {
+    // (as many parts on their way as there are, rounded up: the last is read again in the place of absent ones)
+    auto add = [&](auto batch_c) __attribute__((always_inline)) {
+      constexpr int kBatch = decltype(batch_c)::value;
       const word* from = parts + (c * D + d) / 2;
-      constexpr int kBatch = 16;                        // parts on their way at a time
       for (int s0 = group; s0 < n; s0 += groups * kBatch) {
         f2 x[kBatch], y[kBatch];
 #pragma unroll
@@ -381,6 +382,12 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
         for (int u = 0; u < kBatch; ++u)
           if (s0 + u * groups < n) v += weights[(s0 + u * groups) * kCols + c] * f4{x[u][0], x[u][1], y[u][0], y[u][1]};
       }
+    };
+    if (i < items && group < groups) {
+      if (n <= 2 * groups) add(std::integral_constant<int, 2>{});
+      else if (n <= 4 * groups) add(std::integral_constant<int, 4>{});
+      else if (n <= 8 * groups) add(std::integral_constant<int, 8>{});
+      else add(std::integral_constant<int, 16>{});
     }
     if (groups > 1) {
       quads[tid] = v;
