@@ -136,8 +136,6 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
   float top = -__builtin_inff(), ref = -__builtin_inff(), sum = 0.0f;     // ref: what sum and o are relative to, as a power of 2
   float lift = kLift, limit = 0.0f;                     // kLift - log2 of the factors' power, and where it has to grow
   constexpr _Float16 kLow = -1032.0f16, kHigh = -1152.0f16;
-  const h8 low_off = {kLow, kLow, kLow, kLow, kLow, kLow, kLow, kLow};
-  const h8 high_off = {kHigh, kHigh, kHigh, kHigh, kHigh, kHigh, kHigh, kHigh};
   const h8 key_off = {kLow, kLow, kLow, kLow, kHigh, kHigh, kHigh, kHigh};
 
   for (int it = 0; it < iterations; ++it) {
@@ -235,8 +233,9 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
         x[tile][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tile][i], scale, -now));
         sum += x[tile][i];
       }
-    // ---- O^T: a probability times its token's factor is the right operand.  What the codes have too much goes first,
-    // as a product with the same operand: the sum of both is exact to a unit of the larger.
+    // ---- O^T: a probability times its token's factor is the right operand.  What the codes have too much is taken from them
+    // here, not by a product as for the keys: the matrix instruction cuts what it adds at the largest, always downwards, and
+    // products of 1032 would leave 7e-6 of a value in every output, more than a fp16 output's rounding over long contexts.
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       h2 vf[8];
@@ -258,12 +257,11 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
           }
         }
         const unsigned c = vc[2 * h], d = vc[2 * h + 1];
-        f4 lo = __builtin_amdgcn_mfma_f32_16x16x32_f16(low_off, pr, o[2 * g], 0, 0, 0);
-        f4 hi = __builtin_amdgcn_mfma_f32_16x16x32_f16(high_off, pr, o[2 * g + 1], 0, 0, 0);
-        o[2 * g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join4(un.low(c), un.low(c >> 8), un.low(d), un.low(d >> 8)), pr,
-                                                          lo, 0, 0, 0);
-        o[2 * g + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-            join4(un.high(c), un.high(c >> 8), un.high(d), un.high(d >> 8)), pr, hi, 0, 0, 0);
+        auto low = [&](unsigned w) { return un.low(w) + h2{kLow, kLow}; };
+        auto high = [&](unsigned w) { return un.high(w) + h2{kHigh, kHigh}; };
+        o[2 * g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join4(low(c), low(c >> 8), low(d), low(d >> 8)), pr, o[2 * g], 0, 0, 0);
+        o[2 * g + 1] =
+            __builtin_amdgcn_mfma_f32_16x16x32_f16(join4(high(c), high(c >> 8), high(d), high(d >> 8)), pr, o[2 * g + 1], 0, 0, 0);
       }
     }
     __builtin_amdgcn_s_waitcnt(0xc07f);                 // the stage has been read

@@ -507,6 +507,24 @@ def test_attention_of_flat_and_peaked_rows(B, peak, scale):
         _check_attend(B, _rng(5), [200, 33], [1, 1], 2, 4, 64, 16, kind, peak=peak, scale=scale)
 
 
+@pytest.mark.parametrize("rows", [1, 8])
+def test_attention_averages_a_long_context(B, rows):
+    """Equal weights over many keys: what is left of values that cancel is 1 / sqrt(keys) of them, and what a sum loses in one
+    direction shows.  The output's rounding and that of each product are 2^-12 of their size at most, on average a half of
+    it, with signs that cancel like the values': together they stay below 2^-11 of the output's norm."""
+    rng = _rng(rows, 61)
+    H, ratio, D, page, n = 2, 16, 64, 64, 30000
+    cache, table, keys, values = _filled(B, rng, [n], H, D, page)
+    T = 1 if rows == 1 else 256                                          # (256 tokens of 16 heads: wide tiles)
+    q = torch.zeros((T, H * ratio, D), dtype=torch.float16)
+    lens, first = [torch.tensor(v, dtype=torch.int32, device="cuda") for v in ([n], [0, T])]
+    got = B.kv4_attend(q.cuda(), cache, table, lens, first, workspace=B.kv4_attend_workspace(q, cache, 1, n))
+    upto = np.cumsum(values[0], 0)[n - T:] / np.arange(n - T + 1, n + 1)[:, None, None]
+    want = np.repeat(upto, ratio, 1)
+    off = got.double().cpu().numpy() - want
+    assert np.linalg.norm(off) <= 2.0 ** -11 * np.linalg.norm(want), np.linalg.norm(off) / np.linalg.norm(want)
+
+
 def test_attention_reads_no_page_that_a_request_has_not(B):
     """Pages outside the cache inside a request's length: their tokens are not seen, whatever the table says."""
     rng = _rng(12)
