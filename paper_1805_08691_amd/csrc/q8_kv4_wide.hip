@@ -8,7 +8,7 @@
 // instructions, of which a third of the cycles is full, so three workgroups share a compute unit and two barriers a step
 // are hidden behind each other's.
 // bf16 outputs: a key is its code times its factor, and a query has the scale in it, both rounded to binary16 (2^-12 of
-// each, 6e-4 of an output, under bf16's 1.6e-3); scores come out of the products relative to the running maximum, which
+// each, 6e-4 to 15e-4 of an output by how far scores are apart, under bf16's 1.6e-3); scores come out of the products relative to the running maximum, which
 // they begin with.  fp16 outputs show that: there codes are multiplied, and factors and scale go into the sums.  A maximum
 // that grows by less than 2^8 is left: probabilities are up to 256, and sums are not rescaled.  The sum is that of the
 // probabilities as the values meet them, rounded to binary16.
