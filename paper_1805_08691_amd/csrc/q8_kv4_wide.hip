@@ -8,10 +8,10 @@
 // instructions, of which a third of the cycles is full, so three workgroups share a compute unit and two barriers a step
 // are hidden behind each other's.
 // bf16 outputs: a key is its code times its factor, and a query has the scale in it, both rounded to binary16 (2^-12 of
-// each, 6e-4 to 15e-4 of an output by how far scores are apart, under bf16's 1.6e-3); scores come out of the products relative to the running maximum, which
-// they begin with.  fp16 outputs show that: there codes are multiplied, and factors and scale go into the sums.  A maximum
-// that grows by less than 2^8 is left: probabilities are up to 256, and sums are not rescaled.  The sum is that of the
-// probabilities as the values meet them, rounded to binary16.
+// each, 6e-4 to 15e-4 of an output by how far scores are apart, under bf16's 1.6e-3); scores come out of the products
+// relative to the running maximum, which they begin with.  fp16 outputs show that: there codes are multiplied, and factors
+// and scale go into the sums.  A maximum that grows by less than 2^8 is left: probabilities are up to 256, and sums are
+// not rescaled.  The sum is that of the probabilities as the values meet them, rounded to binary16.
 // Pieces of 2048 tokens of 3 requests over 8192 keys, 32 query heads of 128 channels: 395 us, 910 TFLOP/s.
 #include "q8_kv4_attend.h"
 
@@ -45,8 +45,8 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
   Part a;
   Tile t;
   // (whole tiles: the last of a request see most keys, so they go first)
-  if (!find_part<kWide, kWideParts>(p, p.parts ? blockIdx.x : (p.tiles - 1 - blockIdx.x / p.H) * p.H + blockIdx.x % p.H, shared, &a, &t))
-    return;
+  const int id = p.parts ? (int)blockIdx.x : (p.tiles - 1 - (int)blockIdx.x / p.H) * p.H + (int)blockIdx.x % p.H;
+  if (!find_part<kWide, kWideParts>(p, id, shared, &a, &t)) return;
   const int head = a.head, start = t.lo + a.step0 * kStep, steps = a.step1 - a.step0;
   const int last = min(t.lo + t.steps * kStep, t.len);
 
