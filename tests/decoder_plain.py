@@ -138,3 +138,36 @@ def attend_tolerance(out, values, most, dtype):
     top = max([np.abs(v).max() for v in values if v.size] or [0.0])
     rel = math.expm1(2 * d) + 2.0 ** -11 + 2.0 ** -11 + n * 2.0 ** -25
     return top * rel + np.abs(out) * (2.0 ** -8 if dtype is torch.bfloat16 else 2.0 ** -11) + 1e-7 * top
+
+
+def attend_rows(q, keys, values, lengths, starts, scale, window=0):
+    """As ``attend``, a head of a request at a time: for many rows."""
+    out = np.zeros_like(q)
+    for b, n_keys in enumerate(lengths):
+        rows = slice(starts[b], starts[b + 1])
+        n = starts[b + 1] - starts[b]
+        ratio = q.shape[1] // keys[b].shape[1]
+        behind = np.arange(n_keys)[None] - (np.arange(n) + n_keys - n)[:, None]              # of a key to a row's own
+        seen = (behind <= 0) & (behind > -window if window else True)
+        for h in range(q.shape[1] if n and n_keys else 0):
+            s = np.where(seen, q[rows, h] @ keys[b][:, h // ratio].T * scale, -np.inf)
+            p = np.exp(s - np.where(seen.any(1), s.max(1), 0)[:, None])
+            out[rows, h] = p @ values[b][:, h // ratio] / np.maximum(p.sum(1), 1e-300)[:, None]
+    return out
+
+
+def attend_norm(want, dtype, wide, spread):
+    """What |off| over all outputs (a norm) is expected to stay below.  A rounding to a type whose unit at 1 is u is off by
+    at most u / sqrt(12) of a value in the root mean square (by as little as half of that where the value is just below a
+    power of two), and roundings of different numbers are independent: their squares add up.
+      tiles of 16 columns    a probability times its token's factor is rounded to binary16, the output to its type
+      tiles of 128 columns   a value (code times factor) and a probability to binary16, the output to its type
+        bf16                 ... and a key and a query, channel by channel: a score is then off by that of what scores
+                             spread by, and a probability by as much of itself
+    Outputs in fp16 are off by 2^-25 where they are subnormal."""
+    half, own = 2.0 ** -10 / math.sqrt(12), (2.0 ** -7 if dtype is torch.bfloat16 else 2.0 ** -10) / math.sqrt(12)
+    squares = own ** 2 + half ** 2 * (2 if wide else 1)
+    if wide and dtype is torch.bfloat16:
+        squares += 2 * (spread * half) ** 2
+    subnormal = 2.0 ** -25 * math.sqrt(want.size) if dtype is torch.float16 else 0.0
+    return math.sqrt(squares) * np.linalg.norm(want) + subnormal

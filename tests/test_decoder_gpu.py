@@ -602,6 +602,65 @@ def test_attention_is_the_same_every_time(B):
             assert torch.equal(got, B.kv4_attend(q.cuda(), cache, table, lens, first, workspace=ws))
 
 
+# lengths, added, key heads, query heads to each, page, tokens that the table has places for (0: no workspace): which
+# kernel takes them, and whether it cuts the keys
+PATHS = {"rows": ([300, 200, 70, 1, 513], [1] * 5, 4, 8, 64, 0), "rows, cut": ([5000, 900], [1, 1], 2, 8, 64, 5000),
+         "prompts": ([330, 200, 129], [150, 200, 100], 16, 8, 32, 0), "prompts, cut": ([2300, 700], [64, 130], 4, 8, 32, 140000)}
+
+
+def _path(B, rng, path, kind, D, spread, value_size=None, key_size=1.0, window=0):
+    """Attention on that path over scores that spread by `spread`, values of `value_size(request, tokens)` and keys of
+    `key_size`; -> (outputs, expected ones)."""
+    lengths, added, H, ratio, page, longest = PATHS[path]
+
+    def kv(b, n):
+        size = 1.0 if value_size is None else value_size(b, n)
+        k, v = rng.standard_normal((n, H, D)) * key_size, rng.standard_normal((n, H, D)) * size
+        return torch.from_numpy(k.astype(np.float32)), torch.from_numpy(v.astype(np.float32))
+
+    cache, table, keys, values = _filled(B, rng, lengths, H, D, page, kv=kv)
+    q = torch.from_numpy((rng.standard_normal((sum(added), H * ratio, D)) * spread).astype(np.float32)).to(TYPES[kind])
+    starts = np.concatenate([[0], np.cumsum(added)]).tolist()
+    lens, first = [torch.tensor(v, dtype=torch.int32, device="cuda") for v in (lengths, starts)]
+    ws = None
+    if longest:
+        table = torch.nn.functional.pad(table, (0, max(0, -(-longest // page) - table.shape[1])), value=-1)
+        ws = B.kv4_attend_workspace(q, cache, len(lengths), longest)
+        assert ws.numel()
+    scale = D ** -0.5 / key_size
+    got = B.kv4_attend(q.cuda(), cache, table, lens, first if "prompts" in path else None, scale, window=window, workspace=ws)
+    want = P.attend_rows(q.double().numpy(), keys, values, lengths, starts, scale, window)
+    return got.double().cpu().numpy(), want
+
+
+def _close(got, want, kind, path, spread):
+    off, bound = np.linalg.norm(got - want), P.attend_norm(want, TYPES[kind], "prompts" in path, spread)
+    assert off <= bound, (off / np.linalg.norm(want), bound / np.linalg.norm(want))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("path", sorted(PATHS))
+def test_attention_over_values_of_any_size(B, path, kind):
+    """From the largest that the cache holds to such as have factors that are subnormal in binary16."""
+    for i, size in enumerate((5000.0, 0.05, 1e-2, 1e-4, 1e-6)):
+        got, want = _path(B, _rng(i, 71), path, kind, 64, 2.0, lambda b, n: size)
+        _close(got, want, kind, path, 2.0)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("path", sorted(PATHS))
+def test_attention_over_values_of_different_sizes(B, path, kind):
+    """A context whose first tokens have tiny values and whose later ones large ones, and the other way round; and groups of
+    channels of different size, each held to its own norm."""
+    for first, behind in ((1e-5, 1.0), (300.0, 1e-2)):
+        got, want = _path(B, _rng(72), path, kind, 96, 2.0, lambda b, n: np.where(np.arange(n) < 64, first, behind)[:, None, None])
+        _close(got, want, kind, path, 2.0)
+    sizes = np.repeat([1.0, 1e-3, 30.0], 32)
+    got, want = _path(B, _rng(73), path, kind, 96, 2.0, lambda b, n: sizes)
+    for g in range(3):
+        _close(got[..., 32 * g:32 * g + 32], want[..., 32 * g:32 * g + 32], kind, path, 2.0)
+
+
 # ------------------------------------------------------------------------------ together
 def _block(rng, requests=4, n_pages=60, most=400, **kw):
     from paper_1805_08691_amd.decoder import AttentionBlock
