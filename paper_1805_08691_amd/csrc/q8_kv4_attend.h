@@ -56,7 +56,7 @@ __device__ __forceinline__ bool set_tile(const AttendParams& p, int w, int b, in
   t->len = (int)min((long)max(length, 0), longest);
   const int tok0 = t->first / p.ratio, tok1 = (min(t->first + COLS, t->cols) - 1) / p.ratio;
   const int pos0 = t->len - t->n + tok0, pos1 = t->len - t->n + tok1;
-  t->seen = p.window > 0 ? max(0, pos0 - p.window + 1) : 0;
+  t->seen = p.window > 0 ? max(0, max(pos0, 0) - p.window + 1) : 0;        // (rows in front of the first key see none)
   t->lo = t->seen & ~(kStep - 1);
   t->steps = pos1 < t->lo ? 0 : (pos1 - t->lo) / kStep + 1;
   return true;

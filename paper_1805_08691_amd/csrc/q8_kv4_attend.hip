@@ -499,7 +499,8 @@ extern "C" int q8_kv4_attend(const void* q_dev, int type, size_t T, int n_heads,
   p.n_pages = (long)n_pages;
   p.T = (int)T, p.B = n_requests, p.H = n_heads, p.ratio = ratio, p.width = width;
   p.shift = __builtin_ctz(page) - 4;
-  p.tiles = (int)tiles, p.window = window;
+  p.tiles = (int)tiles;
+  p.window = (size_t)window >= longest ? 0 : window;      // (as long as a request: none; differences of positions fit an int)
   p.scale_log2 = scale * 1.4426950408889634f;
   if (wide) return kv4_attend_wide(D / 32, p, q_dev, out_dev, type, (hipStream_t)stream);
   if (type == Q8_F16)

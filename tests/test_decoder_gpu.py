@@ -661,6 +661,15 @@ def test_attention_over_values_of_different_sizes(B, path, kind):
         _close(got[..., 32 * g:32 * g + 32], want[..., 32 * g:32 * g + 32], kind, path, 2.0)
 
 
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 20, 2 ** 30, 65])
+def test_attention_in_windows_of_any_length(B, window):
+    """Requests with more rows than tokens: rows stand in front of the first key, by more than an int is short of the
+    longest window."""
+    for H, ratio, lengths, added in ((2, 2, [20, 70], [60, 71]), (16, 8, [20, 200], [150, 330])):
+        for kind in ("bf16", "f16"):
+            _check_attend(B, _rng(7, H), lengths, added, H, ratio, 64, 16, kind, window=window)
+
+
 # ------------------------------------------------------------------------------ together
 def _block(rng, requests=4, n_pages=60, most=400, **kw):
     from paper_1805_08691_amd.decoder import AttentionBlock
