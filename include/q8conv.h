@@ -626,7 +626,7 @@ int q8_kv4_read(const void *cache_dev, size_t n_pages, int page, const int64_t *
  * rows' own (written before).  A row at position i of its request sees the keys j <= i, and with
  * window > 0 only those with j > i - window:
  *   out[t] = sum_j softmax_j(scale q[t] . k_j) v_j,   zeros where it sees none.
- * Lengths above width * page count as that; tokens on a page outside the cache are not seen;
+ * Lengths above width * page (at most 2^31 - 2^16) count as that; tokens on a page outside the cache are not seen;
  * rows outside starts[0] .. starts[n_requests] are not written.  Sums and the softmax are fp32,
  * products binary16 x binary16.
  *   workspace   NULL, or device memory (16-byte aligned) with which the keys of few rows are

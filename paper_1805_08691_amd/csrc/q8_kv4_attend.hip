@@ -478,7 +478,8 @@ extern "C" int q8_kv4_attend(const void* q_dev, int type, size_t T, int n_heads,
   Q8_REQUIRE(table_stride >= (size_t)width && (starts_dev || T == (size_t)n_requests), Q8_EINVAL);
   Q8_REQUIRE(T == 1 || (q_stride >= (size_t)D && o_stride >= (size_t)D), Q8_EINVAL);
   Q8_REQUIRE(n_heads * ratio == 1 || (q_head_stride >= (size_t)D && o_head_stride >= (size_t)D), Q8_EINVAL);
-  Q8_REQUIRE(T <= 0x7fffffffu && n_pages <= 0x7fffffffu && (size_t)width * page <= 0x7fffffc0u, Q8_EUNSUPPORTED);
+  // (a table's places end far enough below 2^31 that the sixteens behind a tile's last key still have an int's numbers)
+  Q8_REQUIRE(T <= 0x7fffffffu && n_pages <= 0x7fffffffu && (size_t)width * page <= 0x7fff0000u, Q8_EUNSUPPORTED);
   Q8_REQUIRE(q8_aligned(q_dev, 2) && q8_aligned(out_dev, 2) && q8_aligned(cache_dev, 64) && q8_aligned(table_dev, 4) &&
                  q8_aligned(lengths_dev, 4) && q8_aligned(starts_dev, 4) && q8_aligned(workspace, 16), Q8_EALIGN);
   const size_t wide_tiles = tiles_of(T, n_requests, ratio, true, kWideCols), longest = (size_t)width * page;

@@ -129,6 +129,13 @@ def test_attention_refused():
         assert _attend(**bad) == EALIGN, bad
 
 
+def test_attention_refuses_tables_of_too_many_places():
+    """What a tile looks up behind its last key, up to 2048 tokens, has to have numbers below 2^31."""
+    for page in (16, 64, 1 << 16):
+        wide = 0x7fff0000 // page + 1
+        assert _attend(width=wide, stride=wide, page=page) == EUNSUPPORTED
+
+
 def test_binding_refuses_what_it_cannot_pass_on():
     x = torch.zeros(4, 32)
     for call in (lambda: B.quantize_rows(x), lambda: B.linear_pack(x), lambda: B.kv4_read(x, x),
