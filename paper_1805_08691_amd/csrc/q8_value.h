@@ -23,6 +23,9 @@ inline int with_type(int type, F f) {
 inline size_t type_bytes(int type) { return type == Q8_F32 ? 4 : 2; }
 inline bool type_ok(int type) { return type == Q8_F32 || type == Q8_F16 || type == Q8_BF16; }
 
+// Blocks of so many threads that one launch takes in a dimension, whose threads are counted in 32 bits.
+constexpr size_t most_blocks(size_t threads) { return 0xffffffffu / threads; }
+
 // N consecutive values at p.  ALIGNED: p is 16-byte aligned, or a multiple of the N values' bytes where these are fewer
 // (told to the compiler; the accesses are as wide without it, and take longer where they cross a line).
 template <int N, bool ALIGNED, typename V>

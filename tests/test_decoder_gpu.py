@@ -72,6 +72,19 @@ def test_rows_to_codes_of_special_values(B, kind, K):
     assert np.array_equal(z.cpu().numpy(), want_z)
 
 
+def test_rows_to_codes_of_very_many_rows(B):
+    """More rows than the blocks of one launch take."""
+    M, K = (1 << 26) + 333, 3
+    x = torch.randn((M, K), device="cuda", dtype=torch.float16)
+    q = torch.zeros(M, device="cuda")
+    z, _ = B.quantize_rows(x, factors=q)
+    assert bool((q > 0).all())
+    for a in (0, (1 << 25) - 100, (1 << 26) - 500, M - 700):
+        rows = slice(a, a + 700)
+        want_z, want_q = P.quantize_rows(x[rows].cpu())
+        assert np.array_equal(z[rows].cpu().numpy(), want_z) and np.array_equal(q[rows].cpu().numpy(), want_q)
+
+
 # ------------------------------------------------------------------------------ the product
 def _weights(rng, N, K):
     z_w = rng.integers(-128, 128, (N, K), dtype=np.int8)
