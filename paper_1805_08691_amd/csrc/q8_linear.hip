@@ -175,7 +175,11 @@ constexpr Variant kVariants[] = {
     {"rows_any", 16, 16, 0, 0, -1, 0.0f, 0.0f, 0.0f, 0.0f}};      // rows so far apart that a tile passes 2^31 bytes
 constexpr int kNumVariants = sizeof(kVariants) / sizeof(kVariants[0]);
 constexpr size_t kTileStride = 1 << 22;      // 256 rows of a tile stay below 2^31 bytes
-constexpr int kMostRows = 16 * 65535;        // of the rows builds: a launch's second dimension
+constexpr int kMostRows = 16 * 65535;        // of the builds that are no tiles: a launch's second dimension
+// ... and its first one, blocks of eight wavefronts at most.
+bool reached(const Variant& v, int M, int N) {
+  return v.tile >= 0 || (M <= kMostRows && ((size_t)N + v.bn - 1) / v.bn <= most_blocks(512));
+}
 
 int pick(const LinearParams& p) {
   int best = -1;
@@ -183,7 +187,7 @@ int pick(const LinearParams& p) {
   const float memory = 2.2f + ((float)p.N + (float)p.M) * (float)p.K / 5.4e6f;
   for (int i = 0; i + 1 < kNumVariants; ++i) {
     const Variant& v = kVariants[i];
-    if (v.columns && p.M > kMostRows) continue;
+    if (!reached(v, p.M, p.N)) continue;
     const float tiles = (float)((p.N + v.bn - 1) / v.bn) * (float)((p.M + v.bm - 1) / v.bm), rounds = tiles / 256.0f;
     const float passes = fmaxf(1.0f, v.share * rounds + (1.0f - v.share) * ceilf(rounds));
     const float time = v.base + passes * (v.round + v.per_k * (float)p.K / 1024.0f);
@@ -229,7 +233,7 @@ extern "C" int q8_linear_pack(const int8_t* z_w_dev, int N, int K, void* packed_
   Q8_REQUIRE(z_w_dev && packed_dev, Q8_EINVAL);
   Q8_REQUIRE(q8_aligned(packed_dev, 16), Q8_EALIGN);
   const size_t chunks = q8_linear_packed_bytes(N, K) / 16, blocks = (chunks + 255) / 256;
-  Q8_REQUIRE(blocks <= 0x7fffffffu, Q8_EUNSUPPORTED);
+  Q8_REQUIRE(blocks <= most_blocks(256), Q8_EUNSUPPORTED);
   linear_pack_kernel<<<(unsigned)blocks, 256, 0, (hipStream_t)stream>>>(
       z_w_dev, N, K, (int)(round_up(K, kPackK) / kPackK), chunks, static_cast<int8_t*>(packed_dev));
   return q8_launch_status();
@@ -257,7 +261,7 @@ extern "C" int q8_linear_int8_variant(const int8_t* z_x_dev, size_t z_stride, co
                        y_stride, (int)M, N, K, (int)(round_up(K, kPackK) / kPackK)};
   if (variant < 0) variant = z_stride <= kTileStride ? pick(p) : kNumVariants - 1;
   const Variant& v = kVariants[variant];
-  Q8_REQUIRE(v.tile >= 0 || (int)M <= kMostRows, Q8_EUNSUPPORTED);
+  Q8_REQUIRE(reached(v, (int)M, N), Q8_EUNSUPPORTED);
   if (v.columns) return linear_rows(p, y_dev, type, v.columns, v.squares, (hipStream_t)stream);
   if (v.tile >= 0 && z_stride > kTileStride) return Q8_EUNSUPPORTED;
   if (v.tile >= 0) return linear_tile(p, y_dev, type, v.tile, (hipStream_t)stream);

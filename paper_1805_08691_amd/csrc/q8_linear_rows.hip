@@ -275,7 +275,9 @@ int linear_rows(const LinearParams& p, void* y, int type, int columns, int squar
   });
 }
 
-bool linear_rows_take_real(int M, int N, int K) { return real_rows_of_waves(M, N, K) || real_rows_together(M, K); }
+bool linear_rows_take_real(int M, int N, int K) {
+  return (size_t)N <= kPackN * most_blocks(kThreads8) && (real_rows_of_waves(M, N, K) || real_rows_together(M, K));
+}
 
 int linear_rows_real(const LinearParams& p, const void* x, int x_type, size_t x_stride, void* y, int type,
                      hipStream_t stream) {

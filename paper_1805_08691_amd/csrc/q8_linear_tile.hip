@@ -234,15 +234,23 @@ __global__ __launch_bounds__(Sh::NW * 64) void linear_tile_kernel(const LinearPa
 
 template <typename Sh, typename Y, bool PAIRS>
 int launch(const LinearParams& p, Y* y, hipStream_t stream) {
+  // as many rows of tiles a launch as its blocks reach
+  constexpr size_t kBlocks = most_blocks(Sh::NW * 64) / kXcds * kXcds;
+  const size_t tn = ((size_t)p.N + Sh::BN - 1) / Sh::BN, most = kBlocks / tn * Sh::BM;
+  Q8_REQUIRE(most > 0, Q8_EUNSUPPORTED);
   if constexpr (Sh::LDS_BYTES > 65536) {
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&linear_tile_kernel<Sh, Y, PAIRS>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, Sh::LDS_BYTES);
     if (attr != hipSuccess) return Q8_EHIP;
   }
-  const long tn = (p.N + Sh::BN - 1) / Sh::BN, tm = (p.M + Sh::BM - 1) / Sh::BM;
-  Q8_REQUIRE(tn * tm <= 0x7ffffff0l, Q8_EUNSUPPORTED);
-  const unsigned blocks = (unsigned)((tn * tm + kXcds - 1) / kXcds * kXcds);
-  linear_tile_kernel<Sh, Y, PAIRS><<<blocks, Sh::NW * 64, Sh::LDS_BYTES, stream>>>(p, y, (int)tn, (int)tm);
+  LinearParams part = p;
+  for (size_t m = 0; m < (size_t)p.M; m += most) {
+    part.z = p.z + m * p.z_stride;
+    part.q_x = p.q_x + m;
+    part.M = (int)(p.M - m < most ? p.M - m : most);
+    const size_t tm = ((size_t)part.M + Sh::BM - 1) / Sh::BM, blocks = (tn * tm + kXcds - 1) / kXcds * kXcds;
+    linear_tile_kernel<Sh, Y, PAIRS><<<(unsigned)blocks, Sh::NW * 64, Sh::LDS_BYTES, stream>>>(part, y + m * p.y_stride, (int)tn, (int)tm);
+  }
   return q8_launch_status();
 }
 

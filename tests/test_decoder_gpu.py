@@ -162,6 +162,29 @@ def test_product_of_very_many_rows(B):
     assert torch.equal(y.cpu(), P.linear(z.numpy(), q_x.numpy(), z_w, q_w, bias, torch.float16))
 
 
+@pytest.mark.parametrize("M,N", [((1 << 30) + 77, 5), (1, (1 << 27) + 5)])
+def test_product_of_more_than_a_launch_takes(B, M, N):
+    """Rows in several launches; channels that the builds for few rows do not reach."""
+    rng = _rng(6, 7, N % 100)
+    K = 16 if M > 1 else 1
+    z_w = rng.integers(-128, 128, (min(N, 5000), K), dtype=np.int8)
+    q_w = (rng.random(min(N, 5000)) + 0.5).astype(np.float32)
+    repeat = -(-N // len(q_w))
+    weights = B.linear_pack(torch.from_numpy(z_w).cuda().repeat(repeat, 1)[:N])
+    factors = torch.from_numpy(q_w).cuda().repeat(repeat)[:N].contiguous()
+    x = torch.randint(-128, 128, (1000, 16), device="cuda", dtype=torch.int8)
+    codes = x.repeat(-(-M // 1000), 1)[:M]
+    y = torch.empty((M, N), device="cuda", dtype=torch.float16)
+    B.linear_int8(codes[:, :K], torch.ones(M, device="cuda"), weights, factors, out=y)
+    want = P.linear(x[:, :K].cpu().numpy(), np.ones(1000, np.float32), z_w, q_w, None, torch.float16).cuda()
+    if M > 1:
+        for a in range(0, M, 1 << 22):
+            part = y[a:a + (1 << 22)]
+            assert torch.equal(part, want[(a + torch.arange(len(part), device="cuda")) % 1000]), a
+    else:
+        assert torch.equal(y[0], want[0].repeat(repeat)[:N])
+
+
 def test_product_of_the_largest_sums(B):
     """128 * 128 * 131071 just fits the accumulator, on both sides."""
     K = 131071

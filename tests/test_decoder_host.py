@@ -73,6 +73,15 @@ def test_products_refused():
     assert L.q8_linear_pack(None, 0, 4, None, None) == OK
 
 
+def test_products_beyond_a_launch_refused():
+    """A launch's threads are counted in 32 bits: no weights of 2^36 bytes, no build for few rows on 2^27 channels."""
+    assert L.q8_linear_pack(A, 1 << 22, 16384, A, None) == EUNSUPPORTED
+    for v in range(L.q8_linear_num_variants()):
+        if L.q8_linear_variant_name(v) == b"rows_16x16":
+            assert L.q8_linear_int8_variant(A, 16, A, 1, 1 << 27, 1, A, A, None, A, 0, 1 << 27, v, None) == EUNSUPPORTED
+    assert _product(N=0x7fffffff, ys=0x7fffffff, K=1) == EUNSUPPORTED
+
+
 def _tables(lengths=A, added=A, n=3, page=16, free=A, n_free=5, table=A, width=4, stride=4, slots=A, positions=A,
             n_slots=9, starts=A, grown=A, counts=A):
     return L.q8_page_tables(lengths, added, n, page, free, n_free, table, width, stride, slots, positions, n_slots, starts,
