@@ -518,6 +518,20 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(const Kv4Params p, V* __r
 // Fours of groups that a block takes one after the other: as many as leave the compute units eight blocks each.
 inline int fours_per_block(size_t blocks) { return (int)(blocks / 2048 < 1 ? 1 : blocks / 2048 > 8 ? 8 : blocks / 2048); }
 
+// ... and launches of that: as many tokens as blocks reach.
+template <typename F>
+int launch_tokens(size_t T, size_t group_blocks, F launch) {
+  const size_t all = (T + kTok - 1) / kTok * group_blocks;
+  const int per = fours_per_block(all);
+  const size_t blocks = (group_blocks + per - 1) / per, most = most_blocks(256) / blocks * kTok;
+  Q8_REQUIRE(most > 0, Q8_EUNSUPPORTED);
+  for (size_t t = 0; t < T; t += most) {
+    const size_t n = T - t < most ? T - t : most;
+    launch(t, (int)n, (unsigned)((n + kTok - 1) / kTok * blocks), per);
+  }
+  return q8_launch_status();
+}
+
 int check_tokens(const void* k, const void* v, int type, size_t T, int H, int D, size_t k_stride, size_t k_head,
                  size_t v_stride, size_t v_head, const int64_t* slots, const void* cache, size_t n_pages, int page) {
   Q8_REQUIRE(type_ok(type) && H >= 1, Q8_EINVAL);
@@ -573,18 +587,19 @@ extern "C" int q8_kv4_write(const void* k_dev, const void* v_dev, int type, size
   if (rc != Q8_OK || T == 0) return rc;
   const Kv4Params p{reinterpret_cast<const long*>(slots_dev), static_cast<uint8_t*>(cache_dev), k_stride, k_head_stride,
                     v_stride, v_head_stride, (long)n_pages * page, (int)T, n_heads, D / 32, __builtin_ctz(page)};
-  const size_t group_blocks = ((size_t)n_heads * (D / 32) + kGroups - 1) / kGroups, blocks = (T + kTok - 1) / kTok * group_blocks;
-  const int per = fours_per_block(blocks);
-  const size_t grid = (T + kTok - 1) / kTok * ((group_blocks + per - 1) / per);
-  Q8_REQUIRE(blocks <= 0x7fffffffu, Q8_EUNSUPPORTED);
+  const size_t group_blocks = ((size_t)n_heads * (D / 32) + kGroups - 1) / kGroups;
   return with_type(type, [&](auto one) {
     using V = decltype(one);
-    const V *k = static_cast<const V*>(k_dev), *v = static_cast<const V*>(v_dev);
-    if (kv4_rows_aligned<V>(k_dev, v_dev, k_stride, k_head_stride, v_stride, v_head_stride))
-      kv4_write_kernel<V, true><<<(unsigned)grid, 256, 0, (hipStream_t)stream>>>(p, k, v, (int)group_blocks, per);
-    else
-      kv4_write_kernel<V, false><<<(unsigned)grid, 256, 0, (hipStream_t)stream>>>(p, k, v, (int)group_blocks, per);
-    return q8_launch_status();
+    const V *const k = static_cast<const V*>(k_dev), *const v = static_cast<const V*>(v_dev);
+    const bool aligned = kv4_rows_aligned<V>(k_dev, v_dev, k_stride, k_head_stride, v_stride, v_head_stride);
+    return launch_tokens(T, group_blocks, [&](size_t t, int n, unsigned grid, int per) {
+      Kv4Params part = p;
+      part.slots = p.slots + t, part.T = n;
+      if (aligned)
+        kv4_write_kernel<V, true><<<grid, 256, 0, (hipStream_t)stream>>>(part, k + t * k_stride, v + t * v_stride, (int)group_blocks, per);
+      else
+        kv4_write_kernel<V, false><<<grid, 256, 0, (hipStream_t)stream>>>(part, k + t * k_stride, v + t * v_stride, (int)group_blocks, per);
+    });
   });
 }
 
@@ -597,17 +612,18 @@ extern "C" int q8_kv4_read(const void* cache_dev, size_t n_pages, int page, cons
   const Kv4Params p{reinterpret_cast<const long*>(slots_dev), static_cast<uint8_t*>(const_cast<void*>(cache_dev)),
                     k_stride, k_head_stride, v_stride, v_head_stride, (long)n_pages * page, (int)T, n_heads, D / 32,
                     __builtin_ctz(page)};
-  const size_t group_blocks = ((size_t)n_heads * (D / 32) + kGroups - 1) / kGroups, blocks = (T + kTok - 1) / kTok * group_blocks;
-  const int per = fours_per_block(blocks);
-  const size_t grid = (T + kTok - 1) / kTok * ((group_blocks + per - 1) / per);
-  Q8_REQUIRE(blocks <= 0x7fffffffu, Q8_EUNSUPPORTED);
+  const size_t group_blocks = ((size_t)n_heads * (D / 32) + kGroups - 1) / kGroups;
   return with_type(type, [&](auto one) {
     using V = decltype(one);
-    V *k = static_cast<V*>(k_dev), *v = static_cast<V*>(v_dev);
-    if (kv4_rows_aligned<V>(k_dev, v_dev, k_stride, k_head_stride, v_stride, v_head_stride))
-      kv4_read_kernel<V, true><<<(unsigned)grid, 256, 0, (hipStream_t)stream>>>(p, k, v, (int)group_blocks, per);
-    else
-      kv4_read_kernel<V, false><<<(unsigned)grid, 256, 0, (hipStream_t)stream>>>(p, k, v, (int)group_blocks, per);
-    return q8_launch_status();
+    V *const k = static_cast<V*>(k_dev), *const v = static_cast<V*>(v_dev);
+    const bool aligned = kv4_rows_aligned<V>(k_dev, v_dev, k_stride, k_head_stride, v_stride, v_head_stride);
+    return launch_tokens(T, group_blocks, [&](size_t t, int n, unsigned grid, int per) {
+      Kv4Params part = p;
+      part.slots = p.slots + t, part.T = n;
+      if (aligned)
+        kv4_read_kernel<V, true><<<grid, 256, 0, (hipStream_t)stream>>>(part, k + t * k_stride, v + t * v_stride, (int)group_blocks, per);
+      else
+        kv4_read_kernel<V, false><<<grid, 256, 0, (hipStream_t)stream>>>(part, k + t * k_stride, v + t * v_stride, (int)group_blocks, per);
+    });
   });
 }

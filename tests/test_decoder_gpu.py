@@ -376,6 +376,29 @@ def test_tokens_in_and_out(B, kind, T, H, D, page):
         assert torch.equal(o[:, :, 1:-2], s) and bool((o[:, :, :1] == 5).all()) and bool((o[:, :, -2:] == 5).all())
 
 
+def test_more_tokens_than_a_launch_takes(B):
+    """2^28 tokens and some, most of which go nowhere."""
+    T, D, n = (1 << 28) + 37, 32, 100
+    k = torch.zeros((T, 1, D), dtype=torch.float16, device="cuda")
+    slots = torch.full((T,), -1, dtype=torch.int64, device="cuda")
+    rng = _rng(18)
+    rows = torch.cat([torch.arange(n), (1 << 28) - 66 + torch.arange(n), T - 3 + torch.arange(3)]).cuda()
+    some = _real(rng, (2 * n + 3, 1, D), "f16")
+    k[rows] = some.cuda()
+    at = torch.from_numpy(rng.permutation(2 * n + 3)).cuda()
+    slots[rows] = at
+    cache = B.kv4_cache(13, 1, 16, D)
+    B.kv4_write(cache, k, k, slots)
+    want = torch.from_numpy(P.kv4_values(some.float().numpy())).half()
+    for x in B.kv4_read(cache, at, dtype=torch.float16):
+        assert torch.equal(x.cpu(), want)
+    del k
+    for x in B.kv4_read(cache, slots, dtype=torch.float16):
+        assert torch.equal(x[rows].cpu(), want)
+        x[rows] = 0
+        assert not bool(x.any())
+
+
 @pytest.mark.parametrize("size", [0.0, 1e-9, 1e-6, 1e-3, 100.0, 6e4, 1e6])
 def test_sizes_that_the_cache_holds(B, size):
     """Factors down to binary16's smallest number and up to the largest that 8 of still fit."""
