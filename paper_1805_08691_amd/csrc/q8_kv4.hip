@@ -570,7 +570,7 @@ extern "C" int q8_page_tables(const int32_t* lengths_dev, const int32_t* added_d
     return q8_launch_status();
   }
   page_rows_kernel<<<1, 1024, 0, (hipStream_t)stream>>>(p);
-  if (n_slots) page_slots_kernel<<<(n_slots + 255) / 256, 256, 0, (hipStream_t)stream>>>(p);
+  if (n_slots) page_slots_kernel<<<((unsigned)n_slots + 255) / 256, 256, 0, (hipStream_t)stream>>>(p);
   return q8_launch_status();
 }
 

@@ -324,6 +324,25 @@ def test_tables_of_no_request(B):
     assert got["slots"].tolist() == [-1] * 5 == got["positions"].tolist()
 
 
+def test_tables_with_almost_2_31_slots(B):
+    """The last slots' numbers stand close below what an int holds, for one launch and for two."""
+    room = 2 ** 31 - 100
+    slots = torch.empty(room, dtype=torch.int64, device="cuda")
+    positions = torch.empty(room, dtype=torch.int32, device="cuda")
+    for n in (3, 5000):
+        slots.fill_(99)
+        positions.fill_(99)
+        lengths, added = torch.arange(n, dtype=torch.int32), torch.full((n,), 2, dtype=torch.int32)
+        free, table = np.arange(n * 2 + 400, dtype=np.int32), np.zeros((n, n // 16 + 2), np.int32)
+        want = P.page_tables(lengths.tolist(), added.tolist(), 16, free, table, 2 * n)
+        got = B.page_tables(lengths.cuda(), added.cuda(), 16, torch.from_numpy(free).cuda(), torch.from_numpy(table).cuda(), slots,
+                            positions)
+        assert slots[:2 * n].tolist() == want[1] and positions[:2 * n].tolist() == want[2]
+        for a in range(2 * n, room, 1 << 28):
+            assert bool((slots[a:a + (1 << 28)] == -1).all()) and bool((positions[a:a + (1 << 28)] == -1).all()), a
+        assert got["counts"].tolist() == want[5]
+
+
 # ------------------------------------------------------------------------------ tokens in and out
 def _slots(rng, T, places):
     """Runs of consecutive slots, some alone, some outside the cache."""
