@@ -627,8 +627,9 @@ int q8_kv4_read(const void *cache_dev, size_t n_pages, int page, const int64_t *
  * window > 0 only those with j > i - window:
  *   out[t] = sum_j softmax_j(scale q[t] . k_j) v_j,   zeros where it sees none.
  * Lengths above width * page (at most 2^31 - 2^16) count as that; tokens on a page outside the cache are not seen;
- * rows outside starts[0] .. starts[n_requests] are not written.  Sums and the softmax are fp32,
- * products binary16 x binary16.
+ * rows outside starts[0] .. starts[n_requests] are not written.  Sums and the softmax are fp32, products
+ * binary16 x binary16.  A request's columns (tokens times ratio) make tiles of 16 or 128; a launch takes 2^24 -
+ * 513 of them times n_heads (Q8_EUNSUPPORTED beyond).
  *   workspace   NULL, or device memory (16-byte aligned) with which the keys of few rows are
  *               split over workgroups: q8_kv4_attend_workspace_bytes, `longest` being the largest
  *               length expected (a hint; 0 bytes: nothing is split).  With less memory than a call

@@ -487,7 +487,7 @@ extern "C" int q8_kv4_attend(const void* q_dev, int type, size_t T, int n_heads,
   const bool wide = starts_dev && wide_for(T, n_requests, n_heads, ratio, D, longest, cuts);
   const size_t tiles = wide ? wide_tiles : tiles_of(T, n_requests, ratio, starts_dev != nullptr);
   const bool split = wide ? cuts : workspace && workspace_bytes >= split_bytes(D) && cut(tiles, longest);
-  Q8_REQUIRE((tiles * n_heads + kTarget) * kCols <= 0x7fffffffu && T * ratio <= 0x7fffffffu, Q8_EUNSUPPORTED);
+  Q8_REQUIRE(tiles * n_heads + kTarget <= most_blocks(256) && T * ratio <= 0x7fffffffu, Q8_EUNSUPPORTED);
   AttendParams p{};
   p.cache = static_cast<const uint8_t*>(cache_dev);
   p.table = table_dev;

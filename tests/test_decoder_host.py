@@ -145,6 +145,11 @@ def test_attention_refuses_tables_of_too_many_places():
         assert _attend(width=wide, stride=wide, page=page) == EUNSUPPORTED
 
 
+def test_attention_refuses_more_tiles_than_a_launch_takes():
+    for T, H, ratio in ((1 << 24, 1, 1), (1 << 20, 16, 16), (1 << 21, 4, 17)):
+        assert _attend(T=T, n=T, H=H, ratio=ratio, qs=1 << 20, os_=1 << 20) == EUNSUPPORTED
+
+
 def test_binding_refuses_what_it_cannot_pass_on():
     x = torch.zeros(4, 32)
     for call in (lambda: B.quantize_rows(x), lambda: B.linear_pack(x), lambda: B.kv4_read(x, x),
