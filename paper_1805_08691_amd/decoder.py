@@ -79,12 +79,12 @@ class AttentionBlock:
         H, D = self.heads, self.D
         B.page_tables(self._lengths, added, self.page, free, self.table, slots, positions, self._starts, self._grown,
                       self._counts)
-        joint = self.qkv(x, workspace=self._linear_ws).view(x.shape[0], -1, D)
+        joint = self.qkv(x, workspace=self._linear_ws).view(x.shape[0], H * (self.ratio + 2), D)
         q, k, v = joint[:, :H * self.ratio], joint[:, -2 * H:-H], joint[:, -H:]
         B.kv4_write(self.cache, k, v, slots)
         o = B.kv4_attend(q, self.cache, self.table, self._grown, self._starts, window=self.window,
                          workspace=self._attend_ws)
-        return self.out(o.view(x.shape[0], -1), out=out, workspace=self._linear_ws)
+        return self.out(o.view(x.shape[0], H * self.ratio * D), out=out, workspace=self._linear_ws)
 
     def release(self, request):
         """A request has ended: its pages are free again."""

@@ -882,3 +882,20 @@ def test_steps_on_two_streams(B):
             for r in range(4):
                 b.release(r)
         torch.cuda.synchronize()
+
+
+def test_a_step_without_tokens(B):
+    """None at all, on an empty block and between steps: an empty output, and nothing else."""
+    rng = _rng(34)
+    E, _, _, block = _block(rng)
+    x = torch.from_numpy(rng.standard_normal((40, E)).astype(np.float32)).cuda().bfloat16()
+    want = _block(_rng(34))[3].step(x, [30, 0, 10, 0])
+    for added in ([0] * 4, [30, 0, 10, 0], [0] * 4):
+        before = block.cache.clone(), block.table.clone(), list(block.lengths), block.taken
+        y = block.step(x[:sum(added)], added)
+        assert y.shape == (sum(added), E)
+        if sum(added):
+            assert torch.equal(y, want)
+        else:
+            assert torch.equal(before[0], block.cache) and torch.equal(before[1], block.table)
+            assert before[2:] == (block.lengths, block.taken) and block._lengths.tolist() == block.lengths
