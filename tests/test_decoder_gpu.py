@@ -899,3 +899,16 @@ def test_a_step_without_tokens(B):
         else:
             assert torch.equal(before[0], block.cache) and torch.equal(before[1], block.table)
             assert before[2:] == (block.lengths, block.taken) and block._lengths.tolist() == block.lengths
+
+
+def test_a_step_takes_no_negative_numbers(B):
+    """The tables take them as 0 and the host would not: refused, with nothing done."""
+    E, _, _, block = _block(_rng(35))
+    x = torch.zeros(40, E, dtype=torch.bfloat16, device="cuda")
+    block.step(x, [20, 0, 20, 0])
+    before = block.cache.clone(), block.table.clone(), list(block.lengths), block.taken
+    for added in ([-2, 12, 0, 0], [5, 6, 0, -1]):
+        with pytest.raises(AssertionError):
+            block.step(x[:10], added)
+        assert torch.equal(before[0], block.cache) and torch.equal(before[1], block.table)
+        assert before[2:] == (block.lengths, block.taken) and block._lengths.tolist() == block.lengths
