@@ -58,10 +58,11 @@ class AttentionBlock:
         return sum(-(-(n + a) // self.page) - -(-n // self.page) for n, a in zip(self.lengths, added))
 
     def step(self, x, added):
-        """x [T, E]: the new tokens of request 0, then those of request 1, ...; ``added``: how many each request has.
+        """x [T, E], fp16 or bf16: the new tokens of request 0, then those of request 1, ...; ``added``: how many each request has.
         -> [T, E], the block's output for them.  Raises MemoryError if they do not fit (nothing is done then)."""
         T, need = x.shape[0], self.pages_needed(added)
         assert len(added) == len(self.lengths) and sum(added) == T and all(a >= 0 for a in added)
+        assert x.dim() == 2 and x.shape[1] == self.qkv.K and x.dtype in (torch.float16, torch.bfloat16), (x.shape, x.dtype)
         longest = self.table.shape[1] * self.page
         if need > self.free.numel() - self.taken or T > self._slots.numel() or \
                 any(n + a > longest for n, a in zip(self.lengths, added)):

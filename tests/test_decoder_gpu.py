@@ -912,3 +912,16 @@ def test_a_step_takes_no_negative_numbers(B):
             block.step(x[:10], added)
         assert torch.equal(before[0], block.cache) and torch.equal(before[1], block.table)
         assert before[2:] == (block.lengths, block.taken) and block._lengths.tolist() == block.lengths
+
+
+def test_a_step_refuses_rows_before_it_does_anything(B):
+    """fp32 rows, which the attention has no form for, and rows of another width, also one whose weights take as many bytes."""
+    E, _, _, block = _block(_rng(36))
+    block.step(torch.ones(40, E, dtype=torch.bfloat16, device="cuda"), [20, 0, 20, 0])
+    before = block.cache.clone(), block.table.clone(), block._grown.clone()
+    for x in (torch.zeros(50, E, device="cuda"), torch.zeros(50, E - 16, dtype=torch.bfloat16, device="cuda"),
+              torch.zeros(50, 2 * E, dtype=torch.bfloat16, device="cuda"), torch.zeros(50, 1, E, dtype=torch.float16, device="cuda")):
+        with pytest.raises(AssertionError):
+            block.step(x, [0, 50, 0, 0])
+        assert all(torch.equal(a, b) for a, b in zip(before, (block.cache, block.table, block._grown)))
+        assert block.lengths == [20, 0, 20, 0]
