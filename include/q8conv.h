@@ -631,8 +631,8 @@ int q8_kv4_read(const void *cache_dev, size_t n_pages, int page, const int64_t *
  * binary16 x binary16.  A request's columns (tokens times ratio) make tiles of 16 or 128; a launch takes 2^24 -
  * 513 of them times n_heads (Q8_EUNSUPPORTED beyond).
  *   workspace   NULL, or device memory (16-byte aligned) with which the keys of few rows are
- *               split over workgroups: q8_kv4_attend_workspace_bytes, `longest` being the largest
- *               length expected (a hint; 0 bytes: nothing is split).  With less memory than a call
+ *               split over workgroups: q8_kv4_attend_workspace_bytes, enough for calls of up to T
+ *               tokens, `longest` being the largest length expected (a hint; 0 bytes: nothing is split).  With less memory than a call
  *               would split with it does without.  The caller zeroes it once
  *               after allocating it; every call leaves its counters zero again.  Calls that share
  *               one must not overlap in time.                                              */

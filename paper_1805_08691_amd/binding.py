@@ -737,8 +737,8 @@ def kv4_read(cache, slots, k_out=None, v_out=None, dtype=torch.bfloat16):
 
 
 def kv4_attend_workspace(q, cache, n_requests, longest, device="cuda"):
-    """Device memory with which ``kv4_attend`` splits the keys of few rows (zeros; calls leave its counters zero);
-    ``longest``: the most tokens that a request is expected to have."""
+    """Device memory with which ``kv4_attend`` splits the keys of few rows, for queries of q's shape or fewer tokens (zeros;
+    calls leave its counters zero); ``longest``: the most tokens that a request is expected to have."""
     heads, D = cache.shape[1], cache.shape[3] // 18
     n = lib.q8_kv4_attend_workspace_bytes(q.shape[0], n_requests, heads, q.shape[1] // heads, D, longest)
     return torch.zeros(n, dtype=torch.uint8, device=device)

@@ -459,9 +459,15 @@ bool wide_for(size_t T, int B, int H, int ratio, int D, size_t longest, bool cut
 extern "C" size_t q8_kv4_attend_workspace_bytes(size_t T, int n_requests, int n_heads, int ratio, int D,
                                                 size_t longest) {
   if (n_requests < 1 || n_heads < 1 || ratio < 1 || D < 32 || D > kMaxHead || T > 0x7fffffffu) return 0;
-  const bool cuts = cut(tiles_of(T, n_requests, ratio, true, kWideCols), longest);
-  if (cuts && wide_for(T, n_requests, n_heads, ratio, D, longest, true)) return split_bytes(D, kWideCols);
-  return cut(tiles_of(T, n_requests, ratio, false), longest) ? split_bytes(D) : 0;
+  // The most that any of up to T tokens is split with.  Tiles of 128 columns are cut if there are no more than kMaxTiles,
+  // and the more there are, the sooner they are taken; tiles of 16 are fewest for a single token, or one of each request.
+  const size_t B = (size_t)n_requests, columns = B <= kMaxTiles ? (kMaxTiles + 1 - B) * kWideCols - 1 : 0;
+  const size_t few = columns / ratio < T ? columns / ratio : T;
+  if (few > 0 && cut(tiles_of(few, n_requests, ratio, true, kWideCols), longest) &&
+      wide_for(few, n_requests, n_heads, ratio, D, longest, true))
+    return split_bytes(D, kWideCols);
+  const bool rows = cut(tiles_of(1, n_requests, ratio, true), longest) || cut(tiles_of(B, n_requests, ratio, false), longest);
+  return rows ? split_bytes(D) : 0;
 }
 
 extern "C" int q8_kv4_attend(const void* q_dev, int type, size_t T, int n_heads, int ratio, int D, size_t q_stride,

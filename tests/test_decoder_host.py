@@ -150,6 +150,19 @@ def test_attention_refuses_more_tiles_than_a_launch_takes():
         assert _attend(T=T, n=T, H=H, ratio=ratio, qs=1 << 20, os_=1 << 20) == EUNSUPPORTED
 
 
+def test_workspace_for_many_tokens_serves_fewer():
+    """A program holds one workspace, made for its largest step: more tokens never ask for less."""
+    size = L.q8_kv4_attend_workspace_bytes
+    tokens = sorted({max(1, (1 << e) + d) for e in range(18) for d in (-1, 0, 1)})
+    for n in (1, 3, 64, 200, 255, 256, 257, 1000):
+        for H, ratio, D in ((8, 4, 128), (1, 1, 64), (16, 8, 256), (2, 40, 96), (4, 17, 32)):
+            for longest in (64, 512, 513, 8192, 131072):
+                sizes = [size(T, n, H, ratio, D, longest) for T in tokens]
+                assert sizes == sorted(sizes), (n, H, ratio, D, longest)
+    assert size(8192, 1, 8, 4, 128, 32768) == size(512, 1, 8, 4, 128, 32768) > size(1, 1, 8, 4, 128, 32768) > 0
+    assert size(8192, 256, 8, 4, 128, 8192) >= size(1, 256, 8, 4, 128, 8192) > 0 == size(8192, 257, 8, 4, 128, 8192)
+
+
 def test_binding_refuses_what_it_cannot_pass_on():
     x = torch.zeros(4, 32)
     for call in (lambda: B.quantize_rows(x), lambda: B.linear_pack(x), lambda: B.kv4_read(x, x),
