@@ -296,7 +296,7 @@ PyObject* dequantize(PyObject*, PyObject* const* args, Py_ssize_t n) {
 struct Strided {
   void* p = nullptr;
   long size[4] = {0, 0, 0, 0}, stride[4] = {0, 0, 0, 0}, n = 0;
-  int type = -1;                       // Q8_* of real values
+  int type = -1, dims = 0;             // Q8_* of real values
 };
 struct TensorArgs : Args {
   explicit TensorArgs(PyObject* const* args) : Args{args} {}
@@ -332,6 +332,7 @@ struct TensorArgs : Args {
         run *= t.size(d);
       }
       s.n = t.numel();
+      s.dims = (int)t.dim();
       s.p = t.mutable_data_ptr();
     } catch (...) {            // (none may leave through the interpreter's frames)
       refuse(i, "expected a device tensor with storage");
@@ -381,7 +382,9 @@ struct Product {
         bias(g.get(i + 2, at::kFloat, -1, -1, true)), y(g.get(i + 3, at::ScalarType::Undefined, 2, 1)) {
     if (!g.ok) return;
     const size_t bytes = ((decltype(&q8_linear_packed_bytes))g_fn[kPackedBytes])((int)q_w.n, (int)K);
-    g.check(q_w.n < 0x7fffffff && (size_t)w.n >= bytes, i, "weights packed for other sizes");
+    // (as linear_pack leaves them, [blocks of 16 outputs][blocks of 64 values][bytes], or any memory that holds as much)
+    const bool blocks = w.dims != 3 || (w.size[0] == (q_w.n + 15) / 16 && w.size[1] == (K + 63) / 64);
+    g.check(q_w.n < 0x7fffffff && blocks && (size_t)w.n >= bytes, i, "weights packed for other sizes");
     g.check(!bias.p || bias.n == q_w.n, i + 2, "one bias for each output");
     g.check(y.size[0] == M && y.size[1] == q_w.n, i + 3, "shape");
   }

@@ -272,6 +272,24 @@ def test_linear_of_nothing(B):
     assert B.linear(torch.zeros(3, 40, device="cuda"), none, q_w[:0]).shape == (3, 0)
 
 
+def test_linear_refuses_weights_packed_for_other_sizes(B):
+    """Also such as are as many bytes or more: 128 outputs of 64 values are none for 64 of 128."""
+    packed = B.linear_pack(torch.ones(128, 64, dtype=torch.int8, device="cuda"))
+    assert packed.numel() == B.lib.q8_linear_packed_bytes(128, 64)
+    for N, K in ((64, 128), (64, 64), (128, 65), (129, 64), (112, 64), (32, 256)):
+        x, q_w = torch.ones(3, K, device="cuda"), torch.ones(N, device="cuda")
+        z, q_x = B.quantize_rows(x)
+        with pytest.raises(AssertionError):
+            B.linear(x, packed, q_w)
+        with pytest.raises(AssertionError):
+            B.linear_int8(z, q_x, packed, q_w)
+    for N, K in ((128, 64), (113, 64), (128, 1)):
+        B.linear(torch.ones(3, K, device="cuda"), packed, torch.ones(N, device="cuda"))
+    # memory without a shape is taken as what it is said to hold
+    assert torch.equal(B.linear(torch.ones(3, 64, device="cuda"), packed.flatten(), torch.ones(128, device="cuda")),
+                       B.linear(torch.ones(3, 64, device="cuda"), packed, torch.ones(128, device="cuda")))
+
+
 # ------------------------------------------------------------------------------ block tables
 def _run_tables(B, lengths, added, page, n_free, width, n_slots, pad=0, seed=0):
     rng = _rng(len(lengths), page, n_free, seed)
