@@ -665,8 +665,7 @@ def quantize_rows(x, out=None, factors=None):
 def linear_pack(z_w):
     """int8 weights [N, K] -> the layout that the product reads, [N in blocks of 16, K in blocks of 64, 1024]."""
     N, K = z_w.shape
-    nbytes = lib.q8_linear_packed_bytes(N, K)
-    if nbytes == 0 and N > 0:
+    if max(N, K) > 0x7fffffff or (N > 0 and lib.q8_linear_packed_bytes(N, K) == 0):      # (ctypes would cut them to an int)
         raise Q8Error(-2)
     packed = torch.empty((-(-N // 16), -(-K // 64), 1024), dtype=torch.int8, device=z_w.device)
     _check(lib.q8_linear_pack(_ptr(z_w, torch.int8), N, K, _ptr(packed), _stream()))

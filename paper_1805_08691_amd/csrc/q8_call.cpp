@@ -328,6 +328,7 @@ struct TensorArgs : Args {
       long run = 1;
       for (int d = (int)t.dim() - 1; d >= 0; --d) {
         if (d < 4) s.size[d] = t.size(d), s.stride[d] = t.stride(d);
+        if (d > 0 && t.size(d) > 0x7fffffff) refuse(i, "more than an int counts");       // (the first: as the call says)
         if (d >= t.dim() - dense && t.size(d) > 1 && t.stride(d) != run) refuse(i, "expected dense rows");
         run *= t.size(d);
       }
@@ -450,7 +451,7 @@ struct Cache {
   Strided c;
   int heads, page, D;
   Cache(TensorArgs& g, int i) : c(g.get(i, at::kByte, 4, -1)) {
-    g.check(c.size[3] % 18 == 0, i, "the cache's shape");
+    g.check(c.size[3] % 18 == 0 && c.size[2] <= 0x7ffffff, i, "the cache's shape");
     heads = (int)c.size[1], page = (int)(c.size[2] * 16), D = (int)(c.size[3] / 18);
   }
 };

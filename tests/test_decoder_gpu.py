@@ -290,6 +290,19 @@ def test_linear_refuses_weights_packed_for_other_sizes(B):
                        B.linear(torch.ones(3, 64, device="cuda"), packed, torch.ones(128, device="cuda")))
 
 
+def test_rows_of_more_values_than_an_int_counts_are_refused(B):
+    """2^32 + 64 values a row are none of 64."""
+    x = torch.empty((1, (1 << 32) + 64), dtype=torch.float16, device="cuda")
+    packed, q_w = B.linear_pack(torch.ones(16, 64, dtype=torch.int8, device="cuda")), torch.ones(16, device="cuda")
+    z, q_x = torch.zeros((1, (1 << 32) + 64), dtype=torch.int8, device="cuda"), torch.ones(1, device="cuda")
+    for call in (lambda: B.linear(x, packed.flatten(), q_w, workspace=torch.empty(4096, dtype=torch.uint8, device="cuda")),
+                 lambda: B.quantize_rows(x, out=z, factors=q_x), lambda: B.linear_int8(z, q_x, packed.flatten(), q_w)):
+        with pytest.raises(AssertionError):
+            call()
+    with pytest.raises(B.Q8Error):
+        B.linear_pack(torch.empty(((1 << 32) + 16, 1), dtype=torch.int8, device="cuda"))
+
+
 # ------------------------------------------------------------------------------ block tables
 def _run_tables(B, lengths, added, page, n_free, width, n_slots, pad=0, seed=0):
     rng = _rng(len(lengths), page, n_free, seed)
