@@ -717,9 +717,9 @@ PATHS = {"rows": ([300, 200, 70, 1, 513], [1] * 5, 4, 8, 64, 0), "rows, cut": ([
          "prompts": ([330, 200, 129], [150, 200, 100], 16, 8, 32, 0), "prompts, cut": ([2300, 700], [64, 130], 4, 8, 32, 140000)}
 
 
-def _path(B, rng, path, kind, D, spread, value_size=None, key_size=1.0, window=0):
+def _path(B, rng, path, kind, D, spread, value_size=None, key_size=1.0, window=0, sign=1):
     """Attention on that path over scores that spread by `spread`, values of `value_size(request, tokens)` and keys of
-    `key_size`; -> (outputs, expected ones)."""
+    `key_size`; -> (outputs, expected ones, a function that gives the expected ones with other arguments)."""
     lengths, added, H, ratio, page, longest = PATHS[path]
 
     def kv(b, n):
@@ -736,10 +736,13 @@ def _path(B, rng, path, kind, D, spread, value_size=None, key_size=1.0, window=0
         table = torch.nn.functional.pad(table, (0, max(0, -(-longest // page) - table.shape[1])), value=-1)
         ws = B.kv4_attend_workspace(q, cache, len(lengths), longest)
         assert ws.numel()
-    scale = D ** -0.5 / key_size
+    scale = sign * D ** -0.5 / key_size
     got = B.kv4_attend(q.cuda(), cache, table, lens, first if "prompts" in path else None, scale, window=window, workspace=ws)
-    want = P.attend_rows(q.double().numpy(), keys, values, lengths, starts, scale, window)
-    return got.double().cpu().numpy(), want
+
+    def expected(scale=scale, values=values, window=window):
+        return P.attend_rows(q.double().numpy(), keys, values, lengths, starts, scale, window)
+
+    return got.double().cpu().numpy(), expected(), lambda **kw: expected(**{**kw, "scale": scale * kw.get("scale", 1.0)}), values
 
 
 def _close(got, want, kind, path, spread):
@@ -752,7 +755,7 @@ def _close(got, want, kind, path, spread):
 def test_attention_over_values_of_any_size(B, path, kind):
     """From the largest that the cache holds to such as have factors that are subnormal in binary16."""
     for i, size in enumerate((5000.0, 0.05, 1e-2, 1e-4, 1e-6)):
-        got, want = _path(B, _rng(i, 71), path, kind, 64, 2.0, lambda b, n: size)
+        got, want, *_ = _path(B, _rng(i, 71), path, kind, 64, 2.0, lambda b, n: size)
         _close(got, want, kind, path, 2.0)
 
 
@@ -762,12 +765,57 @@ def test_attention_over_values_of_different_sizes(B, path, kind):
     """A context whose first tokens have tiny values and whose later ones large ones, and the other way round; and groups of
     channels of different size, each held to its own norm."""
     for first, behind in ((1e-5, 1.0), (300.0, 1e-2)):
-        got, want = _path(B, _rng(72), path, kind, 96, 2.0, lambda b, n: np.where(np.arange(n) < 64, first, behind)[:, None, None])
+        got, want, *_ = _path(B, _rng(72), path, kind, 96, 2.0, lambda b, n: np.where(np.arange(n) < 64, first, behind)[:, None, None])
         _close(got, want, kind, path, 2.0)
     sizes = np.repeat([1.0, 1e-3, 30.0], 32)
-    got, want = _path(B, _rng(73), path, kind, 96, 2.0, lambda b, n: sizes)
+    got, want, *_ = _path(B, _rng(73), path, kind, 96, 2.0, lambda b, n: sizes)
     for g in range(3):
         _close(got[..., 32 * g:32 * g + 32], want[..., 32 * g:32 * g + 32], kind, path, 2.0)
+
+
+def _within(got, want, kind, path, spread, window=0):
+    """Whether the outputs, and where scores are not so far apart that a row is one key's value, those of each row and of
+    each head, are as near as roundings leave them; of rows that see 16 keys or more."""
+    lengths, added = PATHS[path][:2]
+    seen = np.concatenate([np.minimum(np.arange(n - a, n) + 1, window or n) for n, a in zip(lengths, added)])
+    got, want = got[seen >= 16], want[seen >= 16]
+    parts = [(got, want)]
+    if spread <= 2.0:
+        parts += list(zip(got, want)) + list(zip(got.swapaxes(0, 1), want.swapaxes(0, 1)))
+    return all(np.linalg.norm(g - w) <= P.attend_norm(w, TYPES[kind], "prompts" in path, spread) for g, w in parts)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("path", sorted(PATHS))
+@pytest.mark.parametrize("D", range(32, 257, 32))
+def test_attention_is_as_near_as_roundings_leave_it(B, D, path, kind):
+    """... and nothing else is: neither zeros, nor a scale that is 2 % off, nor a context whose last value is missing."""
+    got, want, other, values = _path(B, _rng(D, 81), path, kind, D, 2.0)
+    assert _within(got, want, kind, path, 2.0)
+    short = [np.concatenate([v[:-1], 0 * v[-1:]]) for v in values]
+    for wrong in (0 * want, other(scale=1.02), other(values=short)):
+        assert not _within(wrong, want, kind, path, 2.0)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("path", sorted(PATHS))
+@pytest.mark.parametrize("spread,window,sign", [(0.0, 0, 1), (1.0, 0, -1), (8.0, 0, 1), (32.0, 0, -1), (2.0, 17, 1), (2.0, 100, -1)])
+def test_attention_is_as_near_over_other_scores(B, spread, window, sign, path, kind):
+    """Equal weights, scores far apart, windows, negative scales."""
+    got, want, other, _ = _path(B, _rng(int(spread), window, 82), path, kind, 64, spread, window=window, sign=sign)
+    assert _within(got, want, kind, path, spread, window)
+    if window:
+        assert not _within(other(window=window + 1), want, kind, path, spread, window)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("path", sorted(PATHS))
+def test_attention_over_keys_of_any_size(B, path, kind):
+    """From the largest to such as have factors that are subnormal in binary16, at scales that make up for them."""
+    for i, size in enumerate((5000.0, 1e-2, 1e-4, 1e-6)):
+        got, want, other, _ = _path(B, _rng(i, 83), path, kind, 64, 2.0, key_size=size)
+        assert _within(got, want, kind, path, 2.0), size
+        assert not _within(other(scale=1.02), want, kind, path, 2.0), size
 
 
 @pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 20, 2 ** 30, 65])
