@@ -147,7 +147,8 @@ __global__ __launch_bounds__(THREADS) void page_tables_kernel(const PageParams p
   }
 }
 
-// More requests: one block walks over them, 1024 at a time, with the running sums of pages and of tokens.
+// More requests: one block walks over them, 1024 at a time, with the running sums of pages and of tokens.  Bound by that one
+// block's dependent trips to memory (5000 requests 25 us, 9000 37).
 __global__ __launch_bounds__(1024) void page_rows_kernel(const PageParams p) {
   __shared__ long tok_sum[16], page_sum[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -240,8 +241,8 @@ struct Kv4Params {
 // channels each, so that a wavefront reads and writes whole rows of the tokens' values.  Key codes are a word a lane as
 // they lie in the cache.  Value codes lie by channel: they pass through LDS, where 16 tokens make rows of 16 bytes, and
 // leave as words where four tokens' slots are neighbours (bytes elsewhere).  The floor is memory; what bounds it is
-// vector instructions, so places are worked out once for a block.  16001 tokens of 8 heads of 128 channels in bf16: in 23 us
-// (84 MB, vector instructions in 80 % of the cycles), out 22; 64 tokens 4 each, a launch.
+// vector instructions, so places are worked out once for a block.  16001 tokens of 8 heads of 128 channels in bf16, 84 MB: in
+// 23 us (vector instructions in 95 % of the cycles), out 22 (80 %); 64 tokens 4 each, a launch.
 constexpr int kTok = 16, kGroups = 4;
 
 // The block's tokens, in LDS.

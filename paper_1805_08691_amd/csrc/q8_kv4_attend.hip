@@ -7,15 +7,18 @@
 // wavefront multiplies 64 keys by them per step on v_mfma_f32_16x16x32_f16:
 //   S^T[key][column]     = K Q^T      four tiles of 16 keys, G products each
 //   O^T[channel][column] = V^T P^T    2 G tiles of 16 channels, two products each
-// Four codes become binary16 in five instructions (1024 + u is its own bit pattern; u and 16 u are taken out of the
-// bytes as they lie), times their factor exact to half a unit of binary16.  Which 16 keys a tile of S takes is chosen
-// so that a lane's 16 probabilities belong to the 16 tokens whose value codes it loads: nothing is exchanged
-// between lanes but the maximum.
+// Codes are multiplied as they are: four become binary16 in five instructions (1024 + u is its own bit pattern; u and 16 u
+// are taken out of the bytes as they lie), and what they have too much is taken from the keys by a second product, from the
+// values before theirs.  A key's factor goes into the fp32 sum of its group, a value's into its token's probability, whose
+// product, formed in fp32, is rounded to binary16 (by 2^-11 of it at most).  Outputs are off by, in parts of their norm, where
+// scores spread by 1 to 32: fp16 1.8 to 2.7e-4 (their own rounding alone: 2.1e-4), bf16 1.5 to 1.8e-3 (alone: the same).
+// Which 16 keys a tile of S takes is chosen so that a lane's 16 probabilities belong to the 16 tokens whose value codes it
+// loads: nothing is exchanged between lanes but the maximum.
 // The key axis is split over workgroups where columns are few; the last of them to finish adds the parts, in their order.
-// Bound by memory while it loops (48 requests of up to 16384 tokens, 64 query heads on 8 of 128 channels: 415 MB in 102 us,
+// Bound by memory while it loops (48 requests of up to 16384 tokens, 64 query heads on 8 of 128 channels: 415 MB in 100 us,
 // 70 to 80 of them in the loop at 5 to 5.5 TB/s; 2000 cycles of vector instructions a step beside 1000 of the matrix
 // cores) and by dependent trips to memory at both ends (5 us in front of the first keys' products of a split, 4 to 7 behind:
-// one request of 131071 tokens, 151 MB, 41 us; 5 short ones 6.7).  One step in LDS a wavefront: with three workgroups a
+// one request of 131071 tokens, 151 MB, 43 us; 5 short ones 6.7).  One step in LDS a wavefront: with three workgroups a
 // compute unit that is 110 KB on their way, and a second would leave room for fewer of them.
 #include "q8_kv4_attend.h"
 #pragma clang fp contract(fast)
@@ -248,7 +251,8 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int tile = 2 * h + (e >> 1), i = e & 1;
-          // (in fp32, rounded once: a probability alone is 2^lift at most, beyond binary16 where the factors are small)
+          // (in fp32, rounded once: a probability alone is up to 2^lift, beyond binary16 where the factors are small.  Rounded
+          // first and multiplied in binary16, bf16 took 41.6 us for one request of 131071 tokens instead of 42.9)
           pr[2 * e] = (_Float16)__builtin_fmaf(x[tile][i], (float)vf[2 * tile + i][0], 0.0f);
           pr[2 * e + 1] = (_Float16)__builtin_fmaf(x[tile][i + 2], (float)vf[2 * tile + i][1], 0.0f);
         }

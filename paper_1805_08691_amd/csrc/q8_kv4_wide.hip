@@ -7,12 +7,15 @@
 // Bound by vector instructions (unpacking 1.6 a code of a workgroup's keys, the softmax 4.5 a score) beside the matrix
 // instructions, of which a third of the cycles is full, so three workgroups share a compute unit and two barriers a step
 // are hidden behind each other's.
-// bf16 outputs: a key is its code times its factor, and a query has the scale in it, both rounded to binary16 (2^-12 of
-// each, 6e-4 to 15e-4 of an output by how far scores are apart, under bf16's 1.6e-3); scores come out of the products
-// relative to the running maximum, which they begin with.  fp16 outputs show that: there codes are multiplied, and factors
-// and scale go into the sums.  A maximum that grows by less than 2^8 is left: probabilities are up to 256, and sums are
-// not rescaled.  The sum is that of the probabilities as the values meet them, rounded to binary16.
-// Pieces of 2048 tokens of 3 requests over 8192 keys, 32 query heads of 128 channels: 395 us, 910 TFLOP/s.
+// bf16 outputs: a key is its code times its factor, and a query has the scale in it, both rounded to binary16 (2^-11 of
+// each at most); scores come out of the products relative to the running maximum, which they begin with.  fp16 outputs show
+// that: there codes of keys are multiplied, and factors and scale go into the sums.  For both a value is its code times its
+// factor, and a probability what the exponential gives, rounded to binary16; the softmax's sum is that of the probabilities so
+// rounded, as the values meet them.  A maximum that grows by less than 2^8 is left: probabilities are up to 256, and sums are
+// not rescaled.  Outputs are off by, in parts of their norm: fp16 2.4 to 3.4e-4 (their own rounding alone: 2.1e-4); bf16
+// 1.7e-3 for scores that spread by 1 or 2, 1.9e-3 by 8, 2.1e-3 by 16, 2.3 to 2.6e-3 by 32 (alone: 1.66e-3).
+// Pieces of 2048 tokens of 3 requests over 8192 keys, 32 query heads of 128 channels: 395 us, 910 TFLOP/s; in a window of
+// 1024 tokens 110 us; fp16 487 us.
 #include "q8_kv4_attend.h"
 
 namespace {

@@ -6,8 +6,9 @@
 // them; rows of activations are 64 bytes in LDS with their 16-byte chunks swapped (swz) so that neither meets a
 // bank twice.  Rows of activations are the matrix instruction's rows: a lane then holds 16 rows of one channel, 32 lanes store
 // neighbours (the other way round a store touched 64 lines: 4096 x 4096 x 4096 77 us instead of 65).
-// Large products are bound by power: 8192 x 8192 x 8192 takes 465 us, 2.36 POP/s, with the matrix cores busy 65 % of the cycles
-// at 1.7 GHz.  Small ones are bound by the steps of the one or two tiles that a compute unit has: 0.25 us for 128 bytes of K
+// Large products: 8192 x 8192 x 8192 takes 465 us, 2.36 POP/s, with the matrix cores busy 64 % of the cycles and wavefronts
+// waiting in 35 % of theirs (two to a SIMD, two steps in flight), at the 1.76 GHz that power leaves; zeros go 1.2 times as fast.
+// Small ones are bound by the steps of the one or two tiles that a compute unit has: 0.25 us for 128 bytes of K
 // of a 64 x 64 tile, whose 16 KB take half of that out of L2 (777 x 1000 x 2048: 7.7 us).
 #include "q8_linear.h"
 #include <type_traits>
