@@ -85,6 +85,19 @@ def test_rows_to_codes_of_very_many_rows(B):
         assert np.array_equal(z[rows].cpu().numpy(), want_z) and np.array_equal(q[rows].cpu().numpy(), want_q)
 
 
+def test_rows_to_codes_of_very_many_longer_rows(B):
+    """The same where a block takes a row."""
+    M, K = (1 << 24) + 7, 1025
+    x = torch.empty((M, K), device="cuda", dtype=torch.bfloat16).normal_()
+    q = torch.zeros(M, device="cuda")
+    z, _ = B.quantize_rows(x, factors=q)
+    assert bool((q > 0).all())
+    for a in (0, (1 << 24) - 60, M - 64):
+        rows = slice(a, a + 64)
+        want_z, want_q = P.quantize_rows(x[rows].cpu())
+        assert np.array_equal(z[rows].cpu().numpy(), want_z) and np.array_equal(q[rows].cpu().numpy(), want_q)
+
+
 # ------------------------------------------------------------------------------ the product
 def _weights(rng, N, K):
     z_w = rng.integers(-128, 128, (N, K), dtype=np.int8)
