@@ -43,8 +43,6 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
                                                                          V* __restrict__ out) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int D = 32 * G, CT = 2 * G;                 // channels, tiles of 16 of them
-  constexpr int PITCH = D + 4;                          // of a column in LDS: eight lanes' quads meet different banks
-  constexpr size_t kPartWords = kCols * (D + 2) / 2;    // of a part: sums [16][D], then a maximum and a sum for each column
   using St = Stage<G>;
   extern __shared__ __attribute__((aligned(16))) char shared[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -61,7 +59,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
   const int col = t.first + r;
   const bool given = col < t.cols;
   const int tok = min(col, t.cols - 1) / p.ratio, qh = min(col, t.cols - 1) % p.ratio;
-  const int pos = given ? t.len - t.n + tok : -1;       // (no key is at or before -1)
+  const int pos = given ? row_position(p, t, tok) : -1;  // (no key is at or before -1)
   const int from = p.window > 0 ? pos - p.window : -1;  // keys behind this one
   float v[G][8];
   {
@@ -130,7 +128,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
       for (int e = 0; e < 8; ++e) qf[g][e] = (_Float16)(v[g][kKeyOrder[e]] * (e < 4 ? down : down * 0.0625f));
   }
   // steps whose every key is seen by every column: behind `clear0`, up to `clear1`
-  const int pos0 = t.len - t.n + t.first / p.ratio, pos1 = t.len - t.n + (min(t.first + kCols, t.cols) - 1) / p.ratio;
+  const int pos0 = row_position(p, t, t.first / p.ratio), pos1 = row_position(p, t, (min(t.first + kCols, t.cols) - 1) / p.ratio);
   const int clear0 = p.window > 0 ? pos1 - p.window : -1, clear1 = pos0;
 
   f4 o[CT];
@@ -270,146 +268,14 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_attend_kernel(const A
   }
 #pragma unroll
   for (int g = 0; g < G; ++g) o[2 * g + 1] *= 0.0625f;
-  sum += __shfl_xor(sum, 16, 64);
-  sum += __shfl_xor(sum, 32, 64);
-  __syncthreads();                                      // the stages have been read: the columns take their place
-
-  // ---- the four wavefronts' columns together
-  float* const cols = reinterpret_cast<float*>(shared);
-  float* const refs = cols + kWaves * kCols * PITCH;
-  float* const sums = refs + kWaves * kCols;
-  if (j == 0) {
-    refs[wave * kCols + r] = ref;
-    sums[wave * kCols + r] = sum;
-  }
-  __syncthreads();
-  float all = -__builtin_inff();
-#pragma unroll
-  for (int v = 0; v < kWaves; ++v) all = fmaxf(all, refs[v * kCols + r]);
-  const float mine = ref == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ref - all);
-  float* const to = cols + (wave * kCols + r) * PITCH + 4 * j;
-#pragma unroll
-  for (int c = 0; c < CT; ++c) *reinterpret_cast<f4*>(to + 16 * c) = o[c] * mine;
-  __syncthreads();
-  const bool whole = a.parts == 1;
-  const int valid = min(kCols, t.cols - t.first);
-  for (int i = tid; i < valid * D / 4; i += 256) {
-    const int c = i / (D / 4), d = i % (D / 4) * 4;
-    f4 v = {0, 0, 0, 0};
-    float m = -__builtin_inff(), l = 0.0f;
-#pragma unroll
-    for (int u = 0; u < kWaves; ++u) m = fmaxf(m, refs[u * kCols + c]);
-#pragma unroll
-    for (int u = 0; u < kWaves; ++u) {
-      v += *reinterpret_cast<const f4*>(cols + (u * kCols + c) * PITCH + d);
-      const float ru = refs[u * kCols + c];
-      l += ru == -__builtin_inff() ? 0.0f : sums[u * kCols + c] * __builtin_amdgcn_exp2f(ru - m);
-    }
-    if (whole) {
-      const int oc = t.first + c;
-      const float inv = l > 0.0f ? 1.0f / l : l;        // (no key: zeros; no number: none)
-      const float y[4] = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
-      store_values<4, false>(out + (size_t)(t.row + oc / p.ratio) * p.o_stride +
-                                 ((size_t)head * p.ratio + oc % p.ratio) * p.o_head + d, y);
-    } else {
-      // past this XCD's cache, for the workgroup that adds the parts
-      word* part = reinterpret_cast<word*>(p.parts) + ((size_t)(a.slot + a.part) * p.H + head) * kPartWords;
-      put(part + (c * D + d) / 2, v[0], v[1]);
-      put(part + (c * D + d) / 2 + 1, v[2], v[3]);
-      if (d == 0) put(part + kCols * D / 2 + c, m, l);
-    }
-  }
-  if (whole) return;
-
-  // ---- the parts of the tile and head: the workgroup that finishes last adds them, whichever it is in their order
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this wavefront's words have arrived
-  __syncthreads();                                      // and the others'; LDS is free
-  int* const flag = reinterpret_cast<int*>(shared);
-  int* const counter = p.counters + a.rank * p.H + head;
-  if (tid == 0) flag[0] = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
-  __syncthreads();
-  if (flag[0] != a.parts - 1) return;
-  __syncthreads();
-  if (tid == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
-  const word* const parts = reinterpret_cast<const word*>(p.parts) + ((size_t)a.slot * p.H + head) * kPartWords;
-  const size_t stride = (size_t)p.H * kPartWords;
-  const int n = a.parts;
-  f4* const quads = reinterpret_cast<f4*>(shared);      // 256
-  float* const weights = reinterpret_cast<float*>(quads + 256);               // [n][16], then the columns' sums
-  float* const totals = weights + (size_t)kTarget * kCols;
-  for (int c = wave; c < valid; c += kWaves) {
-    float most = -__builtin_inff(), l = 0.0f;
-    f2 rs[kTarget / 64];
-#pragma unroll
-    for (int u = 0; u < kTarget / 64; ++u) {
-      rs[u] = f2{-__builtin_inff(), 0.0f};
-      if (u * 64 < n && u * 64 + lane < n) rs[u] = get(parts + (u * 64 + lane) * stride + kCols * D / 2 + c);
-    }
-#pragma unroll
-    for (int u = 0; u < kTarget / 64; ++u) most = fmaxf(most, rs[u][0]);
-    for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, 64));
-#pragma unroll
-    for (int u = 0; u < kTarget / 64; ++u)
-      if (u * 64 + lane < n) {
-        const float weight = rs[u][0] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(rs[u][0] - most);
-        weights[(u * 64 + lane) * kCols + c] = weight;
-        l += weight * rs[u][1];
-      }
-    for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off, 64);
-    if (lane == 0) totals[c] = l;
-  }
-  __syncthreads();
-  // a thread takes four channels of a column, and where these are few, every so manieth part
-  const int items = valid * (D / 4), groups = items >= 256 ? 1 : 256 / items, each = groups > 1 ? items : 256;
-  for (int i0 = 0; i0 < items; i0 += 256) {
-    const int group = groups > 1 ? tid / each : 0, i = i0 + (groups > 1 ? tid - group * each : tid);
-    const int c = i / (D / 4), d = i % (D / 4) * 4;
-    f4 v = {0, 0, 0, 0};
-    // (as many parts on their way as there are, rounded up: the last is read again in the place of absent ones)
-    auto add = [&](auto batch_c) __attribute__((always_inline)) {
-      constexpr int kBatch = decltype(batch_c)::value;
-      const word* from = parts + (c * D + d) / 2;
-      for (int s0 = group; s0 < n; s0 += groups * kBatch) {
-        f2 x[kBatch], y[kBatch];
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-          const int s = min(s0 + u * groups, n - 1);
-          x[u] = get(from + s * stride), y[u] = get(from + s * stride + 1);
-        }
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u)
-          if (s0 + u * groups < n) v += weights[(s0 + u * groups) * kCols + c] * f4{x[u][0], x[u][1], y[u][0], y[u][1]};
-      }
-    };
-    if (i < items && group < groups) {
-      if (n <= 2 * groups) add(std::integral_constant<int, 2>{});
-      else if (n <= 4 * groups) add(std::integral_constant<int, 4>{});
-      else if (n <= 8 * groups) add(std::integral_constant<int, 8>{});
-      else add(std::integral_constant<int, 16>{});
-    }
-    if (groups > 1) {
-      quads[tid] = v;
-      __syncthreads();
-      if (group == 0)
-        for (int g = 1; g < groups; ++g) v += quads[g * each + tid];
-    }
-    if (group == 0 && i < items) {
-      const int oc = t.first + c;
-      const float l = totals[c], inv = l > 0.0f ? 1.0f / l : l;
-      const float y[4] = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
-      store_values<4, false>(out + (size_t)(t.row + oc / p.ratio) * p.o_stride +
-                                 ((size_t)head * p.ratio + oc % p.ratio) * p.o_head + d, y);
-    }
-  }
+  join_columns<D>(p, a, t, shared, out, o, ref, sum);
 #endif
 }
 
 template <int G, typename V>
 int launch(const AttendParams& p, const V* q, V* out, hipStream_t stream) {
-  const size_t stages = (size_t)kWaves * Stage<G>::SIZE, columns = (size_t)kWaves * kCols * (32 * G + 6) * 4;
-  const size_t adding = 256 * sizeof(f4) + (kTarget + 1) * kCols * sizeof(float);
-  size_t lds = stages > columns ? stages : columns;
-  if (p.parts && lds < adding) lds = adding;
+  const size_t stages = (size_t)kWaves * Stage<G>::SIZE, joining = join_bytes(32 * G, p.parts != nullptr);
+  const size_t lds = stages > joining ? stages : joining;
   if (lds > 65536) {
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_attend_kernel<G, V>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -435,17 +301,6 @@ int launch_any(int G, const AttendParams& p, const V* q, V* out, hipStream_t str
   return Q8_EUNSUPPORTED;
 }
 
-// Tiles of `cols` columns that T rows of B requests can have (find_tile).
-size_t tiles_of(size_t T, int B, int ratio, bool starts, int cols = kCols) {
-  return starts ? T * ratio / cols + B : (size_t)B * ((ratio + cols - 1) / cols);
-}
-// Whether keys of at most `longest` are cut: where tiles are so few that a part of the longest could keep compute units
-// waiting, and two parts of 2 kShortest steps could be made.  (5 requests of up to 300 tokens: 7.3 us, and cut 10.4.)
-bool cut(size_t tiles, size_t longest) { return tiles <= kMaxTiles && longest > (size_t)2 * kShortest * kStep; }
-// Workspace: the counters (in one place for both kernels), then the parts.
-constexpr size_t kCounterBytes = (kTarget + 15) / 16 * 16 * sizeof(int);
-size_t split_bytes(int D, int cols = kCols) { return kCounterBytes + (size_t)2 * kTarget * cols * (D + 2) * 4; }
-
 // Whether tiles of 128 columns, which unpack a key once for all of them, are taken for new tokens in runs of several: where
 // requests have that many columns and the tiles are a workgroup for every compute unit, or can be cut, and parts of them
 // are long enough for what adding them costs.  (3 pieces of 2048 tokens over 8192 keys, 32 query heads on 4 of 128 channels:
@@ -462,16 +317,7 @@ bool wide_for(size_t T, int B, int H, int ratio, int D, size_t longest, bool cut
 
 extern "C" size_t q8_kv4_attend_workspace_bytes(size_t T, int n_requests, int n_heads, int ratio, int D,
                                                 size_t longest) {
-  if (n_requests < 1 || n_heads < 1 || ratio < 1 || D < 32 || D > kMaxHead || T > 0x7fffffffu) return 0;
-  // The most that any of up to T tokens is split with.  Tiles of 128 columns are cut if there are no more than kMaxTiles,
-  // and the more there are, the sooner they are taken; tiles of 16 are fewest for a single token, or one of each request.
-  const size_t B = (size_t)n_requests, columns = B <= kMaxTiles ? (kMaxTiles + 1 - B) * kWideCols - 1 : 0;
-  const size_t few = columns / ratio < T ? columns / ratio : T;
-  if (few > 0 && cut(tiles_of(few, n_requests, ratio, true, kWideCols), longest) &&
-      wide_for(few, n_requests, n_heads, ratio, D, longest, true))
-    return split_bytes(D, kWideCols);
-  const bool rows = cut(tiles_of(1, n_requests, ratio, true), longest) || cut(tiles_of(B, n_requests, ratio, false), longest);
-  return rows ? split_bytes(D) : 0;
+  return attend_workspace_bytes(T, n_requests, n_heads, ratio, D, longest, wide_for);
 }
 
 extern "C" int q8_kv4_attend(const void* q_dev, int type, size_t T, int n_heads, int ratio, int D, size_t q_stride,
@@ -480,39 +326,12 @@ extern "C" int q8_kv4_attend(const void* q_dev, int type, size_t T, int n_heads,
                              const int32_t* starts_dev, int n_requests, float scale, int window, void* out_dev,
                              size_t o_stride, size_t o_head_stride, void* workspace, size_t workspace_bytes,
                              void* stream) {
-  Q8_REQUIRE(type_ok(type) && n_heads >= 1 && ratio >= 1 && width >= 0 && window >= 0 && n_requests >= 0, Q8_EINVAL);
-  Q8_REQUIRE(scale == scale && scale - scale == 0.0f, Q8_EINVAL);
-  Q8_REQUIRE(type != Q8_F32 && kv4_shape_ok(D, page), Q8_EUNSUPPORTED);
-  if (T == 0 || n_requests == 0) return Q8_OK;
-  Q8_REQUIRE(q_dev && out_dev && cache_dev && n_pages >= 1 && lengths_dev && (table_dev || width == 0), Q8_EINVAL);
-  Q8_REQUIRE(table_stride >= (size_t)width && (starts_dev || T == (size_t)n_requests), Q8_EINVAL);
-  Q8_REQUIRE(T == 1 || (q_stride >= (size_t)D && o_stride >= (size_t)D), Q8_EINVAL);
-  Q8_REQUIRE(n_heads * ratio == 1 || (q_head_stride >= (size_t)D && o_head_stride >= (size_t)D), Q8_EINVAL);
-  // (a table's places end far enough below 2^31 that the sixteens behind a tile's last key still have an int's numbers)
-  Q8_REQUIRE(T <= 0x7fffffffu && n_pages <= 0x7fffffffu && (size_t)width * page <= 0x7fff0000u, Q8_EUNSUPPORTED);
-  Q8_REQUIRE(q8_aligned(q_dev, 2) && q8_aligned(out_dev, 2) && q8_aligned(cache_dev, 64) && q8_aligned(table_dev, 4) &&
-                 q8_aligned(lengths_dev, 4) && q8_aligned(starts_dev, 4) && q8_aligned(workspace, 16), Q8_EALIGN);
-  const size_t wide_tiles = tiles_of(T, n_requests, ratio, true, kWideCols), longest = (size_t)width * page;
-  const bool cuts = workspace && workspace_bytes >= split_bytes(D, kWideCols) && cut(wide_tiles, longest);
-  const bool wide = starts_dev && wide_for(T, n_requests, n_heads, ratio, D, longest, cuts);
-  const size_t tiles = wide ? wide_tiles : tiles_of(T, n_requests, ratio, starts_dev != nullptr);
-  const bool split = wide ? cuts : workspace && workspace_bytes >= split_bytes(D) && cut(tiles, longest);
-  Q8_REQUIRE(tiles * n_heads + kTarget <= most_blocks(256) && T * ratio <= 0x7fffffffu, Q8_EUNSUPPORTED);
   AttendParams p{};
-  p.cache = static_cast<const uint8_t*>(cache_dev);
-  p.table = table_dev;
-  p.lengths = lengths_dev;
-  p.starts = starts_dev;
-  p.counters = split ? static_cast<int*>(workspace) : nullptr;
-  p.parts = split ? reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes) : nullptr;
-  p.q_stride = q_stride, p.q_head = q_head_stride, p.o_stride = o_stride, p.o_head = o_head_stride;
-  p.table_stride = table_stride;
-  p.n_pages = (long)n_pages;
-  p.T = (int)T, p.B = n_requests, p.H = n_heads, p.ratio = ratio, p.width = width;
-  p.shift = __builtin_ctz(page) - 4;
-  p.tiles = (int)tiles;
-  p.window = (size_t)window >= longest ? 0 : window;      // (as long as a request: none; differences of positions fit an int)
-  p.scale_log2 = scale * 1.4426950408889634f;
+  bool wide = false;
+  const int rc = attend_params(q_dev, type, T, n_heads, ratio, D, q_stride, q_head_stride, cache_dev, n_pages, page, table_dev,
+                               width, table_stride, lengths_dev, starts_dev, n_requests, scale, window, out_dev, o_stride,
+                               o_head_stride, workspace, workspace_bytes, wide_for, &p, &wide);
+  if (rc != Q8_OK || p.T == 0) return rc;
   if (wide) return kv4_attend_wide(D / 32, p, q_dev, out_dev, type, (hipStream_t)stream);
   if (type == Q8_F16)
     return launch_any(D / 32, p, static_cast<const _Float16*>(q_dev), static_cast<_Float16*>(out_dev),

@@ -22,9 +22,8 @@ namespace {
 
 using namespace q8;
 
-constexpr int kTiles = 2;                       // of 16 columns, of a wavefront
-constexpr int kWide = kWideCols;                // columns of a workgroup
-static_assert(kWide == kWaves * kTiles * kCols, "every wavefront has its own");
+[[maybe_unused]] constexpr int kTiles = kWideTiles;
+constexpr int kWide = kWideCols;
 [[maybe_unused]] constexpr float kSlack = 8.0f; // powers of two that a maximum may grow by
 
 template <int G>
@@ -94,7 +93,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
   for (int c = 0; c < kTiles; ++c) {
     const int col = t.first + (wave * kTiles + c) * kCols + r, in = min(col, t.cols - 1);
     const int tok = in / p.ratio, qh = in % p.ratio;
-    positions[c * kCols] = col < t.cols ? t.len - t.n + tok : -1;
+    positions[c * kCols] = col < t.cols ? row_position(p, t, tok) : -1;
     const V* qr = q + (size_t)(t.row + tok) * p.q_stride + ((size_t)head * p.ratio + qh) * p.q_head + 8 * j;
     float v[G][8], top = 0.0f;
 #pragma unroll
@@ -127,7 +126,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
     for (int i = 0; i < CT; ++i) o[c][i] = f4{0, 0, 0, 0};
   }
   // steps whose every key is seen by every column of the tile
-  const int pos0 = t.len - t.n + t.first / p.ratio, pos1 = t.len - t.n + (min(t.first + kWide, t.cols) - 1) / p.ratio;
+  const int pos0 = row_position(p, t, t.first / p.ratio), pos1 = row_position(p, t, (min(t.first + kWide, t.cols) - 1) / p.ratio);
   const int clear0 = p.window > 0 ? pos1 - p.window : -1, clear1 = pos0;
   constexpr _Float16 kBias = 1032.0f16, kSixteenth = 0.0625f16, kHighBias = -72.0f16;
   auto low = [&](unsigned w) { return un.low(w) - h2{kBias, kBias}; };
@@ -299,103 +298,10 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
       }
     __builtin_amdgcn_s_setprio(0);
   }
-  constexpr int D = 32 * G;
-  constexpr size_t kPartWords = (size_t)kWide * (D + 2) / 2;    // of a part: [tile][CT][2][lane], then maxima and sums
-  word* const part = reinterpret_cast<word*>(p.parts) + ((size_t)(a.slot + a.part) * p.H + head) * kPartWords;
+  bool seen[kTiles];
 #pragma unroll
-  for (int c = 0; c < kTiles; ++c) {
-    sum[c] += __shfl_xor(sum[c], 16, 64);
-    sum[c] += __shfl_xor(sum[c], 32, 64);
-    const int of = (wave * kTiles + c) * kCols + r, col = t.first + of;
-    if (col >= t.cols) continue;
-    const float l = sum[c];
-    if (a.parts == 1) {
-      const float inv = l > 0.0f ? 1.0f / l : l;                // (no key: zeros; no number: none)
-      V* const to = out + (size_t)(t.row + col / p.ratio) * p.o_stride + ((size_t)head * p.ratio + col % p.ratio) * p.o_head + 4 * j;
-#pragma unroll
-      for (int i = 0; i < CT; ++i) {
-        const float y[4] = {o[c][i][0] * inv, o[c][i][1] * inv, o[c][i][2] * inv, o[c][i][3] * inv};
-        store_values<4, false>(to + 16 * i, y);
-      }
-    } else {
-      word* const to = part + (wave * kTiles + c) * CT * 128 + lane;
-#pragma unroll
-      for (int i = 0; i < CT; ++i) {
-        put(to + 128 * i, o[c][i][0], o[c][i][1]);
-        put(to + 128 * i + 64, o[c][i][2], o[c][i][3]);
-      }
-      if (j == 0) put(part + kWide * D / 2 + of, limit[c] > -__builtin_inff() ? ref[c] : -__builtin_inff(), l);
-    }
-  }
-  if (a.parts == 1) return;
-
-  // ---- the parts of the tile and head: the workgroup that finishes last adds them, whichever it is in their order
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this wavefront's words have arrived
-  __syncthreads();                                      // and the others'; LDS is free
-  int* const flag = reinterpret_cast<int*>(shared);
-  int* const counter = p.counters + a.rank * p.H + head;
-  if (tid == 0) flag[0] = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
-  __syncthreads();
-  if (flag[0] != a.parts - 1) return;
-  __syncthreads();
-  if (tid == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
-  const word* const parts = reinterpret_cast<const word*>(p.parts) + ((size_t)a.slot * p.H + head) * kPartWords;
-  const size_t stride = (size_t)p.H * kPartWords;
-  float* const weights = reinterpret_cast<float*>(shared);      // [16][128], then the columns' sums
-  float* const totals = weights + kWideParts * kWide;
-  if (tid < kWide) {
-    f2 rs[kWideParts];
-    float most = -__builtin_inff(), l = 0.0f;
-#pragma unroll
-    for (int u = 0; u < kWideParts; ++u) {
-      rs[u] = f2{-__builtin_inff(), 0.0f};
-      if (u < a.parts && t.first + tid < t.cols) rs[u] = get(parts + u * stride + kWide * D / 2 + tid);
-    }
-#pragma unroll
-    for (int u = 0; u < kWideParts; ++u) most = fmaxf(most, rs[u][0]);
-#pragma unroll
-    for (int u = 0; u < kWideParts; ++u) {
-      const float weight = rs[u][0] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(rs[u][0] - most);
-      weights[u * kWide + tid] = weight;
-      l += weight * rs[u][1];
-    }
-    totals[tid] = l;
-  }
-  __syncthreads();
-  // a thread takes four channels of a column, as a lane had them, and several such, so that enough is on its way
-  const int valid = t.cols - t.first, groups = min((valid + kCols - 1) / kCols, kWide / kCols) * CT;     // of 64 lanes' quads
-  constexpr int kItems = 4, kBatch = 4;
-  for (int g0 = wave; g0 < groups; g0 += kWaves * kItems) {
-    f4 v[kItems];
-#pragma unroll
-    for (int k = 0; k < kItems; ++k) v[k] = f4{0, 0, 0, 0};
-    for (int s0 = 0; s0 < a.parts; s0 += kBatch) {
-      f2 x[kItems][kBatch][2];
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u)
-#pragma unroll
-        for (int k = 0; k < kItems; ++k) {
-          const word* const from = parts + min(s0 + u, a.parts - 1) * stride + min(g0 + k * kWaves, groups - 1) * 128 + lane;
-          x[k][u][0] = get(from), x[k][u][1] = get(from + 64);
-        }
-#pragma unroll
-      for (int k = 0; k < kItems; ++k)
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u)
-          if (s0 + u < a.parts)
-            v[k] += weights[(s0 + u) * kWide + min(g0 + k * kWaves, groups - 1) / CT * kCols + r] *
-                    f4{x[k][u][0][0], x[k][u][0][1], x[k][u][1][0], x[k][u][1][1]};
-    }
-#pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-      const int g = g0 + k * kWaves, of = g / CT * kCols + r, col = t.first + of;
-      if (g >= groups || col >= t.cols) continue;
-      const float l = totals[of], inv = l > 0.0f ? 1.0f / l : l;
-      const float y[4] = {v[k][0] * inv, v[k][1] * inv, v[k][2] * inv, v[k][3] * inv};
-      store_values<4, false>(out + (size_t)(t.row + col / p.ratio) * p.o_stride + ((size_t)head * p.ratio + col % p.ratio) * p.o_head +
-                                 g % CT * 16 + 4 * j, y);
-    }
-  }
+  for (int c = 0; c < kTiles; ++c) seen[c] = limit[c] > -__builtin_inff();
+  join_wide<32 * G>(p, a, t, shared, out, o, ref, sum, seen);
 #endif
 }
 
