@@ -645,6 +645,84 @@ int q8_kv4_attend(const void *q_dev, int type, size_t T, int n_heads, int ratio,
                   float scale, int window, void *out_dev, size_t o_stride,
                   size_t o_head_stride, void *workspace, size_t workspace_bytes, void *stream);
 
+/* The cache in 8 bits: uint8 [n_pages][n_heads][page / 16][32 D + 64], 64-byte aligned, D a multiple of 32 up to 256.
+ * Sixteen consecutive tokens of a head are held by Eq. Q with p = 7 at one factor for their keys and one for their values.
+ * They are, one after the other, a byte holding its code plus 128,
+ *   16 D bytes    key codes    [token / 4][chunk < D / 64][j < 4][token % 4][16 bytes]: channels 64 chunk + 16 j ..; behind
+ *                 the chunks, where D / 32 is odd, [j < 4][token % 4][8 bytes]: channels D - 32 + 8 j ..
+ *   16 D          value codes  [channel][token]
+ *   64            the keys' factor, the values' factor (fp32), and 56 bytes of the library's (any values)
+ * q8_kv8_cache_bytes: its size (0: unsupported).
+ *
+ * q8_kv8_write puts T tokens' keys and values ([T][n_heads][D], strides between tokens and between heads) into their slots.
+ * With m the largest finite magnitude of the call's tokens in a sixteen (keys and values each for themselves),
+ *   its first token is one of them   q = m * fl(1/127), and its places without a token of the call become zeros
+ *   else, at a factor q' so far      q = q' if m * fl(1/127) <= q', or max(m * fl(1/127), fl(1.25 q')), and the codes of
+ *                                    its other places become Round(z fl(q' / q))
+ * and z = Eq. Q(r, q) for the call's tokens (q = 0, where all are zeros: codes 0).  A cache begins as zeros, or each of its
+ * sixteens with its first token.  Slots of one write are distinct, in any order; one outside the cache is not written.
+ * T < 2^24 (Q8_EUNSUPPORTED).
+ *
+ * q8_kv8_read writes what slots hold (q z, rounded to `type`); a slot outside the cache reads as zeros.                  */
+size_t q8_kv8_cache_bytes(size_t n_pages, int n_heads, int page, int D);
+int q8_kv8_write(const void *k_dev, const void *v_dev, int type, size_t T, int n_heads, int D,
+                 size_t k_stride, size_t k_head_stride, size_t v_stride, size_t v_head_stride,
+                 const int64_t *slots_dev, void *cache_dev, size_t n_pages, int page,
+                 void *stream);
+int q8_kv8_read(const void *cache_dev, size_t n_pages, int page, const int64_t *slots_dev,
+                size_t T, int n_heads, int D, void *k_dev, void *v_dev, int type,
+                size_t k_stride, size_t k_head_stride, size_t v_stride, size_t v_head_stride,
+                void *stream);
+
+/* q8_kv4_attend over the 8-bit cache, with its arguments and errors, and `causal`: 1, or 0 where every row of a request sees
+ * all of its lengths[b] keys, as a decoder's rows see an encoder's states (window 0 then; Q8_EINVAL otherwise).  Workspaces
+ * are its own (q8_kv8_attend_workspace_bytes), zeroed once.                               */
+size_t q8_kv8_attend_workspace_bytes(size_t T, int n_requests, int n_heads, int ratio, int D,
+                                     size_t longest);
+int q8_kv8_attend(const void *q_dev, int type, size_t T, int n_heads, int ratio, int D,
+                  size_t q_stride, size_t q_head_stride, const void *cache_dev, size_t n_pages,
+                  int page, const int32_t *table_dev, int width, size_t table_stride,
+                  const int32_t *lengths_dev, const int32_t *starts_dev, int n_requests,
+                  float scale, int window, int causal, void *out_dev, size_t o_stride,
+                  size_t o_head_stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The pages of a cache, of any format.  Request b holds lengths[b] tokens (negative counts as 0, more than width * page as
+ * that), on the first pages that row b of the table names; entries outside 0 .. n_pages - 1 are no pages.
+ * n_pages <= 2^24 (Q8_EUNSUPPORTED); workspaces of q8_page_workspace_bytes (for up to so many new rows and pages; compact: 0
+ * rows), 16-byte aligned, any contents.
+ *
+ * q8_page_select: the requests that go on.  New request c is old request parents[c] (any other number: an empty request): its
+ * length, and its row with -1 behind the pages that it holds.  Several of one parent share its full pages; of a last page that
+ * is not full, every one but the first gets a copy, whose page stands in its row.  Pages that no new row holds, in
+ * ascending order, are the free ones: the i-th of them is for the i-th copy, in the order of the new requests, and those
+ * beyond are listed.  A request without a page for its copy becomes empty.
+ *   out_table     [n_new], out_stride apart, out_lengths [n_new]; neither overlaps what is read (Q8_EINVAL)
+ *   free_pages    [n_pages]: the pages that are free afterwards, then -1
+ *   copies        [n_new][2]: from, to; then -1.  None is read that is written: q8_page_copy takes them as they are, for
+ *                 the cache of every layer that goes by this table
+ *   counts        [4]: free pages, copies, requests left empty, pages in use
+ *
+ * q8_page_compact: the k pages in use to places 0 .. k - 1.  Those at k and behind go to the ones that are not in use in
+ * front, both in ascending order; out_table (the table itself, or one that does not overlap it) names the new places, -1
+ * behind the pages that a request holds.  copies [n_pages / 2][2], free_pages [n_pages] (k, k + 1, .., then -1) and
+ * counts [4] (the third 0) as above.
+ *
+ * q8_page_copy: page `to` of a cache of n_pages pages of page_bytes bytes (a multiple of 16, 16-byte aligned) becomes page
+ * `from`, for n_pairs pairs of them; a pair with a number that is no page is skipped.  No page is written by two pairs, or
+ * written by one and read by another.                                                     */
+size_t q8_page_workspace_bytes(int n_new, size_t n_pages);
+int q8_page_select(const int32_t *parents_dev, int n_new, const int32_t *lengths_dev,
+                   const int32_t *table_dev, size_t table_stride, int n_requests, int width, int page,
+                   size_t n_pages, int32_t *out_table_dev, size_t out_stride,
+                   int32_t *out_lengths_dev, int32_t *free_pages_dev, int32_t *copies_dev,
+                   int32_t *counts_dev, void *workspace, size_t workspace_bytes, void *stream);
+int q8_page_compact(const int32_t *lengths_dev, const int32_t *table_dev, size_t table_stride,
+                    int n_requests, int width, int page, size_t n_pages, int32_t *out_table_dev,
+                    size_t out_stride, int32_t *free_pages_dev, int32_t *copies_dev,
+                    int32_t *counts_dev, void *workspace, size_t workspace_bytes, void *stream);
+int q8_page_copy(void *cache_dev, size_t n_pages, size_t page_bytes, const int32_t *pairs_dev,
+                 int n_pairs, void *stream);
+
 /* Measurement only, not part of the method (no parity claim rests on it): `blocks` workgroups of four wavefronts each issue 4 * iters
  * register-resident v_mfma_i32_32x32x32_i8 (65536 int8 ops each), no memory traffic:
  * ops = blocks * 4 * 4 * iters * 65536.  The caller times the launch; the result is the

@@ -43,6 +43,8 @@ EXPORTS = [
     "q8_linear_variant_name", "q8_linear_int8_variant", "q8_linear_workspace_bytes",
     "q8_linear", "q8_page_tables", "q8_kv4_cache_bytes", "q8_kv4_write", "q8_kv4_read",
     "q8_kv4_attend_workspace_bytes", "q8_kv4_attend",
+    "q8_kv8_cache_bytes", "q8_kv8_write", "q8_kv8_read", "q8_kv8_attend_workspace_bytes", "q8_kv8_attend",
+    "q8_page_workspace_bytes", "q8_page_select", "q8_page_compact", "q8_page_copy",
 ]
 
 
@@ -207,6 +209,19 @@ lib.q8_kv4_attend_workspace_bytes.restype = _sz
 lib.q8_kv4_attend_workspace_bytes.argtypes = [_sz, _i, _i, _i, _i, _sz]
 lib.q8_kv4_attend.argtypes = [_vp, _i, _sz, _i, _i, _i, _sz, _sz, _vp, _sz, _i, _vp, _i, _sz, _vp, _vp, _i, _f, _i,
                               _vp, _sz, _sz, _vp, _sz, _vp]
+lib.q8_kv8_cache_bytes.restype = _sz
+lib.q8_kv8_cache_bytes.argtypes = [_sz, _i, _i, _i]
+lib.q8_kv8_write.argtypes = lib.q8_kv4_write.argtypes
+lib.q8_kv8_read.argtypes = lib.q8_kv4_read.argtypes
+lib.q8_kv8_attend_workspace_bytes.restype = _sz
+lib.q8_kv8_attend_workspace_bytes.argtypes = lib.q8_kv4_attend_workspace_bytes.argtypes
+lib.q8_kv8_attend.argtypes = [_vp, _i, _sz, _i, _i, _i, _sz, _sz, _vp, _sz, _i, _vp, _i, _sz, _vp, _vp, _i, _f, _i, _i,
+                              _vp, _sz, _sz, _vp, _sz, _vp]
+lib.q8_page_workspace_bytes.restype = _sz
+lib.q8_page_workspace_bytes.argtypes = [_i, _sz]
+lib.q8_page_select.argtypes = [_vp, _i, _vp, _vp, _sz, _i, _i, _i, _sz, _vp, _sz, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+lib.q8_page_compact.argtypes = [_vp, _vp, _sz, _i, _i, _i, _sz, _vp, _sz, _vp, _vp, _vp, _vp, _sz, _vp]
+lib.q8_page_copy.argtypes = [_vp, _sz, _sz, _vp, _i, _vp]
 
 
 def _check(code):
@@ -241,7 +256,8 @@ _q8call.bind(_ptr, _device, _raw_stream, ConvDesc, torch.int8, torch.int32, torc
                  lib.q8_quantize, lib.q8_dequantize)))
 _q8call.bind_rows(*(C.cast(f, C.c_void_p).value for f in (
     lib.q8_quantize_rows, lib.q8_linear_int8_variant, lib.q8_linear, lib.q8_linear_packed_bytes, lib.q8_page_tables,
-    lib.q8_kv4_write, lib.q8_kv4_read, lib.q8_kv4_attend)))
+    lib.q8_kv4_write, lib.q8_kv4_read, lib.q8_kv4_attend, lib.q8_kv8_write, lib.q8_kv8_read, lib.q8_kv8_attend,
+    lib.q8_page_select, lib.q8_page_compact, lib.q8_page_copy)))
 
 
 def calibrate_maxabs(x, maxabs):
@@ -752,3 +768,91 @@ def kv4_attend(q, cache, table, lengths, starts=None, scale=None, window=0, out=
     _check(_q8call.kv4_attend(q, cache, table, lengths, starts, q.shape[2] ** -0.5 if scale is None else scale, window,
                               out, workspace))
     return out
+
+
+# ------------------------------------------------------- the 8-bit cache, and the pages of a cache
+def kv8_cache(n_pages, heads, page, D, device="cuda"):
+    """An empty 8-bit cache: uint8 [n_pages, heads, page / 16, 32 D + 64]."""
+    if n_pages and not lib.q8_kv8_cache_bytes(n_pages, heads, page, D):
+        raise Q8Error(-2)
+    return torch.zeros((n_pages, heads, page // 16, 32 * D + 64), dtype=torch.uint8, device=device)
+
+
+def kv8_write(cache, k, v, slots):
+    """Keys and values [T, heads, D] of T tokens into their slots (int64, each once; -1: nowhere).  Sixteen tokens of a head
+    share a factor: a call that writes the first of them begins it anew, others make it grow where they need it."""
+    _check(_q8call.kv8_write(cache, k, v, slots))
+    return cache
+
+
+def kv8_read(cache, slots, k_out=None, v_out=None, dtype=torch.bfloat16):
+    """What the cache holds in these slots (zeros outside it): keys and values [T, heads, D]."""
+    assert cache.dim() == 4, cache.shape
+    shape = (slots.numel(), cache.shape[1], (cache.shape[3] - 64) // 32)
+    if k_out is None:
+        k_out = torch.empty(shape, dtype=dtype if v_out is None else v_out.dtype, device=cache.device)
+    if v_out is None:
+        v_out = torch.empty(shape, dtype=k_out.dtype, device=cache.device)
+    _check(_q8call.kv8_read(cache, slots, k_out, v_out))
+    return k_out, v_out
+
+
+def kv8_attend_workspace(q, cache, n_requests, longest, device="cuda"):
+    """``kv4_attend_workspace`` for ``kv8_attend``."""
+    heads, D = cache.shape[1], (cache.shape[3] - 64) // 32
+    n = lib.q8_kv8_attend_workspace_bytes(q.shape[0], n_requests, heads, q.shape[1] // heads, D, longest)
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def kv8_attend(q, cache, table, lengths, starts=None, scale=None, window=0, causal=True, out=None, workspace=None):
+    """``kv4_attend`` over the 8-bit cache.  Without ``causal`` every row sees all of its request's keys, whose number has
+    nothing to do with that of its rows: cross attention to an encoder's states."""
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _check(_q8call.kv8_attend(q, cache, table, lengths, starts, q.shape[2] ** -0.5 if scale is None else scale, window,
+                              int(causal), out, workspace))
+    return out
+
+
+def page_workspace(n_rows, n_pages, device="cuda"):
+    """Device memory for ``page_select`` and ``page_compact`` on up to so many rows and pages."""
+    return torch.empty(lib.q8_page_workspace_bytes(n_rows, n_pages), dtype=torch.uint8, device=device)
+
+
+def page_select(parents, lengths, rows, page, n_pages, table=None, grown=None, free_pages=None, copies=None, counts=None,
+                workspace=None):
+    """The requests that go on: new request c is old request ``parents[c]`` of ``rows`` [requests, width], which hold
+    ``lengths`` tokens (any other number: an empty one).  Full pages are shared by the requests of one parent; of a last page
+    that is not full, all but the first get a copy (``page_copy``).  Every request of the pool has its row here: pages that
+    no new one holds are free.  -> dict of table, lengths, free_pages [n_pages] (ascending, then -1), copies
+    [requests, 2] (from, to; then -1) and counts (free pages, copies, requests left empty for want of a page, pages in use)."""
+    dev, i32, m = rows.device, torch.int32, parents.numel()
+    table = torch.empty((m, rows.shape[1]), dtype=i32, device=dev) if table is None else table
+    grown = torch.empty(m, dtype=i32, device=dev) if grown is None else grown
+    free_pages = torch.empty(n_pages, dtype=i32, device=dev) if free_pages is None else free_pages
+    copies = torch.empty((m, 2), dtype=i32, device=dev) if copies is None else copies
+    counts = torch.empty(4, dtype=i32, device=dev) if counts is None else counts
+    workspace = page_workspace(m, n_pages, dev) if workspace is None else workspace
+    _check(_q8call.page_select(parents, lengths, rows, page, n_pages, table, grown, free_pages, copies, counts, workspace))
+    return dict(table=table, lengths=grown, free_pages=free_pages, copies=copies, counts=counts)
+
+
+def page_compact(lengths, rows, page, n_pages, table=None, free_pages=None, copies=None, counts=None, workspace=None):
+    """The pages in use moved to the front of the pool, as few of them as possible: table (``rows`` itself, or another one)
+    names their new places, copies [n_pages / 2, 2] what ``page_copy`` has to move (from, to; then -1).  -> dict of these,
+    free_pages [n_pages] (then -1) and counts (free pages, copies, 0, pages in use)."""
+    dev, i32 = rows.device, torch.int32
+    table = torch.empty(rows.shape, dtype=i32, device=dev) if table is None else table
+    free_pages = torch.empty(n_pages, dtype=i32, device=dev) if free_pages is None else free_pages
+    copies = torch.empty((n_pages // 2, 2), dtype=i32, device=dev) if copies is None else copies
+    counts = torch.empty(4, dtype=i32, device=dev) if counts is None else counts
+    workspace = page_workspace(0, n_pages, dev) if workspace is None else workspace
+    _check(_q8call.page_compact(lengths, rows, page, n_pages, table, free_pages, copies, counts, workspace))
+    return dict(table=table, free_pages=free_pages, copies=copies, counts=counts)
+
+
+def page_copy(cache, pairs):
+    """Pages of a cache [pages, ..] copied: pairs int32 [n, 2] of (from, to); those with a page outside it are skipped.  No
+    page is written twice, or written and read."""
+    _check(_q8call.page_copy(cache, pairs))
+    return cache

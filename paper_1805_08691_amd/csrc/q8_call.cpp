@@ -17,7 +17,8 @@ namespace {
 PyObject *g_ptr, *g_device, *g_stream, *g_desc_type, *g_int8, *g_int32, *g_float32, *g_uint8;
 enum {
   kInt8, kU8, kPerChannel, kReal, kF32, kMaxabs, kQuantize, kDequantize, kLayerFunctions,
-  kRows = kLayerFunctions, kLinearInt8, kLinear, kPackedBytes, kPages, kKv4Write, kKv4Read, kKv4Attend, kFunctions
+  kRows = kLayerFunctions, kLinearInt8, kLinear, kPackedBytes, kPages, kKv4Write, kKv4Read, kKv4Attend,
+  kKv8Write, kKv8Read, kKv8Attend, kPageSelect, kPageCompact, kPageCopy, kFunctions
 };
 void* g_fn[kFunctions];
 
@@ -291,12 +292,13 @@ PyObject* dequantize(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return finish(g, [&] { return ((decltype(&q8_dequantize))g_fn[kDequantize])(z, (size_t)len, q, r, s); });
 }
 
-// ---- the operators on rows and on the 4-bit cache: tensors with strides, of several types.  What a call cannot pass on
+// ---- the operators on rows, on the caches and on their pages: tensors with strides, of several types.  What a call cannot pass on
 // raises an AssertionError; tensors' subclasses (parameters) are taken as tensors.
 struct Strided {
   void* p = nullptr;
   long size[4] = {0, 0, 0, 0}, stride[4] = {0, 0, 0, 0}, n = 0;
   int type = -1, dims = 0;             // Q8_* of real values
+  int device = -1;
 };
 struct TensorArgs : Args {
   explicit TensorArgs(PyObject* const* args) : Args{args} {}
@@ -329,11 +331,12 @@ struct TensorArgs : Args {
       for (int d = (int)t.dim() - 1; d >= 0; --d) {
         if (d < 4) s.size[d] = t.size(d), s.stride[d] = t.stride(d);
         if (d > 0 && t.size(d) > 0x7fffffff) refuse(i, "more than an int counts");       // (the first: as the call says)
-        if (d >= t.dim() - dense && t.size(d) > 1 && t.stride(d) != run) refuse(i, "expected dense rows");
+        if (d >= t.dim() - dense && t.size(d) > 1 && t.stride(d) != run && t.numel() > 0) refuse(i, "expected dense rows");
         run *= t.size(d);
       }
       s.n = t.numel();
       s.dims = (int)t.dim();
+      s.device = t.get_device();
       s.p = t.mutable_data_ptr();
     } catch (...) {            // (none may leave through the interpreter's frames)
       refuse(i, "expected a device tensor with storage");
@@ -356,6 +359,15 @@ struct TensorArgs : Args {
   }
   void check(bool fine, int i, const char* what) {
     if (ok && !fine) refuse(i, what);
+  }
+  // All of them on the device whose stream the call takes.
+  void check_device(std::initializer_list<const Strided*> all) {
+    if (!ok) return;
+    PyObject* d = PyObject_CallNoArgs(g_device);
+    const long current = d ? PyLong_AsLong(d) : -1;
+    Py_XDECREF(d);
+    if (PyErr_Occurred()) ok = false;
+    for (const Strided* s : all) check(s->device < 0 || s->device == current, 0, "every tensor on the current device");
   }
 };
 
@@ -446,13 +458,14 @@ PyObject* page_tables(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
-// A cache uint8 [pages][heads][page / 16][18 D].
+// A cache uint8 [pages][heads][page / 16][18 D] (4 bits) or [32 D + 64] (8 bits).
 struct Cache {
   Strided c;
   int heads, page, D;
-  Cache(TensorArgs& g, int i) : c(g.get(i, at::kByte, 4, -1)) {
-    g.check(c.size[3] % 18 == 0 && c.size[2] <= 0x7ffffff, i, "the cache's shape");
-    heads = (int)c.size[1], page = (int)(c.size[2] * 16), D = (int)(c.size[3] / 18);
+  Cache(TensorArgs& g, int i, int bits = 4) : c(g.get(i, at::kByte, 4, -1)) {
+    const long per = bits == 4 ? 18 : 32, more = bits == 4 ? 0 : 64, channels = c.size[3] - more;
+    g.check(channels >= 0 && channels % per == 0 && c.size[2] <= 0x7ffffff, i, "the cache's shape");
+    heads = (int)c.size[1], page = (int)(c.size[2] * 16), D = (int)(channels / per);
   }
 };
 // [tokens][heads][D]: elements between tokens and between heads, also where there is one only.
@@ -531,6 +544,132 @@ PyObject* kv4_attend(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// (cache, k, v, slots)
+PyObject* kv8_write(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!count(n, 4)) return nullptr;
+  TensorArgs g{args};
+  const Cache c(g, 0, 8);
+  const Tokens k(g, 1), v(g, 2);
+  const Strided slots = g.get(3, at::kLong, -1, -1);
+  check_tokens(g, c, k, v, slots, 1);
+  g.check_device({&c.c, &k.t, &v.t, &slots});
+  void* s = g.stream();
+  return finish(g, [&] {
+    return ((decltype(&q8_kv8_write))g_fn[kKv8Write])(k.t.p, v.t.p, k.t.type, slots.n, c.heads, c.D, k.token, k.head,
+                                                      v.token, v.head, (const int64_t*)slots.p, c.c.p, c.c.size[0],
+                                                      c.page, s);
+  });
+}
+
+// (cache, slots, k, v)
+PyObject* kv8_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!count(n, 4)) return nullptr;
+  TensorArgs g{args};
+  const Cache c(g, 0, 8);
+  const Strided slots = g.get(1, at::kLong, -1, -1);
+  const Tokens k(g, 2), v(g, 3);
+  check_tokens(g, c, k, v, slots, 2);
+  g.check_device({&c.c, &k.t, &v.t, &slots});
+  void* s = g.stream();
+  return finish(g, [&] {
+    return ((decltype(&q8_kv8_read))g_fn[kKv8Read])(c.c.p, c.c.size[0], c.page, (const int64_t*)slots.p, slots.n,
+                                                    c.heads, c.D, k.t.p, v.t.p, k.t.type, k.token, k.head, v.token,
+                                                    v.head, s);
+  });
+}
+
+// (q, cache, table, lengths, starts, scale, window, causal, out, workspace)
+PyObject* kv8_attend(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!count(n, 10)) return nullptr;
+  TensorArgs g{args};
+  const Tokens q(g, 0);
+  const Cache c(g, 1, 8);
+  const Strided table = g.get(2, at::kInt, 2, 1), len = g.get(3, at::kInt, -1, -1),
+                starts = g.get(4, at::kInt, -1, -1, true);
+  const float scale = g.factor(5);
+  const int window = g.integer(6), causal = g.integer(7);
+  const Tokens out(g, 8);
+  const Strided ws = g.get(9, at::kByte, -1, -1, true);
+  g.check(q.t.size[2] == c.D && c.heads > 0 && q.t.size[1] % c.heads == 0, 0, "[tokens, a multiple of the heads, D]");
+  g.check(out.t.size[0] == q.t.size[0] && out.t.size[1] == q.t.size[1] && out.t.size[2] == q.t.size[2], 8, "shape");
+  g.check(out.t.type == q.t.type, 8, "queries and outputs of one type");
+  g.check(table.size[0] == len.n && len.n < 0x7fffffff && table.size[1] < 0x7fffffff, 2, "one row for each request");
+  if (g.ok && g.a[4] == Py_None) g.check(q.t.size[0] == len.n, 0, "one row for each request");
+  else g.check(starts.n == len.n + 1, 4, "one start for each request, and the end");
+  g.check_device({&q.t, &c.c, &table, &len, &starts, &out.t, &ws});
+  void* s = g.stream();
+  return finish(g, [&] {
+    return ((decltype(&q8_kv8_attend))g_fn[kKv8Attend])(
+        q.t.p, q.t.type, q.t.size[0], c.heads, (int)(q.t.size[1] / c.heads), c.D, q.token, q.head, c.c.p, c.c.size[0],
+        c.page, (const int32_t*)table.p, (int)table.size[1], g.row_stride(table), (const int32_t*)len.p,
+        (const int32_t*)starts.p, (int)len.n, scale, window, causal, out.t.p, out.token, out.head, ws.p, ws.n, s);
+  });
+}
+
+// (parents, lengths, table, page, pages, out table, out lengths, free, copies, counts, workspace)
+PyObject* page_select(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!count(n, 11)) return nullptr;
+  TensorArgs g{args};
+  const Strided parents = g.get(0, at::kInt, -1, -1), len = g.get(1, at::kInt, -1, -1), table = g.get(2, at::kInt, 2, 1),
+                rows = g.get(5, at::kInt, 2, 1), grown = g.get(6, at::kInt, -1, -1), fr = g.get(7, at::kInt, -1, -1),
+                copies = g.get(8, at::kInt, 2, -1), counts = g.get(9, at::kInt, -1, -1), ws = g.get(10, at::kByte, -1, -1);
+  const int page = g.integer(3), pool = g.integer(4);
+  g.check(table.size[0] == len.n, 2, "one row for each request");
+  g.check(rows.size[0] == parents.n && rows.size[1] == table.size[1] && grown.n == parents.n, 5,
+          "one row, as long as the requests', and one length for each parent");
+  g.check(pool >= 0 && fr.n == pool, 7, "as many places as pages");
+  g.check(copies.size[0] == parents.n && copies.size[1] == 2, 8, "one pair for each parent");
+  g.check(counts.n == 4, 9, "four counts");
+  g.check((len.n | parents.n) < 0x7fffffff, 0, "sizes");
+  g.check_device({&parents, &len, &table, &rows, &grown, &fr, &copies, &counts, &ws});
+  void* s = g.stream();
+  return finish(g, [&] {
+    return ((decltype(&q8_page_select))g_fn[kPageSelect])(
+        (const int32_t*)parents.p, (int)parents.n, (const int32_t*)len.p, (const int32_t*)table.p, g.row_stride(table),
+        (int)len.n, (int)table.size[1], page, (size_t)pool, (int32_t*)rows.p, g.row_stride(rows), (int32_t*)grown.p,
+        (int32_t*)fr.p, (int32_t*)copies.p, (int32_t*)counts.p, ws.p, ws.n, s);
+  });
+}
+
+// (lengths, table, page, pages, out table, free, copies, counts, workspace)
+PyObject* page_compact(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!count(n, 9)) return nullptr;
+  TensorArgs g{args};
+  const Strided len = g.get(0, at::kInt, -1, -1), table = g.get(1, at::kInt, 2, 1), rows = g.get(4, at::kInt, 2, 1),
+                fr = g.get(5, at::kInt, -1, -1), copies = g.get(6, at::kInt, 2, -1), counts = g.get(7, at::kInt, -1, -1),
+                ws = g.get(8, at::kByte, -1, -1);
+  const int page = g.integer(2), pool = g.integer(3);
+  g.check(table.size[0] == len.n, 1, "one row for each request");
+  g.check(rows.size[0] == table.size[0] && rows.size[1] == table.size[1], 4, "shape");
+  g.check(pool >= 0 && fr.n == pool, 5, "as many places as pages");
+  g.check(copies.size[0] == pool / 2 && copies.size[1] == 2, 6, "one pair for two pages");
+  g.check(counts.n == 4, 7, "four counts");
+  g.check(len.n < 0x7fffffff, 0, "sizes");
+  g.check_device({&len, &table, &rows, &fr, &copies, &counts, &ws});
+  void* s = g.stream();
+  return finish(g, [&] {
+    return ((decltype(&q8_page_compact))g_fn[kPageCompact])(
+        (const int32_t*)len.p, (const int32_t*)table.p, g.row_stride(table), (int)len.n, (int)table.size[1], page,
+        (size_t)pool, (int32_t*)rows.p, g.row_stride(rows), (int32_t*)fr.p, (int32_t*)copies.p, (int32_t*)counts.p, ws.p,
+        ws.n, s);
+  });
+}
+
+// (cache [pages, ..], pairs)
+PyObject* page_copy(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (!count(n, 2)) return nullptr;
+  TensorArgs g{args};
+  const Strided c = g.get(0, at::kByte, -1, -1), pairs = g.get(1, at::kInt, 2, -1);
+  g.check(c.dims >= 1, 0, "number of dimensions");
+  g.check(pairs.size[1] == 2 && pairs.size[0] < 0x7fffffff, 1, "pairs of pages");
+  g.check_device({&c, &pairs});
+  void* s = g.stream();
+  return finish(g, [&] {
+    return ((decltype(&q8_page_copy))g_fn[kPageCopy])(c.p, c.size[0], c.size[0] ? c.n / c.size[0] : 0,
+                                                      (const int32_t*)pairs.p, (int)pairs.size[0], s);
+  });
+}
+
 bool bind_functions(PyObject* const* args, int first, int end) {
   for (int i = first; i < end; ++i) {
     g_fn[i] = PyLong_AsVoidPtr(args[i - first]);
@@ -551,7 +690,7 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
-// bind_rows(the addresses of the operators on rows and on the 4-bit cache)
+// bind_rows(the addresses of the operators on rows, on the caches and on their pages)
 PyObject* bind_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (!count(n, kFunctions - kLayerFunctions)) return nullptr;
   if (!bind_functions(args, kLayerFunctions, kFunctions)) return nullptr;
@@ -563,6 +702,8 @@ PyMethodDef methods[] = {Q8_METHOD(conv_int8), Q8_METHOD(conv_u8), Q8_METHOD(con
                          Q8_METHOD(conv_real), Q8_METHOD(conv_f32), Q8_METHOD(maxabs), Q8_METHOD(quantize),
                          Q8_METHOD(dequantize), Q8_METHOD(quantize_rows), Q8_METHOD(linear_int8), Q8_METHOD(linear),
                          Q8_METHOD(page_tables), Q8_METHOD(kv4_write), Q8_METHOD(kv4_read), Q8_METHOD(kv4_attend),
+                         Q8_METHOD(kv8_write), Q8_METHOD(kv8_read), Q8_METHOD(kv8_attend), Q8_METHOD(page_select),
+                         Q8_METHOD(page_compact), Q8_METHOD(page_copy),
                          Q8_METHOD(bind), Q8_METHOD(bind_rows), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_q8call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,262 @@
+// Attention of new tokens over the paged 8-bit cache (q8_kv8.h):
+//   s[j] = scale q . D(k_j),   o = sum_j exp(s[j] - max s) D(v_j) / sum_j exp(s[j] - max s)
+// over the keys j <= position (and > position - window) of the token's request, or over all of them; 0 where there are none.
+// One pass over the keys with the running maximum and sum of the softmax in fp32.
+//
+// A column is a query head of a token; the columns of a request that share a key head are taken 16 at a time, and a
+// wavefront multiplies 64 keys (four sixteens) by them per step on v_mfma_f32_16x16x32_f16:
+//   S^T[key][column]     = K Q^T      four tiles of 16 keys, G products each
+//   O^T[channel][column] = V^T P^T    2 G tiles of 16 channels, two products each
+// Codes are multiplied as they are: whole numbers up to 128 are binary16 numbers.  Lane (r, j) of S has 16 keys of sixteen j
+// and loads the values of the same 16: a score meets its sixteen's factor as one fp32 number of the lane, and a
+// probability, times the values' factor in fp32, is rounded to binary16 once (by 2^-11 of it at most).
+// The key axis is split over workgroups where columns are few; the last of them to finish adds the parts, in their order.
+#include "q8_kv8_attend.h"
+#pragma clang fp contract(fast)
+
+namespace {
+
+using namespace q8;
+
+[[maybe_unused]] constexpr int kLift = 10;          // probabilities are up to 2^10 times what factors are below their power
+
+template <int G, typename V>
+__global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_attend_kernel(const AttendParams p, const V* __restrict__ q,
+                                                                         V* __restrict__ out) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int D = 32 * G, CT = 2 * G, CHUNKS = (G + 1) / 2, SIXTEEN = kv8_sixteen(D);
+  extern __shared__ __attribute__((aligned(16))) char shared[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = lane & 15, j = lane >> 4;
+  Part a;
+  Tile t;
+  if (!find_part<kCols, kTarget>(p, blockIdx.x, shared, &a, &t)) return;
+  const int head = a.head, step0 = a.step0, step1 = a.step1;
+  const Codes codes;
+  const int last = min(t.lo + t.steps * kStep, t.len);         // keys of the tile end here
+  const int iterations = step0 + wave < step1 ? (step1 - step0 - wave + kWaves - 1) / kWaves : 0;
+
+  // ---- the column of this lane
+  const int col = t.first + r;
+  const bool given = col < t.cols;
+  const int tok = min(col, t.cols - 1) / p.ratio, qh = min(col, t.cols - 1) % p.ratio;
+  const int pos = given ? row_position(p, t, tok) : -1;        // (no key is at or before -1)
+  const int from = p.window > 0 ? pos - p.window : -1;         // keys behind this one
+  float v[G][8];
+  {
+    const V* qr = q + (size_t)(t.row + tok) * p.q_stride + ((size_t)head * p.ratio + qh) * p.q_head;
+#pragma unroll
+    for (int g = 0; g < G; ++g) load_values<8, false>(qr + key_channel<G>(g, j), v[g]);
+  }
+
+  // ---- loads: lane l holds where sixteen l % 4 of iteration l / 4 (of 16) lies, bit l of `held` whether it is there.  One that
+  // is not is read as the cache's first, and its factors count as zeros.
+  const int* __restrict__ table = p.table + t.b * p.table_stride;
+  long where = 0;
+  unsigned long held = 0;
+  auto find_sixteens = [&](int it0) {
+    const int s = step0 + wave + (it0 + (lane >> 2)) * kWaves, at = (t.lo >> 4) + s * 4 + (lane & 3);
+    int page = -1;
+    if (s < step1 && at * 16 < last) page = table[at >> p.shift];
+    const bool in = page >= 0 && page < p.n_pages;
+    where = in ? (((((long)page * p.H + head) << p.shift) + (at & ((1 << p.shift) - 1))) * SIXTEEN) : 0;
+    held = __ballot(in);
+  };
+  uint4 kc[4][CHUNKS], vc[CT];
+  float2 factors = {0.0f, 0.0f};
+  const uint8_t* values = p.cache;                             // of this lane's sixteen, in the next iteration
+  unsigned there = 0, next_there = 0;                          // the iteration's sixteens that there are
+  auto issue_keys = [&](int it) __attribute__((always_inline)) {
+    if (it > 0 && (it & 15) == 0) find_sixteens(it);
+    next_there = (unsigned)(held >> ((it & 15) * 4)) & 15u;
+    const uint8_t* const keys = p.cache + __shfl(where, (it & 15) * 4 + (r >> 2), 64);
+    values = p.cache + __shfl(where, (it & 15) * 4 + j, 64);
+#pragma unroll
+    for (int tile = 0; tile < 4; ++tile)
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) {
+        const uint8_t* const at = keys + tile * 4 * D + c * 256;
+        if (c < G / 2) kc[tile][c] = *reinterpret_cast<const uint4*>(at + (j * 4 + (r & 3)) * 16);
+        else __builtin_memcpy(&kc[tile][c], __builtin_assume_aligned(at + (j * 4 + (r & 3)) * 8, 8), 8);
+      }
+    factors = *reinterpret_cast<const float2*>(values + 32 * D);
+  };
+  auto issue_values = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c) vc[c] = *reinterpret_cast<const uint4*>(values + 16 * D + (16 * c + r) * 16);
+  };
+  find_sixteens(0);
+  if (iterations > 0) {
+    issue_keys(0);
+    issue_values();
+  }
+
+  // ---- its queries as the right operand, scaled to [1, 2) by a power of two and turned so that scores grow with the products
+  h8 qf[G];
+  float scale;
+  {
+    float top = 0.0f;
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[g][e]));
+    top = column_max(top);
+    const unsigned e2 = min(max(__float_as_uint(top) >> 23, 1u), 253u);
+    const float down = copysignf(__uint_as_float((254u - e2) << 23), p.scale_log2);
+    scale = fmaxf(fabsf(p.scale_log2) * __uint_as_float(e2 << 23), 1e-30f);    // (no 0 times infinity)
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) qf[g][e] = (_Float16)(v[g][e] * down);
+  }
+  // steps whose every key is seen by every column: behind `clear0`, up to `clear1`
+  const int pos0 = row_position(p, t, t.first / p.ratio), pos1 = row_position(p, t, (min(t.first + kCols, t.cols) - 1) / p.ratio);
+  const int clear0 = p.window > 0 ? pos1 - p.window : -1, clear1 = pos0;
+
+  f4 o[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) o[c] = f4{0, 0, 0, 0};
+  float ref = -__builtin_inff(), sum = 0.0f;            // what sum and o are relative to, as a power of 2
+  Power<5> scaled;                                      // o is relative to 2^(its power - kLift)
+
+  for (int it = 0; it < iterations; ++it) {
+    const int key0 = t.lo + (step0 + wave + it * kWaves) * kStep;
+    const bool more = it + 1 < iterations;
+    there = next_there;
+    const bool clear = key0 > clear0 && key0 + kStep - 1 <= clear1 && there == 15u;
+    const int base = key0 + 16 * j;
+
+    // ---- S^T, keys 16 j + 4 tile + i in register i of tile `tile`
+    float x[4][4];
+    const float fk = factors.x * scale;
+#pragma unroll
+    for (int tile = 0; tile < 4; ++tile) {
+      f4 s = {0, 0, 0, 0};
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const uint4& w = kc[tile][g / 2];
+        const h8 k8 = g & 1 ? codes.eight(w.z, w.w) : codes.eight(w.x, w.y);
+        s = __builtin_amdgcn_mfma_f32_16x16x32_f16(k8, qf[g], s, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[tile][i] = s[i] * fk;
+    }
+    float fv = factors.y;
+    if (!clear) {
+      unsigned see = token_bits(from + 1 - base, (there >> j & 1u) ? pos + 1 - base : 0);
+      asm volatile("" : "+v"(see));                     // (a branch, not selects in every step)
+#pragma unroll
+      for (int tile = 0; tile < 4; ++tile)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[tile][i] = see >> (4 * tile + i) & 1u ? x[tile][i] : -__builtin_inff();
+      // (a sixteen that no row sees: its factor may be anything)
+      if (!(there >> j & 1u) || base + 15 < t.seen || base >= last) fv = 0.0f;
+    }
+    bool grown;
+    const float down = scaled.grow(fv, &grown);
+    if (grown) {
+#pragma unroll
+      for (int c = 0; c < CT; ++c) o[c] *= down;
+    }
+    const float weight = __builtin_amdgcn_ldexpf(fv, kLift - scaled.power);
+    // ---- running maximum and sum
+    float m = x[0][0];
+#pragma unroll
+    for (int tile = 0; tile < 4; ++tile)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m = fmaxf(m, x[tile][i]);
+    const float top = fmaxf(ref, column_max(m));
+    const float now = top == -__builtin_inff() ? 0.0f : top;
+    const float shrink = __builtin_amdgcn_exp2f(ref - now);
+    ref = top;
+    sum *= shrink;
+    if (__any(shrink != 1.0f)) {
+#pragma unroll
+      for (int c = 0; c < CT; ++c) o[c] *= shrink;
+    }
+    // ---- O^T: a probability times its sixteen's factor is the right operand
+    h8 pr[2];
+#pragma unroll
+    for (int tile = 0; tile < 4; ++tile)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float e = __builtin_amdgcn_exp2f(x[tile][i] - now);
+        sum += e;
+        pr[tile >> 1][(tile & 1) * 4 + i] = (_Float16)(e * weight);
+      }
+    if (more) issue_keys(it + 1);
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes.eight(vc[c].x, vc[c].y), pr[0], o[c], 0, 0, 0);
+      o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes.eight(vc[c].z, vc[c].w), pr[1], o[c], 0, 0, 0);
+    }
+    if (more) issue_values();
+  }
+  const float back = two_to(scaled.power - kLift);
+#pragma unroll
+  for (int c = 0; c < CT; ++c) o[c] *= back;
+  join_columns<D>(p, a, t, shared, out, o, ref, sum);
+#endif
+}
+
+template <int G, typename V>
+int launch(const AttendParams& p, const V* q, V* out, hipStream_t stream) {
+  const size_t lds = join_bytes(32 * G, p.parts != nullptr);
+  if (lds > 65536) {
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_attend_kernel<G, V>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)join_bytes(32 * G, true));
+    if (attr != hipSuccess) return Q8_EHIP;
+  }
+  const unsigned blocks = (unsigned)(p.tiles * p.H) + (p.parts ? kTarget : 0);
+  kv8_attend_kernel<G, V><<<blocks, 256, lds, stream>>>(p, q, out);
+  return q8_launch_status();
+}
+
+template <typename V>
+int launch_any(int G, const AttendParams& p, const V* q, V* out, hipStream_t stream) {
+  switch (G) {
+    case 1: return launch<1>(p, q, out, stream);
+    case 2: return launch<2>(p, q, out, stream);
+    case 3: return launch<3>(p, q, out, stream);
+    case 4: return launch<4>(p, q, out, stream);
+    case 5: return launch<5>(p, q, out, stream);
+    case 6: return launch<6>(p, q, out, stream);
+    case 7: return launch<7>(p, q, out, stream);
+    case 8: return launch<8>(p, q, out, stream);
+  }
+  return Q8_EUNSUPPORTED;
+}
+
+bool wide_for(size_t T, int B, int H, int ratio, int D, size_t longest, bool cuts) {
+  const size_t tiles = tiles_of(T, B, ratio, true, kWideCols) * H;
+  if (T * ratio < (size_t)B * (kWideCols / 2)) return false;
+  return tiles >= 256 || (cuts && tiles >= 32 && tiles * (longest / kStep) / kTarget >= (D <= 128 ? 32u : 64u));
+}
+
+}  // namespace
+
+extern "C" size_t q8_kv8_attend_workspace_bytes(size_t T, int n_requests, int n_heads, int ratio, int D,
+                                                size_t longest) {
+  return attend_workspace_bytes(T, n_requests, n_heads, ratio, D, longest, wide_for);
+}
+
+extern "C" int q8_kv8_attend(const void* q_dev, int type, size_t T, int n_heads, int ratio, int D, size_t q_stride,
+                             size_t q_head_stride, const void* cache_dev, size_t n_pages, int page,
+                             const int32_t* table_dev, int width, size_t table_stride, const int32_t* lengths_dev,
+                             const int32_t* starts_dev, int n_requests, float scale, int window, int causal, void* out_dev,
+                             size_t o_stride, size_t o_head_stride, void* workspace, size_t workspace_bytes,
+                             void* stream) {
+  Q8_REQUIRE((causal == 0 || causal == 1) && (causal || window == 0), Q8_EINVAL);
+  AttendParams p{};
+  bool wide = false;
+  const int rc = attend_params(q_dev, type, T, n_heads, ratio, D, q_stride, q_head_stride, cache_dev, n_pages, page, table_dev,
+                               width, table_stride, lengths_dev, starts_dev, n_requests, scale, window, out_dev, o_stride,
+                               o_head_stride, workspace, workspace_bytes, wide_for, &p, &wide);
+  if (rc != Q8_OK || p.T == 0) return rc;
+  p.all = !causal;
+  if (wide) return kv8_attend_wide(D / 32, p, q_dev, out_dev, type, (hipStream_t)stream);
+  if (type == Q8_F16)
+    return launch_any(D / 32, p, static_cast<const _Float16*>(q_dev), static_cast<_Float16*>(out_dev),
+                      (hipStream_t)stream);
+  return launch_any(D / 32, p, static_cast<const __bf16*>(q_dev), static_cast<__bf16*>(out_dev), (hipStream_t)stream);
+}
