@@ -128,9 +128,9 @@ struct Part {
   int step0, step1;
 };
 
-// The part of workgroup `id` (of MOST that a tile is cut into at most), and its tile; false: there is none.  `shared`: LDS
-// that is free until then.
-template <int COLS, int MOST>
+// The part of workgroup `id` (of MOST that a tile is cut into at most), and its tile; false: there is none.  SORTED: the
+// longest tiles first.  `shared`: LDS that is free until then.
+template <int COLS, int MOST, bool SORTED = false>
 __device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* shared, Part* a, Tile* out) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int at = id / p.H;
@@ -149,6 +149,14 @@ __device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* s
   int* const rows = lengths + kMaxTiles;                       // rows, with the last one's end
   Tile t;
   bool is = false;
+  auto tile = [&](int w) __attribute__((always_inline)) {
+    int b = 0, hi = p.B - 1;
+    while (b < hi) {
+      const int mid = (b + hi + 1) >> 1;
+      if (bases[mid] <= w) b = mid; else hi = mid - 1;
+    }
+    return w < p.tiles && set_tile<COLS>(p, w, b, bases[b], rows[b], rows[b + 1], lengths[b], &t);
+  };
   if (!p.starts) {
     const int per = (p.ratio + COLS - 1) / COLS, b = tid / per;
     if (tid < p.tiles) is = set_tile<COLS>(p, tid, b, b * per, b, b + 1, p.lengths[b], &t);
@@ -159,12 +167,22 @@ __device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* s
       if (i < p.B) bases[i] = first_tile<COLS>(p, start, i), lengths[i] = length;
     }
     __syncthreads();
-    int b = 0, hi = p.B - 1;
-    while (b < hi) {
-      const int mid = (b + hi + 1) >> 1;
-      if (bases[mid] <= tid) b = mid; else hi = mid - 1;
+    is = tile(tid);
+    if constexpr (SORTED) {            // (all keys differ: a tile's place is the number of larger ones)
+      unsigned* const keys = reinterpret_cast<unsigned*>(rows + kMaxTiles + 4);
+      unsigned char* const order = reinterpret_cast<unsigned char*>(keys + kMaxTiles);
+      const unsigned key = (is ? (unsigned)min(max(t.steps, 1), 0xffffff) : 0u) << 8 | (255u - tid);
+      keys[tid] = key;
+      __syncthreads();
+      int larger = 0;
+      for (int i = 0; i < kMaxTiles; i += 4) {
+        const uint4 k = *reinterpret_cast<const uint4*>(keys + i);
+        larger += (k.x > key) + (k.y > key) + (k.z > key) + (k.w > key);
+      }
+      order[larger] = (unsigned char)tid;
+      __syncthreads();
+      is = tile(order[tid]);
     }
-    if (tid < p.tiles) is = set_tile<COLS>(p, tid, b, bases[b], rows[b], rows[b + 1], lengths[b], &t);
   }
   // all tiles' steps, in two halves: less than 2^25 of each, 2^8 tiles
   const unsigned steps = is ? max(t.steps, 1) : 0;
@@ -182,7 +200,7 @@ __device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* s
   __syncthreads();
   for (int u = 0; u < wave; ++u) v += sums[u];
   // (the last tiles of a request see most keys: where tiles take longest they go first)
-  const int place = COLS == kCols ? at : (int)(((sums[0] + sums[1]) + (sums[2] + sums[3])) & 0x3ffu) - 1 - at;
+  const int place = COLS == kCols || SORTED ? at : (int)(((sums[0] + sums[1]) + (sums[2] + sums[3])) & 0x3ffu) - 1 - at;
   const unsigned before = v - own;
   const int first = (int)(before & 0x3ffu), slot = (int)(before >> 10 & 0x3ffu), rank = (int)(before >> 20);
   if (place >= first && place < first + (int)n) {
@@ -366,22 +384,23 @@ __device__ __forceinline__ void join_columns(const AttendParams& p, const Part& 
   }
 }
 
-// The same for workgroups of kWideCols columns that all wavefronts' keys are: wavefront w has columns (w kWideTiles + c) 16 + r
-// in o[c][i], channels 16 i + 4 j ..; seen[c]: whether the column has seen a key.
-template <int D, typename V>
+// The same for workgroups of WAVES wavefronts that have all seen the same keys, each with TILES tiles of W columns: lane (r, j),
+// r < W, of wavefront w has channels 256 / W i + 4 j .. of column (w TILES + c) W + r in o[c][i]; seen[c]: whether the column has
+// seen a key.
+template <int D, int WAVES, int W, int TILES, typename V>
 __device__ __forceinline__ void join_wide(const AttendParams& p, const Part& a, const Tile& t, char* shared, V* __restrict__ out,
-                                          const f4 (&o)[kWideTiles][D / 16], const float (&ref)[kWideTiles],
-                                          float (&sum)[kWideTiles], const bool (&seen)[kWideTiles]) {
-  constexpr int CT = D / 16;
+                                          const f4 (&o)[TILES][D * W / 256], const float (&ref)[TILES],
+                                          float (&sum)[TILES], const bool (&seen)[TILES]) {
+  constexpr int CT = D * W / 256, COLS = WAVES * TILES * W, NEXT = 256 / W;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int r = lane & 15, j = lane >> 4, head = a.head;
-  constexpr size_t kPartWords = (size_t)kWideCols * (D + 2) / 2;    // of a part: [tile][CT][2][lane], then maxima and sums
+  const int r = lane % W, j = lane / W, head = a.head;
+  constexpr size_t kPartWords = (size_t)COLS * (D + 2) / 2;    // of a part: [tile][CT][2][lane], then maxima and sums
   word* const part = reinterpret_cast<word*>(p.parts) + ((size_t)(a.slot + a.part) * p.H + head) * kPartWords;
 #pragma unroll
-  for (int c = 0; c < kWideTiles; ++c) {
-    sum[c] += __shfl_xor(sum[c], 16, 64);
+  for (int c = 0; c < TILES; ++c) {
+    if constexpr (W == 16) sum[c] += __shfl_xor(sum[c], 16, 64);
     sum[c] += __shfl_xor(sum[c], 32, 64);
-    const int of = (wave * kWideTiles + c) * kCols + r, col = t.first + of;
+    const int of = (wave * TILES + c) * W + r, col = t.first + of;
     if (col >= t.cols) continue;
     const float l = sum[c];
     if (a.parts == 1) {
@@ -390,16 +409,16 @@ __device__ __forceinline__ void join_wide(const AttendParams& p, const Part& a, 
 #pragma unroll
       for (int i = 0; i < CT; ++i) {
         const float y[4] = {o[c][i][0] * inv, o[c][i][1] * inv, o[c][i][2] * inv, o[c][i][3] * inv};
-        store_values<4, false>(to + 16 * i, y);
+        store_values<4, false>(to + NEXT * i, y);
       }
     } else {
-      word* const to = part + (wave * kWideTiles + c) * CT * 128 + lane;
+      word* const to = part + (wave * TILES + c) * CT * 128 + lane;
 #pragma unroll
       for (int i = 0; i < CT; ++i) {
         put(to + 128 * i, o[c][i][0], o[c][i][1]);
         put(to + 128 * i + 64, o[c][i][2], o[c][i][3]);
       }
-      if (j == 0) put(part + kWideCols * D / 2 + of, seen[c] ? ref[c] : -__builtin_inff(), l);
+      if (j == 0) put(part + COLS * D / 2 + of, seen[c] ? ref[c] : -__builtin_inff(), l);
     }
   }
   if (a.parts == 1) return;
@@ -416,31 +435,31 @@ __device__ __forceinline__ void join_wide(const AttendParams& p, const Part& a, 
   if (tid == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
   const word* const parts = reinterpret_cast<const word*>(p.parts) + ((size_t)a.slot * p.H + head) * kPartWords;
   const size_t stride = (size_t)p.H * kPartWords;
-  float* const weights = reinterpret_cast<float*>(shared);      // [16][128], then the columns' sums
-  float* const totals = weights + kWideParts * kWideCols;
-  if (tid < kWideCols) {
+  float* const weights = reinterpret_cast<float*>(shared);      // [16][COLS], then the columns' sums
+  float* const totals = weights + kWideParts * COLS;
+  if (tid < COLS) {
     f2 rs[kWideParts];
     float most = -__builtin_inff(), l = 0.0f;
 #pragma unroll
     for (int u = 0; u < kWideParts; ++u) {
       rs[u] = f2{-__builtin_inff(), 0.0f};
-      if (u < a.parts && t.first + tid < t.cols) rs[u] = get(parts + u * stride + kWideCols * D / 2 + tid);
+      if (u < a.parts && t.first + tid < t.cols) rs[u] = get(parts + u * stride + COLS * D / 2 + tid);
     }
 #pragma unroll
     for (int u = 0; u < kWideParts; ++u) most = fmaxf(most, rs[u][0]);
 #pragma unroll
     for (int u = 0; u < kWideParts; ++u) {
       const float weight = rs[u][0] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(rs[u][0] - most);
-      weights[u * kWideCols + tid] = weight;
+      weights[u * COLS + tid] = weight;
       l += weight * rs[u][1];
     }
     totals[tid] = l;
   }
   __syncthreads();
   // a thread takes four channels of a column, as a lane had them, and several such, so that enough is on its way
-  const int valid = t.cols - t.first, groups = min((valid + kCols - 1) / kCols, kWideCols / kCols) * CT;     // of 64 lanes' quads
+  const int valid = t.cols - t.first, groups = min((valid + W - 1) / W, COLS / W) * CT;     // of 64 lanes' quads
   constexpr int kItems = 4, kBatch = 4;
-  for (int g0 = wave; g0 < groups; g0 += kWaves * kItems) {
+  for (int g0 = wave; g0 < groups; g0 += WAVES * kItems) {
     f4 v[kItems];
 #pragma unroll
     for (int k = 0; k < kItems; ++k) v[k] = f4{0, 0, 0, 0};
@@ -450,7 +469,7 @@ __device__ __forceinline__ void join_wide(const AttendParams& p, const Part& a, 
       for (int u = 0; u < kBatch; ++u)
 #pragma unroll
         for (int k = 0; k < kItems; ++k) {
-          const word* const from = parts + min(s0 + u, a.parts - 1) * stride + min(g0 + k * kWaves, groups - 1) * 128 + lane;
+          const word* const from = parts + min(s0 + u, a.parts - 1) * stride + min(g0 + k * WAVES, groups - 1) * 128 + lane;
           x[k][u][0] = get(from), x[k][u][1] = get(from + 64);
         }
 #pragma unroll
@@ -458,17 +477,17 @@ __device__ __forceinline__ void join_wide(const AttendParams& p, const Part& a, 
 #pragma unroll
         for (int u = 0; u < kBatch; ++u)
           if (s0 + u < a.parts)
-            v[k] += weights[(s0 + u) * kWideCols + min(g0 + k * kWaves, groups - 1) / CT * kCols + r] *
+            v[k] += weights[(s0 + u) * COLS + min(g0 + k * WAVES, groups - 1) / CT * W + r] *
                     f4{x[k][u][0][0], x[k][u][0][1], x[k][u][1][0], x[k][u][1][1]};
     }
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
-      const int g = g0 + k * kWaves, of = g / CT * kCols + r, col = t.first + of;
+      const int g = g0 + k * WAVES, of = g / CT * W + r, col = t.first + of;
       if (g >= groups || col >= t.cols) continue;
       const float l = totals[of], inv = l > 0.0f ? 1.0f / l : l;
       const float y[4] = {v[k][0] * inv, v[k][1] * inv, v[k][2] * inv, v[k][3] * inv};
       store_values<4, false>(out + (size_t)(t.row + col / p.ratio) * p.o_stride + ((size_t)head * p.ratio + col % p.ratio) * p.o_head +
-                                 g % CT * 16 + 4 * j, y);
+                                 g % CT * NEXT + 4 * j, y);
     }
   }
 }
@@ -485,7 +504,8 @@ inline bool cut(size_t tiles, size_t longest) { return tiles <= kMaxTiles && lon
 constexpr size_t kCounterBytes = (kTarget + 15) / 16 * 16 * sizeof(int);
 inline size_t split_bytes(int D, int cols = kCols) { return kCounterBytes + (size_t)2 * kTarget * cols * (D + 2) * 4; }
 
-// Whether tiles of kWideCols columns are taken for T new tokens of B requests in runs of several; cuts: they could be cut.
+// Whether tiles of kWideCols columns are taken for T new tokens of B requests in runs of several (and then for more tokens of as
+// many requests); cuts: they could be cut.
 typedef bool WideFor(size_t T, int B, int H, int ratio, int D, size_t longest, bool cuts);
 
 inline size_t attend_workspace_bytes(size_t T, int n_requests, int n_heads, int ratio, int D, size_t longest, WideFor* wide_for) {

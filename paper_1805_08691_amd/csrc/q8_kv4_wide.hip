@@ -301,7 +301,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 3 : 1) void kv4_wide_kernel(const Att
   bool seen[kTiles];
 #pragma unroll
   for (int c = 0; c < kTiles; ++c) seen[c] = limit[c] > -__builtin_inff();
-  join_wide<32 * G>(p, a, t, shared, out, o, ref, sum, seen);
+  join_wide<32 * G, kWaves, kCols, kTiles>(p, a, t, shared, out, o, ref, sum, seen);
 #endif
 }
 

@@ -40,10 +40,9 @@ template <int SPARE>
 struct Power {
   float limit = 0.0f;
   int power = -100;
-  // With the four sixteens' factors of a step, a lane's own: what sums so far are multiplied by, where `changed`.
-  __device__ __forceinline__ float grow(float fv, bool* changed) {
-    *changed = __any(fv > limit);
-    if (!*changed) return 1.0f;
+  // With the four sixteens' factors of a step, a lane's own: what sums so far are multiplied by (a wavefront's one number).
+  __device__ __forceinline__ float grow(float fv) {
+    if (!__any(fv > limit)) return 1.0f;
     const int grown = max(power_above(column_max(fv)), power);
     const float down = limit > 0.0f ? two_to(power - grown) : 1.0f;
     power = grown;

@@ -152,9 +152,8 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_attend_kernel(const A
       // (a sixteen that no row sees: its factor may be anything)
       if (!(there >> j & 1u) || base + 15 < t.seen || base >= last) fv = 0.0f;
     }
-    bool grown;
-    const float down = scaled.grow(fv, &grown);
-    if (grown) {
+    const float down = scaled.grow(fv);
+    if (down != 1.0f) {
 #pragma unroll
       for (int c = 0; c < CT; ++c) o[c] *= down;
     }
@@ -227,10 +226,17 @@ int launch_any(int G, const AttendParams& p, const V* q, V* out, hipStream_t str
   return Q8_EUNSUPPORTED;
 }
 
+// Whether tiles of 128 columns, whose keys and values are unpacked once for all of them, are taken for new tokens in runs of
+// several: where requests fill most of a tile, and the tiles are workgroups enough, or can be cut and the parts are long enough
+// for what adding them costs.  us in tiles of 16 and of 128 columns, 32 query heads on 8: of 64 channels 16 x 300 tokens 35
+// and 26, 32 pieces of up to 100 tokens over up to 2000 63 and 70, 512 over 8192 91 and 72; of 128 channels 512 tokens 17
+// and 21, 2 x 1000 47 and 41, 64 pieces of up to 30 81 and 85, 128 over 8192 48 and 69, 512 over 8192 148 and 105; of 256
+// channels 512 tokens 40 and 34, 2048 293 and 162, 64 pieces of up to 30 225 and 173, 128 over 8192 117 and 146.
 bool wide_for(size_t T, int B, int H, int ratio, int D, size_t longest, bool cuts) {
   const size_t tiles = tiles_of(T, B, ratio, true, kWideCols) * H;
-  if (T * ratio < (size_t)B * (kWideCols / 2)) return false;
-  return tiles >= 256 || (cuts && tiles >= 32 && tiles * (longest / kStep) / kTarget >= (D <= 128 ? 32u : 64u));
+  if (T * ratio < (size_t)B * (D <= 128 ? 96 : 64)) return false;
+  if (tiles >= (D <= 64 ? 768 : D <= 128 ? 256 : 96)) return true;
+  return cuts && tiles >= 32 && tiles * (longest / kStep) / kTarget >= (D <= 128 ? 32u : 16u);
 }
 
 }  // namespace

@@ -1,244 +1,379 @@
 // Attention over the paged 8-bit cache where a request has many columns (prompts, in pieces or whole; a decoder's rows over an
-// encoder's states): the mathematics and the layouts of q8_kv8_attend.hip.
+// encoder's states): the mathematics of q8_kv8_attend.hip, on v_mfma_f32_32x32x16_f16.
 //
-// A workgroup of four wavefronts owns 128 columns that share a key head, 32 of each wavefront's, and walks over the
-// keys they see, 64 at a time.  The codes of the next step go from memory to registers, a quarter to a wavefront, and become
-// operands of the matrix instruction in LDS, whole numbers in binary16, in the order in which a wavefront reads them; all
-// wavefronts multiply all of them.
+// A workgroup owns 32 columns of each of its wavefronts, which share a key head, and walks over the keys they see, 64 at a
+// time.  The codes go from memory to registers, a share to a wavefront, and become operands of the matrix instruction in
+// LDS, in the order in which a wavefront reads them; all wavefronts multiply all of them.
+//   S^T[key][column]     = K Q^T   two tiles of 32 keys, 2 G products each
+//   O^T[channel][column] = V^T P^T G tiles of 32 channels, four products each
+// Lane (r, h) of S has 16 keys of sixteens h and 2 + h for column r, so that a factor is one number of a lane, and probabilities
+// are operands as they come.
 #include "q8_kv8_attend.h"
 
 namespace {
 
 using namespace q8;
 
-[[maybe_unused]] constexpr int kTiles = kWideTiles;
-[[maybe_unused]] constexpr float kSlack = 8.0f; // powers of two that a maximum may grow by before sums are made relative to it
-[[maybe_unused]] constexpr int kLift = 3;       // and that probabilities are scaled by beside their factors: 3 + 4 + 8 < 16
+typedef float f16v __attribute__((ext_vector_type(16)));
+
+// Probabilities are made relative to a maximum so that its own is 2^kTop, and again where their sum in a lane (32 of them)
+// passes 2^kMost; values are codes times their factor over a power of two, 2^(7 + 4 + kLift) at most: both are binary16 numbers.
+[[maybe_unused]] constexpr float kTop = 7.0f, kMost = 15.0f;
+[[maybe_unused]] constexpr int kLift = 4;
+constexpr int kRing = 128;                      // steps whose sixteens' places and factors are in LDS
 
 template <int G>
 struct Wide {
-  static constexpr int OPERANDS = 4096 * G, LDS = 2 * OPERANDS;
+  static constexpr int OPERANDS = 4096 * G;     // of a step's keys, and of its values; two steps of each
+  static constexpr int V_AT = 2 * OPERANDS, RING_AT = 4 * OPERANDS, FACTORS_AT = RING_AT + kRing * 4 * 4;
+  static constexpr int HOLE_AT = FACTORS_AT + kRing * 4 * 8, LDS = HOLE_AT + 16;
 };
 
+// Product n of a key tile: lane half h has eight channels from here on, 16 neighbours in two products (q8_kv8.h).
+template <int G>
+__device__ __forceinline__ constexpr int channel_of(int n, int h) {
+  return n < G / 2 * 4 ? n / 4 * 64 + 16 * (2 * (n >> 1 & 1) + h) + 8 * (n & 1) : 32 * (G - 1) + 8 * (2 * (n & 1) + h);
+}
+
 template <int G, typename V>
-__global__ __launch_bounds__(256, G <= 5 ? 2 : 1) void kv8_wide_kernel(const AttendParams p, const V* __restrict__ q,
-                                                          V* __restrict__ out) {
+__global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const AttendParams p, const V* __restrict__ q,
+                                                                       V* __restrict__ out) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int D = 32 * G, CT = 2 * G, CHUNKS = (G + 1) / 2, SIXTEEN = kv8_sixteen(D), MINE = (CT + kWaves - 1) / kWaves;
+  constexpr int D = 32 * G, SIXTEEN = kv8_sixteen(D);
+  constexpr int PAIRS = (2 * G + kWaves - 1) / kWaves;      // of operands that a wavefront makes, of keys and of values
   using W = Wide<G>;
   extern __shared__ __attribute__((aligned(16))) char shared[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int r = lane & 15, j = lane >> 4;
+  const int r = lane & 31, h = lane >> 5;
   const Codes codes;
   Part a;
   Tile t;
   // (whole tiles: the last of a request see most keys, so they go first)
   const int id = p.parts ? (int)blockIdx.x : (p.tiles - 1 - (int)blockIdx.x / p.H) * p.H + (int)blockIdx.x % p.H;
-  if (!find_part<kWideCols, kWideParts>(p, id, shared, &a, &t)) return;
+  if (!find_part<kWideCols, kWideParts, true>(p, id, shared, &a, &t)) return;
   const int head = a.head, start = t.lo + a.step0 * kStep, steps = a.step1 - a.step0;
   const int last = min(t.lo + t.steps * kStep, t.len);
 
-  // ---- loads: lane l holds where sixteen l % 4 of step l / 4 (of 16) lies, bit l of `held` whether it is there.  One that is
-  // not is read as the cache's first.  Wave w takes keys' tile w and the values' tiles w, w + 4, ..
+  // ---- where sixteens lie, as numbers of them in the cache, and their factors.  One that is not there is read as the cache's
+  // first, and its keys' factor is -1; the values' factor of one that no row sees, which may be anything, counts as zero.
   const int* __restrict__ table = p.table + t.b * p.table_stride;
-  long where = 0;
-  unsigned long held = 0;
-  auto find_sixteens = [&](int s0) {
-    const int at = (start >> 4) + s0 * 4 + lane;
-    int page = -1;
-    if (at * 16 < last) page = table[at >> p.shift];
-    const bool in = page >= 0 && page < p.n_pages;
-    where = in ? ((((long)page * p.H + head) << p.shift) + (at & ((1 << p.shift) - 1))) * SIXTEEN : 0;
-    held = __ballot(in);
-  };
-  uint4 kc[CHUNKS], vc[MINE];
-  float2 factors = {0.0f, 0.0f};
-  unsigned next_there = 0;
-  auto issue = [&](int s) __attribute__((always_inline)) {
-    if ((s & 15) == 0) find_sixteens(s);
-    next_there = (unsigned)(held >> ((s & 15) * 4)) & 15u;
-    const uint8_t* const keys = p.cache + __shfl(where, (s & 15) * 4 + (r >> 2), 64) + wave * 4 * D;
-    const uint8_t* const values = p.cache + __shfl(where, (s & 15) * 4 + j, 64);
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-      if (c < G / 2) kc[c] = *reinterpret_cast<const uint4*>(keys + c * 256 + (j * 4 + (r & 3)) * 16);
-      else __builtin_memcpy(&kc[c], __builtin_assume_aligned(keys + c * 256 + (j * 4 + (r & 3)) * 8, 8), 8);
+  unsigned* const places = reinterpret_cast<unsigned*>(shared + W::RING_AT);
+  float2* const factors = reinterpret_cast<float2*>(shared + W::FACTORS_AT);
+  int* const hole = reinterpret_cast<int*>(shared + W::HOLE_AT);        // whether one that should be there is not
+  auto find_sixteens = [&](int i0, int n) {           // i0: of the part's, four to a step
+    for (int i = i0 + tid; i < i0 + n; i += 256) {
+      const int at = (start >> 4) + i;
+      int page = -1;
+      if (at * 16 < last) page = table[at >> p.shift];
+      const bool in = page >= 0 && page < p.n_pages;
+      const unsigned place = in ? (unsigned)((((long)page * p.H + head) << p.shift) + (at & ((1 << p.shift) - 1))) : 0u;
+      float2 f = {-1.0f, 0.0f};
+      if (in) f = *reinterpret_cast<const float2*>(p.cache + (size_t)place * SIXTEEN + 32 * D);
+      if (at * 16 + 15 < t.seen) f.y = 0.0f;
+      places[i & (4 * kRing - 1)] = place;
+      factors[i & (4 * kRing - 1)] = f;
+      if (!in && at * 16 < last) *hole = 1;
     }
-#pragma unroll
-    for (int i = 0; i < MINE; ++i) {
-      const int c = wave + i * kWaves;
-      if (CT % kWaves == 0 || c < CT) vc[i] = *reinterpret_cast<const uint4*>(values + 16 * D + (16 * c + r) * 16);
-    }
-    factors = *reinterpret_cast<const float2*>(values + 32 * D);
   };
-  if (steps > 0) issue(0);
+  if (tid == 0) *hole = 0;
+  lds_barrier();
+  find_sixteens(0, min(4 * (steps + 3), 4 * kRing));
+  lds_barrier();
+  bool holes = __builtin_amdgcn_readfirstlane(*hole) != 0;
+  auto slot_of = [&](int s, int c) { return (4 * s + c) & (4 * kRing - 1); };
 
-  // ---- the columns of this lane
-  h8 qf[kTiles][G];
-  float rest[kTiles], ref[kTiles], limit[kTiles], sum[kTiles];   // scores are products times `rest` and the keys' factor
-  int pos[kTiles];
-  f4 o[kTiles][CT];
-#pragma unroll
-  for (int c = 0; c < kTiles; ++c) {
-    const int col = t.first + (wave * kTiles + c) * kCols + r, in = min(col, t.cols - 1);
-    const int tok = in / p.ratio, qh = in % p.ratio;
-    pos[c] = col < t.cols ? row_position(p, t, tok) : -1;
-    const V* qr = q + (size_t)(t.row + tok) * p.q_stride + ((size_t)head * p.ratio + qh) * p.q_head;
-    float v[G][8], top = 0.0f;
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      load_values<8, false>(qr + key_channel<G>(g, j), v[g]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[g][e]));
+  // ---- loads.  Pair u of a step's keys: products 2 m and 2 m + 1 of tile u / G, m = u % G, whose row r is token 4 (r / 8) + r % 4
+  // of the tile's sixteen (r / 4) % 2; of the values: channel tile u / 2, keys of sixteens 2 (u % 2) and the next.
+  uint4 kc[PAIRS], vc[PAIRS];
+  unsigned key_place[PAIRS], value_place[PAIRS];      // of the next loads
+  auto find_pair = [&](int s, int i) __attribute__((always_inline)) {           // keys of s + 1, values of s
+    const int u = wave + i * kWaves;
+    if (2 * G % kWaves != 0 && u >= 2 * G) return;
+    key_place[i] = places[slot_of(s + 1, 2 * (u / G) + (r >> 2 & 1))];
+    value_place[i] = places[slot_of(s, 2 * (u & 1) + h)];
+  };
+  auto issue_keys = [&](int i) __attribute__((always_inline)) {
+    const int u = wave + i * kWaves, m = u % G;
+    if (2 * G % kWaves != 0 && u >= 2 * G) return;
+    const uint8_t* const from = p.cache + (size_t)key_place[i] * SIXTEEN + (r >> 3) * 4 * D + (m >> 1) * 256;
+    if (m < G / 2 * 2) {
+      kc[i] = *reinterpret_cast<const uint4*>(from + ((2 * (m & 1) + h) * 4 + (r & 3)) * 16);
+    } else {
+      const uint2 x = *reinterpret_cast<const uint2*>(from + (h * 4 + (r & 3)) * 8);
+      const uint2 y = *reinterpret_cast<const uint2*>(from + ((2 + h) * 4 + (r & 3)) * 8);
+      kc[i] = uint4{x.x, x.y, y.x, y.y};
     }
-    top = column_max(top);
+  };
+  auto issue_values = [&](int i) __attribute__((always_inline)) {
+    const int u = wave + i * kWaves;
+    if (2 * G % kWaves != 0 && u >= 2 * G) return;
+    vc[i] = *reinterpret_cast<const uint4*>(p.cache + (size_t)value_place[i] * SIXTEEN + 16 * D + (32 * (u >> 1) + r) * 16);
+  };
+  // Operands of step s: keys as codes; values as codes times their factor.
+  auto unpack_key = [&](int s, auto k_c) __attribute__((always_inline)) {        // half k % 2 of pair k / 2
+    constexpr int k = decltype(k_c)::value, i = k / 2;
+    const int u = wave + i * kWaves;
+    if (2 * G % kWaves != 0 && u >= 2 * G) return;
+    char* const to = shared + (s & 1) * W::OPERANDS + u * 2048 + k % 2 * 1024 + lane * 16;
+    *reinterpret_cast<h8*>(to) = k % 2 ? codes.eight(kc[i].z, kc[i].w) : codes.eight(kc[i].x, kc[i].y);
+  };
+  Power<4> scaled;
+  float2 next[2];                                     // factors of a step's sixteens h and 2 + h
+  float weight0 = 0.0f, weight1 = 0.0f;
+  auto find_factors = [&](int s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) next[b] = factors[slot_of(s, 2 * b + h)];
+  };
+  auto weigh = [&]() __attribute__((always_inline)) {
+    weight0 = __builtin_amdgcn_ldexpf(next[0].y, kLift - scaled.power);
+    weight1 = __builtin_amdgcn_ldexpf(next[1].y, kLift - scaled.power);
+  };
+  auto unpack_value = [&](int s, auto k_c) __attribute__((always_inline)) {
+    constexpr int k = decltype(k_c)::value, i = k / 2;
+    const int u = wave + i * kWaves;
+    if (2 * G % kWaves != 0 && u >= 2 * G) return;
+    const _Float16 w = (_Float16)(u & 1 ? weight1 : weight0);
+    const h8 w8 = {w, w, w, w, w, w, w, w};
+    char* const to = shared + W::V_AT + (s & 1) * W::OPERANDS + u * 2048 + k % 2 * 1024 + lane * 16;
+    *reinterpret_cast<h8*>(to) = (k % 2 ? codes.eight(vc[i].z, vc[i].w) : codes.eight(vc[i].x, vc[i].y)) * w8;
+  };
+  constexpr std::integral_constant<int, PAIRS> kPairs{};
+  auto all_of = [&](auto n_c, auto f) __attribute__((always_inline)) {
+    auto each = [&](auto self, auto k_c) __attribute__((always_inline)) -> void {
+      constexpr int k = decltype(k_c)::value;
+      if constexpr (k < decltype(n_c)::value) {
+        f(k_c);
+        self(self, std::integral_constant<int, k + 1>{});
+      }
+    };
+    each(each, std::integral_constant<int, 0>{});
+  };
+  all_of(kPairs, [&](auto i_c) { find_pair(-1, decltype(i_c)::value), issue_keys(decltype(i_c)::value); });
+
+  // ---- the column of this lane
+  const int col = t.first + wave * 32 + r, in = min(col, t.cols - 1), tok = in / p.ratio;
+  const int pos = col < t.cols ? row_position(p, t, tok) : -1;
+  h8 qf[2 * G];
+  float rest;                                         // scores are products times `rest` and the keys' factor
+  {
+    const V* qr = q + (size_t)(t.row + tok) * p.q_stride + ((size_t)head * p.ratio + in % p.ratio) * p.q_head;
+    float v[2 * G][8], top = 0.0f;
+#pragma unroll
+    for (int n = 0; n < 2 * G; ++n) {
+      load_values<8, false>(qr + channel_of<G>(n, h), v[n]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[n][e]));
+    }
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
     const unsigned e2 = min(max(__float_as_uint(top) >> 23, 1u), 253u);
     const float down = copysignf(__uint_as_float((254u - e2) << 23), p.scale_log2);
-    rest[c] = fmaxf(fabsf(p.scale_log2) * __uint_as_float(e2 << 23), 1e-30f);    // (no 0 times infinity)
+    rest = fmaxf(fabsf(p.scale_log2) * __uint_as_float(e2 << 23), 1e-30f);    // (no 0 times infinity)
 #pragma unroll
-    for (int g = 0; g < G; ++g)
+    for (int n = 0; n < 2 * G; ++n)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) qf[c][g][e] = (_Float16)(v[g][e] * down);
-    ref[c] = 0.0f;
-    limit[c] = -__builtin_inff();
-    sum[c] = 0.0f;
-#pragma unroll
-    for (int i = 0; i < CT; ++i) o[c][i] = f4{0, 0, 0, 0};
+      for (int e = 0; e < 8; ++e) qf[n][e] = (_Float16)(v[n][e] * down);
   }
+  float ref = 0.0f, sum = 0.0f;
+  bool begun = col >= t.cols;                         // (a column that there is not: it has no maximum to find)
+  f16v o[G];
+#pragma unroll
+  for (int i = 0; i < G; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] = 0.0f;
   // steps whose every key is seen by every column of the tile
   const int pos0 = row_position(p, t, t.first / p.ratio), pos1 = row_position(p, t, (min(t.first + kWideCols, t.cols) - 1) / p.ratio);
   const int clear0 = p.window > 0 ? pos1 - p.window : -1, clear1 = pos0;
-  Power<4> scaled;
 
+  // ---- products, register e of s2[b] being token e of sixteen 2 b + h: kProducts of a step's keys, and of its values, one after
+  // the other, with what is to be done beside the i-th; operands are read kAhead products before.
+  constexpr int kProducts = 4 * G, kAhead = kProducts < 4 ? kProducts : 4;
+  using std::integral_constant;
+  f16v s2[2], x[2];
+  h8 pr[2][2];
+  auto products = [&](const char* from, auto multiply, auto beside) __attribute__((always_inline)) {
+    h8 operand[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) operand[i] = *reinterpret_cast<const h8*>(from + i * 1024 + lane * 16);
+    __builtin_amdgcn_sched_barrier(0);
+    auto each = [&](auto self, auto i_c) __attribute__((always_inline)) -> void {
+      constexpr int i = decltype(i_c)::value;
+      if constexpr (i < kProducts) {
+        multiply(i_c, operand[i % kAhead]);
+        if constexpr (i + kAhead < kProducts) operand[i % kAhead] = *reinterpret_cast<const h8*>(from + (i + kAhead) * 1024 + lane * 16);
+        beside(i_c);
+        __builtin_amdgcn_sched_barrier(0);
+        self(self, integral_constant<int, i + 1>{});
+      }
+    };
+    each(each, integral_constant<int, 0>{});
+  };
+  auto nothing = [&](auto) {};
+  auto scores = [&](int s, auto beside) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s2[0][e] = s2[1][e] = 0.0f;
+    products(shared + (s & 1) * W::OPERANDS, [&](auto i_c, const h8& k8) __attribute__((always_inline)) {
+      constexpr int i = decltype(i_c)::value, b = i / (2 * G), n = i % (2 * G);
+      s2[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k8, qf[n], s2[b], 0, 0, 0);
+    }, beside);
+  };
+  auto add_values = [&](int s, auto beside) __attribute__((always_inline)) {
+    products(shared + W::V_AT + (s & 1) * W::OPERANDS, [&](auto i_c, const h8& v8) __attribute__((always_inline)) {
+      constexpr int i = decltype(i_c)::value;
+      o[i / 4] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v8, pr[i / 2 % 2][i % 2], o[i / 4], 0, 0, 0);
+    }, beside);
+  };
+  // The share of N things that is done beside product i.
+  auto share = [&](auto i_c, auto n_c, auto f) __attribute__((always_inline)) {
+    constexpr int i = decltype(i_c)::value, N = decltype(n_c)::value, first = N * i / kProducts, end = N * (i + 1) / kProducts;
+    auto each = [&](auto self, auto k_c) __attribute__((always_inline)) -> void {
+      constexpr int k = decltype(k_c)::value;
+      if constexpr (k < end) {
+        f(k_c);
+        self(self, integral_constant<int, k + 1>{});
+      }
+    };
+    each(each, integral_constant<int, first>{});
+  };
+  // Scores 2 k and 2 k + 1 relative to `ref`, as powers of two; none of keys that the column does not see.
+  float by[2];
+  auto scale_two = [&](auto k_c) __attribute__((always_inline)) {
+    constexpr int k = decltype(k_c)::value, b = k / 8, e = k % 8 * 2;
+    x[b][e] = __builtin_fmaf(s2[b][e], by[b], -ref);
+    x[b][e + 1] = __builtin_fmaf(s2[b][e + 1], by[b], -ref);
+    float pinned[2] = {x[b][e], x[b][e + 1]};
+    asm volatile("" : "+v"(pinned[0]), "+v"(pinned[1]));        // (here, beside the product, not where they are used)
+    x[b][e] = pinned[0], x[b][e + 1] = pinned[1];
+  };
+  auto hide = [&](int s) __attribute__((always_inline)) {
+    const int key0 = start + s * kStep;
+    if (key0 > clear0 && key0 + kStep - 1 <= clear1 && !holes) return;
+    const bool there[2] = {factors[slot_of(s, h)].x >= 0.0f, factors[slot_of(s, 2 + h)].x >= 0.0f};
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int at = pos + 1 - (key0 + 16 * (2 * b + h));
+      unsigned see = token_bits(p.window > 0 ? at - p.window : 0, there[b] ? at : 0);
+      asm volatile("" : "+v"(see));                   // (a branch, not selects in every step)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[b][e] = see >> e & 1u ? x[b][e] : -__builtin_inff();
+    }
+  };
+  float part = 0.0f;                                  // sum of a lane's probabilities as the values meet them
+  float raised[2];
+  auto raise_two = [&](auto k_c) __attribute__((always_inline)) {
+    constexpr int k = decltype(k_c)::value, b = k / 8, e = k % 8 * 2;
+    raised[0] = __builtin_amdgcn_exp2f(x[b][e]);
+    raised[1] = __builtin_amdgcn_exp2f(x[b][e + 1]);
+  };
+  auto keep_two = [&](auto k_c) __attribute__((always_inline)) {
+    constexpr int k = decltype(k_c)::value, b = k / 8, e = k % 8 * 2;
+    const h2 two = {(_Float16)raised[0], (_Float16)raised[1]}, ones = {1.0f16, 1.0f16};
+    part = __builtin_amdgcn_fdot2(two, ones, part, false);
+    pr[b][e >> 3][e & 7] = two[0], pr[b][e >> 3][(e & 7) + 1] = two[1];
+  };
+  constexpr integral_constant<int, 16> kTwos{};
+
+  // ---- step s multiplies keys of s + 1 beside the exponentials of s, and values of s beside the unpacking of keys s + 2 and
+  // values s + 1, whose codes were loaded a step before.  (What is done for steps behind the last goes nowhere.)
+  constexpr integral_constant<int, 2 * PAIRS> kHalves{};
+  all_of(kHalves, [&](auto k_c) { unpack_key(0, k_c); });
+  all_of(kPairs, [&](auto i_c) {
+    constexpr int i = decltype(i_c)::value;
+    find_pair(0, i), issue_keys(i), issue_values(i);
+  });
+  lds_barrier();
+  scores(0, nothing);
+  find_factors(0);
+  float down = scaled.grow(fmaxf(next[0].y, next[1].y));        // what sums are multiplied by before the next values are added
+  weigh();
+  all_of(kHalves, [&](auto k_c) { unpack_key(1, k_c), unpack_value(0, k_c); });
+  by[0] = next[0].x * rest, by[1] = next[1].x * rest;
+  all_of(kTwos, scale_two);
+  hide(0);
+  all_of(kPairs, [&](auto i_c) {
+    constexpr int i = decltype(i_c)::value;
+    find_pair(1, i), issue_keys(i), issue_values(i);
+  });
+  lds_barrier();
   for (int s = 0; s < steps; ++s) {
-    const int key0 = start + s * kStep, base = key0 + 16 * j;
-    const unsigned there = next_there;
-    lds_barrier();                                    // the operands of the step before have been read
-    // ---- a quarter of the keys: tile `wave`, whose row r is token 4 wave + r % 4 of sixteen r / 4; and of the values
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      const uint4& w = kc[g / 2];
-      *reinterpret_cast<h8*>(shared + ((wave * G + g) * 64 + lane) * 16) = g & 1 ? codes.eight(w.z, w.w) : codes.eight(w.x, w.y);
-    }
-#pragma unroll
-    for (int i = 0; i < MINE; ++i) {
-      const int c = wave + i * kWaves;
-      if (CT % kWaves == 0 || c < CT) {
-        char* const to = shared + W::OPERANDS + c * 2048 + lane * 16;
-        *reinterpret_cast<h8*>(to) = codes.eight(vc[i].x, vc[i].y);
-        *reinterpret_cast<h8*>(to + 1024) = codes.eight(vc[i].z, vc[i].w);
+    if ((s & 63) == 0 && s > 0) find_sixteens((s + 64) * 4, 256);
+    if ((s & 63) == 1) holes = __builtin_amdgcn_readfirstlane(*hole) != 0;
+    part = 0.0f;
+    bool grows = false;
+    scores(s + 1, [&](auto i_c) __attribute__((always_inline)) {
+      constexpr int i = decltype(i_c)::value;
+      share(i_c, kTwos, [&](auto k_c) __attribute__((always_inline)) {
+        constexpr int k = decltype(k_c)::value;
+        if constexpr (k > 0) keep_two(integral_constant<int, k - 1>{});
+        raise_two(k_c);
+      });
+      if constexpr (i == 0) find_factors(s + 1);
+      if constexpr (i == kProducts / 2) {
+        all_of(kPairs, [&](auto i_c) __attribute__((always_inline)) { find_pair(s + 2, decltype(i_c)::value); });
+        by[0] = next[0].x * rest, by[1] = next[1].x * rest;
+        grows = down != 1.0f || fmaxf(next[0].y, next[1].y) > scaled.limit;
       }
+    });
+    keep_two(integral_constant<int, 15>{});
+    // the first keys that a column sees, and where one or a factor grows
+    if (__any(!begun || part > 32768.0f || grows)) {
+#pragma unroll
+      for (int i = 0; i < G; ++i) o[i] *= down;
+      down = scaled.grow(fmaxf(next[0].y, next[1].y));
+      float m = x[0][0];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) m = fmaxf(m, x[b][e]);
+      m = fmaxf(m, __shfl_xor(m, 32, 64));
+      const bool seen = m > -__builtin_inff();
+      // (32 probabilities whose sum is 2^15 have one of 2^10)
+      const float more = seen && (!begun || m > kMost - 5.0f) ? m - kTop : 0.0f, shrink = begun ? __builtin_amdgcn_exp2f(-more) : 1.0f;
+      ref += more;
+      begun |= seen;
+      sum *= shrink;
+#pragma unroll
+      for (int i = 0; i < G; ++i) o[i] *= shrink;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) x[b] -= more;
+      part = 0.0f;
+      all_of(kTwos, [&](auto k_c) { raise_two(k_c), keep_two(k_c); });
     }
-    const float fk = factors.x;
-    float fv = factors.y;
-    if (s + 1 < steps) issue(s + 1);
-    lds_barrier();
-
-    // ---- S^T, keys 16 j + 4 tile + i in register i of tile `tile`
-    f4 x[kTiles][4];
-#pragma unroll
-    for (int tile = 0; tile < 4; ++tile) {
-#pragma unroll
-      for (int c = 0; c < kTiles; ++c) x[c][tile] = f4{0, 0, 0, 0};
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        const h8 k8 = *reinterpret_cast<const h8*>(shared + ((tile * G + g) * 64 + lane) * 16);
-#pragma unroll
-        for (int c = 0; c < kTiles; ++c) x[c][tile] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k8, qf[c][g], x[c][tile], 0, 0, 0);
-      }
-    }
-#pragma unroll
-    for (int c = 0; c < kTiles; ++c) {
-      const float f = fk * rest[c];
-#pragma unroll
-      for (int tile = 0; tile < 4; ++tile)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[c][tile][i] = __builtin_fmaf(x[c][tile][i], f, -ref[c]);
-    }
-    const bool clear = key0 > clear0 && key0 + kStep - 1 <= clear1 && there == 15u;
-    if (!clear) {
-#pragma unroll
-      for (int c = 0; c < kTiles; ++c) {
-        const int at = pos[c] + 1 - base;
-        unsigned see = token_bits(p.window > 0 ? at - p.window : 0, there >> j & 1u ? at : 0);
-        asm volatile("" : "+v"(see));                 // (a branch, not selects in every step)
-#pragma unroll
-        for (int tile = 0; tile < 4; ++tile)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[c][tile][i] = see >> (4 * tile + i) & 1u ? x[c][tile][i] : -__builtin_inff();
-      }
-      // (a sixteen that no row sees: its factor may be anything)
-      if (!(there >> j & 1u) || base + 15 < t.seen || base >= last) fv = 0.0f;
-    }
-    bool grown;
-    const float down = scaled.grow(fv, &grown);
-    if (grown) {
-#pragma unroll
-      for (int c = 0; c < kTiles; ++c)
-#pragma unroll
-        for (int i = 0; i < CT; ++i) o[c][i] *= down;
-    }
-    const float weight = __builtin_amdgcn_ldexpf(fv, kLift - scaled.power);
-    // ---- probabilities
-    h8 pr[kTiles][2];
-#pragma unroll
-    for (int c = 0; c < kTiles; ++c) {
-      float m = x[c][0][0];
-#pragma unroll
-      for (int tile = 0; tile < 4; ++tile)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) m = fmaxf(m, x[c][tile][i]);
-      m = column_max(m);
-      if (__any(m > limit[c])) {                      // (the first keys that a column sees: no limit yet)
-        const bool begun = limit[c] > -__builtin_inff(), seen = m > -__builtin_inff();
-        const float more = begun ? fmaxf(m, 0.0f) : seen ? m : 0.0f;
-        const float shrink = begun ? __builtin_amdgcn_exp2f(-more) : 1.0f;
-        ref[c] += more;
-        if (seen) limit[c] = kSlack;
-        sum[c] *= shrink;
-#pragma unroll
-        for (int i = 0; i < CT; ++i) o[c][i] *= shrink;
-#pragma unroll
-        for (int tile = 0; tile < 4; ++tile)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[c][tile][i] -= more;
-      }
-#pragma unroll
-      for (int tile = 0; tile < 4; ++tile)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float e = __builtin_amdgcn_exp2f(x[c][tile][i]);
-          sum[c] += e;
-          pr[c][tile >> 1][(tile & 1) * 4 + i] = (_Float16)(e * weight);
+    sum += part;
+    add_values(s, [&](auto i_c) __attribute__((always_inline)) {
+      if constexpr (decltype(i_c)::value == 0) weigh();
+      share(i_c, integral_constant<int, 4 * PAIRS>{}, [&](auto k_c) __attribute__((always_inline)) {
+        constexpr int k = decltype(k_c)::value;
+        if constexpr (k < 2 * PAIRS) {
+          unpack_key(s + 2, integral_constant<int, k>{});
+          if constexpr (k % 2 == 1) issue_keys(k / 2);
+        } else {
+          unpack_value(s + 1, integral_constant<int, k - 2 * PAIRS>{});
+          if constexpr (k % 2 == 1) issue_values((k - 2 * PAIRS) / 2);
         }
-    }
-    // ---- O^T
-#pragma unroll
-    for (int i = 0; i < CT; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const h8 v8 = *reinterpret_cast<const h8*>(shared + W::OPERANDS + (i * 2 + h) * 1024 + lane * 16);
-#pragma unroll
-        for (int c = 0; c < kTiles; ++c) o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v8, pr[c][h], o[c][i], 0, 0, 0);
-      }
+      });
+      share(i_c, kTwos, scale_two);
+    });
+    hide(s + 1);
+    lds_barrier();
   }
-  const float back = two_to(scaled.power - kLift);
-  bool seen[kTiles];
+  // (a power that has grown for values behind the last step's)
+  const float back = two_to(scaled.power - kLift) * down;
+  f4 all[1][D / 8];
 #pragma unroll
-  for (int c = 0; c < kTiles; ++c) {
-    seen[c] = limit[c] > -__builtin_inff();
+  for (int i = 0; i < G; ++i)
 #pragma unroll
-    for (int i = 0; i < CT; ++i) o[c][i] *= back;
-  }
-  join_wide<D>(p, a, t, shared, out, o, ref, sum, seen);
+    for (int e = 0; e < 16; ++e) all[0][4 * i + (e >> 2)][e & 3] = o[i][e] * back;
+  const float refs[1] = {ref};
+  float sums[1] = {sum};
+  const bool seen[1] = {begun};
+  __syncthreads();
+  join_wide<D, kWaves, 32, 1>(p, a, t, shared, out, all, refs, sums, seen);
 #endif
 }
 
-// (what a cut tile needs of LDS: find_part's and join_wide's)
 template <int G, typename V>
 int launch(const AttendParams& p, const V* q, V* out, hipStream_t stream) {
-  constexpr size_t kJoin = (kWideParts + 1) * kWideCols * 4, kFind = 16 * 4 + 3 * kWaves * 4 + (3 * kMaxTiles + 1) * 4;
-  constexpr size_t kLds = Wide<G>::LDS > kJoin ? (Wide<G>::LDS > kFind ? Wide<G>::LDS : kFind) : kJoin;
+  constexpr size_t kJoin = (kWideParts + 1) * kWideCols * 4, kLds = Wide<G>::LDS > kJoin ? Wide<G>::LDS : kJoin;
   if constexpr (kLds > 65536) {
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_wide_kernel<G, V>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
