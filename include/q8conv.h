@@ -688,8 +688,8 @@ int q8_kv8_attend(const void *q_dev, int type, size_t T, int n_heads, int ratio,
 
 /* The pages of a cache, of any format.  Request b holds lengths[b] tokens (negative counts as 0, more than width * page as
  * that), on the first pages that row b of the table names; entries outside 0 .. n_pages - 1 are no pages.
- * n_pages <= 2^24 (Q8_EUNSUPPORTED); workspaces of q8_page_workspace_bytes (for up to so many new rows and pages; compact: 0
- * rows), 16-byte aligned, any contents.
+ * n_pages <= 2^24 (Q8_EUNSUPPORTED); workspaces of q8_page_workspace_bytes (for up to so many rows, old or new, and pages;
+ * compact: 0 rows), 16-byte aligned, any contents.
  *
  * q8_page_select: the requests that go on.  New request c is old request parents[c] (any other number: an empty request): its
  * length, and its row with -1 behind the pages that it holds.  Several of one parent share its full pages; of a last page that
@@ -708,9 +708,9 @@ int q8_kv8_attend(const void *q_dev, int type, size_t T, int n_heads, int ratio,
  * counts [4] (the third 0) as above.
  *
  * q8_page_copy: page `to` of a cache of n_pages pages of page_bytes bytes (a multiple of 16, 16-byte aligned) becomes page
- * `from`, for n_pairs pairs of them; a pair with a number that is no page is skipped.  No page is written by two pairs, or
+ * `from`, for n_pairs pairs of them (8-byte aligned); a pair with a number that is no page is skipped.  No page is written by two pairs, or
  * written by one and read by another.                                                     */
-size_t q8_page_workspace_bytes(int n_new, size_t n_pages);
+size_t q8_page_workspace_bytes(int n_rows, size_t n_pages);
 int q8_page_select(const int32_t *parents_dev, int n_new, const int32_t *lengths_dev,
                    const int32_t *table_dev, size_t table_stride, int n_requests, int width, int page,
                    size_t n_pages, int32_t *out_table_dev, size_t out_stride,

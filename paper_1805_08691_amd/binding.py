@@ -832,7 +832,7 @@ def page_select(parents, lengths, rows, page, n_pages, table=None, grown=None, f
     free_pages = torch.empty(n_pages, dtype=i32, device=dev) if free_pages is None else free_pages
     copies = torch.empty((m, 2), dtype=i32, device=dev) if copies is None else copies
     counts = torch.empty(4, dtype=i32, device=dev) if counts is None else counts
-    workspace = page_workspace(m, n_pages, dev) if workspace is None else workspace
+    workspace = page_workspace(max(m, lengths.numel()), n_pages, dev) if workspace is None else workspace
     _check(_q8call.page_select(parents, lengths, rows, page, n_pages, table, grown, free_pages, copies, counts, workspace))
     return dict(table=table, lengths=grown, free_pages=free_pages, copies=copies, counts=counts)
 

@@ -11,7 +11,7 @@ namespace {
 using namespace q8;
 
 constexpr int kMostPages = 1 << 24;
-constexpr int kBlockWords = 256;               // words of 32 pages that a block lists
+constexpr int kBlockWords = 64, kBlockPages = 32 * kBlockWords;        // words of 32 pages that a block lists
 
 struct PagesParams {
   const int* __restrict__ parents;             // null: row c goes on as row c
@@ -22,11 +22,13 @@ struct PagesParams {
   int* __restrict__ free_pages;
   int* __restrict__ copies;                    // [n_copies][2]
   int* __restrict__ counts;
-  unsigned* __restrict__ used;                 // [words]
-  int* __restrict__ before;                    // compact: of each word, pages in use before it
+  uint8_t* __restrict__ marks;                 // of each page, up to whole blocks of them: whether a row holds it
+  unsigned* __restrict__ used;                 // the same as bits, [blocks][kBlockWords]
+  unsigned* __restrict__ counts_of;            // and their number in each block
+  int* __restrict__ before;                    // compact: of each word, pages in use before it; select: parents' first rows
   unsigned* __restrict__ flags;                // select: of each new row, whether it needs a copy of its last page
   size_t stride, out_stride;
-  int n, m, shift, width, pool, words, n_copies;           // old rows, new rows; shift: page = 1 << shift tokens
+  int n, m, shift, width, pool, blocks, n_copies;          // old rows, new rows; shift: page = 1 << shift tokens
 };
 
 __device__ __forceinline__ int length_of(const PagesParams& p, int b) {
@@ -36,33 +38,61 @@ __device__ __forceinline__ int pages_of(const PagesParams& p, int tokens) {
   return (int)(((long)tokens + (1 << p.shift) - 1) >> p.shift);
 }
 
-// Sum over a block of 256.
-__device__ __forceinline__ long block_sum(long v, long (&sums)[4]) {
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (sums[0] + sums[1]) + (sums[2] + sums[3]);
-}
-// Sums before a thread, and of the block of 256.
-__device__ __forceinline__ unsigned block_scan(unsigned v, unsigned (&sums)[4], unsigned* total) {
-  const unsigned upto = scan64(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = upto;
-  __syncthreads();
-  unsigned base = 0;
-  for (unsigned w = 0; w < threadIdx.x >> 6; ++w) base += sums[w];
-  *total = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-  return base + upto - v;
+// Sums before a thread of a block of WAVES wavefronts, and of the block.
+template <int WAVES>
+__device__ __forceinline__ unsigned block_scan(unsigned v, unsigned (&sums)[WAVES], unsigned* total) {
+  const unsigned upto = scan64(v), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  lds_barrier();                                           // the sums of a scan before have been read
+  if (lane == 63) sums[wave] = upto;
+  lds_barrier();
+  const unsigned waves = scan64(lane < WAVES ? sums[lane] : 0u);
+  *total = __builtin_amdgcn_readlane(waves, WAVES - 1);
+  return upto - v + (wave ? __shfl(waves, wave - 1, 64) : 0u);
 }
 
-__global__ __launch_bounds__(256) void pages_clear_kernel(unsigned* used, int words) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i < words) used[i] = 0;
+// Pages in use, of all blocks and of those in front of block `end`, for every thread of a block of 256.
+__device__ __forceinline__ void count_used(const PagesParams& p, int end, unsigned (&sums)[4], int* all, int* front) {
+  unsigned n = 0, m = 0, total;
+  for (int i = threadIdx.x; i < p.blocks; i += 256) {
+    const unsigned c = p.counts_of[i];
+    n += c;
+    if (i < end) m += c;
+  }
+  block_scan(n, sums, &total);
+  *all = (int)total;
+  block_scan(m, sums, &total);
+  *front = (int)total;
+}
+
+__global__ __launch_bounds__(256) void pages_clear_kernel(uint4* marks, size_t n_marks, int* first, int n) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n_marks) marks[i] = uint4{0, 0, 0, 0};
+  if (i < (size_t)n) first[i] = 0x7fffffff;
+}
+// Marks to bits and their numbers: eight pages a thread.
+__global__ __launch_bounds__(256) void pages_count_kernel(const PagesParams p) {
+  __shared__ unsigned sums[4];
+  const uint2 m = reinterpret_cast<const uint2*>(p.marks)[blockIdx.x * 256 + threadIdx.x];
+  // (bytes of 0 or 1: bit 0 of each to the upper byte, in order)
+  const unsigned bits = (m.x * 0x10204080u >> 28) | (m.y * 0x10204080u >> 28 << 4);
+  unsigned word = bits << (8 * (threadIdx.x & 3)), total;
+  word |= __shfl_xor(word, 1, 64);
+  word |= __shfl_xor(word, 2, 64);
+  if ((threadIdx.x & 3) == 0) p.used[blockIdx.x * kBlockWords + threadIdx.x / 4] = word;
+  block_scan(__popc(bits), sums, &total);
+  if (threadIdx.x == 0) p.counts_of[blockIdx.x] = total;
+}
+
+// The first new row of each parent, where rows are so many that looking through them all for every one takes longer.
+__global__ __launch_bounds__(256) void select_first_kernel(const PagesParams p) {
+  const int c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= p.m) return;
+  const int parent = p.parents[c];
+  if (parent >= 0 && parent < p.n) atomicMin(&p.before[parent], c);
 }
 
 __device__ __forceinline__ void mark(const PagesParams& p, int page) {
-  if (page >= 0 && page < p.pool) atomicOr(&p.used[page >> 5], 1u << (page & 31));
+  if (page >= 0 && page < p.pool) p.marks[page] = 1;
 }
 
 // A wavefront takes a new row: its parent's places, whose pages are in use.  Of several rows of a parent, the first has its
@@ -72,15 +102,38 @@ __global__ __launch_bounds__(256) void select_rows_kernel(const PagesParams p) {
   if (c >= p.m) return;
   const int parent = p.parents[c];
   const bool given = parent >= 0 && parent < p.n;
-  bool again = false;
-  for (int i = 0; given && i < c && !again; i += 64) again = __any(i + lane < c && p.parents[i + lane] == parent);
   const int len = given ? length_of(p, parent) : 0, held = pages_of(p, len);
   const int* const from = p.table + (given ? parent : 0) * p.stride;
   int* const to = p.out_table + c * p.out_stride;
-  for (int i = lane; i < p.width; i += 64) {
-    const int page = i < held ? from[i] : -1;
-    to[i] = page;
-    if (!again) mark(p, page);
+  constexpr int kAhead = 4;                                // places of a lane that are on their way during the search
+  int page[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) page[u] = u * 64 + lane < held ? from[u * 64 + lane] : -1;
+  bool again = false;
+  if (given && p.before) {
+    again = p.before[parent] < c;
+  } else if (given) {
+    constexpr int kBatch = 16;
+    for (int i0 = 0; i0 < c; i0 += 64 * kBatch) {
+      int v[kBatch];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) v[u] = i0 + u * 64 + lane < c ? p.parents[i0 + u * 64 + lane] : -1;
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) again |= v[u] == parent;
+    }
+    again = __any(again);
+  }
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u)
+    if (u * 64 + lane < p.width) {
+      to[u * 64 + lane] = page[u];
+      if (!again) mark(p, page[u]);
+    }
+#pragma unroll 4
+  for (int i = kAhead * 64 + lane; i < p.width; i += 64) {
+    const int x = i < held ? from[i] : -1;
+    to[i] = x;
+    if (!again) mark(p, x);
   }
   if (lane == 0) {
     p.out_lengths[c] = len;
@@ -89,64 +142,209 @@ __global__ __launch_bounds__(256) void select_rows_kernel(const PagesParams p) {
 }
 
 // Free pages in order: the first of them become copies, of the rows that need one in their order; the others are listed.  Rows
-// that find none become empty.
+// that find none become empty.  A block lists kBlockPages pages; every block adds up all blocks and rows for itself.
 __global__ __launch_bounds__(256) void select_free_kernel(const PagesParams p) {
-  __shared__ long sums[4];
-  __shared__ unsigned scans[4];
-  __shared__ int list[kBlockWords * 32];
-  const int tid = threadIdx.x, word0 = blockIdx.x * kBlockWords;
-  long all = 0, mine = 0, needed = 0;
-  for (int i = tid; i < p.words; i += 256) {
-    const int n = 32 - __popc(p.used[i]) - max(0, 32 * (i + 1) - p.pool);      // (bits behind the pool are never set)
-    all += n;
-    if (i < word0) mine += n;
+  __shared__ unsigned sums[4], ranks[kBlockWords], words[kBlockWords];
+  __shared__ int list[kBlockPages], rows[kBlockPages];
+  const int tid = threadIdx.x, page0 = blockIdx.x * kBlockPages;
+  // ---- rows that need a copy: those of this thread, one after the other
+  const int each = (p.m + 255) / 256, row0 = tid * each, row1 = min(row0 + each, p.m);
+  unsigned flags = 0;
+  unsigned long which = 0;                                 // of the first 64
+#pragma unroll 8
+  for (int c = row0; c < row1; ++c) {
+    const unsigned flag = p.flags[c];
+    flags += flag;
+    if (c - row0 < 64) which |= (unsigned long)flag << (c - row0);
   }
-  for (int i = tid; i < p.m; i += 256) needed += p.flags[i];
-  const int n_free = (int)block_sum(all, sums), first = (int)block_sum(mine, sums), n_needed = (int)block_sum(needed, sums);
-  const int taken = min(n_needed, n_free);
+  unsigned bits = tid < kBlockWords && blockIdx.x < p.blocks ? p.used[blockIdx.x * kBlockWords + tid] : 0xffffffffu;
+  int used, used_before;
+  count_used(p, blockIdx.x, sums, &used, &used_before);
+  unsigned needed;
+  int rank = (int)block_scan(flags, sums, &needed);
+  const int n_free = p.pool - used, n_needed = (int)needed, taken = min(n_needed, n_free), first = page0 - used_before;
   // ---- this block's free pages
-  unsigned bits = 0;
-  if (word0 + tid < p.words) {
-    bits = ~p.used[word0 + tid];
-    const int behind = 32 * (word0 + tid + 1) - p.pool;
-    if (behind > 0) bits &= 0xffffffffu >> behind;
-  }
+  const int behind = page0 + 32 * (tid + 1) - p.pool;
+  bits = behind >= 32 ? 0 : behind > 0 ? ~bits & 0xffffffffu >> behind : ~bits;
   unsigned here;
-  int at = (int)block_scan(__popc(bits), scans, &here);
+  const unsigned before = block_scan(__popc(bits), sums, &here);
+  if (tid < kBlockWords) ranks[tid] = before, words[tid] = bits;
   const int end = first + (int)here;
-  for (; bits; bits &= bits - 1, ++at) {
-    const int page = 32 * (word0 + tid) + __builtin_ctz(bits);
-    list[at] = page;
+  lds_barrier();
+#pragma unroll
+  for (int i = tid; i < kBlockPages; i += 256) {
+    const unsigned word = words[i >> 5], e = i & 31;
+    if (!(word >> e & 1u)) continue;
+    const int at = (int)ranks[i >> 5] + __popc(word & ((1u << e) - 1u)), page = page0 + i;
     if (first + at >= taken) p.free_pages[first + at - taken] = page;
+    else list[at] = page;
   }
-  __syncthreads();
+  lds_barrier();
   // ---- places behind the last of the lists
-  for (int i = word0 * 32 + tid; i < min((word0 + kBlockWords) * 32, p.pool); i += 256)
+  for (int i = page0 + tid; i < min(page0 + kBlockPages, p.pool); i += 256)
     if (i >= n_free - taken) p.free_pages[i] = -1;
   for (int i = blockIdx.x * 256 + tid; i < p.m; i += gridDim.x * 256)
     if (i >= taken) p.copies[2 * i] = -1, p.copies[2 * i + 1] = -1;
-  if (blockIdx.x == 0 && tid == 0) {
+  if (blockIdx.x == 0 && tid == 0)
     p.counts[0] = n_free - taken, p.counts[1] = taken, p.counts[2] = n_needed - taken, p.counts[3] = p.pool - n_free + taken;
-  }
-  // ---- rows that need a copy: of rank first .. end - 1 here; the last block empties those behind the last free page
+  // ---- copies of rank first .. end - 1 are here, a row to a thread; the last block empties the rows behind the last free page
   const bool empties = blockIdx.x == gridDim.x - 1 && n_needed > n_free;
   if (first >= taken && !empties) return;
-  int rank0 = 0;
-  for (int c0 = 0; c0 < p.m; c0 += 256) {
-    const int c = c0 + tid;
-    const unsigned flag = c < p.m ? p.flags[c] : 0;
-    unsigned n;
-    const int rank = rank0 + (int)block_scan(flag, scans, &n);
-    if (flag && rank >= first && rank < end && rank < taken) {
-      int* const entry = p.out_table + c * p.out_stride + pages_of(p, p.out_lengths[c]) - 1;
-      p.copies[2 * rank] = *entry;
-      *entry = p.copies[2 * rank + 1] = list[rank - first];
+  for (int i = 0; flags && i < row1 - row0; ++i) {
+    if (i < 64 ? !(which >> i & 1ul) : !p.flags[row0 + i]) continue;
+    if (rank >= first && rank < end && rank < taken) rows[rank - first] = row0 + i;
+    if (empties && rank >= n_free) {
+      for (int col = 0; col < p.width; ++col) p.out_table[(row0 + i) * p.out_stride + col] = -1;
+      p.out_lengths[row0 + i] = 0;
     }
-    if (flag && empties && rank >= n_free) {
-      for (int i = 0; i < p.width; ++i) p.out_table[c * p.out_stride + i] = -1;
-      p.out_lengths[c] = 0;
+    ++rank;
+  }
+  lds_barrier();
+  for (int i = tid; i < min(end, taken) - first; i += 256) {
+    const int c = rows[i];
+    int* const entry = p.out_table + c * p.out_stride + pages_of(p, p.out_lengths[c]) - 1;
+    p.copies[2 * (first + i)] = *entry;
+    *entry = p.copies[2 * (first + i) + 1] = list[i];
+  }
+}
+
+// Both for tables of few places, in one launch of one block: a row to a thread, and kFewPlaces of the tables' places, of any
+// row, which it keeps in registers.  Bound by three dependent trips to memory and the barriers of the sums.
+constexpr int kFewRows = 1024, kFewPlaces = 16, kFewWords = 4096;
+struct Few {
+  int parent[kFewRows];                        // select: of new row c; -1: none, or none that holds pages
+  int held[kFewRows];                          // pages of new row c, or (again) minus them
+  unsigned used[kFewWords];
+  int before[kFewWords];                       // pages in use before a word
+  int list[kFewRows * kFewPlaces];             // select: free pages for copies; compact: where pages go, by rank
+  unsigned sums[16];
+};
+inline bool few(int rows, int width, size_t n_pages) {
+  return rows <= kFewRows && (size_t)rows * width <= (size_t)kFewRows * kFewPlaces && n_pages <= (size_t)kFewWords * 32;
+}
+
+template <bool SELECT>
+__global__ __launch_bounds__(1024) void pages_few_kernel(const PagesParams p) {
+  extern __shared__ __attribute__((aligned(16))) char shared[];
+  Few& s = *reinterpret_cast<Few*>(shared);
+  const int tid = threadIdx.x;
+  for (int i = tid; i < kFewWords; i += 1024) s.used[i] = 0;
+  int parent = -1, len = 0, held = 0;
+  if (tid < p.m) {
+    parent = SELECT ? p.parents[tid] : tid;
+    if (parent < 0 || parent >= p.n) parent = -1;
+    len = parent >= 0 ? length_of(p, parent) : 0;
+    held = pages_of(p, len);
+    s.parent[tid] = parent;
+  }
+  bool again = false;
+  if constexpr (SELECT) {
+    lds_barrier();
+    if (parent >= 0)
+      for (int i = 0; i < tid; ++i) again |= s.parent[i] == parent;
+  }
+  if (tid < p.m) s.held[tid] = again ? -held : held;
+  lds_barrier();
+  // ---- the places: what they name is in use (once for all rows of a parent)
+  const int all = p.m * p.width;
+  int page[kFewPlaces];
+#pragma unroll
+  for (int u = 0; u < kFewPlaces; ++u) {
+    const int i = u * 1024 + tid, c = i / max(p.width, 1), col = i - c * p.width;
+    page[u] = -1;
+    if (i < all && col < abs(s.held[c])) page[u] = p.table[s.parent[c] * p.stride + col];
+  }
+#pragma unroll
+  for (int u = 0; u < kFewPlaces; ++u) {
+    const int i = u * 1024 + tid;
+    if (page[u] >= 0 && page[u] < p.pool && s.held[i / max(p.width, 1)] > 0)
+      atomicOr(&s.used[page[u] >> 5], 1u << (page[u] & 31));
+  }
+  lds_barrier();
+  // ---- ranks: kFewWords / 1024 neighbouring words a thread
+  constexpr int kWords = kFewWords / 1024;
+  unsigned bits[kWords], n = 0, used;
+#pragma unroll
+  for (int u = 0; u < kWords; ++u) {
+    bits[u] = s.used[tid * kWords + u];
+    n += __popc(bits[u]);
+  }
+  int rank = (int)block_scan(n, s.sums, &used);
+#pragma unroll
+  for (int u = 0; u < kWords; ++u) {
+    s.before[tid * kWords + u] = rank;
+    rank += __popc(bits[u]);
+  }
+  lds_barrier();
+  if constexpr (SELECT) {
+    const bool flag = again && (len & ((1 << p.shift) - 1));
+    unsigned needed;
+    const int place = (int)block_scan(flag ? 1u : 0u, s.sums, &needed);
+    const int n_free = p.pool - (int)used, taken = min((int)needed, n_free);
+    // ---- free pages
+    for (int i = tid; i < p.pool; i += 1024) {
+      const unsigned word = s.used[i >> 5], e = i & 31;
+      if (word >> e & 1u) continue;
+      const int at = i - s.before[i >> 5] - __popc(word & ((1u << e) - 1u));
+      if (at < taken) s.list[at] = i;
+      else p.free_pages[at - taken] = i;
     }
-    rank0 += (int)n;
+    for (int i = n_free - taken + tid; i < p.pool; i += 1024) p.free_pages[i] = -1;
+    for (int i = taken + tid; i < p.m; i += 1024) p.copies[2 * i] = -1, p.copies[2 * i + 1] = -1;
+    lds_barrier();
+    // ---- rows that need a copy: its place among them, or (behind the last free page) none of the row
+    if (tid < p.m) {
+      const bool out = flag && place >= taken;
+      p.out_lengths[tid] = out ? 0 : len;
+      s.held[tid] = out ? 0 : held;
+      s.parent[tid] = flag && !out ? place : -1;
+    }
+    if (tid == 0) p.counts[0] = n_free - taken, p.counts[1] = taken, p.counts[2] = (int)needed - taken, p.counts[3] = p.pool - n_free + taken;
+    lds_barrier();
+#pragma unroll
+    for (int u = 0; u < kFewPlaces; ++u) {
+      const int i = u * 1024 + tid;
+      if (i >= all) continue;
+      const int c = i / p.width, col = i - c * p.width, place = s.parent[c];
+      int x = col < s.held[c] ? page[u] : -1;
+      if (place >= 0 && col == s.held[c] - 1) {
+        p.copies[2 * place] = x;
+        x = p.copies[2 * place + 1] = s.list[place];
+      }
+      p.out_table[c * p.out_stride + col] = x;
+    }
+  } else {
+    const int k = (int)used;
+    unsigned n_front = 0, stay;                            // in use in front of k: they stay
+#pragma unroll
+    for (int u = 0; u < kWords; ++u) {
+      const int left = k - 32 * (tid * kWords + u);
+      n_front += left >= 32 ? __popc(bits[u]) : left > 0 ? __popc(bits[u] & ((1u << left) - 1u)) : 0;
+    }
+    block_scan(n_front, s.sums, &stay);
+    const int moves = k - (int)stay;
+    for (int i = tid; i < p.pool; i += 1024) {
+      const unsigned word = s.used[i >> 5], e = i & 31;
+      const int before = s.before[i >> 5] + __popc(word & ((1u << e) - 1u));
+      p.free_pages[i] = k + i < p.pool ? k + i : -1;
+      if (word >> e & 1u) {
+        if (i >= k) p.copies[2 * (before - (int)stay)] = i;
+      } else if (i < k) {
+        p.copies[2 * (i - before) + 1] = s.list[i - before] = i;
+      }
+    }
+    for (int i = moves + tid; i < p.n_copies; i += 1024) p.copies[2 * i] = -1, p.copies[2 * i + 1] = -1;
+    if (tid == 0) p.counts[0] = p.pool - k, p.counts[1] = moves, p.counts[2] = 0, p.counts[3] = k;
+    lds_barrier();
+#pragma unroll
+    for (int u = 0; u < kFewPlaces; ++u) {
+      const int i = u * 1024 + tid;
+      if (i >= all) continue;
+      const int c = i / p.width, col = i - c * p.width;
+      int x = page[u];
+      if (x >= k && x < p.pool) x = s.list[s.before[x >> 5] + __popc(s.used[x >> 5] & ((1u << (x & 31)) - 1u)) - (int)stay];
+      p.out_table[c * p.out_stride + col] = x;
+    }
   }
 }
 
@@ -159,34 +357,35 @@ __global__ __launch_bounds__(256) void compact_mark_kernel(const PagesParams p) 
 
 // Of the k pages in use, those at k and behind go to the free ones in front of k, both in ascending order.
 __global__ __launch_bounds__(256) void compact_list_kernel(const PagesParams p) {
-  __shared__ long sums[4];
-  __shared__ unsigned scans[4];
-  const int tid = threadIdx.x, word0 = blockIdx.x * kBlockWords;
-  long all = 0, mine = 0;
-  for (int i = tid; i < p.words; i += 256) {
-    const int n = __popc(p.used[i]);
-    all += n;
-    if (i < word0) mine += n;
+  __shared__ unsigned sums[4], ranks[kBlockWords], words[kBlockWords];
+  const int tid = threadIdx.x, page0 = blockIdx.x * kBlockPages;
+  const unsigned bits = tid < kBlockWords && blockIdx.x < p.blocks ? p.used[blockIdx.x * kBlockWords + tid] : 0;
+  int k, first, front;
+  count_used(p, blockIdx.x, sums, &k, &first);
+  // in use in front of k: they stay
+  const int of = k / kBlockPages, left = k - of * kBlockPages - 32 * tid;        // (of k's block, to this thread's word)
+  count_used(p, of, sums, &front, &front);
+  unsigned n = 0, here, more;
+  if (tid < kBlockWords && of < p.blocks && left > 0) n = p.used[of * kBlockWords + tid];
+  block_scan(__popc(left >= 32 ? n : n & ((1u << max(left, 0)) - 1u)), sums, &more);
+  const int stay = front + (int)more, moves = k - stay;
+  const int rank = first + (int)block_scan(__popc(bits), sums, &here);
+  if (tid < kBlockWords) {
+    if (blockIdx.x < p.blocks) p.before[blockIdx.x * kBlockWords + tid] = rank;
+    ranks[tid] = (unsigned)rank, words[tid] = bits;
   }
-  const int k = (int)block_sum(all, sums), first = (int)block_sum(mine, sums);
-  long front = 0;                                          // in use in front of k: they stay
-  for (int i = tid; i <= k >> 5 && i < p.words; i += 256)
-    front += __popc(i < k >> 5 ? p.used[i] : p.used[i] & ((1u << (k & 31)) - 1u));
-  const int stay = (int)block_sum(front, sums), moves = k - stay;
-  const unsigned bits = word0 + tid < p.words ? p.used[word0 + tid] : 0;
-  unsigned here;
-  int rank = first + (int)block_scan(__popc(bits), scans, &here);
-  if (word0 + tid < p.words) p.before[word0 + tid] = rank;
-  for (int e = 0; e < 32; ++e) {
-    const int page = 32 * (word0 + tid) + e;
+  lds_barrier();
+#pragma unroll
+  for (int i = tid; i < kBlockPages; i += 256) {
+    const unsigned word = words[i >> 5], e = i & 31;
+    const int page = page0 + i, before = (int)ranks[i >> 5] + __popc(word & ((1u << e) - 1u));
     if (page >= p.pool) break;
-    if (bits >> e & 1u) {
-      if (page >= k) p.copies[2 * (rank - stay)] = page;
-      ++rank;
-    } else if (page < k) {
-      p.copies[2 * (page - rank) + 1] = page;
-    }
     p.free_pages[page] = k + page < p.pool ? k + page : -1;
+    if (word >> e & 1u) {
+      if (page >= k) p.copies[2 * (before - stay)] = page;
+    } else if (page < k) {
+      p.copies[2 * (page - before) + 1] = page;
+    }
   }
   for (int i = blockIdx.x * 256 + tid; i < p.n_copies; i += gridDim.x * 256)
     if (i >= moves) p.copies[2 * i] = -1, p.copies[2 * i + 1] = -1;
@@ -207,29 +406,52 @@ __global__ __launch_bounds__(256) void compact_rows_kernel(const PagesParams p) 
   }
 }
 
-// A block copies 16 KB of a page at a time, from the pairs in turn.
-constexpr size_t kCopyBytes = 16384;
+// A block copies 4 KB of a page at a time, 16 bytes a thread, from the pairs in turn.  (16 KB a block, four loads a thread behind a
+// test each: 1500 pages of 17 KB 24 us instead of 10.)
+constexpr size_t kCopyBytes = 4096;
+constexpr unsigned kCopyBlocks = 8192;
 __global__ __launch_bounds__(256) void page_copy_kernel(char* __restrict__ cache, size_t page_bytes, int pool,
-                                                        const int* __restrict__ pairs, size_t items, int chunks) {
+                                                        const int2* __restrict__ pairs, size_t items, int chunks) {
   for (size_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const size_t pair = item / chunks;
-    const size_t at = (item - pair * chunks) * kCopyBytes + threadIdx.x * 16;
-    const int from = pairs[2 * pair], to = pairs[2 * pair + 1];
-    if (from < 0 || from >= pool || to < 0 || to >= pool || from == to) continue;
-    const char* const src = cache + from * page_bytes;
-    char* const dst = cache + to * page_bytes;
-    uint4 v[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (at + u * 4096 < page_bytes) v[u] = *reinterpret_cast<const uint4*>(src + at + u * 4096);
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (at + u * 4096 < page_bytes) *reinterpret_cast<uint4*>(dst + at + u * 4096) = v[u];
+    const size_t pair = item / (unsigned)chunks, at = (item - pair * chunks) * kCopyBytes + threadIdx.x * 16;
+    const int2 of = pairs[pair];
+    if (of.x < 0 || of.x >= pool || of.y < 0 || of.y >= pool || of.x == of.y || at >= page_bytes) continue;
+    *reinterpret_cast<uint4*>(cache + of.y * page_bytes + at) = *reinterpret_cast<const uint4*>(cache + of.x * page_bytes + at);
   }
 }
 
 size_t round_up(size_t a, size_t b) { return (a + b - 1) / b * b; }
-size_t words_of(size_t n_pages) { return (n_pages + 31) / 32; }
+size_t blocks_of(size_t n_pages) { return (n_pages + kBlockPages - 1) / kBlockPages; }
+// Workspace: marks, bits, numbers in front of words, of blocks; rows' flags, and their parents' first rows.
+struct Space {
+  size_t used, before, counts, flags, first, bytes;
+  Space(size_t rows, size_t n_pages) {
+    const size_t blocks = blocks_of(n_pages), words = blocks * kBlockWords * 4;
+    used = blocks * kBlockPages, before = used + words, counts = before + words;
+    flags = counts + round_up(blocks * 4, 256), first = flags + round_up(rows * 4, 256);
+    bytes = first + round_up(rows * 4, 256);
+  }
+  void set(PagesParams* p, void* workspace) const {
+    char* const at = static_cast<char*>(workspace);
+    p->marks = reinterpret_cast<uint8_t*>(at);
+    p->used = reinterpret_cast<unsigned*>(at + used);
+    p->before = reinterpret_cast<int*>(at + before);
+    p->counts_of = reinterpret_cast<unsigned*>(at + counts);
+    p->flags = reinterpret_cast<unsigned*>(at + flags);
+  }
+};
+
+// More new rows than this have their parents' first ones found by a launch of its own.
+constexpr int kSearched = 4096;
+
+template <bool SELECT>
+int launch_few(const PagesParams& p, hipStream_t stream) {
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&pages_few_kernel<SELECT>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Few));
+  if (attr != hipSuccess) return Q8_EHIP;
+  pages_few_kernel<SELECT><<<1, 1024, sizeof(Few), stream>>>(p);
+  return q8_launch_status();
+}
 
 // Whether two tables of n and m rows, `width` entries each, have places in common.
 bool overlap(const int* a, int n, size_t a_stride, const int* b, int m, size_t b_stride, int width) {
@@ -242,7 +464,7 @@ bool overlap(const int* a, int n, size_t a_stride, const int* b, int m, size_t b
 
 extern "C" size_t q8_page_workspace_bytes(int n_rows, size_t n_pages) {
   if (n_rows < 0 || n_pages > (size_t)kMostPages) return 0;
-  return round_up(words_of(n_pages) * 4, 256) + round_up((words_of(n_pages) > (size_t)n_rows ? words_of(n_pages) : n_rows) * 4, 256);
+  return Space(n_rows, n_pages).bytes;
 }
 
 extern "C" int q8_page_select(const int32_t* parents_dev, int n_new, const int32_t* lengths_dev, const int32_t* table_dev,
@@ -252,7 +474,7 @@ extern "C" int q8_page_select(const int32_t* parents_dev, int n_new, const int32
                               void* stream) {
   Q8_REQUIRE(n_new >= 0 && n_requests >= 0 && width >= 0, Q8_EINVAL);
   Q8_REQUIRE(kv4_page_ok(page) && n_pages <= (size_t)kMostPages && (size_t)width * page <= 0x7fff0000u, Q8_EUNSUPPORTED);
-  Q8_REQUIRE(counts_dev && (workspace || n_pages + n_new == 0) && (n_pages == 0 || free_pages_dev), Q8_EINVAL);
+  Q8_REQUIRE(counts_dev && (workspace || n_pages + n_new + n_requests == 0) && (n_pages == 0 || free_pages_dev), Q8_EINVAL);
   Q8_REQUIRE(n_new == 0 || (parents_dev && out_lengths_dev && copies_dev && (out_table_dev || width == 0)), Q8_EINVAL);
   Q8_REQUIRE(n_requests == 0 || (lengths_dev && (table_dev || width == 0)), Q8_EINVAL);
   Q8_REQUIRE(table_stride >= (size_t)width && out_stride >= (size_t)width, Q8_EINVAL);
@@ -261,19 +483,26 @@ extern "C" int q8_page_select(const int32_t* parents_dev, int n_new, const int32
   Q8_REQUIRE(q8_aligned(parents_dev, 4) && q8_aligned(lengths_dev, 4) && q8_aligned(table_dev, 4) &&
                  q8_aligned(out_table_dev, 4) && q8_aligned(out_lengths_dev, 4) && q8_aligned(free_pages_dev, 4) &&
                  q8_aligned(copies_dev, 4) && q8_aligned(counts_dev, 4) && q8_aligned(workspace, 16), Q8_EALIGN);
-  Q8_REQUIRE(workspace_bytes >= q8_page_workspace_bytes(n_new, n_pages), Q8_EWORKSPACE);
+  Q8_REQUIRE(workspace_bytes >= q8_page_workspace_bytes(n_new > n_requests ? n_new : n_requests, n_pages), Q8_EWORKSPACE);
   PagesParams p{};
   p.parents = parents_dev, p.lengths = lengths_dev, p.table = table_dev, p.out_table = out_table_dev;
   p.out_lengths = out_lengths_dev, p.free_pages = free_pages_dev, p.copies = copies_dev, p.counts = counts_dev;
-  p.used = static_cast<unsigned*>(workspace);
-  p.flags = p.used + round_up(words_of(n_pages) * 4, 256) / 4;
+  const Space space(n_new > n_requests ? n_new : n_requests, n_pages);
+  space.set(&p, workspace);
+  p.before = n_new > kSearched ? reinterpret_cast<int*>(static_cast<char*>(workspace) + space.first) : nullptr;
   p.stride = table_stride, p.out_stride = out_stride;
   p.n = n_requests, p.m = n_new, p.shift = __builtin_ctz(page), p.width = width, p.pool = (int)n_pages;
-  p.words = (int)words_of(n_pages), p.n_copies = n_new;
+  p.blocks = (int)blocks_of(n_pages), p.n_copies = n_new;
   const hipStream_t s = (hipStream_t)stream;
-  if (p.words) pages_clear_kernel<<<(p.words + 255) / 256, 256, 0, s>>>(p.used, p.words);
+  if (few(n_new, width, n_pages)) return launch_few<true>(p, s);
+  const size_t marks = (size_t)p.blocks * kBlockPages / 16, first = p.before ? n_requests : 0;
+  if (marks || first)
+    pages_clear_kernel<<<(unsigned)(((marks > first ? marks : first) + 255) / 256), 256, 0, s>>>(
+        reinterpret_cast<uint4*>(p.marks), marks, p.before, (int)first);
+  if (p.before) select_first_kernel<<<(unsigned)(((size_t)n_new + 255) / 256), 256, 0, s>>>(p);
   if (n_new) select_rows_kernel<<<(unsigned)(((size_t)n_new + 3) / 4), 256, 0, s>>>(p);
-  select_free_kernel<<<p.words ? (p.words + kBlockWords - 1) / kBlockWords : 1, 256, 0, s>>>(p);
+  if (p.blocks) pages_count_kernel<<<p.blocks, 256, 0, s>>>(p);
+  select_free_kernel<<<p.blocks ? p.blocks : 1, 256, 0, s>>>(p);
   return q8_launch_status();
 }
 
@@ -295,16 +524,18 @@ extern "C" int q8_page_compact(const int32_t* lengths_dev, const int32_t* table_
   PagesParams p{};
   p.lengths = lengths_dev, p.table = table_dev, p.out_table = out_table_dev;
   p.free_pages = free_pages_dev, p.copies = copies_dev, p.counts = counts_dev;
-  p.used = static_cast<unsigned*>(workspace);
-  p.before = static_cast<int*>(workspace) + round_up(words_of(n_pages) * 4, 256) / 4;
+  Space(0, n_pages).set(&p, workspace);
   p.stride = table_stride, p.out_stride = out_stride;
   p.n = p.m = n_requests, p.shift = __builtin_ctz(page), p.width = width, p.pool = (int)n_pages;
-  p.words = (int)words_of(n_pages), p.n_copies = (int)(n_pages / 2);
+  p.blocks = (int)blocks_of(n_pages), p.n_copies = (int)(n_pages / 2);
   const hipStream_t s = (hipStream_t)stream;
+  if (few(n_requests, width, n_pages)) return launch_few<false>(p, s);
   const unsigned rows = (unsigned)(((size_t)n_requests + 3) / 4);
-  if (p.words) pages_clear_kernel<<<(p.words + 255) / 256, 256, 0, s>>>(p.used, p.words);
+  const size_t marks = (size_t)p.blocks * kBlockPages / 16;
+  if (marks) pages_clear_kernel<<<(unsigned)((marks + 255) / 256), 256, 0, s>>>(reinterpret_cast<uint4*>(p.marks), marks, nullptr, 0);
   if (rows) compact_mark_kernel<<<rows, 256, 0, s>>>(p);
-  compact_list_kernel<<<p.words ? (p.words + kBlockWords - 1) / kBlockWords : 1, 256, 0, s>>>(p);
+  if (p.blocks) pages_count_kernel<<<p.blocks, 256, 0, s>>>(p);
+  compact_list_kernel<<<p.blocks ? p.blocks : 1, 256, 0, s>>>(p);
   if (rows) compact_rows_kernel<<<rows, 256, 0, s>>>(p);
   return q8_launch_status();
 }
@@ -315,9 +546,9 @@ extern "C" int q8_page_copy(void* cache_dev, size_t n_pages, size_t page_bytes, 
   Q8_REQUIRE(n_pages <= 0x7fffffffu && page_bytes < (size_t)1 << 40, Q8_EUNSUPPORTED);
   if (n_pairs == 0 || n_pages == 0 || page_bytes == 0) return Q8_OK;
   Q8_REQUIRE(cache_dev && pairs_dev, Q8_EINVAL);
-  Q8_REQUIRE(q8_aligned(cache_dev, 16) && page_bytes % 16 == 0 && q8_aligned(pairs_dev, 4), Q8_EALIGN);
+  Q8_REQUIRE(q8_aligned(cache_dev, 16) && page_bytes % 16 == 0 && q8_aligned(pairs_dev, 8), Q8_EALIGN);
   const size_t chunks = (page_bytes + kCopyBytes - 1) / kCopyBytes, items = chunks * n_pairs;
-  page_copy_kernel<<<(unsigned)(items < 4096 ? items : 4096), 256, 0, (hipStream_t)stream>>>(
-      static_cast<char*>(cache_dev), page_bytes, (int)n_pages, pairs_dev, items, (int)chunks);
+  page_copy_kernel<<<(unsigned)(items < kCopyBlocks ? items : kCopyBlocks), 256, 0, (hipStream_t)stream>>>(
+      static_cast<char*>(cache_dev), page_bytes, (int)n_pages, reinterpret_cast<const int2*>(pairs_dev), items, (int)chunks);
   return q8_launch_status();
 }

@@ -160,7 +160,7 @@ def pages_held(tokens, page, width):
 def select(parents, lengths, table, page, n_pages):
     n, width = table.shape
     out = np.full((len(parents), width), -1, np.int32)
-    lens, used, wants = [], set(), []
+    lens, used, wants, seen = [], set(), [], set()
     for c, b in enumerate(parents):
         if not 0 <= b < n:
             lens.append(0)
@@ -169,13 +169,14 @@ def select(parents, lengths, table, page, n_pages):
         held = pages_held(length, page, width)
         lens.append(length)
         out[c, :held] = table[b, :held]
-        if b in parents[:c]:
+        if b in seen:
             if length % page:
                 wants.append(c)
         else:
             used.update(int(x) for x in table[b, :held] if 0 <= x < n_pages)
+        seen.add(b)
     free = [x for x in range(n_pages) if x not in used]
-    copies, refused = [], 0
+    copies, refused, free = [], 0, free[::-1]
     for c in wants:
         if not free:
             refused += 1
@@ -183,9 +184,9 @@ def select(parents, lengths, table, page, n_pages):
             out[c] = -1
             continue
         last = lens[c] // page
-        copies.append((int(out[c, last]), free.pop(0)))
+        copies.append((int(out[c, last]), free.pop()))
         out[c, last] = copies[-1][1]
-    counts = [len(free), len(copies), refused, n_pages - len(free)]
+    counts, free = [len(free), len(copies), refused, n_pages - len(free)], free[::-1]
     return out, lens, free + [-1] * (n_pages - len(free)), copies + [(-1, -1)] * (len(parents) - len(copies)), counts
 
 
@@ -194,7 +195,7 @@ def compact(lengths, table, page, n_pages):
     held = [pages_held(t, page, width) for t in lengths]
     used = sorted({int(x) for b in range(n) for x in table[b, :held[b]] if 0 <= x < n_pages})
     k = len(used)
-    goes, takes = [x for x in used if x >= k], [x for x in range(k) if x not in set(used)]
+    goes, takes = [x for x in used if x >= k], sorted(set(range(k)) - set(used))
     to = dict(zip(goes, takes))
     out = np.full((n, width), -1, np.int32)
     for b in range(n):

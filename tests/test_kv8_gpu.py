@@ -457,11 +457,26 @@ def test_requests_that_go_on(B, page, n, m, longest, spare, shared):
     _check_select(B, rng.integers(-2, n + 2, m).tolist(), lengths, table, page, pool)
 
 
-def test_requests_without_pages_for_their_copies(B):
-    rng = _rng(30)
-    lengths, table, pool = _pool(rng, 12, 16, 100, 4)
-    got = _check_select(B, [3] * 20 + list(range(12)), lengths, table, 16, pool)
+@pytest.mark.parametrize("n,copies,longest", [(12, 20, 100), (300, 900, 900), (1500, 6000, 100)])
+def test_requests_without_pages_for_their_copies(B, n, copies, longest):
+    rng = _rng(30, n)
+    lengths, table, pool = _pool(rng, n, 16, longest, 4)
+    got = _check_select(B, [3] * copies + list(range(n)), lengths, table, 16, pool)
     assert got["counts"].tolist()[2] > 0
+
+
+@pytest.mark.parametrize("n,m,width,pages", [(1024, 1024, 16, 20000), (1025, 1025, 15, 20000), (1, 1024, 16, 131072), (1, 1024, 16, 131073),
+                                             (16, 4096, 5, 300), (16, 4097, 5, 300), (5000, 9000, 3, 12288), (5000, 3, 3, 2048)])
+def test_requests_at_the_limits_of_a_launch(B, n, m, width, pages):
+    """Rows, places and pages where another way is taken, and tables of more pages than are named."""
+    rng = _rng(n, m, width, pages)
+    table = rng.integers(-2, pages + 2, (n, width)).astype(np.int32)
+    lengths = rng.integers(0, width * 16 + 3, n).tolist()
+    _check_select(B, rng.integers(0, n, m).tolist(), lengths, table, 16, pages)
+    got = B.page_compact(torch.tensor(lengths, dtype=torch.int32).cuda(), torch.from_numpy(table).cuda(), 16, pages)
+    out, free, moves, counts = P.compact(lengths, table, 16, pages)
+    assert np.array_equal(got["table"].cpu().numpy(), out) and got["counts"].tolist() == counts
+    assert [tuple(x) for x in got["copies"].tolist()] == moves and got["free_pages"].tolist() == free
 
 
 def test_requests_of_any_numbers(B):
