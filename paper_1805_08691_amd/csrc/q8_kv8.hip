@@ -60,6 +60,22 @@ __device__ __forceinline__ unsigned again4(unsigned w, float by) {
   return out;
 }
 
+// The largest of a wavefront's numbers, none of which is negative or no number.
+__device__ __forceinline__ float largest64(float v) {
+  auto turn = [&](auto ctrl_c) {
+    constexpr int ctrl = decltype(ctrl_c)::value;            // (within 16 lanes, by 8, 4, 2, 1)
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), ctrl, 0xf, 0xf, true)));
+  };
+  turn(std::integral_constant<int, 0x128>{});
+  turn(std::integral_constant<int, 0x124>{});
+  turn(std::integral_constant<int, 0x122>{});
+  turn(std::integral_constant<int, 0x121>{});
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 struct Factor {
   float q, by;                     // the new one; old over new where what stands there changes, 1 where not
 };
@@ -71,17 +87,19 @@ __device__ __forceinline__ Factor new_factor(float most, float old, bool begun) 
   return {q, __fdiv_rn(old, q)};
 }
 
-// A block takes the sixteens of one head that its token begins (INDEXED: its 16 tokens), i.e. those of whose tokens in the
-// call it is the first.  A thread has 8 channels of a token, twice beyond 128 channels.
-template <typename V, bool ALIGNED, bool INDEXED>
-__global__ __launch_bounds__(256) void kv8_write_kernel(const Kv8Params p, const V* __restrict__ k, const V* __restrict__ v) {
+// A block takes, in `per` heads one after the other, the sixteens that its token begins (INDEXED: its 16 tokens), i.e. those of
+// whose tokens in the call it is the first.  A thread has 8 channels of a token, twice beyond 128 channels (UNITS); the next
+// head's values are on their way meanwhile, and barriers wait for LDS only.
+template <typename V, bool ALIGNED, bool INDEXED, int UNITS>
+__global__ __launch_bounds__(256, UNITS == 1 ? 5 : 3) void kv8_write_kernel(const Kv8Params p, const V* __restrict__ k, const V* __restrict__ v, int per) {
   constexpr int CHUNK = INDEXED ? 16 : 1;
   __shared__ int member[CHUNK][16];
   __shared__ int leads[CHUNK];
-  __shared__ float most[2][4];
-  __shared__ __attribute__((aligned(16))) unsigned char rows[kMaxHead][20];          // value codes [channel][token]
+  __shared__ float most[2][2][4];
+  __shared__ __attribute__((aligned(16))) unsigned char rows[2][128 * UNITS][20];    // value codes [channel][token]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int head = blockIdx.x % p.H, chunk = p.first + (int)(blockIdx.x / p.H), D = p.D;
+  const int groups = (p.H + per - 1) / per, head0 = (int)(blockIdx.x % groups) * per, head1 = min(head0 + per, p.H);
+  const int chunk = p.first + (int)(blockIdx.x / groups), D = p.D;
   const int ti = tid >> 4, l = tid & 15;
   if constexpr (INDEXED) {
     const int t = chunk * 16 + ti;
@@ -101,89 +119,128 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(const Kv8Params p, const
     const long slot = p.slots[chunk];
     if (!in_cache(p, slot)) return;
     if (tid < 16) member[0][tid] = -1;
-    __syncthreads();
+    lds_barrier();
     for (int i = tid; i < p.T; i += 256) {
       const long s = p.slots[i];
       if (s >> 4 == slot >> 4) atomicMax(&member[0][s & 15], i);
     }
-    __syncthreads();
+    lds_barrier();
     if (tid == 0) {
       int first = 0x7fffffff;
       for (int e = 0; e < 16; ++e) first = member[0][e] < 0 ? first : min(first, member[0][e]);
       leads[0] = first == chunk;
     }
   }
-  __syncthreads();
+  lds_barrier();
+  const size_t head_bytes = (size_t)kv8_sixteen(D) << (p.shift - 4);
   for (int i = 0; i < CHUNK; ++i) {
     if (!leads[i]) continue;
-    const long slot = p.slots[chunk * CHUNK + i];
-    uint8_t* const at = p.cache + sixteen_of(p, slot, head);
-    const bool begun = member[i][0] >= 0;
+    uint8_t* at = p.cache + sixteen_of(p, p.slots[chunk * CHUNK + i], head0);
     const int token = member[i][ti];
-    float x[2][2][8];
-    bool finite[2] = {true, true};
-    float top[2] = {0.0f, 0.0f};
+    const bool begun = member[i][0] >= 0;
+    // which of the sixteen are tokens of the call, a byte of ones each
+    unsigned given[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const V* const from = s ? v + (size_t)max(token, 0) * p.v_stride + head * p.v_head
-                              : k + (size_t)max(token, 0) * p.k_stride + head * p.k_head;
-      unsigned all = 0;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[s][u][e] = 0.0f;
-        if (token >= 0 && 8 * l + 128 * u < D) load_values<8, ALIGNED>(from + 8 * l + 128 * u, x[s][u]);
-        all = row_bits8(x[s][u], all);
-      }
-      finite[s] = all < kNotFinite;
-      top[s] = finite[s] ? __uint_as_float(all) : row_max8(x[s][1], row_max8(x[s][0], 0.0f));
-      for (int off = 32; off > 0; off >>= 1) top[s] = fmaxf(top[s], __shfl_xor(top[s], off, 64));
-      if (lane == 0) most[s][wave] = top[s];
-    }
-    const float2 old = *reinterpret_cast<const float2*>(at + 32 * D);
-    __syncthreads();
-#pragma unroll
-    for (int s = 0; s < 2; ++s) top[s] = fmaxf(fmaxf(most[s][0], most[s][1]), fmaxf(most[s][2], most[s][3]));
-    const Factor fk = new_factor(top[0], old.x, begun), fv = new_factor(top[1], old.y, begun);
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int c = 8 * l + 128 * u;
-      if (c >= D) continue;
-      uint2* const to = reinterpret_cast<uint2*>(at + kv8_key(D, ti, c));
-      if (token >= 0) {
-        // (all zero: any factor)
-        const float qk = fk.q > 0.0f ? fk.q : 1.0f, qv = fv.q > 0.0f ? fv.q : 1.0f;
-        const uint2 zk = row_codes(x[0][u], qk, __fdiv_rn(1.0f, qk), finite[0]);
-        *to = uint2{zk.x ^ 0x80808080u, zk.y ^ 0x80808080u};
-        const uint2 zv = row_codes(x[1][u], qv, __fdiv_rn(1.0f, qv), finite[1]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) rows[c + e][ti] = (unsigned char)(((e < 4 ? zv.x : zv.y) >> (8 * (e & 3)) & 255u) ^ 128u);
-      } else if (begun) {
-        *to = uint2{0x80808080u, 0x80808080u};
-      } else if (fk.by != 1.0f) {
-        const uint2 z = *to;
-        *to = uint2{again4(z.x, fk.by), again4(z.y, fk.by)};
-      }
-    }
-    __syncthreads();
-    if (tid < D) {
-      uint4* const to = reinterpret_cast<uint4*>(at + 16 * D + 16 * tid);
-      unsigned z[4] = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
+    for (int e = 0; e < 16; ++e) given[e >> 2] |= member[i][e] >= 0 ? 255u << (8 * (e & 3)) : 0u;
+    const V *from_k = k + (size_t)max(token, 0) * p.k_stride + head0 * p.k_head + 8 * l,
+            *from_v = v + (size_t)max(token, 0) * p.v_stride + head0 * p.v_head + 8 * l;
+    V raw[2][UNITS][8];
+    float2 old = {0.0f, 0.0f};
+    uint4 was = {0, 0, 0, 0};
+    auto fetch = [&](const uint8_t* sixteen) __attribute__((always_inline)) {
       if (!begun) {
-        const uint4 was = *to;
-        z[0] = was.x, z[1] = was.y, z[2] = was.z, z[3] = was.w;
-        if (fv.by != 1.0f) {
+        old = *reinterpret_cast<const float2*>(sixteen + 32 * D);
+        if (tid < D) was = *reinterpret_cast<const uint4*>(sixteen + 16 * D + 16 * tid);
+      }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) z[e] = again4(z[e], fv.by);
+      for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const V* const from = (s ? from_v : from_k) + 128 * u;
+          if (token >= 0 && 8 * l + 128 * u < D)
+            __builtin_memcpy(raw[s][u], __builtin_assume_aligned(from, ALIGNED ? 16 : sizeof(V)), sizeof(raw[s][u]));
+          else
+#pragma unroll
+            for (int e = 0; e < 8; ++e) raw[s][u][e] = (V)0.0f;
+        }
+    };
+    fetch(at);
+    for (int head = head0; head < head1; ++head) {
+      const int turn = head & 1;
+      float x[2][UNITS][8], top[2];
+      bool finite[2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        unsigned all = 0;
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[s][u][e] = (float)raw[s][u][e];
+          all = row_bits8(x[s][u], all);
+        }
+        finite[s] = all < kNotFinite;
+        top[s] = __uint_as_float(all);
+        if (!finite[s]) {
+          top[s] = 0.0f;
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) top[s] = row_max8(x[s][u], top[s]);
         }
       }
+      const float2 q_old = old;
+      const uint4 v_old = was;
+      uint8_t* const sixteen = at;
+      at += head_bytes, from_k += p.k_head, from_v += p.v_head;
+      if (head + 1 < head1) fetch(at);
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (member[i][e] >= 0) z[e >> 2] = (z[e >> 2] & ~(255u << (8 * (e & 3)))) | (unsigned)rows[tid][e] << (8 * (e & 3));
-      *to = uint4{z[0], z[1], z[2], z[3]};
+      for (int s = 0; s < 2; ++s) {
+        top[s] = largest64(top[s]);
+        if (lane == 0) most[turn][s][wave] = top[s];
+      }
+      lds_barrier();
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        top[s] = fmaxf(fmaxf(most[turn][s][0], most[turn][s][1]), fmaxf(most[turn][s][2], most[turn][s][3]));
+      const Factor fk = new_factor(top[0], q_old.x, begun), fv = new_factor(top[1], q_old.y, begun);
+      // (all zero: any factor)
+      const float qk = fk.q > 0.0f ? fk.q : 1.0f, qv = fv.q > 0.0f ? fv.q : 1.0f;
+      const float inv_k = __fdiv_rn(1.0f, qk), inv_v = __fdiv_rn(1.0f, qv);
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) {
+        const int c = 8 * l + 128 * u;
+        if (c >= D) continue;
+        uint2* const to = reinterpret_cast<uint2*>(sixteen + kv8_key(D, ti, c));
+        if (token >= 0) {
+          const uint2 zk = row_codes(x[0][u], qk, inv_k, finite[0]);
+          *to = uint2{zk.x ^ 0x80808080u, zk.y ^ 0x80808080u};
+          const uint2 zv = row_codes(x[1][u], qv, inv_v, finite[1]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) rows[turn][c + e][ti] = (unsigned char)(((e < 4 ? zv.x : zv.y) >> (8 * (e & 3)) & 255u) ^ 128u);
+        } else if (begun) {
+          *to = uint2{0x80808080u, 0x80808080u};
+        } else if (fk.by != 1.0f) {
+          const uint2 z = *to;
+          *to = uint2{again4(z.x, fk.by), again4(z.y, fk.by)};
+        }
+      }
+      lds_barrier();
+      if (tid < D) {
+        unsigned z[4] = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
+        if (!begun) {
+          z[0] = v_old.x, z[1] = v_old.y, z[2] = v_old.z, z[3] = v_old.w;
+          if (fv.by != 1.0f) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] = again4(z[e], fv.by);
+          }
+        }
+        // (bytes of places without a token are not read as such)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          z[e] = (z[e] & ~given[e]) | (*reinterpret_cast<const unsigned*>(&rows[turn][tid][4 * e]) & given[e]);
+        *reinterpret_cast<uint4*>(sixteen + 16 * D + 16 * tid) = uint4{z[0], z[1], z[2], z[3]};
+      }
+      if (tid == 0) *reinterpret_cast<float2*>(sixteen + 32 * D) = float2{fk.q, fv.q};
     }
-    if (tid == 0) *reinterpret_cast<float2*>(at + 32 * D) = float2{fk.q, fv.q};
-    __syncthreads();                                      // LDS has been read
+    lds_barrier();                                        // LDS has been read
   }
 }
 
@@ -244,11 +301,11 @@ int check_tokens(const void* k, const void* v, int type, size_t T, int H, int D,
   return Q8_OK;
 }
 
-// `chunks` blocks a head, in as many launches as they need.
+// `chunks` blocks a group of heads, in as many launches as they need.
 template <typename F>
-int launch_chunks(size_t chunks, int H, F launch) {
-  const size_t most = most_blocks(256) / H;
-  for (size_t c = 0; c < chunks; c += most) launch(c, (unsigned)((chunks - c < most ? chunks - c : most) * H));
+int launch_chunks(size_t chunks, int groups, F launch) {
+  const size_t most = most_blocks(256) / groups;
+  for (size_t c = 0; c < chunks; c += most) launch(c, (unsigned)((chunks - c < most ? chunks - c : most) * groups));
   return q8_launch_status();
 }
 
@@ -274,12 +331,19 @@ extern "C" int q8_kv8_write(const void* k_dev, const void* v_dev, int type, size
     using V = decltype(one);
     const V *const k = static_cast<const V*>(k_dev), *const v = static_cast<const V*>(v_dev);
     const bool aligned = kv4_rows_aligned<V>(k_dev, v_dev, k_stride, k_head_stride, v_stride, v_head_stride);
-    return launch_chunks(indexed ? (T + 15) / 16 : T, n_heads, [&](size_t chunk, unsigned grid) {
+    // (heads of a block: as many as leave the compute units eight blocks each)
+    const size_t chunks = indexed ? (T + 15) / 16 : T, all = chunks * n_heads / 2048;
+    const int per = (int)(all < 1 ? 1 : all > 8 ? 8 : all);
+    return launch_chunks(chunks, (n_heads + per - 1) / per, [&](size_t chunk, unsigned grid) {
       Kv8Params part = p;
       part.first = (int)chunk;
       auto go = [&](auto aligned_c, auto indexed_c) {
-        kv8_write_kernel<V, decltype(aligned_c)::value, decltype(indexed_c)::value>
-            <<<grid, 256, 0, (hipStream_t)stream>>>(part, k, v);
+        if (D <= 128)
+          kv8_write_kernel<V, decltype(aligned_c)::value, decltype(indexed_c)::value, 1>
+              <<<grid, 256, 0, (hipStream_t)stream>>>(part, k, v, per);
+        else
+          kv8_write_kernel<V, decltype(aligned_c)::value, decltype(indexed_c)::value, 2>
+              <<<grid, 256, 0, (hipStream_t)stream>>>(part, k, v, per);
       };
       using T_ = std::true_type;
       using F_ = std::false_type;
