@@ -129,8 +129,9 @@ struct Part {
 };
 
 // The part of workgroup `id` (of MOST that a tile is cut into at most), and its tile; false: there is none.  SORTED: the
-// longest tiles first.  `shared`: LDS that is free until then.
-template <int COLS, int MOST, bool SORTED = false>
+// longest tiles first.  LEAST: steps of the shortest part where tiles and heads are a workgroup for every second compute
+// unit.  `shared`: LDS that is free until then.
+template <int COLS, int MOST, bool SORTED = false, int LEAST = 0>
 __device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* shared, Part* a, Tile* out) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int at = id / p.H;
@@ -191,7 +192,8 @@ __device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* s
   if (tid == 0) found[0] = 0;
   __syncthreads();
   const long total = ((long)((low[0] + low[1]) + (low[2] + low[3])) + ((long)((high[0] + high[1]) + (high[2] + high[3])) << 16)) * p.H;
-  const long least = min(max((2 * total + kTarget - 1) / kTarget, (long)kShortest), 2l * kShortest);
+  long least = min(max((2 * total + kTarget - 1) / kTarget, (long)kShortest), 2l * kShortest);
+  if (LEAST && p.tiles * p.H >= 128) least = LEAST;
   const unsigned per = (unsigned)max((total + kTarget - 1) / kTarget, least);
   // the sums before each tile: parts (kTarget + kMaxTiles at most); those of cut tiles (10 bits up); cut tiles (20 bits up)
   const unsigned n = steps ? min((steps + per - 1) / per, (unsigned)MOST) : 0, own = n > 1 ? n | n << 10 | 1u << 20 : n;

@@ -18,6 +18,10 @@ namespace {
 
 using namespace q8;
 
+// Steps of the shortest part that keys are cut into where tiles and heads are many: adding parts takes as long as eight
+// steps of a wavefront.  (us with no such limit, 16, 24 and 32 steps, 32 query heads on 8 of 128 channels, one row a request: 64 of
+// up to 2048 keys 35.6, 35.6, 33.6, 31.4; 16 of 4096 24.7, 22.0, 22.4, 20.7; 32 of 1000 15.7, 12.0, 12.0, 11.8.)
+[[maybe_unused]] constexpr int kLeast = 32;
 [[maybe_unused]] constexpr int kLift = 10;          // probabilities are up to 2^10 times what factors are below their power
 
 template <int G, typename V>
@@ -30,7 +34,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_attend_kernel(const A
   const int r = lane & 15, j = lane >> 4;
   Part a;
   Tile t;
-  if (!find_part<kCols, kTarget>(p, blockIdx.x, shared, &a, &t)) return;
+  if (!find_part<kCols, kTarget, false, kLeast>(p, blockIdx.x, shared, &a, &t)) return;
   const int head = a.head, step0 = a.step0, step1 = a.step1;
   const Codes codes;
   const int last = min(t.lo + t.steps * kStep, t.len);         // keys of the tile end here
