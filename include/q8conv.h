@@ -688,15 +688,16 @@ int q8_kv8_attend(const void *q_dev, int type, size_t T, int n_heads, int ratio,
 
 /* The pages of a cache, of any format.  Request b holds lengths[b] tokens (negative counts as 0, more than width * page as
  * that), on the first pages that row b of the table names; entries outside 0 .. n_pages - 1 are no pages.
- * n_pages <= 2^24 (Q8_EUNSUPPORTED); workspaces of q8_page_workspace_bytes (for up to so many rows, old or new, and pages;
- * compact: 0 rows), 16-byte aligned, any contents.
+ * Up to 2^24 pages and rows (Q8_EUNSUPPORTED beyond); workspaces of q8_page_workspace_bytes (for up to so many rows, old or new,
+ * and pages; compact: 0 rows), 16-byte aligned, any contents.  What is written does not overlap what is read (Q8_EINVAL).
  *
  * q8_page_select: the requests that go on.  New request c is old request parents[c] (any other number: an empty request): its
  * length, and its row with -1 behind the pages that it holds.  Several of one parent share its full pages; of a last page that
  * is not full, every one but the first gets a copy, whose page stands in its row.  Pages that no new row holds, in
  * ascending order, are the free ones: the i-th of them is for the i-th copy, in the order of the new requests, and those
  * beyond are listed.  A request without a page for its copy becomes empty.
- *   out_table     [n_new], out_stride apart, out_lengths [n_new]; neither overlaps what is read (Q8_EINVAL)
+ * (A length is not taken back into a page that other requests hold: each would write to it.)
+ *   out_table     [n_new], out_stride apart, and out_lengths [n_new]
  *   free_pages    [n_pages]: the pages that are free afterwards, then -1
  *   copies        [n_new][2]: from, to; then -1.  None is read that is written: q8_page_copy takes them as they are, for
  *                 the cache of every layer that goes by this table

@@ -10,7 +10,7 @@ namespace {
 
 using namespace q8;
 
-constexpr int kMostPages = 1 << 24;
+constexpr int kMostPages = 1 << 24, kMostRows = 1 << 24;
 constexpr int kBlockWords = 64, kBlockPages = 32 * kBlockWords;        // words of 32 pages that a block lists
 
 struct PagesParams {
@@ -453,12 +453,13 @@ int launch_few(const PagesParams& p, hipStream_t stream) {
   return q8_launch_status();
 }
 
-// Whether two tables of n and m rows, `width` entries each, have places in common.
-bool overlap(const int* a, int n, size_t a_stride, const int* b, int m, size_t b_stride, int width) {
-  if (n == 0 || m == 0 || width == 0) return false;
-  const int *a_end = a + (n - 1) * a_stride + width, *b_end = b + (m - 1) * b_stride + width;
-  return a < b_end && b < a_end;
-}
+// Memory from a table's first place to behind its last one, and whether two have any in common.
+struct Span {
+  const int *begin, *end;
+  Span(const int* at, size_t rows, size_t stride, size_t width) : begin(at), end(rows && width ? at + (rows - 1) * stride + width : at) {}
+  Span(const int* at, size_t n) : begin(at), end(at + n) {}
+  bool meets(const Span& o) const { return begin < o.end && o.begin < end && begin != end && o.begin != o.end; }
+};
 
 }  // namespace
 
@@ -473,17 +474,22 @@ extern "C" int q8_page_select(const int32_t* parents_dev, int n_new, const int32
                               int32_t* copies_dev, int32_t* counts_dev, void* workspace, size_t workspace_bytes,
                               void* stream) {
   Q8_REQUIRE(n_new >= 0 && n_requests >= 0 && width >= 0, Q8_EINVAL);
-  Q8_REQUIRE(kv4_page_ok(page) && n_pages <= (size_t)kMostPages && (size_t)width * page <= 0x7fff0000u, Q8_EUNSUPPORTED);
+  Q8_REQUIRE(kv4_page_ok(page) && n_pages <= (size_t)kMostPages && (size_t)width * page <= 0x7fff0000u &&
+                 n_new <= kMostRows && n_requests <= kMostRows, Q8_EUNSUPPORTED);
   Q8_REQUIRE(counts_dev && (workspace || n_pages + n_new + n_requests == 0) && (n_pages == 0 || free_pages_dev), Q8_EINVAL);
   Q8_REQUIRE(n_new == 0 || (parents_dev && out_lengths_dev && copies_dev && (out_table_dev || width == 0)), Q8_EINVAL);
   Q8_REQUIRE(n_requests == 0 || (lengths_dev && (table_dev || width == 0)), Q8_EINVAL);
   Q8_REQUIRE(table_stride >= (size_t)width && out_stride >= (size_t)width, Q8_EINVAL);
-  Q8_REQUIRE(!overlap(table_dev, n_requests, table_stride, out_table_dev, n_new, out_stride, width), Q8_EINVAL);
-  Q8_REQUIRE(!overlap(lengths_dev, 1, 0, out_lengths_dev, 1, 0, n_requests < n_new ? n_requests : n_new), Q8_EINVAL);
   Q8_REQUIRE(q8_aligned(parents_dev, 4) && q8_aligned(lengths_dev, 4) && q8_aligned(table_dev, 4) &&
                  q8_aligned(out_table_dev, 4) && q8_aligned(out_lengths_dev, 4) && q8_aligned(free_pages_dev, 4) &&
                  q8_aligned(copies_dev, 4) && q8_aligned(counts_dev, 4) && q8_aligned(workspace, 16), Q8_EALIGN);
   Q8_REQUIRE(workspace_bytes >= q8_page_workspace_bytes(n_new > n_requests ? n_new : n_requests, n_pages), Q8_EWORKSPACE);
+  const Span reads[] = {{parents_dev, (size_t)n_new}, {lengths_dev, (size_t)n_requests},
+                        {table_dev, (size_t)n_requests, table_stride, (size_t)width}};
+  for (const Span& in : reads)
+    Q8_REQUIRE(!in.meets({out_table_dev, (size_t)n_new, out_stride, (size_t)width}) && !in.meets({out_lengths_dev, (size_t)n_new}) &&
+                   !in.meets({free_pages_dev, n_pages}) && !in.meets({copies_dev, 2 * (size_t)n_new}) && !in.meets({counts_dev, 4}),
+               Q8_EINVAL);
   PagesParams p{};
   p.parents = parents_dev, p.lengths = lengths_dev, p.table = table_dev, p.out_table = out_table_dev;
   p.out_lengths = out_lengths_dev, p.free_pages = free_pages_dev, p.copies = copies_dev, p.counts = counts_dev;
@@ -511,16 +517,21 @@ extern "C" int q8_page_compact(const int32_t* lengths_dev, const int32_t* table_
                                int32_t* free_pages_dev, int32_t* copies_dev, int32_t* counts_dev, void* workspace,
                                size_t workspace_bytes, void* stream) {
   Q8_REQUIRE(n_requests >= 0 && width >= 0, Q8_EINVAL);
-  Q8_REQUIRE(kv4_page_ok(page) && n_pages <= (size_t)kMostPages && (size_t)width * page <= 0x7fff0000u, Q8_EUNSUPPORTED);
+  Q8_REQUIRE(kv4_page_ok(page) && n_pages <= (size_t)kMostPages && (size_t)width * page <= 0x7fff0000u &&
+                 n_requests <= kMostRows, Q8_EUNSUPPORTED);
   Q8_REQUIRE(counts_dev && (n_pages == 0 || (workspace && free_pages_dev)) && (n_pages < 2 || copies_dev), Q8_EINVAL);
   Q8_REQUIRE(n_requests == 0 || (lengths_dev && ((table_dev && out_table_dev) || width == 0)), Q8_EINVAL);
   Q8_REQUIRE(table_stride >= (size_t)width && out_stride >= (size_t)width, Q8_EINVAL);
-  Q8_REQUIRE((table_dev == out_table_dev && (table_stride == out_stride || n_requests < 2)) ||
-                 !overlap(table_dev, n_requests, table_stride, out_table_dev, n_requests, out_stride, width), Q8_EINVAL);
   Q8_REQUIRE(q8_aligned(lengths_dev, 4) && q8_aligned(table_dev, 4) && q8_aligned(out_table_dev, 4) &&
                  q8_aligned(free_pages_dev, 4) && q8_aligned(copies_dev, 4) && q8_aligned(counts_dev, 4) &&
                  q8_aligned(workspace, 16), Q8_EALIGN);
   Q8_REQUIRE(workspace_bytes >= q8_page_workspace_bytes(0, n_pages), Q8_EWORKSPACE);
+  const Span lengths{lengths_dev, (size_t)n_requests}, table{table_dev, (size_t)n_requests, table_stride, (size_t)width},
+      out{out_table_dev, (size_t)n_requests, out_stride, (size_t)width};
+  Q8_REQUIRE((table_dev == out_table_dev && (table_stride == out_stride || n_requests < 2)) || !table.meets(out), Q8_EINVAL);
+  Q8_REQUIRE(!lengths.meets(out), Q8_EINVAL);
+  for (const Span& in : {lengths, table})
+    Q8_REQUIRE(!in.meets({free_pages_dev, n_pages}) && !in.meets({copies_dev, n_pages / 2 * 2}) && !in.meets({counts_dev, 4}), Q8_EINVAL);
   PagesParams p{};
   p.lengths = lengths_dev, p.table = table_dev, p.out_table = out_table_dev;
   p.free_pages = free_pages_dev, p.copies = copies_dev, p.counts = counts_dev;

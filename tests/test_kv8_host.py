@@ -115,6 +115,25 @@ def test_pages_refused():
     assert _select(grown=A) == EINVAL == _select(grown=_at(4))
     for bad in (dict(out=_at(4)), dict(out=_at(16)), dict(out=A, ostride=5)):
         assert _compact(**bad) == EINVAL, bad
+    # a call whose memory is all apart would run: here each of them meets something that is read
+    apart = dict(parents=_at(1024), lengths=_at(2048), table=_at(4096), free=_at(8192), copies=_at(16384), counts=_at(32768))
+    for name in ("parents", "lengths", "table"):
+        at = apart[name]
+        for bad in (dict(out=at), dict(grown=at), dict(free=at), dict(copies=at), dict(counts=at)):
+            assert _select(**dict(apart, **bad)) == EINVAL, (name, bad)
+    del apart["parents"]
+    for name in ("lengths", "table"):
+        at = apart[name]
+        for bad in (dict(free=at), dict(copies=at), dict(counts=at)) + ((dict(out=at),) if name == "lengths" else ()):
+            assert _compact(**dict(apart, **bad)) == EINVAL, (name, bad)
+
+
+def test_most_rows():
+    most, width = 1 << 24, 1
+    for f in (_select, _compact):
+        assert f(n=most + 1, width=width) == EUNSUPPORTED
+        assert f(n=most, width=width, nb=100) == EWORKSPACE
+    assert _select(m=most + 1, width=width) == EUNSUPPORTED
 
 
 def test_copies_refused():
