@@ -60,8 +60,8 @@ __device__ __forceinline__ unsigned again4(unsigned w, float by) {
   return out;
 }
 
-// The largest of a wavefront's numbers, none of which is negative or no number.
-__device__ __forceinline__ float largest64(float v) {
+// The largest of half a wavefront's numbers, none of which is negative or no number.
+__device__ __forceinline__ float largest32(float v) {
   auto turn = [&](auto ctrl_c) {
     constexpr int ctrl = decltype(ctrl_c)::value;            // (within 16 lanes, by 8, 4, 2, 1)
     v = fmaxf(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), ctrl, 0xf, 0xf, true)));
@@ -71,7 +71,11 @@ __device__ __forceinline__ float largest64(float v) {
   turn(std::integral_constant<int, 0x122>{});
   turn(std::integral_constant<int, 0x121>{});
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+// And of all of them.
+__device__ __forceinline__ float largest64(float v) {
+  v = largest32(v);
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
@@ -87,20 +91,80 @@ __device__ __forceinline__ Factor new_factor(float most, float old, bool begun) 
   return {q, __fdiv_rn(old, q)};
 }
 
+// One token of a sixteen, of one head, by a wavefront: keys in its lower half, values in its upper half, 8 channels a lane.
+// Nothing else of the sixteen is touched unless its factor begins or grows.  (A step's tokens, 8 heads of 128 channels, us with
+// blocks for whole sixteens and so: 256 requests 9.7 and 6.7, 1000 25.7 and 16.8, 2000 48 and 20; its bytes are worth 1 to 4.
+// Bound by the trips to memory: slots, then rows and factors, then what is stored by the byte.)
+template <typename V, bool ALIGNED>
+__device__ __forceinline__ void write_one(const Kv8Params& p, const V* k, const V* v, uint8_t* sixteen, int token, int head, int place) {
+  const int lane = threadIdx.x & 63, l = lane & 31, D = p.D, c = 8 * l;
+  const bool upper = lane >= 32, in = c < D, begun = place == 0;
+  float* const factor = reinterpret_cast<float*>(sixteen + 32 * D) + upper;
+  const V* const from = upper ? v + token * p.v_stride + head * p.v_head : k + token * p.k_stride + head * p.k_head;
+  V raw[8];
+  float old = 0.0f, x[8];
+  if (in) {
+    __builtin_memcpy(raw, __builtin_assume_aligned(from + c, ALIGNED ? 16 : sizeof(V)), sizeof(raw));
+    if (!begun) old = *factor;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = in ? (float)raw[e] : 0.0f;
+  const unsigned all = row_bits8(x, 0);
+  const bool finite = all < kNotFinite;
+  const Factor f = new_factor(largest32(finite ? __uint_as_float(all) : row_max8(x, 0.0f)), old, begun);
+  const float q = f.q > 0.0f ? f.q : 1.0f;               // (all zero: any factor)
+  if (!in) return;
+  uint2 z = row_codes(x, q, __fdiv_rn(1.0f, q), finite);
+  z.x ^= 0x80808080u, z.y ^= 0x80808080u;
+  if (l == 0) *factor = f.q;
+  auto code = [&](int e) { return (e < 4 ? z.x : z.y) >> (8 * (e & 3)) & 255u; };
+  if (!upper) {
+    *reinterpret_cast<uint2*>(sixteen + kv8_key(D, place, c)) = z;
+    if (begun || f.by != 1.0f)
+      for (int t = 0; t < 16; ++t) {
+        uint2* const at = reinterpret_cast<uint2*>(sixteen + kv8_key(D, t, c));
+        if (t != place) *at = begun ? uint2{0x80808080u, 0x80808080u} : uint2{again4(at->x, f.by), again4(at->y, f.by)};
+      }
+  } else if (!begun && f.by == 1.0f) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sixteen[16 * D + 16 * (c + e) + place] = (unsigned char)code(e);
+  } else {
+    const unsigned shift = 8 * (place & 3);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      uint4* const at = reinterpret_cast<uint4*>(sixteen + 16 * D + 16 * (c + e));
+      unsigned w[4] = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
+      if (!begun) {
+        const uint4 was = *at;
+        w[0] = again4(was.x, f.by), w[1] = again4(was.y, f.by), w[2] = again4(was.z, f.by), w[3] = again4(was.w, f.by);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i == place >> 2) w[i] = (w[i] & ~(255u << shift)) | code(e) << shift;
+      *at = uint4{w[0], w[1], w[2], w[3]};
+    }
+  }
+}
+
 // A block takes, in `per` heads one after the other, the sixteens that its token begins (INDEXED: its 16 tokens), i.e. those of
 // whose tokens in the call it is the first.  A thread has 8 channels of a token, twice beyond 128 channels (UNITS); the next
-// head's values are on their way meanwhile, and barriers wait for LDS only.
+// head's values are on their way meanwhile, and barriers wait for LDS only: value codes change places there, so that both the
+// token-major side and the cache's side are whole lines.  (16001 tokens, 8 heads of 128 channels: 35 us; bytes 20.  Bound by vector
+// instructions: five a value for its code and for being sure of it.)
 template <typename V, bool ALIGNED, bool INDEXED, int UNITS>
 __global__ __launch_bounds__(256, UNITS == 1 ? 5 : 3) void kv8_write_kernel(const Kv8Params p, const V* __restrict__ k, const V* __restrict__ v, int per) {
   constexpr int CHUNK = INDEXED ? 16 : 1;
   __shared__ int member[CHUNK][16];
-  __shared__ int leads[CHUNK];
+  __shared__ int leads[CHUNK];                          // how many they are
+  __shared__ long slots[CHUNK];
   __shared__ float most[2][2][4];
   __shared__ __attribute__((aligned(16))) unsigned char rows[2][128 * UNITS][20];    // value codes [channel][token]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int groups = (p.H + per - 1) / per, head0 = (int)(blockIdx.x % groups) * per, head1 = min(head0 + per, p.H);
   const int chunk = p.first + (int)(blockIdx.x / groups), D = p.D;
   const int ti = tid >> 4, l = tid & 15;
+  int members;                                          // of the sixteen that token `lane` (the only one) begins, or none
+  long slot0 = 0;
   if constexpr (INDEXED) {
     const int t = chunk * 16 + ti;
     const long slot = t < p.T ? p.slots[t] : -1;
@@ -114,28 +178,39 @@ __global__ __launch_bounds__(256, UNITS == 1 ? 5 : 3) void kv8_write_kernel(cons
     member[ti][l] = e;
     int first = e < 0 ? 0x7fffffff : e;
     for (int off = 8; off > 0; off >>= 1) first = min(first, __shfl_xor(first, off, 16));
-    if (l == 0) leads[ti] = in && first == t;
+    const int n = __popc((unsigned)(__ballot(e >= 0) >> (lane & 48)) & 0xffffu);
+    if (l == 0) leads[ti] = in && first == t ? n : 0, slots[ti] = slot;
+    lds_barrier();
+    members = lane < CHUNK ? leads[lane] : 0;
   } else {
     const long slot = p.slots[chunk];
+    long s[kScan / 256];
+#pragma unroll
+    for (int u = 0; u < kScan / 256; ++u) s[u] = u * 256 + tid < p.T ? p.slots[u * 256 + tid] : -1;
     if (!in_cache(p, slot)) return;
     if (tid < 16) member[0][tid] = -1;
     lds_barrier();
-    for (int i = tid; i < p.T; i += 256) {
-      const long s = p.slots[i];
-      if (s >> 4 == slot >> 4) atomicMax(&member[0][s & 15], i);
-    }
+#pragma unroll
+    for (int u = 0; u < kScan / 256; ++u)
+      if (s[u] >> 4 == slot >> 4) atomicMax(&member[0][s[u] & 15], u * 256 + tid);
     lds_barrier();
-    if (tid == 0) {
-      int first = 0x7fffffff;
-      for (int e = 0; e < 16; ++e) first = member[0][e] < 0 ? first : min(first, member[0][e]);
-      leads[0] = first == chunk;
-    }
+    const int e = lane < 16 ? member[0][lane] : -1;
+    if (__any(e >= 0 && e < chunk) || !__any(e == chunk)) return;
+    members = __popcll(__ballot(e >= 0));
+    slot0 = slot;
   }
-  lds_barrier();
   const size_t head_bytes = (size_t)kv8_sixteen(D) << (p.shift - 4);
-  for (int i = 0; i < CHUNK; ++i) {
-    if (!leads[i]) continue;
-    uint8_t* at = p.cache + sixteen_of(p, p.slots[chunk * CHUNK + i], head0);
+  // ---- the only ones of their sixteens, a wavefront each
+  for (unsigned ones = INDEXED ? (unsigned)__ballot(members == 1) : members == 1; ones; ones &= ones - 1) {
+    const int i = INDEXED ? __builtin_ctz(ones) : 0, t = chunk * CHUNK + i;
+    const long slot = INDEXED ? slots[i] : slot0;
+    for (int head = head0 + ((wave - i) & 3); head < head1; head += 4)
+      write_one<V, ALIGNED>(p, k, v, p.cache + sixteen_of(p, slot, head), t, head, (int)(slot & 15));
+  }
+  // ---- the others
+  for (unsigned more = INDEXED ? (unsigned)__ballot(members > 1) : members > 1; more; more &= more - 1) {
+    const int i = INDEXED ? __builtin_ctz(more) : 0;
+    uint8_t* at = p.cache + sixteen_of(p, INDEXED ? slots[i] : slot0, head0);
     const int token = member[i][ti];
     const bool begun = member[i][0] >= 0;
     // which of the sixteen are tokens of the call, a byte of ones each

@@ -1,5 +1,6 @@
 """Plain references of the 8-bit cache and of its pages, on the CPU: fixed sequences of fp32 operations where that is the
 definition, whole numbers, or 64 bits, written apart from the kernels."""
+import functools
 import math
 
 import numpy as np
@@ -20,6 +21,7 @@ def key_at(D, t, c):
     return t // 4 * 4 * D + chunk * 256 + (c % 64 // 8 * 4 + t % 4) * 8 + c % 8
 
 
+@functools.lru_cache(maxsize=None)
 def key_order(D):
     return np.array([[key_at(D, t, c) for c in range(D)] for t in range(16)])
 

@@ -147,6 +147,32 @@ def test_tokens_of_strided_rows(B):
         assert bool((out[:, 2 * H:] == 7).all()) and bool((out[..., D + offset:] == 7).all())
 
 
+@pytest.mark.parametrize("T", [3, 300, 1024, 1300])
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 160, 192, 224, 256])
+def test_tokens_alone_in_their_sixteens(B, D, T):
+    """A step of many requests, one token each: at any place, over zeros or over what a step before left, of any size; among
+    them pairs that share a sixteen, and rows of no alignment."""
+    H, page = 5, 32
+    rng = _rng(D, T, 21)
+    kind = sorted(TYPES)[(D // 32 + T) % 3]
+    pages = -(-T // 2) + 3
+    cache, want = B.kv8_cache(pages, H, page, D), P.empty(pages, H, page, D)
+    for step in range(4):
+        sixteens = rng.permutation(2 * pages)[:T]
+        place = rng.integers(0, 16, T) if step else np.zeros(T, np.int64)
+        slots = sixteens * 16 + place
+        if step == 2 and T > 10:
+            slots[1::7] = (slots[0::7][:len(slots[1::7])] // 16) * 16 + (slots[0::7][:len(slots[1::7])] + 5) % 16
+        joint = _tokens(rng, (T, 2 * H, D + 1), "f32") * torch.from_numpy(np.exp(rng.standard_normal((T, 1, 1)))).float()
+        joint[:2] = 0
+        joint[T // 2, :, D // 3], joint[T // 2, :, D // 2] = float("inf"), float("nan")
+        joint = joint.to(TYPES[kind]).cuda()
+        k, v = joint[:, :H, step % 2:D + step % 2], joint[:, H:, step % 2:D + step % 2]
+        B.kv8_write(cache, k, v, torch.from_numpy(slots).cuda())
+        P.write(want, k.float().cpu().numpy(), v.float().cpu().numpy(), slots, page)
+        _same_cache(cache, want)
+
+
 def test_no_tokens(B):
     cache = B.kv8_cache(2, 2, 16, 64)
     none = torch.empty(0, 2, 64, device="cuda")
