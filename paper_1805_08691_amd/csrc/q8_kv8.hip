@@ -60,31 +60,36 @@ __device__ __forceinline__ unsigned again4(unsigned w, float by) {
   return out;
 }
 
-// The largest of half a wavefront's numbers, none of which is negative or no number.
-__device__ __forceinline__ float largest32(float v) {
+// The largest of half a wavefront's magnitudes, as bit patterns (whose order is theirs, and which need no care of what is no
+// number).
+__device__ __forceinline__ unsigned largest32(unsigned v) {
   auto turn = [&](auto ctrl_c) {
     constexpr int ctrl = decltype(ctrl_c)::value;            // (within 16 lanes, by 8, 4, 2, 1)
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), ctrl, 0xf, 0xf, true)));
+    v = max(v, (unsigned)__builtin_amdgcn_mov_dpp((int)v, ctrl, 0xf, 0xf, true));
   };
   turn(std::integral_constant<int, 0x128>{});
   turn(std::integral_constant<int, 0x124>{});
   turn(std::integral_constant<int, 0x122>{});
   turn(std::integral_constant<int, 0x121>{});
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return max((unsigned)a[0], (unsigned)a[1]);
 }
 // And of all of them.
-__device__ __forceinline__ float largest64(float v) {
+__device__ __forceinline__ unsigned largest64(unsigned v) {
   v = largest32(v);
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max((unsigned)b[0], (unsigned)b[1]);
 }
+
+// 1 / q for row_codes, within 2^-23 of itself: a quotient of up to 127.1 is then off by 127.1 (2^-23 + 2^-24) = 2.3e-5, less
+// than the 7e-5 from a tie within which it divides.
+__device__ __forceinline__ float about_one_over(float q) { return __builtin_amdgcn_rcpf(q); }
 
 struct Factor {
   float q, by;                     // the new one; old over new where what stands there changes, 1 where not
 };
-__device__ __forceinline__ Factor new_factor(float most, float old, bool begun) {
-  const float need = __fmul_rn(most, 1.0f / 127.0f);
+__device__ __forceinline__ Factor new_factor(unsigned most, float old, bool begun) {
+  const float need = __fmul_rn(__uint_as_float(most), 1.0f / 127.0f);
   if (begun) return {need, 1.0f};
   if (need <= old) return {old, 1.0f};
   const float q = fmaxf(need, __fmul_rn(old, kGrowth));
@@ -111,16 +116,17 @@ __device__ __forceinline__ void write_one(const Kv8Params& p, const V* k, const 
   for (int e = 0; e < 8; ++e) x[e] = in ? (float)raw[e] : 0.0f;
   const unsigned all = row_bits8(x, 0);
   const bool finite = all < kNotFinite;
-  const Factor f = new_factor(largest32(finite ? __uint_as_float(all) : row_max8(x, 0.0f)), old, begun);
+  const Factor f = new_factor(largest32(finite ? all : __float_as_uint(row_max8(x, 0.0f))), old, begun);
   const float q = f.q > 0.0f ? f.q : 1.0f;               // (all zero: any factor)
   if (!in) return;
-  uint2 z = row_codes(x, q, __fdiv_rn(1.0f, q), finite);
+  uint2 z = row_codes(x, q, about_one_over(q), finite);
   z.x ^= 0x80808080u, z.y ^= 0x80808080u;
   if (l == 0) *factor = f.q;
   auto code = [&](int e) { return (e < 4 ? z.x : z.y) >> (8 * (e & 3)) & 255u; };
   if (!upper) {
     *reinterpret_cast<uint2*>(sixteen + kv8_key(D, place, c)) = z;
     if (begun || f.by != 1.0f)
+#pragma unroll 1
       for (int t = 0; t < 16; ++t) {
         uint2* const at = reinterpret_cast<uint2*>(sixteen + kv8_key(D, t, c));
         if (t != place) *at = begun ? uint2{0x80808080u, 0x80808080u} : uint2{again4(at->x, f.by), again4(at->y, f.by)};
@@ -149,7 +155,7 @@ __device__ __forceinline__ void write_one(const Kv8Params& p, const V* k, const 
 // A block takes, in `per` heads one after the other, the sixteens that its token begins (INDEXED: its 16 tokens), i.e. those of
 // whose tokens in the call it is the first.  A thread has 8 channels of a token, twice beyond 128 channels (UNITS); the next
 // head's values are on their way meanwhile, and barriers wait for LDS only: value codes change places there, so that both the
-// token-major side and the cache's side are whole lines.  (16001 tokens, 8 heads of 128 channels: 35 us; bytes 20.  Bound by vector
+// token-major side and the cache's side are whole lines.  (16001 tokens, 8 heads of 128 channels: 29 us; bytes 20.  Bound by vector
 // instructions: five a value for its code and for being sure of it.)
 template <typename V, bool ALIGNED, bool INDEXED, int UNITS>
 __global__ __launch_bounds__(256, UNITS == 1 ? 5 : 3) void kv8_write_kernel(const Kv8Params p, const V* __restrict__ k, const V* __restrict__ v, int per) {
@@ -157,7 +163,7 @@ __global__ __launch_bounds__(256, UNITS == 1 ? 5 : 3) void kv8_write_kernel(cons
   __shared__ int member[CHUNK][16];
   __shared__ int leads[CHUNK];                          // how many they are
   __shared__ long slots[CHUNK];
-  __shared__ float most[2][2][4];
+  __shared__ unsigned most[2][2][4];
   __shared__ __attribute__((aligned(16))) unsigned char rows[2][128 * UNITS][20];    // value codes [channel][token]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int groups = (p.H + per - 1) / per, head0 = (int)(blockIdx.x % groups) * per, head1 = min(head0 + per, p.H);
@@ -242,7 +248,8 @@ __global__ __launch_bounds__(256, UNITS == 1 ? 5 : 3) void kv8_write_kernel(cons
     fetch(at);
     for (int head = head0; head < head1; ++head) {
       const int turn = head & 1;
-      float x[2][UNITS][8], top[2];
+      float x[2][UNITS][8];
+      unsigned top[2];
       bool finite[2];
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
@@ -254,11 +261,12 @@ __global__ __launch_bounds__(256, UNITS == 1 ? 5 : 3) void kv8_write_kernel(cons
           all = row_bits8(x[s][u], all);
         }
         finite[s] = all < kNotFinite;
-        top[s] = __uint_as_float(all);
+        top[s] = all;
         if (!finite[s]) {
-          top[s] = 0.0f;
+          float m = 0.0f;
 #pragma unroll
-          for (int u = 0; u < UNITS; ++u) top[s] = row_max8(x[s][u], top[s]);
+          for (int u = 0; u < UNITS; ++u) m = row_max8(x[s][u], m);
+          top[s] = __float_as_uint(m);
         }
       }
       const float2 q_old = old;
@@ -274,11 +282,11 @@ __global__ __launch_bounds__(256, UNITS == 1 ? 5 : 3) void kv8_write_kernel(cons
       lds_barrier();
 #pragma unroll
       for (int s = 0; s < 2; ++s)
-        top[s] = fmaxf(fmaxf(most[turn][s][0], most[turn][s][1]), fmaxf(most[turn][s][2], most[turn][s][3]));
+        top[s] = max(max(most[turn][s][0], most[turn][s][1]), max(most[turn][s][2], most[turn][s][3]));
       const Factor fk = new_factor(top[0], q_old.x, begun), fv = new_factor(top[1], q_old.y, begun);
       // (all zero: any factor)
       const float qk = fk.q > 0.0f ? fk.q : 1.0f, qv = fv.q > 0.0f ? fv.q : 1.0f;
-      const float inv_k = __fdiv_rn(1.0f, qk), inv_v = __fdiv_rn(1.0f, qv);
+      const float inv_k = about_one_over(qk), inv_v = about_one_over(qv);
 #pragma unroll
       for (int u = 0; u < UNITS; ++u) {
         const int c = 8 * l + 128 * u;
