@@ -26,7 +26,7 @@ struct PagesParams {
   unsigned* __restrict__ used;                 // the same as bits, [blocks][kBlockWords]
   unsigned* __restrict__ counts_of;            // and their number in each block
   int* __restrict__ before;                    // compact: of each word, pages in use before it; select: parents' first rows
-  unsigned* __restrict__ flags;                // select: of each new row, whether it needs a copy of its last page
+  uint8_t* __restrict__ flags;                 // select: of each new row, whether it needs a copy of its last page
   size_t stride, out_stride;
   int n, m, shift, width, pool, blocks, n_copies;          // old rows, new rows; shift: page = 1 << shift tokens
 };
@@ -50,18 +50,33 @@ __device__ __forceinline__ unsigned block_scan(unsigned v, unsigned (&sums)[WAVE
   return upto - v + (wave ? __shfl(waves, wave - 1, 64) : 0u);
 }
 
-// Pages in use, of all blocks and of those in front of block `end`, for every thread of a block of 256.
-__device__ __forceinline__ void count_used(const PagesParams& p, int end, unsigned (&sums)[4], int* all, int* front) {
-  unsigned n = 0, m = 0, total;
+// The same of N numbers at once, in a block of 256: one trip through LDS.
+template <int N>
+__device__ __forceinline__ void block_scans(const unsigned (&v)[N], unsigned (&sums)[N][4], unsigned (&before)[N], unsigned (&total)[N]) {
+  const unsigned lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const unsigned upto = scan64(v[i]);
+    if (lane == 63) sums[i][wave] = upto;
+    before[i] = upto - v[i];
+  }
+  lds_barrier();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    total[i] = sums[i][0] + sums[i][1] + sums[i][2] + sums[i][3];
+#pragma unroll
+    for (unsigned w = 0; w < 3; ++w) before[i] += w < wave ? sums[i][w] : 0u;
+  }
+}
+
+// A thread's share of the pages in use, of all blocks and of those in front of block `end`.
+__device__ __forceinline__ void count_used(const PagesParams& p, int end, unsigned* all, unsigned* front) {
+  *all = *front = 0;
   for (int i = threadIdx.x; i < p.blocks; i += 256) {
     const unsigned c = p.counts_of[i];
-    n += c;
-    if (i < end) m += c;
+    *all += c;
+    if (i < end) *front += c;
   }
-  block_scan(n, sums, &total);
-  *all = (int)total;
-  block_scan(m, sums, &total);
-  *front = (int)total;
 }
 
 __global__ __launch_bounds__(256) void pages_clear_kernel(uint4* marks, size_t n_marks, int* first, int n) {
@@ -69,12 +84,14 @@ __global__ __launch_bounds__(256) void pages_clear_kernel(uint4* marks, size_t n
   if (i < n_marks) marks[i] = uint4{0, 0, 0, 0};
   if (i < (size_t)n) first[i] = 0x7fffffff;
 }
+// Four bytes of 0 or 1 as four bits, in order.
+__device__ __forceinline__ unsigned bits_of(unsigned w) { return (w & 0x01010101u) * 0x10204080u >> 28; }
+
 // Marks to bits and their numbers: eight pages a thread.
 __global__ __launch_bounds__(256) void pages_count_kernel(const PagesParams p) {
   __shared__ unsigned sums[4];
   const uint2 m = reinterpret_cast<const uint2*>(p.marks)[blockIdx.x * 256 + threadIdx.x];
-  // (bytes of 0 or 1: bit 0 of each to the upper byte, in order)
-  const unsigned bits = (m.x * 0x10204080u >> 28) | (m.y * 0x10204080u >> 28 << 4);
+  const unsigned bits = bits_of(m.x) | bits_of(m.y) << 4;
   unsigned word = bits << (8 * (threadIdx.x & 3)), total;
   word |= __shfl_xor(word, 1, 64);
   word |= __shfl_xor(word, 2, 64);
@@ -144,32 +161,31 @@ __global__ __launch_bounds__(256) void select_rows_kernel(const PagesParams p) {
 // Free pages in order: the first of them become copies, of the rows that need one in their order; the others are listed.  Rows
 // that find none become empty.  A block lists kBlockPages pages; every block adds up all blocks and rows for itself.
 __global__ __launch_bounds__(256) void select_free_kernel(const PagesParams p) {
-  __shared__ unsigned sums[4], ranks[kBlockWords], words[kBlockWords];
+  __shared__ __attribute__((aligned(16))) unsigned sums[4][4];
+  __shared__ unsigned ranks[kBlockWords], words[kBlockWords];
   __shared__ int list[kBlockPages], rows[kBlockPages];
   const int tid = threadIdx.x, page0 = blockIdx.x * kBlockPages;
   // ---- rows that need a copy: those of this thread, one after the other
-  const int each = (p.m + 255) / 256, row0 = tid * each, row1 = min(row0 + each, p.m);
+  const int each = (p.m + 4095) / 4096 * 16, row0 = tid * each, row1 = min(row0 + each, p.m);
   unsigned flags = 0;
   unsigned long which = 0;                                 // of the first 64
-#pragma unroll 8
-  for (int c = row0; c < row1; ++c) {
-    const unsigned flag = p.flags[c];
-    flags += flag;
-    if (c - row0 < 64) which |= (unsigned long)flag << (c - row0);
+  for (int c = row0; c < row1; c += 16) {
+    const uint4 w = *reinterpret_cast<const uint4*>(p.flags + c);
+    const unsigned some = (bits_of(w.x) | bits_of(w.y) << 4 | bits_of(w.z) << 8 | bits_of(w.w) << 12) & (row1 - c < 16 ? (1u << (row1 - c)) - 1u : 0xffffu);
+    flags += __popc(some);
+    if (c - row0 < 64) which |= (unsigned long)some << (c - row0);
   }
   unsigned bits = tid < kBlockWords && blockIdx.x < p.blocks ? p.used[blockIdx.x * kBlockWords + tid] : 0xffffffffu;
-  int used, used_before;
-  count_used(p, blockIdx.x, sums, &used, &used_before);
-  unsigned needed;
-  int rank = (int)block_scan(flags, sums, &needed);
-  const int n_free = p.pool - used, n_needed = (int)needed, taken = min(n_needed, n_free), first = page0 - used_before;
-  // ---- this block's free pages
   const int behind = page0 + 32 * (tid + 1) - p.pool;
   bits = behind >= 32 ? 0 : behind > 0 ? ~bits & 0xffffffffu >> behind : ~bits;
-  unsigned here;
-  const unsigned before = block_scan(__popc(bits), sums, &here);
-  if (tid < kBlockWords) ranks[tid] = before, words[tid] = bits;
-  const int end = first + (int)here;
+  unsigned v[4] = {0, 0, flags, (unsigned)__popc(bits)}, before[4], total[4];
+  count_used(p, blockIdx.x, &v[0], &v[1]);
+  block_scans(v, sums, before, total);
+  const int n_needed = (int)total[2], n_free = p.pool - (int)total[0], taken = min(n_needed, n_free), first = page0 - (int)total[1];
+  int rank = (int)before[2];
+  // ---- this block's free pages
+  if (tid < kBlockWords) ranks[tid] = before[3], words[tid] = bits;
+  const int end = first + (int)total[3];
   lds_barrier();
 #pragma unroll
   for (int i = tid; i < kBlockPages; i += 256) {
@@ -357,22 +373,27 @@ __global__ __launch_bounds__(256) void compact_mark_kernel(const PagesParams p) 
 
 // Of the k pages in use, those at k and behind go to the free ones in front of k, both in ascending order.
 __global__ __launch_bounds__(256) void compact_list_kernel(const PagesParams p) {
-  __shared__ unsigned sums[4], ranks[kBlockWords], words[kBlockWords];
+  __shared__ __attribute__((aligned(16))) unsigned sums[3][4], sums_of[2][4];
+  __shared__ unsigned ranks[kBlockWords], words[kBlockWords];
   const int tid = threadIdx.x, page0 = blockIdx.x * kBlockPages;
   const unsigned bits = tid < kBlockWords && blockIdx.x < p.blocks ? p.used[blockIdx.x * kBlockWords + tid] : 0;
-  int k, first, front;
-  count_used(p, blockIdx.x, sums, &k, &first);
+  unsigned v[3] = {0, 0, (unsigned)__popc(bits)}, before[3], total[3];
+  count_used(p, blockIdx.x, &v[0], &v[1]);
+  block_scans(v, sums, before, total);
+  const int k = (int)total[0], rank0 = (int)(total[1] + before[2]);
   // in use in front of k: they stay
   const int of = k / kBlockPages, left = k - of * kBlockPages - 32 * tid;        // (of k's block, to this thread's word)
-  count_used(p, of, sums, &front, &front);
-  unsigned n = 0, here, more;
-  if (tid < kBlockWords && of < p.blocks && left > 0) n = p.used[of * kBlockWords + tid];
-  block_scan(__popc(left >= 32 ? n : n & ((1u << max(left, 0)) - 1u)), sums, &more);
-  const int stay = front + (int)more, moves = k - stay;
-  const int rank = first + (int)block_scan(__popc(bits), sums, &here);
+  unsigned in_front[2] = {0, 0}, front_before[2], front[2], all;
+  count_used(p, of, &all, &in_front[0]);
+  if (tid < kBlockWords && of < p.blocks && left > 0) {
+    const unsigned n = p.used[of * kBlockWords + tid];
+    in_front[1] = __popc(left >= 32 ? n : n & ((1u << left) - 1u));
+  }
+  block_scans(in_front, sums_of, front_before, front);
+  const int stay = (int)(front[0] + front[1]), moves = k - stay;
   if (tid < kBlockWords) {
-    if (blockIdx.x < p.blocks) p.before[blockIdx.x * kBlockWords + tid] = rank;
-    ranks[tid] = (unsigned)rank, words[tid] = bits;
+    if (blockIdx.x < p.blocks) p.before[blockIdx.x * kBlockWords + tid] = rank0;
+    ranks[tid] = (unsigned)rank0, words[tid] = bits;
   }
   lds_barrier();
 #pragma unroll
@@ -437,7 +458,7 @@ struct Space {
     p->used = reinterpret_cast<unsigned*>(at + used);
     p->before = reinterpret_cast<int*>(at + before);
     p->counts_of = reinterpret_cast<unsigned*>(at + counts);
-    p->flags = reinterpret_cast<unsigned*>(at + flags);
+    p->flags = reinterpret_cast<uint8_t*>(at + flags);
   }
 };
 
