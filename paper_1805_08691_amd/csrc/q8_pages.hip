@@ -231,12 +231,13 @@ struct Few {
   int parent[kFewRows];                        // select: of new row c; -1: none, or none that holds pages
   int held[kFewRows];                          // pages of new row c, or (again) minus them
   unsigned used[kFewWords];
-  int before[kFewWords];                       // pages in use before a word
+  int before[kFewWords];                       // pages in use before a word; select: at first, a parent's first new row
   int list[kFewRows * kFewPlaces];             // select: free pages for copies; compact: where pages go, by rank
   unsigned sums[16];
 };
-inline bool few(int rows, int width, size_t n_pages) {
-  return rows <= kFewRows && (size_t)rows * width <= (size_t)kFewRows * kFewPlaces && n_pages <= (size_t)kFewWords * 32;
+inline bool few(int rows, int parents, int width, size_t n_pages) {
+  return rows <= kFewRows && parents <= kFewWords && (size_t)rows * width <= (size_t)kFewRows * kFewPlaces &&
+         n_pages <= (size_t)kFewWords * 32;
 }
 
 template <bool SELECT>
@@ -244,7 +245,7 @@ __global__ __launch_bounds__(1024) void pages_few_kernel(const PagesParams p) {
   extern __shared__ __attribute__((aligned(16))) char shared[];
   Few& s = *reinterpret_cast<Few*>(shared);
   const int tid = threadIdx.x;
-  for (int i = tid; i < kFewWords; i += 1024) s.used[i] = 0;
+  for (int i = tid; i < kFewWords; i += 1024) s.used[i] = 0, s.before[i] = 0x7fffffff;
   int parent = -1, len = 0, held = 0;
   if (tid < p.m) {
     parent = SELECT ? p.parents[tid] : tid;
@@ -256,8 +257,9 @@ __global__ __launch_bounds__(1024) void pages_few_kernel(const PagesParams p) {
   bool again = false;
   if constexpr (SELECT) {
     lds_barrier();
-    if (parent >= 0)
-      for (int i = 0; i < tid; ++i) again |= s.parent[i] == parent;
+    if (parent >= 0) atomicMin(&s.before[parent], tid);
+    lds_barrier();
+    again = parent >= 0 && s.before[parent] < tid;
   }
   if (tid < p.m) s.held[tid] = again ? -held : held;
   lds_barrier();
@@ -522,7 +524,7 @@ extern "C" int q8_page_select(const int32_t* parents_dev, int n_new, const int32
   p.n = n_requests, p.m = n_new, p.shift = __builtin_ctz(page), p.width = width, p.pool = (int)n_pages;
   p.blocks = (int)blocks_of(n_pages), p.n_copies = n_new;
   const hipStream_t s = (hipStream_t)stream;
-  if (few(n_new, width, n_pages)) return launch_few<true>(p, s);
+  if (few(n_new, n_requests, width, n_pages)) return launch_few<true>(p, s);
   const size_t marks = (size_t)p.blocks * kBlockPages / 16, first = p.before ? n_requests : 0;
   if (marks || first)
     pages_clear_kernel<<<(unsigned)(((marks > first ? marks : first) + 255) / 256), 256, 0, s>>>(
@@ -562,7 +564,7 @@ extern "C" int q8_page_compact(const int32_t* lengths_dev, const int32_t* table_
   p.n = p.m = n_requests, p.shift = __builtin_ctz(page), p.width = width, p.pool = (int)n_pages;
   p.blocks = (int)blocks_of(n_pages), p.n_copies = (int)(n_pages / 2);
   const hipStream_t s = (hipStream_t)stream;
-  if (few(n_requests, width, n_pages)) return launch_few<false>(p, s);
+  if (few(n_requests, 0, width, n_pages)) return launch_few<false>(p, s);
   const unsigned rows = (unsigned)(((size_t)n_requests + 3) / 4);
   const size_t marks = (size_t)p.blocks * kBlockPages / 16;
   if (marks) pages_clear_kernel<<<(unsigned)((marks + 255) / 256), 256, 0, s>>>(reinterpret_cast<uint4*>(p.marks), marks, nullptr, 0);

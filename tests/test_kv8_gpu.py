@@ -492,7 +492,8 @@ def test_requests_without_pages_for_their_copies(B, n, copies, longest):
 
 
 @pytest.mark.parametrize("n,m,width,pages", [(1024, 1024, 16, 20000), (1025, 1025, 15, 20000), (1, 1024, 16, 131072), (1, 1024, 16, 131073),
-                                             (16, 4096, 5, 300), (16, 4097, 5, 300), (5000, 9000, 3, 12288), (5000, 3, 3, 2048)])
+                                             (16, 2400, 7, 300), (16, 2401, 7, 300), (16, 4096, 5, 300), (16, 4097, 5, 300),
+                                             (4096, 100, 5, 300), (4097, 100, 5, 300), (5000, 9000, 3, 12288), (5000, 3, 3, 2048)])
 def test_requests_at_the_limits_of_a_launch(B, n, m, width, pages):
     """Rows, places and pages where another way is taken, and tables of more pages than are named."""
     rng = _rng(n, m, width, pages)
@@ -619,6 +620,30 @@ def test_a_block_serves_beams(B, bits):
         block.release(b)
     assert block.taken == 0 and block.lengths == [0] * 4
     assert sorted(block.free.tolist()) == list(range(64))
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_a_block_without_pages_for_copies_stays_as_it_was(B, bits):
+    E, _, _, block = _block(bits, n_pages=6)
+    other = _block(bits, n_pages=6)[3]
+    x = torch.randn(120, E, device="cuda").bfloat16()
+    for one in (block, other):
+        one.step(x[:78], [40, 38, 0, 0])                         # all six pages
+    table, lengths, free = block.table.clone(), list(block.lengths), block.free.clone()
+    for parents in ([0, 0, 1, 1], [0, 1, 1, -1]):
+        with pytest.raises(MemoryError):
+            block.select(parents)
+        assert torch.equal(block.table, table) and block.lengths == lengths and block.taken == 6
+        assert torch.equal(block.free, free)
+    assert torch.equal(block.step(x[78:84], [4, 2, 0, 0]), other.step(x[78:84], [4, 2, 0, 0]))
+    with pytest.raises(AssertionError):
+        block.select([0, 1, 2])
+    with pytest.raises(AssertionError):
+        block.select([0, 1, 4, -1])
+    block.select([0, 0, -1, -1])                                 # (three pages and a copy)
+    assert block.taken == 4 and block.lengths == [44, 44, 0, 0]
+    y = block.step(x[84:86], [1, 1, 0, 0])
+    assert torch.equal(y[0], other.step(x[84:85], [1, 0, 0, 0])[0])
 
 
 def test_a_block_in_8_bits_is_near_the_fp32_block(B):
