@@ -303,6 +303,33 @@ def test_attention_of_flat_and_peaked_rows(B, peak, scale, prompt):
            peak=peak, scale=scale)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("prompt", [False, True])
+def test_rows_that_are_no_numbers_stay_by_themselves(B, kind, prompt):
+    """Queries with infinities and NaN, zeros and the type's extremes, beside ordinary ones of the same tile."""
+    rng = _rng(18)
+    H, ratio, D, page = 16 if prompt else 2, 4, 64, 16
+    lengths, added = [700, 64, 333], [130, 64, 100] if prompt else [3, 2, 4]
+    table, pool = _table(rng, lengths, page)
+    cache = _filled(rng, pool, H, page, D)
+    starts = np.concatenate([[0], np.cumsum(added)]).astype(np.int32)
+    T = int(starts[-1])
+    q = torch.from_numpy(rng.standard_normal((T, H * ratio, D)).astype(np.float32)).to(TYPES[kind])
+    q[1, 1::ratio, 3], q[1, 2::ratio, 5], q[4, ::ratio, D - 1] = float("nan"), float("inf"), float("-inf")
+    q[T - 2, 3::ratio] = 0
+    q[T - 1, 1::ratio] = torch.finfo(q.dtype).tiny
+    dev = [torch.from_numpy(x).cuda() for x in (cache, table, np.array(lengths, np.int32), starts)]
+    out = B.kv8_attend(q.cuda(), *dev, workspace=B.kv8_attend_workspace(q, dev[0], 3, 700)).double().cpu().numpy()
+    fine = torch.isfinite(q).all(-1).numpy()
+    assert np.isfinite(out[fine]).all() and np.isnan(out[~fine]).all()
+    kv = [P.held(cache, table, b, n, page) for b, n in enumerate(lengths)]
+    keys, values = [x[0] for x in kv], [x[1] for x in kv]
+    want, noise = P.attend(torch.where(torch.isfinite(q), q, 0).double().numpy(), keys, values, lengths, starts,
+                           float(np.float32(D ** -0.5)), 0, True)
+    bound = P.tolerance(want, noise, values, TYPES[kind])
+    assert (np.abs(out - want) <= bound)[fine].all()
+
+
 @pytest.mark.parametrize("prompt", [False, True])
 @pytest.mark.parametrize("size", [1e-30, 1e-9, 1e-3, 1e4, 1e9])
 def test_attention_over_factors_of_any_size(B, size, prompt):
