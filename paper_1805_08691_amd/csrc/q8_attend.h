@@ -117,6 +117,7 @@ constexpr int kTarget = 512;
 // request of 2000 tokens 11.6 us, never shorter than 8 or 16 steps 13.2 and 16.9; 8 of 4096, 64 channels, 14.0, with 4 14.8.)
 constexpr int kShortest = 4;
 constexpr int kMaxTiles = 256;         // beyond them nothing is cut: a thread each
+constexpr int kManyTiles = 128;        // times heads: a workgroup for every second compute unit
 
 // The split of the key axis.  The steps of all tiles and heads over kTarget are what a part should hold (`least` at
 // least); a tile of more steps is cut into equal parts of no more.  Every workgroup works this out for itself from the
@@ -129,8 +130,8 @@ struct Part {
 };
 
 // The part of workgroup `id` (of MOST that a tile is cut into at most), and its tile; false: there is none.  SORTED: the
-// longest tiles first.  LEAST: steps of the shortest part where tiles and heads are a workgroup for every second compute
-// unit.  `shared`: LDS that is free until then.
+// longest tiles first.  LEAST: steps of the shortest part where tiles and heads are kManyTiles.  `shared`: LDS that is free until
+// then.
 template <int COLS, int MOST, bool SORTED = false, int LEAST = 0>
 __device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* shared, Part* a, Tile* out) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -193,7 +194,7 @@ __device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* s
   __syncthreads();
   const long total = ((long)((low[0] + low[1]) + (low[2] + low[3])) + ((long)((high[0] + high[1]) + (high[2] + high[3])) << 16)) * p.H;
   long least = min(max((2 * total + kTarget - 1) / kTarget, (long)kShortest), 2l * kShortest);
-  if (LEAST && p.tiles * p.H >= 128) least = LEAST;
+  if (LEAST && p.tiles * p.H >= kManyTiles) least = LEAST;
   const unsigned per = (unsigned)max((total + kTarget - 1) / kTarget, least);
   // the sums before each tile: parts (kTarget + kMaxTiles at most); those of cut tiles (10 bits up); cut tiles (20 bits up)
   const unsigned n = steps ? min((steps + per - 1) / per, (unsigned)MOST) : 0, own = n > 1 ? n | n << 10 | 1u << 20 : n;
@@ -524,11 +525,12 @@ inline size_t attend_workspace_bytes(size_t T, int n_requests, int n_heads, int 
 }
 
 // A call's arguments, checked, as *p, and whether it goes to the kernel for many columns.  p->T = 0: there is nothing to do.
+// least: find_part's LEAST of the kernel for few.
 inline int attend_params(const void* q_dev, int type, size_t T, int n_heads, int ratio, int D, size_t q_stride,
                          size_t q_head_stride, const void* cache_dev, size_t n_pages, int page, const int32_t* table_dev, int width,
                          size_t table_stride, const int32_t* lengths_dev, const int32_t* starts_dev, int n_requests, float scale,
                          int window, void* out_dev, size_t o_stride, size_t o_head_stride, void* workspace,
-                         size_t workspace_bytes, WideFor* wide_for, AttendParams* out, bool* is_wide) {
+                         size_t workspace_bytes, WideFor* wide_for, AttendParams* out, bool* is_wide, int least = 0) {
   Q8_REQUIRE(type_ok(type) && n_heads >= 1 && ratio >= 1 && width >= 0 && window >= 0 && n_requests >= 0, Q8_EINVAL);
   Q8_REQUIRE(scale == scale && scale - scale == 0.0f, Q8_EINVAL);
   Q8_REQUIRE(type != Q8_F32 && kv4_shape_ok(D, page), Q8_EUNSUPPORTED);
@@ -545,7 +547,8 @@ inline int attend_params(const void* q_dev, int type, size_t T, int n_heads, int
   const bool cuts = workspace && workspace_bytes >= split_bytes(D, kWideCols) && cut(wide_tiles, longest);
   const bool wide = starts_dev && wide_for(T, n_requests, n_heads, ratio, D, longest, cuts);
   const size_t tiles = wide ? wide_tiles : tiles_of(T, n_requests, ratio, starts_dev != nullptr);
-  const bool split = wide ? cuts : workspace && workspace_bytes >= split_bytes(D) && cut(tiles, longest);
+  const bool whole = tiles * n_heads >= (size_t)kManyTiles && longest <= (size_t)least * kStep;       // (none has two parts)
+  const bool split = wide ? cuts : workspace && workspace_bytes >= split_bytes(D) && cut(tiles, longest) && !whole;
   Q8_REQUIRE(tiles * n_heads + kTarget <= most_blocks(256) && T * ratio <= 0x7fffffffu, Q8_EUNSUPPORTED);
   AttendParams& p = *out;
   p.cache = static_cast<const uint8_t*>(cache_dev);

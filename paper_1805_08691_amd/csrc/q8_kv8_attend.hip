@@ -261,7 +261,7 @@ extern "C" int q8_kv8_attend(const void* q_dev, int type, size_t T, int n_heads,
   bool wide = false;
   const int rc = attend_params(q_dev, type, T, n_heads, ratio, D, q_stride, q_head_stride, cache_dev, n_pages, page, table_dev,
                                width, table_stride, lengths_dev, starts_dev, n_requests, scale, window, out_dev, o_stride,
-                               o_head_stride, workspace, workspace_bytes, wide_for, &p, &wide);
+                               o_head_stride, workspace, workspace_bytes, wide_for, &p, &wide, kLeast);
   if (rc != Q8_OK || p.T == 0) return rc;
   p.all = !causal;
   if (wide) return kv8_attend_wide(D / 32, p, q_dev, out_dev, type, (hipStream_t)stream);
