@@ -243,11 +243,11 @@ struct Join {
   static constexpr int PITCH = D + 4;                   // of a column in LDS: eight lanes' quads meet different banks
   static constexpr size_t kPartWords = kCols * (D + 2) / 2;      // of a part: sums [16][D], then a maximum and a sum for each column
 };
-constexpr size_t join_bytes(int D, bool cut) {
-  const size_t columns = (size_t)kWaves * kCols * (D + 6) * 4, adding = 256 * 16 + (kTarget + 1) * kCols * sizeof(float);
+constexpr size_t join_bytes(int D, bool cut, int waves = kWaves) {
+  const size_t columns = (size_t)waves * kCols * (D + 6) * 4, adding = 256 * 16 + (kTarget + 1) * kCols * sizeof(float);
   return cut && columns < adding ? adding : columns;
 }
-template <int D, typename V>
+template <int D, int WAVES = kWaves, typename V>
 __device__ __forceinline__ void join_columns(const AttendParams& p, const Part& a, const Tile& t, char* shared, V* __restrict__ out,
                                              const f4 (&o)[D / 16], float ref, float sum) {
   constexpr int CT = Join<D>::CT, PITCH = Join<D>::PITCH;
@@ -258,10 +258,10 @@ __device__ __forceinline__ void join_columns(const AttendParams& p, const Part& 
   sum += __shfl_xor(sum, 32, 64);
   __syncthreads();                                      // LDS has been read: the columns take its place
 
-  // ---- the four wavefronts' columns together
+  // ---- the wavefronts' columns together
   float* const cols = reinterpret_cast<float*>(shared);
-  float* const refs = cols + kWaves * kCols * PITCH;
-  float* const sums = refs + kWaves * kCols;
+  float* const refs = cols + WAVES * kCols * PITCH;
+  float* const sums = refs + WAVES * kCols;
   if (j == 0) {
     refs[wave * kCols + r] = ref;
     sums[wave * kCols + r] = sum;
@@ -269,7 +269,7 @@ __device__ __forceinline__ void join_columns(const AttendParams& p, const Part& 
   __syncthreads();
   float all = -__builtin_inff();
 #pragma unroll
-  for (int v = 0; v < kWaves; ++v) all = fmaxf(all, refs[v * kCols + r]);
+  for (int v = 0; v < WAVES; ++v) all = fmaxf(all, refs[v * kCols + r]);
   const float mine = ref == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ref - all);
   float* const to = cols + (wave * kCols + r) * PITCH + 4 * j;
 #pragma unroll
@@ -277,14 +277,14 @@ __device__ __forceinline__ void join_columns(const AttendParams& p, const Part& 
   __syncthreads();
   const bool whole = a.parts == 1;
   const int valid = min(kCols, t.cols - t.first);
-  for (int i = tid; i < valid * D / 4; i += 256) {
+  for (int i = tid; i < valid * D / 4; i += 64 * WAVES) {
     const int c = i / (D / 4), d = i % (D / 4) * 4;
     f4 v = {0, 0, 0, 0};
     float m = -__builtin_inff(), l = 0.0f;
 #pragma unroll
-    for (int u = 0; u < kWaves; ++u) m = fmaxf(m, refs[u * kCols + c]);
+    for (int u = 0; u < WAVES; ++u) m = fmaxf(m, refs[u * kCols + c]);
 #pragma unroll
-    for (int u = 0; u < kWaves; ++u) {
+    for (int u = 0; u < WAVES; ++u) {
       v += *reinterpret_cast<const f4*>(cols + (u * kCols + c) * PITCH + d);
       const float ru = refs[u * kCols + c];
       l += ru == -__builtin_inff() ? 0.0f : sums[u * kCols + c] * __builtin_amdgcn_exp2f(ru - m);

@@ -24,8 +24,8 @@ using namespace q8;
 [[maybe_unused]] constexpr int kLeast = 32;
 [[maybe_unused]] constexpr int kLift = 10;          // probabilities are up to 2^10 times what factors are below their power
 
-template <int G, typename V>
-__global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_attend_kernel(const AttendParams p, const V* __restrict__ q,
+template <int G, int WAVES, typename V>
+__global__ __launch_bounds__(64 * WAVES, G <= 4 ? 2 : 1) void kv8_attend_kernel(const AttendParams p, const V* __restrict__ q,
                                                                          V* __restrict__ out) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int D = 32 * G, CT = 2 * G, CHUNKS = (G + 1) / 2, SIXTEEN = kv8_sixteen(D);
@@ -38,7 +38,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_attend_kernel(const A
   const int head = a.head, step0 = a.step0, step1 = a.step1;
   const Codes codes;
   const int last = min(t.lo + t.steps * kStep, t.len);         // keys of the tile end here
-  const int iterations = step0 + wave < step1 ? (step1 - step0 - wave + kWaves - 1) / kWaves : 0;
+  const int iterations = step0 + wave < step1 ? (step1 - step0 - wave + WAVES - 1) / WAVES : 0;
 
   // ---- the column of this lane
   const int col = t.first + r;
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_attend_kernel(const A
   long where = 0;
   unsigned long held = 0;
   auto find_sixteens = [&](int it0) {
-    const int s = step0 + wave + (it0 + (lane >> 2)) * kWaves, at = (t.lo >> 4) + s * 4 + (lane & 3);
+    const int s = step0 + wave + (it0 + (lane >> 2)) * WAVES, at = (t.lo >> 4) + s * 4 + (lane & 3);
     int page = -1;
     if (s < step1 && at * 16 < last) page = table[at >> p.shift];
     const bool in = page >= 0 && page < p.n_pages;
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_attend_kernel(const A
   Power<5> scaled;                                      // o is relative to 2^(its power - kLift)
 
   for (int it = 0; it < iterations; ++it) {
-    const int key0 = t.lo + (step0 + wave + it * kWaves) * kStep;
+    const int key0 = t.lo + (step0 + wave + it * WAVES) * kStep;
     const bool more = it + 1 < iterations;
     there = next_there;
     const bool clear = key0 > clear0 && key0 + kStep - 1 <= clear1 && there == 15u;
@@ -198,21 +198,30 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_attend_kernel(const A
   const float back = two_to(scaled.power - kLift);
 #pragma unroll
   for (int c = 0; c < CT; ++c) o[c] *= back;
-  join_columns<D>(p, a, t, shared, out, o, ref, sum);
+  join_columns<D, WAVES>(p, a, t, shared, out, o, ref, sum);
 #endif
 }
 
-template <int G, typename V>
+template <int G, int WAVES, typename V>
 int launch(const AttendParams& p, const V* q, V* out, hipStream_t stream) {
-  const size_t lds = join_bytes(32 * G, p.parts != nullptr);
+  const size_t lds = join_bytes(32 * G, p.parts != nullptr, WAVES);
   if (lds > 65536) {
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_attend_kernel<G, V>),
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)join_bytes(32 * G, true));
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_attend_kernel<G, WAVES, V>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)join_bytes(32 * G, WAVES == kWaves, WAVES));
     if (attr != hipSuccess) return Q8_EHIP;
   }
   const unsigned blocks = (unsigned)(p.tiles * p.H) + (p.parts ? kTarget : 0);
-  kv8_attend_kernel<G, V><<<blocks, 256, lds, stream>>>(p, q, out);
+  kv8_attend_kernel<G, WAVES, V><<<blocks, 64 * WAVES, lds, stream>>>(p, q, out);
   return q8_launch_status();
+}
+template <int G, typename V>
+int launch(const AttendParams& p, const V* q, V* out, hipStream_t stream) {
+  // Whole tiles, fewer than compute units, of many steps: eight wavefronts share them.  (us with four and eight, 16 requests of up to
+  // 1500 keys, 12 heads of 64 channels 9.9 and 9.2, 8 of 128 12.8 and 12.2; but 256 tiles and heads of up to 1000 keys 11.1 and
+  // 11.8, 60 of up to 300 6.0 and 6.5.)
+  if constexpr (G <= 4)
+    if (!p.parts && p.tiles * p.H <= 224 && ((long)p.width << p.shift) > 64) return launch<G, 8>(p, q, out, stream);
+  return launch<G, kWaves>(p, q, out, stream);
 }
 
 template <typename V>

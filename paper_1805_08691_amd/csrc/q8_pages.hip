@@ -245,7 +245,10 @@ __global__ __launch_bounds__(1024) void pages_few_kernel(const PagesParams p) {
   extern __shared__ __attribute__((aligned(16))) char shared[];
   Few& s = *reinterpret_cast<Few*>(shared);
   const int tid = threadIdx.x;
-  for (int i = tid; i < kFewWords; i += 1024) s.used[i] = 0, s.before[i] = 0x7fffffff;
+  for (int i = tid; i < kFewWords; i += 1024) {
+    s.used[i] = 0;
+    if (SELECT) s.before[i] = 0x7fffffff;
+  }
   int parent = -1, len = 0, held = 0;
   if (tid < p.m) {
     parent = SELECT ? p.parents[tid] : tid;

@@ -251,6 +251,21 @@ def test_attention_over_long_contexts(B, lengths, workspace):
     _check(B, _rng(*lengths), lengths, [1] * len(lengths), 2, 4, 128, 64, "f16", workspace=workspace, single=True)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 160])
+@pytest.mark.parametrize("H,added", [(2, [1] * 5), (28, [1] * 5), (32, [1] * 5), (6, [5, 1, 2, 0, 9])])
+def test_attention_over_contexts_that_are_not_cut(B, kind, D, H, added):
+    """Long ones of few tiles and heads, which nothing cuts: without a workspace, or as none would have two parts."""
+    for lengths, causal in (([1500, 1025, 3, 0, 1100], True), ([64, 1407, 512, 513, 0], False)):
+        for workspace in (False, H * len(added) >= 128):
+            # (Element by element: the norm of ten rows is that of one or two with few large probabilities, each off by up to 2^-11 =
+            # 4.9e-4 of itself and with it all of a row's outputs, where a norm's bound takes the root mean square of many, 2^-10 /
+            # sqrt(12) = 2.8e-4.  Three keys of 64 channels make 11.1 of 11.4; rounding their six probabilities, and nothing else, in
+            # 64 bits gives 4.17e-4 of the norm there and 4.18e-4 is measured; with 128 channels 4.29e-4 and 4.08e-4; the bound is 3.99e-4.)
+            _check(B, _rng(D, H, len(lengths)), lengths, added, H, 1, D, 64, kind, workspace=workspace, causal=causal, single=max(added) == 1,
+                   near=False)
+
+
 @pytest.mark.parametrize("window", [1, 2, 15, 16, 17, 63, 64, 65, 100, 5000, 2 ** 31 - 1])
 def test_attention_in_a_window(B, window):
     _check(B, _rng(window), [300, 5, 64, 700], [3, 5, 1, 70], 2, 2, 64, 16, "bf16", window=window)
