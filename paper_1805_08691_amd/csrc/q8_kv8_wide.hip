@@ -9,7 +9,7 @@
 // Lane (r, h) of S has 16 keys of sixteens h and 2 + h for column r, so that a factor is one number of a lane, and probabilities
 // are operands as they come.
 //
-// Measured: 2048 tokens of each of three requests over up to 8192 keys, 32 query heads on 4 of 128 channels, 358 us, 0.82 PFLOP/s;
+// Measured: 2048 tokens of each of three requests over up to 8192 keys, 32 query heads on 4 of 128 channels, 353 us, 0.84 PFLOP/s;
 // matrix instructions in 40 %, vector instructions in 50 % of the cycles of two wavefronts a SIMD, at 1.83 GHz.  The order below,
 // exponentials between key products and unpacking between value products, took it from 383 to 354.  Eight wavefronts that share
 // keys, products of 16 x 16, and two groups that multiply in turn were no faster; 64 columns a wavefront, which halve what is read
@@ -23,9 +23,11 @@ using namespace q8;
 typedef float f16v __attribute__((ext_vector_type(16)));
 
 // Probabilities are made relative to a maximum so that its own is 2^kTop, and again where their sum in a lane (32 of them)
-// passes 2^kMost; values are codes times their factor over a power of two, 2^(7 + 4 + kLift) at most: both are binary16 numbers.
-[[maybe_unused]] constexpr float kTop = 7.0f, kMost = 15.0f;
-[[maybe_unused]] constexpr int kLift = 4;
+// passes 2^kMost; their products with the values' factor over a power of two, which is below 2^(4 + kLift), are binary16 numbers.
+// The factor is part of the exponent (its logarithm is added to the score), and taken out of their sums again, in fp32: a sixteen
+// whose factor is 0, whose codes are 0, has kLeastWeight instead.
+[[maybe_unused]] constexpr float kTop = 7.0f, kMost = 15.0f, kLeastWeight = 0x1p-40f;
+[[maybe_unused]] constexpr int kLift = -4;
 constexpr int kRing = 128;                      // steps whose sixteens' places and factors are in LDS
 
 template <int G>
@@ -115,7 +117,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
     if (2 * G % kWaves != 0 && u >= 2 * G) return;
     vc[i] = *reinterpret_cast<const uint4*>(p.cache + (size_t)value_place[i] * SIXTEEN + 16 * D + (32 * (u >> 1) + r) * 16);
   };
-  // Operands of step s: keys as codes; values as codes times their factor.
+  // Operands of step s: codes.
   auto unpack_key = [&](int s, auto k_c) __attribute__((always_inline)) {        // half k % 2 of pair k / 2
     constexpr int k = decltype(k_c)::value, i = k / 2;
     const int u = wave + i * kWaves;
@@ -125,23 +127,23 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
   };
   Power<4> scaled;
   float2 next[2];                                     // factors of a step's sixteens h and 2 + h
-  float weight0 = 0.0f, weight1 = 0.0f;
+  float ref = 0.0f;                                   // a column's, as a power of two
+  float offset[2];                                    // log2 of the values' factors over their power, less `ref`
   auto find_factors = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) next[b] = factors[slot_of(s, 2 * b + h)];
   };
   auto weigh = [&]() __attribute__((always_inline)) {
-    weight0 = __builtin_amdgcn_ldexpf(next[0].y, kLift - scaled.power);
-    weight1 = __builtin_amdgcn_ldexpf(next[1].y, kLift - scaled.power);
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+      offset[b] = __builtin_amdgcn_logf(fmaxf(__builtin_amdgcn_ldexpf(next[b].y, kLift - scaled.power), kLeastWeight)) - ref;
   };
   auto unpack_value = [&](int s, auto k_c) __attribute__((always_inline)) {
     constexpr int k = decltype(k_c)::value, i = k / 2;
     const int u = wave + i * kWaves;
     if (2 * G % kWaves != 0 && u >= 2 * G) return;
-    const _Float16 w = (_Float16)(u & 1 ? weight1 : weight0);
-    const h8 w8 = {w, w, w, w, w, w, w, w};
     char* const to = shared + W::V_AT + (s & 1) * W::OPERANDS + u * 2048 + k % 2 * 1024 + lane * 16;
-    *reinterpret_cast<h8*>(to) = (k % 2 ? codes.eight(vc[i].z, vc[i].w) : codes.eight(vc[i].x, vc[i].y)) * w8;
+    *reinterpret_cast<h8*>(to) = k % 2 ? codes.eight(vc[i].z, vc[i].w) : codes.eight(vc[i].x, vc[i].y);
   };
   constexpr std::integral_constant<int, PAIRS> kPairs{};
   auto all_of = [&](auto n_c, auto f) __attribute__((always_inline)) {
@@ -179,7 +181,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
 #pragma unroll
       for (int e = 0; e < 8; ++e) qf[n][e] = (_Float16)(v[n][e] * down);
   }
-  float ref = 0.0f, sum = 0.0f;
+  float sum = 0.0f;
   bool begun = col >= t.cols;                         // (a column that there is not: it has no maximum to find)
   f16v o[G];
 #pragma unroll
@@ -191,8 +193,9 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
   const int clear0 = p.window > 0 ? pos1 - p.window : -1, clear1 = pos0;
 
   // ---- products, register e of s2[b] being token e of sixteen 2 b + h: kProducts of a step's keys, and of its values, one after
-  // the other, with what is to be done beside the i-th; operands are read kAhead products before.
-  constexpr int kProducts = 4 * G, kAhead = kProducts < 4 ? kProducts : 4;
+  // the other, with what is to be done beside the i-th; operands are read kAhead products before.  (Four before: 128
+  // channels spill ten registers, 386 us for the three requests instead of 367.)
+  constexpr int kProducts = 4 * G, kAhead = 2;
   using std::integral_constant;
   f16v s2[2], x[2];
   h8 pr[2][2];
@@ -240,12 +243,12 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
     };
     each(each, integral_constant<int, first>{});
   };
-  // Scores 2 k and 2 k + 1 relative to `ref`, as powers of two; none of keys that the column does not see.
+  // Scores 2 k and 2 k + 1 relative to `ref`, as powers of two, with their values' factor; none of keys that the column does not see.
   float by[2];
   auto scale_two = [&](auto k_c) __attribute__((always_inline)) {
     constexpr int k = decltype(k_c)::value, b = k / 8, e = k % 8 * 2;
-    x[b][e] = __builtin_fmaf(s2[b][e], by[b], -ref);
-    x[b][e + 1] = __builtin_fmaf(s2[b][e + 1], by[b], -ref);
+    x[b][e] = __builtin_fmaf(s2[b][e], by[b], offset[b]);
+    x[b][e + 1] = __builtin_fmaf(s2[b][e + 1], by[b], offset[b]);
     float pinned[2] = {x[b][e], x[b][e + 1]};
     asm volatile("" : "+v"(pinned[0]), "+v"(pinned[1]));        // (here, beside the product, not where they are used)
     x[b][e] = pinned[0], x[b][e + 1] = pinned[1];
@@ -263,7 +266,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
       for (int e = 0; e < 16; ++e) x[b][e] = see >> e & 1u ? x[b][e] : -__builtin_inff();
     }
   };
-  float part = 0.0f;                                  // sum of a lane's probabilities as the values meet them
+  float part[2];                                      // sums of a lane's probabilities of a sixteen, times its factor
   float raised[2];
   auto raise_two = [&](auto k_c) __attribute__((always_inline)) {
     constexpr int k = decltype(k_c)::value, b = k / 8, e = k % 8 * 2;
@@ -272,8 +275,9 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
   };
   auto keep_two = [&](auto k_c) __attribute__((always_inline)) {
     constexpr int k = decltype(k_c)::value, b = k / 8, e = k % 8 * 2;
-    const h2 two = {(_Float16)raised[0], (_Float16)raised[1]}, ones = {1.0f16, 1.0f16};
-    part = __builtin_amdgcn_fdot2(two, ones, part, false);
+    const h2 two = {(_Float16)raised[0], (_Float16)raised[1]};
+    part[b] += raised[0];
+    part[b] += raised[1];
     pr[b][e >> 3][e & 7] = two[0], pr[b][e >> 3][(e & 7) + 1] = two[1];
   };
   constexpr integral_constant<int, 16> kTwos{};
@@ -303,7 +307,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
   for (int s = 0; s < steps; ++s) {
     if ((s & 63) == 0 && s > 0) find_sixteens((s + 64) * 4, 256);
     if ((s & 63) == 1) holes = __builtin_amdgcn_readfirstlane(*hole) != 0;
-    part = 0.0f;
+    part[0] = part[1] = 0.0f;
     bool grows = false;
     scores(s + 1, [&](auto i_c) __attribute__((always_inline)) {
       constexpr int i = decltype(i_c)::value;
@@ -321,15 +325,18 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
     });
     keep_two(integral_constant<int, 15>{});
     // the first keys that a column sees, and where one or a factor grows
-    if (__any(!begun || part > 32768.0f || grows)) {
+    float all = part[0] * __builtin_amdgcn_exp2f(-offset[0] - ref) + part[1] * __builtin_amdgcn_exp2f(-offset[1] - ref);
+    if (__any(!begun || all > 32768.0f || grows)) {
 #pragma unroll
       for (int i = 0; i < G; ++i) o[i] *= down;
       down = scaled.grow(fmaxf(next[0].y, next[1].y));
-      float m = x[0][0];
+      float most[2] = {x[0][0], x[1][0]};
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) m = fmaxf(m, x[b][e]);
+        for (int e = 1; e < 16; ++e) most[b] = fmaxf(most[b], x[b][e]);
+      const float weight[2] = {offset[0] + ref, offset[1] + ref};
+      float m = fmaxf(most[0] - weight[0], most[1] - weight[1]);
       m = fmaxf(m, __shfl_xor(m, 32, 64));
       const bool seen = m > -__builtin_inff();
       // (32 probabilities whose sum is 2^15 have one of 2^10)
@@ -341,10 +348,11 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
       for (int i = 0; i < G; ++i) o[i] *= shrink;
 #pragma unroll
       for (int b = 0; b < 2; ++b) x[b] -= more;
-      part = 0.0f;
+      part[0] = part[1] = 0.0f;
       all_of(kTwos, [&](auto k_c) { raise_two(k_c), keep_two(k_c); });
+      all = part[0] * __builtin_amdgcn_exp2f(-weight[0]) + part[1] * __builtin_amdgcn_exp2f(-weight[1]);
     }
-    sum += part;
+    sum += all;
     add_values(s, [&](auto i_c) __attribute__((always_inline)) {
       if constexpr (decltype(i_c)::value == 0) weigh();
       share(i_c, integral_constant<int, 4 * PAIRS>{}, [&](auto k_c) __attribute__((always_inline)) {
