@@ -24,8 +24,9 @@ typedef float f16v __attribute__((ext_vector_type(16)));
 
 // Probabilities are made relative to a maximum so that its own is 2^kTop, and again where their sum in a lane (32 of them)
 // passes 2^kMost; their products with the values' factor over a power of two, which is below 2^(4 + kLift), are binary16 numbers.
-// The factor is part of the exponent (its logarithm is added to the score), and taken out of their sums again, in fp32: a sixteen
-// whose factor is 0, whose codes are 0, has kLeastWeight instead.
+// The factor is part of the exponent (its logarithm is added to the score), and taken out of their sums again, in fp32, so that
+// what an exponent loses beside a large score is the score's error alone.  A sixteen whose factor is 0, whose codes are 0, has
+// kLeastWeight instead.
 [[maybe_unused]] constexpr float kTop = 7.0f, kMost = 15.0f, kLeastWeight = 0x1p-40f;
 [[maybe_unused]] constexpr int kLift = -4;
 constexpr int kRing = 128;                      // steps whose sixteens' places and factors are in LDS
@@ -128,15 +129,17 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
   Power<4> scaled;
   float2 next[2];                                     // factors of a step's sixteens h and 2 + h
   float ref = 0.0f;                                   // a column's, as a power of two
-  float offset[2];                                    // log2 of the values' factors over their power, less `ref`
+  float weight[2], offset[2];                         // log2 of the values' factors over their power; the same less `ref`
   auto find_factors = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) next[b] = factors[slot_of(s, 2 * b + h)];
   };
   auto weigh = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-      offset[b] = __builtin_amdgcn_logf(fmaxf(__builtin_amdgcn_ldexpf(next[b].y, kLift - scaled.power), kLeastWeight)) - ref;
+    for (int b = 0; b < 2; ++b) {
+      weight[b] = __builtin_amdgcn_logf(fmaxf(__builtin_amdgcn_ldexpf(next[b].y, kLift - scaled.power), kLeastWeight));
+      offset[b] = weight[b] - ref;
+    }
   };
   auto unpack_value = [&](int s, auto k_c) __attribute__((always_inline)) {
     constexpr int k = decltype(k_c)::value, i = k / 2;
@@ -325,7 +328,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
     });
     keep_two(integral_constant<int, 15>{});
     // the first keys that a column sees, and where one or a factor grows
-    float all = part[0] * __builtin_amdgcn_exp2f(-offset[0] - ref) + part[1] * __builtin_amdgcn_exp2f(-offset[1] - ref);
+    float all = part[0] * __builtin_amdgcn_exp2f(-weight[0]) + part[1] * __builtin_amdgcn_exp2f(-weight[1]);
     if (__any(!begun || all > 32768.0f || grows)) {
 #pragma unroll
       for (int i = 0; i < G; ++i) o[i] *= down;
@@ -335,7 +338,6 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int e = 1; e < 16; ++e) most[b] = fmaxf(most[b], x[b][e]);
-      const float weight[2] = {offset[0] + ref, offset[1] + ref};
       float m = fmaxf(most[0] - weight[0], most[1] - weight[1]);
       m = fmaxf(m, __shfl_xor(m, 32, 64));
       const bool seen = m > -__builtin_inff();

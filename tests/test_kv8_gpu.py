@@ -319,6 +319,40 @@ def test_attention_of_flat_and_peaked_rows(B, peak, scale, prompt):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("size", [1e2, 1e4, 1e6, 1e9])
+@pytest.mark.parametrize("prompt", [False, True])
+def test_rows_that_see_one_key_alone(B, kind, size, prompt):
+    """Scores so far apart that all of a row's weight is on one key: its value, whatever the scores' own size."""
+    rng = _rng(19)
+    H, ratio, D, page = 16 if prompt else 2, 4, 64, 16
+    lengths, added = [700, 64, 333], [130, 64, 100] if prompt else [3, 2, 4]
+    table, pool = _table(rng, lengths, page)
+    cache = _filled(rng, pool, H, page, D)
+    starts = np.concatenate([[0], np.cumsum(added)]).astype(np.int32)
+    q = torch.from_numpy(rng.standard_normal((int(starts[-1]), H * ratio, D)).astype(np.float32)).to(TYPES[kind])
+    dev = [torch.from_numpy(x).cuda() for x in (cache, table, np.array(lengths, np.int32), starts)]
+    out = B.kv8_attend(q.cuda(), *dev, scale=size).double().cpu().numpy()
+    half, checked = (2.0 ** -8 if kind == "bf16" else 2.0 ** -11), 0
+    for b, n in enumerate(lengths):
+        keys, values = P.held(cache, table, b, n, page)
+        for t in range(starts[b], starts[b + 1]):
+            last = n - (starts[b + 1] - t) + 1
+            for h in range(0, H * ratio, 5):
+                x = q[t, h].double().numpy()
+                s = keys[:last, h // ratio] @ x * size
+                # (scores are off by 2^-20 of the sum of their terms' magnitudes at most)
+                noise = (np.abs(keys[:last, h // ratio]) @ np.abs(x)).max() * size * 2.0 ** -20
+                top = np.argmax(s)
+                if last > 1 and np.delete(s, top).max() > s[top] - 2 * noise - 40:
+                    continue
+                v = values[top, h // ratio]
+                # (the probability 2^-11, its product with the factor 2^-16 in the exponent, fp32 sums, the output's own rounding)
+                assert (np.abs(out[t, h] - v) <= np.abs(v) * (2.0 ** -11 + 2.0 ** -14 + half) + 2.0 ** -24).all(), (b, t, h)
+                checked += 1
+    assert checked > (100 if prompt else 3)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
 @pytest.mark.parametrize("prompt", [False, True])
 def test_rows_that_are_no_numbers_stay_by_themselves(B, kind, prompt):
     """Queries with infinities and NaN, zeros and the type's extremes, beside ordinary ones of the same tile."""
