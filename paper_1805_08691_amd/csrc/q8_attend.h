@@ -123,6 +123,27 @@ constexpr int kManyTiles = 128;        // times heads: a workgroup for every sec
 // least); a tile of more steps is cut into equal parts of no more.  Every workgroup works this out for itself from the
 // lengths, a tile to a thread.  Parts of cut tiles have a place in the workspace, no more than 2 kTarget of them (a cut
 // tile has more than `per` steps), and the cut tiles' heads, no more than kTarget, a counter.
+//
+// Parts of a tile are of equal numbers of steps, rounded up, but the last: that one has a step at least.  Where `most` keeps their
+// number down, as many such parts may be fewer (65 steps in at most 16 parts: 13 of five).
+__host__ __device__ constexpr unsigned parts_of(unsigned steps, unsigned per, unsigned most) {
+  unsigned n = steps == 0 ? 0 : (steps + per - 1) / per;
+  if (n > most) {
+    const unsigned each = (steps + most - 1) / most;
+    n = (steps + each - 1) / each;
+  }
+  return n;
+}
+constexpr bool no_part_is_empty(unsigned most) {
+  for (unsigned per = kShortest; per <= 2 * kShortest; ++per)
+    for (unsigned steps = 1; steps <= 512; ++steps) {
+      const unsigned n = parts_of(steps, per, most), each = (steps + n - 1) / n;
+      if (n > most || (n - 1) * each >= steps) return false;
+    }
+  return true;
+}
+static_assert(no_part_is_empty(kWideParts) && no_part_is_empty(kTarget), "the last part of a tile has a step at least");
+
 struct Part {
   int head, part, parts;
   int slot, rank;                      // of a cut tile: its first part's place and its number, in units of H
@@ -197,7 +218,7 @@ __device__ __forceinline__ bool find_part(const AttendParams& p, int id, char* s
   if (LEAST && p.tiles * p.H >= kManyTiles) least = LEAST;
   const unsigned per = (unsigned)max((total + kTarget - 1) / kTarget, least);
   // the sums before each tile: parts (kTarget + kMaxTiles at most); those of cut tiles (10 bits up); cut tiles (20 bits up)
-  const unsigned n = steps ? min((steps + per - 1) / per, (unsigned)MOST) : 0, own = n > 1 ? n | n << 10 | 1u << 20 : n;
+  const unsigned n = parts_of(steps, per, MOST), own = n > 1 ? n | n << 10 | 1u << 20 : n;
   unsigned v = scan64(own);
   if (lane == 63) sums[wave] = v;
   __syncthreads();
