@@ -676,9 +676,14 @@ int q8_kv8_read(const void *cache_dev, size_t n_pages, int page, const int64_t *
 
 /* q8_kv4_attend over the 8-bit cache, with its arguments and errors, and `causal`: 1, or 0 where every row of a request sees
  * all of its lengths[b] keys, as a decoder's rows see an encoder's states (window 0 then; Q8_EINVAL otherwise).  Workspaces
- * are its own (q8_kv8_attend_workspace_bytes), zeroed once.                               */
+ * are its own (q8_kv8_attend_workspace_bytes), zeroed once.
+ * q8_kv8_attend_call_form: what such a call runs as, for tables of `longest` (width * page) tokens, `ragged` saying whether it
+ * gives starts: in tiles of 16 or of 128 columns, plus 1 where it may split the keys; 0: of no size that there is.  (For tests
+ * and measurements; results are near each other within roundings.)                        */
 size_t q8_kv8_attend_workspace_bytes(size_t T, int n_requests, int n_heads, int ratio, int D,
                                      size_t longest);
+int q8_kv8_attend_call_form(size_t T, int n_requests, int n_heads, int ratio, int D, size_t longest,
+                            int ragged, size_t workspace_bytes);
 int q8_kv8_attend(const void *q_dev, int type, size_t T, int n_heads, int ratio, int D,
                   size_t q_stride, size_t q_head_stride, const void *cache_dev, size_t n_pages,
                   int page, const int32_t *table_dev, int width, size_t table_stride,

@@ -43,7 +43,8 @@ EXPORTS = [
     "q8_linear_variant_name", "q8_linear_int8_variant", "q8_linear_workspace_bytes",
     "q8_linear", "q8_page_tables", "q8_kv4_cache_bytes", "q8_kv4_write", "q8_kv4_read",
     "q8_kv4_attend_workspace_bytes", "q8_kv4_attend",
-    "q8_kv8_cache_bytes", "q8_kv8_write", "q8_kv8_read", "q8_kv8_attend_workspace_bytes", "q8_kv8_attend",
+    "q8_kv8_cache_bytes", "q8_kv8_write", "q8_kv8_read", "q8_kv8_attend_workspace_bytes",
+    "q8_kv8_attend_call_form", "q8_kv8_attend",
     "q8_page_workspace_bytes", "q8_page_select", "q8_page_compact", "q8_page_copy",
 ]
 
@@ -215,6 +216,7 @@ lib.q8_kv8_write.argtypes = lib.q8_kv4_write.argtypes
 lib.q8_kv8_read.argtypes = lib.q8_kv4_read.argtypes
 lib.q8_kv8_attend_workspace_bytes.restype = _sz
 lib.q8_kv8_attend_workspace_bytes.argtypes = lib.q8_kv4_attend_workspace_bytes.argtypes
+lib.q8_kv8_attend_call_form.argtypes = [_sz, _i, _i, _i, _i, _sz, _i, _sz]
 lib.q8_kv8_attend.argtypes = [_vp, _i, _sz, _i, _i, _i, _sz, _sz, _vp, _sz, _i, _vp, _i, _sz, _vp, _vp, _i, _f, _i, _i,
                               _vp, _sz, _sz, _vp, _sz, _vp]
 lib.q8_page_workspace_bytes.restype = _sz
@@ -812,6 +814,14 @@ def kv8_attend(q, cache, table, lengths, starts=None, scale=None, window=0, caus
     _check(_q8call.kv8_attend(q, cache, table, lengths, starts, q.shape[2] ** -0.5 if scale is None else scale, window,
                               int(causal), out, workspace))
     return out
+
+
+def kv8_attend_form(q, cache, table, starts=None, workspace=None):
+    """What ``kv8_attend`` runs as with these: (columns of a tile, whether keys may be split)."""
+    heads, D = cache.shape[1], (cache.shape[3] - 64) // 32
+    form = lib.q8_kv8_attend_call_form(q.shape[0], table.shape[0], heads, q.shape[1] // heads, D, table.shape[1] * cache.shape[2] * 16,
+                                       starts is not None, 0 if workspace is None else workspace.numel())
+    return form & ~1, bool(form & 1)
 
 
 def page_workspace(n_rows, n_pages, device="cuda"):

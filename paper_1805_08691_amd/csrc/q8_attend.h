@@ -545,8 +545,22 @@ inline size_t attend_workspace_bytes(size_t T, int n_requests, int n_heads, int 
   return rows ? split_bytes(D) : 0;
 }
 
+// What a call runs as: tiles of kWideCols or of kCols columns, how many there can be, and whether keys may be split.  least: find_part's
+// LEAST of the kernel for few columns.
+struct Form {
+  bool wide, split;
+  size_t tiles;
+};
+inline Form form_of(size_t T, int B, int H, int ratio, int D, size_t longest, bool starts, size_t workspace_bytes, WideFor* wide_for,
+                    int least) {
+  const size_t wide_tiles = tiles_of(T, B, ratio, true, kWideCols), narrow_tiles = tiles_of(T, B, ratio, starts);
+  const bool cuts = workspace_bytes >= split_bytes(D, kWideCols) && cut(wide_tiles, longest);
+  if (starts && wide_for(T, B, H, ratio, D, longest, cuts)) return {true, cuts, wide_tiles};
+  const bool whole = narrow_tiles * H >= (size_t)kManyTiles && longest <= (size_t)least * kStep;       // (none has two parts)
+  return {false, workspace_bytes >= split_bytes(D) && cut(narrow_tiles, longest) && !whole, narrow_tiles};
+}
+
 // A call's arguments, checked, as *p, and whether it goes to the kernel for many columns.  p->T = 0: there is nothing to do.
-// least: find_part's LEAST of the kernel for few.
 inline int attend_params(const void* q_dev, int type, size_t T, int n_heads, int ratio, int D, size_t q_stride,
                          size_t q_head_stride, const void* cache_dev, size_t n_pages, int page, const int32_t* table_dev, int width,
                          size_t table_stride, const int32_t* lengths_dev, const int32_t* starts_dev, int n_requests, float scale,
@@ -564,12 +578,10 @@ inline int attend_params(const void* q_dev, int type, size_t T, int n_heads, int
   Q8_REQUIRE(T <= 0x7fffffffu && n_pages <= 0x7fffffffu && (size_t)width * page <= 0x7fff0000u, Q8_EUNSUPPORTED);
   Q8_REQUIRE(q8_aligned(q_dev, 2) && q8_aligned(out_dev, 2) && q8_aligned(cache_dev, 64) && q8_aligned(table_dev, 4) &&
                  q8_aligned(lengths_dev, 4) && q8_aligned(starts_dev, 4) && q8_aligned(workspace, 16), Q8_EALIGN);
-  const size_t wide_tiles = tiles_of(T, n_requests, ratio, true, kWideCols), longest = (size_t)width * page;
-  const bool cuts = workspace && workspace_bytes >= split_bytes(D, kWideCols) && cut(wide_tiles, longest);
-  const bool wide = starts_dev && wide_for(T, n_requests, n_heads, ratio, D, longest, cuts);
-  const size_t tiles = wide ? wide_tiles : tiles_of(T, n_requests, ratio, starts_dev != nullptr);
-  const bool whole = tiles * n_heads >= (size_t)kManyTiles && longest <= (size_t)least * kStep;       // (none has two parts)
-  const bool split = wide ? cuts : workspace && workspace_bytes >= split_bytes(D) && cut(tiles, longest) && !whole;
+  const Form form = form_of(T, n_requests, n_heads, ratio, D, (size_t)width * page, starts_dev != nullptr,
+                            workspace ? workspace_bytes : 0, wide_for, least);
+  const bool split = form.split;
+  const size_t tiles = form.tiles, longest = (size_t)width * page;
   Q8_REQUIRE(tiles * n_heads + kTarget <= most_blocks(256) && T * ratio <= 0x7fffffffu, Q8_EUNSUPPORTED);
   AttendParams& p = *out;
   p.cache = static_cast<const uint8_t*>(cache_dev);
@@ -586,7 +598,7 @@ inline int attend_params(const void* q_dev, int type, size_t T, int n_heads, int
   p.tiles = (int)tiles;
   p.window = (size_t)window >= longest ? 0 : window;      // (as long as a request: none; differences of positions fit an int)
   p.scale_log2 = scale * 1.4426950408889634f;
-  *is_wide = wide;
+  *is_wide = form.wide;
   return Q8_OK;
 }
 

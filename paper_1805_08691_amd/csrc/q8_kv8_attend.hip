@@ -265,6 +265,13 @@ extern "C" size_t q8_kv8_attend_workspace_bytes(size_t T, int n_requests, int n_
   return attend_workspace_bytes(T, n_requests, n_heads, ratio, D, longest, wide_for);
 }
 
+extern "C" int q8_kv8_attend_call_form(size_t T, int n_requests, int n_heads, int ratio, int D, size_t longest, int ragged,
+                                       size_t workspace_bytes) {
+  if (n_requests < 1 || n_heads < 1 || ratio < 1 || T < 1 || T > 0x7fffffffu || D < 32 || D > kMaxHead || D % 32 != 0) return 0;
+  const Form form = form_of(T, n_requests, n_heads, ratio, D, longest, ragged != 0, workspace_bytes, wide_for, kLeast);
+  return (form.wide ? kWideCols : kCols) + form.split;
+}
+
 extern "C" int q8_kv8_attend(const void* q_dev, int type, size_t T, int n_heads, int ratio, int D, size_t q_stride,
                              size_t q_head_stride, const void* cache_dev, size_t n_pages, int page,
                              const int32_t* table_dev, int width, size_t table_stride, const int32_t* lengths_dev,
