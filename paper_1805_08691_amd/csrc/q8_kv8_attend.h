@@ -1,5 +1,5 @@
-// Shared by the kernels of attention over the paged 8-bit cache: the unpacking of codes, factors' powers, and the launch for
-// many columns.
+// Shared by the kernels of attention over the paged 8-bit cache: the unpacking of codes, factors' logarithms, and the launch
+// for many columns.
 #pragma once
 #include "q8_attend.h"
 #include "q8_kv8.h"
@@ -30,26 +30,8 @@ __device__ __forceinline__ constexpr int key_channel(int g, int j) {
   return g < G / 2 * 2 ? g / 2 * 64 + 16 * j + 8 * (g & 1) : 32 * g + 8 * j;
 }
 
-// A power of two above a factor (f < 2^e), and one of them as a number.
-__device__ __forceinline__ int power_above(float f) { return max((int)(__float_as_uint(f) >> 23) - 126, -100); }
-__device__ __forceinline__ float two_to(int e) { return __builtin_amdgcn_ldexpf(1.0f, e); }
-
-// What values' factors are divided by so that probabilities times them are binary16 numbers: a power of two above all of
-// them so far, which is left until one is 2^SPARE times as large.
-template <int SPARE>
-struct Power {
-  float limit = 0.0f;
-  int power = -100;
-  // With the four sixteens' factors of a step, a lane's own: what sums so far are multiplied by (a wavefront's one number).
-  __device__ __forceinline__ float grow(float fv) {
-    if (!__any(fv > limit)) return 1.0f;
-    const int grown = max(power_above(column_max(fv)), power);
-    const float down = limit > 0.0f ? two_to(power - grown) : 1.0f;
-    power = grown;
-    limit = two_to(min(power + SPARE, 127));
-    return down;
-  }
-};
+// The logarithm of a values' factor, and a number below all of them for 0.
+__device__ __forceinline__ float log2_of(float f) { return fmaxf(__builtin_log2f(f), -200.0f); }
 
 }  // namespace
 

@@ -8,8 +8,9 @@
 //   S^T[key][column]     = K Q^T      four tiles of 16 keys, G products each
 //   O^T[channel][column] = V^T P^T    2 G tiles of 16 channels, two products each
 // Codes are multiplied as they are: whole numbers up to 128 are binary16 numbers.  Lane (r, j) of S has 16 keys of sixteen j
-// and loads the values of the same 16: a score meets its sixteen's factor as one fp32 number of the lane, and a
-// probability, times the values' factor in fp32, is rounded to binary16 once (by 2^-11 of it at most).
+// and loads the values of the same 16: a score meets its sixteen's factor as one fp32 number of the lane.  A probability times the
+// values' factor is rounded to binary16 once, relative to the largest such product that the column itself has met (kLift below):
+// whatever other columns of the tile see has no effect.
 // The key axis is split over workgroups where columns are few; the last of them to finish adds the parts, in their order.
 //
 // Measured: 48 rows of 64 query heads on 8 of 128 channels over up to 16384 keys 151 us, 4.85 TB/s, which bounds it (without LDS
@@ -28,7 +29,13 @@ using namespace q8;
 // steps of a wavefront.  (us with no such limit, 16, 24 and 32 steps, 32 query heads on 8 of 128 channels, one row a request: 64 of
 // up to 2048 keys 35.6, 35.6, 33.6, 31.4; 16 of 4096 24.7, 22.0, 22.4, 20.7; 32 of 1000 15.7, 12.0, 12.0, 11.8.)
 [[maybe_unused]] constexpr int kLeast = 32;
-[[maybe_unused]] constexpr int kLift = 10;          // probabilities are up to 2^10 times what factors are below their power
+// Products of probabilities and values' factors are made relative to a column's largest so far so that this is 2^kLift, and again
+// where one is 2^kSlack times that: binary16 numbers, off by 2^-11 of themselves, or by 2^-35 of the largest.  The factor is part
+// of the exponent (its logarithm is added to the score), and taken out of the probabilities' sum again, in fp32, so that what an
+// exponent loses beside a large score is the score's error alone.  A factor that is 2^-kFar of what matters to the column or
+// less counts as that in its sums: its product is 0 in binary16, and its probability is still an fp32 number.
+[[maybe_unused]] constexpr float kLift = 10.0f, kSlack = 5.0f, kFar = 60.0f;
+[[maybe_unused]] constexpr float kNothing = -300.0f;          // the logarithm of no product so far
 
 template <int G, int WAVES, typename V>
 __global__ __launch_bounds__(64 * WAVES, G <= 4 ? 2 : 1) void kv8_attend_kernel(const AttendParams p, const V* __restrict__ q,
@@ -127,7 +134,7 @@ __global__ __launch_bounds__(64 * WAVES, G <= 4 ? 2 : 1) void kv8_attend_kernel(
 #pragma unroll
   for (int c = 0; c < CT; ++c) o[c] = f4{0, 0, 0, 0};
   float ref = -__builtin_inff(), sum = 0.0f;            // what sum and o are relative to, as a power of 2
-  Power<5> scaled;                                      // o is relative to 2^(its power - kLift)
+  float products = kNothing;                            // o is relative to 2^(ref + products - kLift)
 
   for (int it = 0; it < iterations; ++it) {
     const int key0 = t.lo + (step0 + wave + it * WAVES) * kStep;
@@ -162,12 +169,6 @@ __global__ __launch_bounds__(64 * WAVES, G <= 4 ? 2 : 1) void kv8_attend_kernel(
       // (a sixteen that no row sees: its factor may be anything)
       if (!(there >> j & 1u) || base + 15 < t.seen || base >= last) fv = 0.0f;
     }
-    const float down = scaled.grow(fv);
-    if (down != 1.0f) {
-#pragma unroll
-      for (int c = 0; c < CT; ++c) o[c] *= down;
-    }
-    const float weight = __builtin_amdgcn_ldexpf(fv, kLift - scaled.power);
     // ---- running maximum and sum
     float m = x[0][0];
 #pragma unroll
@@ -176,23 +177,31 @@ __global__ __launch_bounds__(64 * WAVES, G <= 4 ? 2 : 1) void kv8_attend_kernel(
       for (int i = 0; i < 4; ++i) m = fmaxf(m, x[tile][i]);
     const float top = fmaxf(ref, column_max(m));
     const float now = top == -__builtin_inff() ? 0.0f : top;
-    const float shrink = __builtin_amdgcn_exp2f(ref - now);
-    ref = top;
-    sum *= shrink;
+    const float kept = ref == -__builtin_inff() ? 0.0f : ref - now;
+    const float factor = log2_of(fv), before = products + kept;
+    const float most = column_max(m - now + factor);
+    products = most > before + kSlack ? most : fmaxf(before, kNothing);
+    const float shrink = __builtin_amdgcn_exp2f(before - products);
     if (__any(shrink != 1.0f)) {
 #pragma unroll
       for (int c = 0; c < CT; ++c) o[c] *= shrink;
     }
     // ---- O^T: a probability times its sixteen's factor is the right operand
+    const float raise = fmaxf(factor - products, -kFar) + kLift;
+    float beside = now - raise;
+    if (m - beside > kLift + kSlack + 0.5f) beside = m;    // (rounded beside a large score: no infinity)
+    float all = 0.0f;
     h8 pr[2];
 #pragma unroll
     for (int tile = 0; tile < 4; ++tile)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float e = __builtin_amdgcn_exp2f(x[tile][i] - now);
-        sum += e;
-        pr[tile >> 1][(tile & 1) * 4 + i] = (_Float16)(e * weight);
+        const float e = __builtin_amdgcn_exp2f(x[tile][i] - beside);
+        all += e;
+        pr[tile >> 1][(tile & 1) * 4 + i] = (_Float16)e;
       }
+    sum = sum * __builtin_amdgcn_exp2f(kept) + all * __builtin_amdgcn_exp2f(-raise);
+    ref = top;
     if (more) issue_keys(it + 1);
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
@@ -201,9 +210,9 @@ __global__ __launch_bounds__(64 * WAVES, G <= 4 ? 2 : 1) void kv8_attend_kernel(
     }
     if (more) issue_values();
   }
-  const float back = two_to(scaled.power - kLift);
+  const float back = __builtin_amdgcn_exp2f(0.5f * (products - kLift));      // (twice: the power itself may be no normal number)
 #pragma unroll
-  for (int c = 0; c < CT; ++c) o[c] *= back;
+  for (int c = 0; c < CT; ++c) o[c] = o[c] * back * back;
   join_columns<D, WAVES>(p, a, t, shared, out, o, ref, sum);
 #endif
 }

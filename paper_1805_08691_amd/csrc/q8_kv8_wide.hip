@@ -22,13 +22,14 @@ using namespace q8;
 
 typedef float f16v __attribute__((ext_vector_type(16)));
 
-// Probabilities are made relative to a maximum so that its own is 2^kTop, and again where their sum in a lane (32 of them)
-// passes 2^kMost; their products with the values' factor over a power of two, which is below 2^(4 + kLift), are binary16 numbers.
-// The factor is part of the exponent (its logarithm is added to the score), and taken out of their sums again, in fp32, so that
-// what an exponent loses beside a large score is the score's error alone.  A sixteen whose factor is 0, whose codes are 0, has
-// kLeastWeight instead.
-[[maybe_unused]] constexpr float kTop = 7.0f, kMost = 15.0f, kLeastWeight = 0x1p-40f;
-[[maybe_unused]] constexpr int kLift = -4;
+// Products of probabilities and values' factors are made relative to a column's largest so that this is 2^kTop, and again where
+// their sum over a lane's keys of a sixteen passes 2^kMost: binary16 numbers, off by 2^-11 of themselves, or by 2^-32 of the
+// largest.  Probabilities' sums have a reference of their own, made and left alike.  The factor is part of the exponent (its
+// logarithm is added to the score), and taken out of the probabilities' sums again, in fp32, so that what an exponent loses
+// beside a large score is the score's error alone.  A factor that is 2^-kFar of what matters to the column or less counts as that: its
+// product is as good as 0 in binary16, and its probability is still an fp32 number.  All of it is a column's own: what others of
+// the tile see has no effect.
+[[maybe_unused]] constexpr float kTop = 7.0f, kMost = 15.0f, kFar = 40.0f;
 constexpr int kRing = 128;                      // steps whose sixteens' places and factors are in LDS
 
 template <int G>
@@ -126,10 +127,10 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
     char* const to = shared + (s & 1) * W::OPERANDS + u * 2048 + k % 2 * 1024 + lane * 16;
     *reinterpret_cast<h8*>(to) = k % 2 ? codes.eight(kc[i].z, kc[i].w) : codes.eight(kc[i].x, kc[i].y);
   };
-  Power<4> scaled;
   float2 next[2];                                     // factors of a step's sixteens h and 2 + h
-  float ref = 0.0f;                                   // a column's, as a power of two
-  float weight[2], offset[2];                         // log2 of the values' factors over their power; the same less `ref`
+  float ref = 0.0f;                                   // of a column's products, as a power of two
+  float above = 0.0f;                                 // and how far it is above that of its probabilities' sum
+  float factor[2], weight[2], offset[2];              // log2 of the values' factors; what they count as; the same less `ref`
   auto find_factors = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) next[b] = factors[slot_of(s, 2 * b + h)];
@@ -137,7 +138,8 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
   auto weigh = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      weight[b] = __builtin_amdgcn_logf(fmaxf(__builtin_amdgcn_ldexpf(next[b].y, kLift - scaled.power), kLeastWeight));
+      factor[b] = log2_of(next[b].y);
+      weight[b] = fmaxf(factor[b], above - kFar);
       offset[b] = weight[b] - ref;
     }
   };
@@ -269,7 +271,10 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
       for (int e = 0; e < 16; ++e) x[b][e] = see >> e & 1u ? x[b][e] : -__builtin_inff();
     }
   };
-  float part[2];                                      // sums of a lane's probabilities of a sixteen, times its factor
+  float part[2];                                      // sums of a lane's products of a sixteen
+  auto probabilities = [&]() __attribute__((always_inline)) {          // what they are the sums of, without the factors
+    return part[0] * __builtin_amdgcn_exp2f(above - weight[0]) + part[1] * __builtin_amdgcn_exp2f(above - weight[1]);
+  };
   float raised[2];
   auto raise_two = [&](auto k_c) __attribute__((always_inline)) {
     constexpr int k = decltype(k_c)::value, b = k / 8, e = k % 8 * 2;
@@ -278,7 +283,9 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
   };
   auto keep_two = [&](auto k_c) __attribute__((always_inline)) {
     constexpr int k = decltype(k_c)::value, b = k / 8, e = k % 8 * 2;
-    const h2 two = {(_Float16)raised[0], (_Float16)raised[1]};
+    unsigned both = __builtin_bit_cast(unsigned, h2{(_Float16)raised[0], (_Float16)raised[1]});
+    asm volatile("" : "+v"(both));                    // (here, not behind the branch in which it may be made again)
+    const h2 two = __builtin_bit_cast(h2, both);
     part[b] += raised[0];
     part[b] += raised[1];
     pr[b][e >> 3][e & 7] = two[0], pr[b][e >> 3][(e & 7) + 1] = two[1];
@@ -296,7 +303,6 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
   lds_barrier();
   scores(0, nothing);
   find_factors(0);
-  float down = scaled.grow(fmaxf(next[0].y, next[1].y));        // what sums are multiplied by before the next values are added
   weigh();
   all_of(kHalves, [&](auto k_c) { unpack_key(1, k_c), unpack_value(0, k_c); });
   by[0] = next[0].x * rest, by[1] = next[1].x * rest;
@@ -311,7 +317,6 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
     if ((s & 63) == 0 && s > 0) find_sixteens((s + 64) * 4, 256);
     if ((s & 63) == 1) holes = __builtin_amdgcn_readfirstlane(*hole) != 0;
     part[0] = part[1] = 0.0f;
-    bool grows = false;
     scores(s + 1, [&](auto i_c) __attribute__((always_inline)) {
       constexpr int i = decltype(i_c)::value;
       share(i_c, kTwos, [&](auto k_c) __attribute__((always_inline)) {
@@ -323,37 +328,45 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
       if constexpr (i == kProducts / 2) {
         all_of(kPairs, [&](auto i_c) __attribute__((always_inline)) { find_pair(s + 2, decltype(i_c)::value); });
         by[0] = next[0].x * rest, by[1] = next[1].x * rest;
-        grows = down != 1.0f || fmaxf(next[0].y, next[1].y) > scaled.limit;
       }
     });
     keep_two(integral_constant<int, 15>{});
-    // the first keys that a column sees, and where one or a factor grows
-    float all = part[0] * __builtin_amdgcn_exp2f(-weight[0]) + part[1] * __builtin_amdgcn_exp2f(-weight[1]);
-    if (__any(!begun || all > 32768.0f || grows)) {
-#pragma unroll
-      for (int i = 0; i < G; ++i) o[i] *= down;
-      down = scaled.grow(fmaxf(next[0].y, next[1].y));
+    // the first keys that a column sees, and where products or probabilities grow
+    float all = probabilities();
+    bool again = !begun || fmaxf(all, fmaxf(part[0], part[1])) > 32768.0f;
+    if (__any(again)) {
+      again |= __shfl_xor((int)again, 32, 64) != 0;
       float most[2] = {x[0][0], x[1][0]};
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int e = 1; e < 16; ++e) most[b] = fmaxf(most[b], x[b][e]);
-      float m = fmaxf(most[0] - weight[0], most[1] - weight[1]);
-      m = fmaxf(m, __shfl_xor(m, 32, 64));
+      float top = fmaxf(most[0] + (factor[0] - weight[0]), most[1] + (factor[1] - weight[1]));
+      float m = fmaxf(most[0] + (above - weight[0]), most[1] + (above - weight[1]));
+      top = fmaxf(top, __shfl_xor(top, 32, 64)), m = fmaxf(m, __shfl_xor(m, 32, 64));
       const bool seen = m > -__builtin_inff();
-      // (32 probabilities whose sum is 2^15 have one of 2^10)
-      const float more = seen && (!begun || m > kMost - 5.0f) ? m - kTop : 0.0f, shrink = begun ? __builtin_amdgcn_exp2f(-more) : 1.0f;
-      ref += more;
+      // (a sum of 32 that is 2^15 has a term of 2^10)
+      again &= seen;
+      const float more = again && (!begun || top > kMost - 5.0f) ? top - kTop : 0.0f;
+      const float more_sum = again && (!begun || m > kMost - 5.0f) ? m - kTop : 0.0f;
+      const float shrink = begun ? __builtin_amdgcn_exp2f(-more) : 1.0f;
+      sum *= begun ? __builtin_amdgcn_exp2f(-more_sum) : 1.0f;
       begun |= seen;
-      sum *= shrink;
+      ref += more;
+      above += more - more_sum;
 #pragma unroll
       for (int i = 0; i < G; ++i) o[i] *= shrink;
 #pragma unroll
-      for (int b = 0; b < 2; ++b) x[b] -= more;
+      for (int b = 0; b < 2; ++b) {
+        const float was = weight[b];
+        weight[b] = fmaxf(factor[b], above - kFar);
+        x[b] += weight[b] - was - more;
+      }
       part[0] = part[1] = 0.0f;
       all_of(kTwos, [&](auto k_c) { raise_two(k_c), keep_two(k_c); });
-      all = part[0] * __builtin_amdgcn_exp2f(-weight[0]) + part[1] * __builtin_amdgcn_exp2f(-weight[1]);
+      all = probabilities();
     }
+    asm volatile("" : "+v"(above));                   // (what depends on it is not made twice: 128 channels would spill 50 registers)
     sum += all;
     add_values(s, [&](auto i_c) __attribute__((always_inline)) {
       if constexpr (decltype(i_c)::value == 0) weigh();
@@ -372,14 +385,13 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
     hide(s + 1);
     lds_barrier();
   }
-  // (a power that has grown for values behind the last step's)
-  const float back = two_to(scaled.power - kLift) * down;
+  const float back = __builtin_amdgcn_exp2f(0.5f * above);      // (twice: the power itself may be no normal number)
   f4 all[1][D / 8];
 #pragma unroll
   for (int i = 0; i < G; ++i)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) all[0][4 * i + (e >> 2)][e & 3] = o[i][e] * back;
-  const float refs[1] = {ref};
+    for (int e = 0; e < 16; ++e) all[0][4 * i + (e >> 2)][e & 3] = o[i][e] * back * back;
+  const float refs[1] = {ref - above};
   float sums[1] = {sum};
   const bool seen[1] = {begun};
   __syncthreads();

@@ -91,19 +91,23 @@ def _bound(out, size, noise, n, dtype):
     most, which moves weights by a factor of exp(2 d); the same for n products of values, 2^-23 each of the sum of magnitudes.  A
     probability times its sixteen's factor is rounded once (2^-11), or off by 2^-25 of 2^-7 of the row's largest such product where
     it is below binary16's normal numbers: with codes up to 128 and n keys, n 2^-25 of the largest sum of magnitudes of the row.
-    Logarithms of factors (below 2^6) are off by 2^-18, four such numbers are added; the exponential is off by 2^-22, the output's own
-    rounding by half a step of its type (fp16 below 2^-14: steps of 2^-24)."""
-    rel = np.expm1(2 * noise * 2.0 ** -20) + 2.0 ** -11 + n * 2.0 ** -23 + 2.0 ** -16 + 2.0 ** -21
+    Logarithms of factors (below 2^7) are off by 2^-17, four such numbers are added; the exponential is off by 2^-22, the output's own
+    rounding by half a step of its type (fp16 below 2^-14: steps of 2^-24; bf16 below 2^-126: of 2^-133)."""
+    rel = np.expm1(2 * noise * 2.0 ** -20) + 2.0 ** -11 + n * 2.0 ** -23 + 2.0 ** -15 + 2.0 ** -21
     half = 2.0 ** -8 if dtype is torch.bfloat16 else 2.0 ** -11
     few = n * 2.0 ** -25 * size.max(-1, keepdims=True)
-    return size * rel[..., None] + few + np.abs(out) * half + (2.0 ** -25 if dtype is torch.float16 else 0.0)
+    return size * rel[..., None] + few + np.abs(out) * half + (2.0 ** -25 if dtype is torch.float16 else 2.0 ** -134)
 
 
 def _check(B, rng, lengths, added, H, ratio, D, page, kind, scale=None, window=0, causal=True, workspace=True, peak=1.0, width=0,
-           holes=(), form=(128, False)):
-    """form: what the call has to run as (kv8_attend_form).  holes: (request, place, entry) of the table."""
+           holes=(), form=(128, False), factors=None):
+    """form: what the call has to run as (kv8_attend_form).  holes: (request, place, entry) of the table.  factors: what becomes of the
+    cache's, [pages, heads, sixteens, 2]."""
     table, pool = _table(rng, lengths, page, width)
     cache = _cache(rng, pool, H, page, D)
+    if factors is not None:
+        k, v, f = P.codes_of(cache, D)
+        P.put(cache, D, k, v, factors(f).astype(np.float32))
     for b, place, entry in holes:
         table[b, place] = entry if entry >= 0 else -1
     starts = np.concatenate([[0], np.cumsum(added)]).astype(np.int32)
@@ -208,16 +212,16 @@ def test_missing_pages_in_tiles_of_many_columns(B, window, causal, workspace):
                holes=[(0, 139, -1), (0, 60, -1)], form=(128, workspace))
 
 
-def _pieces(B, seed, kind, workspace=True, D=128, H=16, ratio=8, page=16, lengths=_PIECES[0], added=_PIECES[1]):
+def _pieces(B, seed, kind, workspace=True, D=128, H=16, ratio=8, page=16, lengths=_PIECES[0], added=_PIECES[1], columns=128):
     """What a call takes, on the device, and its cache and table on the host."""
     rng = _rng(seed)
-    table, pool = _table(rng, lengths, page)
+    table, pool = _table(rng, lengths, page, 2560 // page)
     cache = _cache(rng, pool, H, page, D)
     starts = np.concatenate([[0], np.cumsum(added)]).astype(np.int32)
     q = torch.from_numpy(rng.standard_normal((int(starts[-1]), H * ratio, D)).astype(np.float32)).to(TYPES[kind])
     dev = [torch.from_numpy(x).cuda() for x in (cache, table, np.array(lengths, np.int32), starts)]
-    ws = B.kv8_attend_workspace(q, dev[0], len(lengths), max(lengths)) if workspace else None
-    assert B.kv8_attend_form(q, dev[0], dev[1], dev[3], ws) == (128, workspace)
+    ws = B.kv8_attend_workspace(q, dev[0], len(lengths), table.shape[1] * page) if workspace else None
+    assert B.kv8_attend_form(q, dev[0], dev[1], dev[3], ws) == (columns, workspace)
     return q, dev, ws, cache, table, starts
 
 
@@ -286,3 +290,93 @@ def test_tiles_of_many_columns_are_the_same_every_time(B, workspace):
         torch.cuda.synchronize()
         assert torch.equal(out, first)
         assert torch.equal(B.kv8_attend(x, *dev, workspace=ws), first)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("workspace", [False, True])
+@pytest.mark.parametrize("columns,H", [(16, 2), (128, 16)])
+def test_rows_that_are_no_numbers(B, kind, workspace, columns, H):
+    """Queries with infinities and NaN, zeros and the type's smallest, beside ordinary ones of the same tile, whose outputs are bit for
+    bit the ones without them."""
+    q, dev, ws, *_ = _pieces(B, 12, kind, workspace, H=H, columns=columns)
+    T = len(q)
+    want = B.kv8_attend(q.cuda(), *dev, workspace=ws)
+    q[1, 1::8, 3], q[1, 2::8, 5], q[4, ::8, 127] = float("nan"), float("inf"), float("-inf")
+    q[T - 2, 3::8] = 0
+    q[T - 1, 1::8] = torch.finfo(q.dtype).tiny
+    out = B.kv8_attend(q.cuda(), *dev, workspace=ws)
+    fine = torch.isfinite(q).all(-1)
+    assert bool(torch.isfinite(out.cpu()[fine]).all()) and bool(torch.isnan(out.cpu()[~fine]).all())
+    same = fine.clone()
+    same[T - 2, 3::8] = same[T - 1, 1::8] = False
+    assert torch.equal(out.cpu()[same], want.cpu()[same])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("workspace", [False, True])
+@pytest.mark.parametrize("columns,H", [(16, 2), (128, 16)])
+@pytest.mark.parametrize("window", [0, 40])
+def test_hidden_keys_have_no_effect(B, kind, workspace, columns, H, window):
+    """Sixteens that a row sees nothing of, though others of its tile do: whatever they hold, and however large their factors, the
+    row's outputs are the same bits."""
+    q, dev, ws, cache, table, starts = _pieces(B, 20, kind, workspace, H=H, columns=columns)
+    lengths, added = _PIECES
+    args = [torch.from_numpy(x).cuda() for x in (table, np.array(lengths, np.int32), starts)]
+    want = B.kv8_attend(q.cuda(), dev[0], *args, window=window, workspace=ws)
+    for size in (2.0 ** -30, 2.0 ** 12, 2.0 ** 24, 2.0 ** 70):
+        other = cache.copy()
+        changed = []
+        for b, n in enumerate(lengths):
+            first = n - added[b]
+            sixteens = [first // 16 + 2, first // 16 + 3] if n > 200 else [first // 16 + 1]
+            for s in sixteens:
+                block = other[table[b, s], :, 0]
+                k, v, f = P.codes_of(block, 128)
+                P.put(block, 128, -k.clip(-127) if size > 1 else k, v[:, ::-1], f * np.array([min(size, 4.0), size], np.float32))
+            changed.append((min(sixteens) * 16, max(sixteens) * 16 + 15))
+        got = B.kv8_attend(q.cuda(), torch.from_numpy(other).cuda(), *args, window=window, workspace=ws)
+        for b, n in enumerate(lengths):
+            pos = np.arange(n - added[b], n)
+            apart = (pos < changed[b][0]) | ((pos - window + 1 > changed[b][1]) if window else False)
+            rows = starts[b] + np.flatnonzero(apart)
+            assert len(rows) >= 16 and torch.equal(got[rows], want[rows]), (size, b)
+            rows = starts[b] + np.flatnonzero(~apart)
+            assert not torch.equal(got[rows], want[rows])
+
+
+@pytest.mark.parametrize("spread", [3, 20, 60])
+@pytest.mark.parametrize("window", [0, 40])
+@pytest.mark.parametrize("columns,H,workspace", [(16, 2, False), (16, 2, True), (128, 16, False), (128, 16, True)])
+def test_rows_are_as_near_as_their_own_keys_allow(B, spread, window, columns, H, workspace):
+    """Values' factors that spread over many powers of two in one context, zeros among them, rising and falling."""
+    def factors(f):
+        f[..., 1] *= 2.0 ** rng.integers(-spread, spread, f[..., 1].shape)
+        f[..., 1][rng.random(f[..., 1].shape) < 0.2] = 0
+        f[..., 0][rng.random(f[..., 0].shape) < 0.1] = 0
+        return f
+
+    for peak in (1.0, 12.0):
+        rng = _rng(21, spread, window)
+        _check(B, rng, *_PIECES, H, 8, 128, 16, "bf16", window=window, workspace=workspace, peak=peak, factors=factors, width=160,
+               form=(columns, workspace))
+
+
+@pytest.mark.parametrize("size", [1e-36, 1e-30, 1e-9, 1e-3, 1e4, 1e9, 1e30])
+@pytest.mark.parametrize("columns,H", [(16, 2), (128, 16)])
+def test_factors_of_any_size(B, size, columns, H):
+    for workspace in (False, True):
+        _check(B, _rng(22), *_PIECES, H, 8, 128, 16, "bf16", workspace=workspace, factors=lambda f: f * np.array([1, size]), width=160,
+               form=(columns, workspace))
+
+
+@pytest.mark.parametrize("columns,H", [(16, 2), (128, 16)])
+def test_a_likely_key_of_small_values_beside_unlikely_ones_of_large(B, columns, H):
+    """Probabilities and factors whose products differ the other way round than they do themselves."""
+    for workspace in (False, True):
+        for exponent in (-40, -12, 12, 40):
+            def factors(f):
+                f[..., 1] *= np.exp2(np.clip(exponent * (f[..., 0] * 40 - 1), -60, 60))
+                f[..., 0] *= 8
+                return f
+            _check(B, _rng(23, exponent + 50), *_PIECES, H, 8, 128, 16, "bf16", workspace=workspace, factors=factors, width=160,
+                   form=(columns, workspace))
