@@ -206,17 +206,20 @@ __global__ __launch_bounds__(256) void select_free_kernel(const PagesParams p) {
     if (i >= taken) p.copies[2 * i] = -1, p.copies[2 * i + 1] = -1;
   if (blockIdx.x == 0 && tid == 0)
     p.counts[0] = n_free - taken, p.counts[1] = taken, p.counts[2] = n_needed - taken, p.counts[3] = p.pool - n_free + taken;
-  // ---- copies of rank first .. end - 1 are here, a row to a thread; the last block empties the rows behind the last free page
-  const bool empties = blockIdx.x == gridDim.x - 1 && n_needed > n_free;
+  // ---- copies of rank first .. end - 1 are here, a row to a thread; rows behind the last free page are emptied, each by a wavefront
+  // of one of the blocks
+  const bool empties = n_needed > n_free;
   if (first >= taken && !empties) return;
-  for (int i = 0; flags && i < row1 - row0; ++i) {
-    if (i < 64 ? !(which >> i & 1ul) : !p.flags[row0 + i]) continue;
-    if (rank >= first && rank < end && rank < taken) rows[rank - first] = row0 + i;
-    if (empties && rank >= n_free) {
-      for (int col = 0; col < p.width; ++col) p.out_table[(row0 + i) * p.out_stride + col] = -1;
-      p.out_lengths[row0 + i] = 0;
-    }
-    ++rank;
+  for (int i = 0; i < each && __any(flags != 0); ++i) {
+    const bool needs = flags && i < row1 - row0 && (i < 64 ? which >> i & 1ul : p.flags[row0 + i] != 0);
+    if (needs && rank >= first && rank < end && rank < taken) rows[rank - first] = row0 + i;
+    if (empties)
+      for (unsigned long none = __ballot(needs && rank >= n_free && (row0 + i) % gridDim.x == blockIdx.x); none; none &= none - 1) {
+        const int c = __builtin_amdgcn_readlane(row0, __builtin_ctzl(none)) + i;
+        for (int col = tid & 63; col < p.width; col += 64) p.out_table[c * p.out_stride + col] = -1;
+        if ((tid & 63) == 0) p.out_lengths[c] = 0;
+      }
+    rank += needs;
   }
   lds_barrier();
   for (int i = tid; i < min(end, taken) - first; i += 256) {
