@@ -231,8 +231,12 @@ __global__ __launch_bounds__(256) void select_free_kernel(const PagesParams p) {
 }
 
 // Both for tables of few places, in one launch of one block: a row to a thread, and kFewPlaces of the tables' places, of any
-// row, which it keeps in registers.  Bound by three dependent trips to memory and the barriers of the sums.
-constexpr int kFewRows = 1024, kFewPlaces = 16, kFewWords = 4096;
+// row, which it keeps in registers.  Bound by three dependent trips to memory and the barriers of the sums, and by what one block
+// writes where pages are many.  (us of select and of compact, 512 requests of 16 places, and 1025 of 15 in several launches: pools of
+// 1000 pages 9.2, 8.3 and 12.5, 13.5; 8000 10.0, 10.1 and 12.2, 13.1; 16000 11.2, 12.0 and 12.4, 13.4; 24000 12.4, 13.5 and 12.6,
+// 13.7; 32000 13.5, 15.3 and 12.3, 13.7; 131072 26.5, 34.8 and 12.4, 13.7.)
+constexpr int kFewRows = 1024, kFewPlaces = 16, kFewPages = 24 << 10;
+constexpr int kFewWords = 4096;                // of LDS: pages in use as bits, or parents
 struct Few {
   int parent[kFewRows];                        // select: of new row c; -1: none, or none that holds pages
   int held[kFewRows];                          // pages of new row c, or (again) minus them
@@ -241,9 +245,10 @@ struct Few {
   int list[kFewRows * kFewPlaces];             // select: free pages for copies; compact: where pages go, by rank
   unsigned sums[16];
 };
+static_assert(kFewPages <= kFewWords * 32, "a bit for every page");
 inline bool few(int rows, int parents, int width, size_t n_pages) {
   return rows <= kFewRows && parents <= kFewWords && (size_t)rows * width <= (size_t)kFewRows * kFewPlaces &&
-         n_pages <= (size_t)kFewWords * 32;
+         n_pages <= (size_t)kFewPages;
 }
 
 template <bool SELECT>

@@ -32,13 +32,15 @@ def _pool(rng, n, width, spare):
 
 
 @pytest.mark.parametrize("n,m,width,spare", [(50000, 70000, 7, 60000), (3000, 70000, 5, 20000), (3000, 30000, 40, 700), (9000, 17000, 3, 0),
-                                             (20, 66000, 4, 64), (70000, 300, 3, 100000)])
+                                             (20, 66000, 4, 64), (70000, 300, 3, 100000),
+                                             # the last sizes that one block takes, and the first that it does not
+                                             (512, 1024, 3, 23587), (512, 1024, 3, 23588), (100, 1000, 16, 130000)])
 def test_very_many_requests(B, n, m, width, spare):
     """More than 64 rows a thread, pages in hundreds of blocks, and requests of which most find no page for their copy."""
     rng = np.random.Generator(np.random.PCG64([1805, 8691, 90, n, m]))
     lengths, table, pool = _pool(rng, n, width, spare)
     parents = rng.integers(-1, n + 1, m)
-    parents[m // 2:m // 2 + 4000] = n // 3                       # (one of them very often)
+    parents[m // 2:m // 2 + min(4000, m // 4)] = n // 3                       # (one of them very often)
     rows = _dev(table)
     got = B.page_select(_dev(parents), _dev(lengths), rows, 16, pool)
     out, lens, free, copies, counts = P.select(parents.tolist(), lengths, table, 16, pool)
