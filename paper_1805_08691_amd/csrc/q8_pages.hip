@@ -210,16 +210,24 @@ __global__ __launch_bounds__(256) void select_free_kernel(const PagesParams p) {
   // of one of the blocks
   const bool empties = n_needed > n_free;
   if (first >= taken && !empties) return;
-  for (int i = 0; i < each && __any(flags != 0); ++i) {
-    const bool needs = flags && i < row1 - row0 && (i < 64 ? which >> i & 1ul : p.flags[row0 + i] != 0);
-    if (needs && rank >= first && rank < end && rank < taken) rows[rank - first] = row0 + i;
-    if (empties)
-      for (unsigned long none = __ballot(needs && rank >= n_free && (row0 + i) % gridDim.x == blockIdx.x); none; none &= none - 1) {
+  auto needs = [&](int i) { return i < 64 ? (which >> i & 1ul) != 0 : p.flags[row0 + i] != 0; };
+  if (!empties) {
+    for (int i = 0; flags && i < row1 - row0; ++i) {
+      if (!needs(i)) continue;
+      if (rank >= first && rank < end) rows[rank - first] = row0 + i;
+      ++rank;
+    }
+  } else {
+    for (int i = 0; i < each && __any(flags != 0); ++i) {
+      const bool one = flags && i < row1 - row0 && needs(i);
+      if (one && rank >= first && rank < min(end, n_free)) rows[rank - first] = row0 + i;
+      for (unsigned long none = __ballot(one && rank >= n_free && (row0 + i) % gridDim.x == blockIdx.x); none; none &= none - 1) {
         const int c = __builtin_amdgcn_readlane(row0, __builtin_ctzl(none)) + i;
         for (int col = tid & 63; col < p.width; col += 64) p.out_table[c * p.out_stride + col] = -1;
         if ((tid & 63) == 0) p.out_lengths[c] = 0;
       }
-    rank += needs;
+      rank += one;
+    }
   }
   lds_barrier();
   for (int i = tid; i < min(end, taken) - first; i += 256) {
