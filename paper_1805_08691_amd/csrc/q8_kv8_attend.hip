@@ -178,11 +178,12 @@ __global__ __launch_bounds__(64 * WAVES, G <= 4 ? 2 : 1) void kv8_attend_kernel(
     const float top = fmaxf(ref, column_max(m));
     const float now = top == -__builtin_inff() ? 0.0f : top;
     const float kept = ref == -__builtin_inff() ? 0.0f : ref - now;
-    const float factor = log2_of(fv), before = products + kept;
-    const float most = column_max(m - now + factor);
-    products = most > before + kSlack ? most : fmaxf(before, kNothing);
-    const float shrink = __builtin_amdgcn_exp2f(before - products);
-    if (__any(shrink != 1.0f)) {
+    const float factor = log2_of(fv), before = products + kept, own = m - now + factor;
+    products = fmaxf(before, kNothing);
+    if (__any(own > before + kSlack || before < kNothing)) {
+      const float most = column_max(own);
+      if (most > before + kSlack) products = most;
+      const float shrink = __builtin_amdgcn_exp2f(before - products);
 #pragma unroll
       for (int c = 0; c < CT; ++c) o[c] *= shrink;
     }
