@@ -676,7 +676,9 @@ int q8_kv8_read(const void *cache_dev, size_t n_pages, int page, const int64_t *
 
 /* q8_kv4_attend over the 8-bit cache, with its arguments and errors, and `causal`: 1, or 0 where every row of a request sees
  * all of its lengths[b] keys, as a decoder's rows see an encoder's states (window 0 then; Q8_EINVAL otherwise).  Workspaces
- * are its own (q8_kv8_attend_workspace_bytes), zeroed once.
+ * are its own (q8_kv8_attend_workspace_bytes), zeroed once.  Factors may be of any size (a values' factor below 2^-126 loses what
+ * fp32 loses): a probability times its sixteen's values' factor is rounded to binary16 relative to the largest such product of the
+ * row itself, by 2^-11 of itself or 2^-32 of that one, and what a row does not see has no effect on its bits.
  * q8_kv8_attend_call_form: what such a call runs as, for tables of `longest` (width * page) tokens, `ragged` saying whether it
  * gives starts: in tiles of 16 or of 128 columns, plus 1 where it may split the keys; 0: of no size that there is.  (For tests
  * and measurements; results are near each other within roundings.)                        */

@@ -110,11 +110,13 @@ __device__ __forceinline__ float column_max(float v) {
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// Parts that the keys are cut into where tiles are few: two for a compute unit.  (48 requests of up to 16384 tokens, 64 query
-// heads on 8 of 128 channels, 107 us; for 384 parts 125, 640 114, 768 115.  One of 131071, 32 heads on 8: 44, 51, 49, 47.)
+// Parts that the keys are cut into where tiles are few: two for a compute unit.  (Over the 4-bit cache, us: 48 requests of up to 16384
+// tokens, 64 query heads on 8 of 128 channels, 107; for 384 parts 125, 640 114, 768 115.  One of 131071, 32 heads on 8: 44, 51,
+// 49, 47.  Over the 8-bit one these take 151 and 58, at the memory's rate.)
 constexpr int kTarget = 512;
-// A part is not shorter than a step for each wavefront, and than two of them where that makes kTarget / 2 parts.  (One
-// request of 2000 tokens 11.6 us, never shorter than 8 or 16 steps 13.2 and 16.9; 8 of 4096, 64 channels, 14.0, with 4 14.8.)
+// A part is not shorter than a step for each wavefront, and than two of them where that makes kTarget / 2 parts.  (Over the 4-bit
+// cache: one request of 2000 tokens 11.6 us, never shorter than 8 or 16 steps 13.2 and 16.9; 8 of 4096, 64 channels, 14.0, with 4
+// 14.8.)
 constexpr int kShortest = 4;
 constexpr int kMaxTiles = 256;         // beyond them nothing is cut: a thread each
 constexpr int kManyTiles = 128;        // times heads: a workgroup for every second compute unit

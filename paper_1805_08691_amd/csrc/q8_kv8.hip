@@ -156,7 +156,8 @@ __device__ __forceinline__ void write_one(const Kv8Params& p, const V* k, const 
 // whose tokens in the call it is the first.  A thread has 8 channels of a token, twice beyond 128 channels (UNITS); the next
 // head's values are on their way meanwhile, and barriers wait for LDS only: value codes change places there, so that both the
 // token-major side and the cache's side are whole lines.  (16001 tokens, 8 heads of 128 channels: 29 us; bytes 20.  Bound by vector
-// instructions: five a value for its code and for being sure of it.)
+// instructions, 76 % of the cycles, 20 a value: five for its code and for being sure of it, the others for its type, the maximum, and
+// the way of a value's code through LDS by the byte, where half the cycles are conflicts between banks.)
 template <typename V, bool ALIGNED, bool INDEXED, int UNITS>
 __global__ __launch_bounds__(256, UNITS == 1 ? 5 : 3) void kv8_write_kernel(const Kv8Params p, const V* __restrict__ k, const V* __restrict__ v, int per) {
   constexpr int CHUNK = INDEXED ? 16 : 1;
@@ -329,7 +330,8 @@ __global__ __launch_bounds__(256, UNITS == 1 ? 5 : 3) void kv8_write_kernel(cons
 
 // A block takes 16 tokens of a head: key codes 8 a thread; value codes through LDS, a channel of a sixteen a thread where the
 // tokens are one's, and by the byte where not.  (16001 tokens, 8 heads of 128 channels, bf16: 19 us, 5.2 TB/s; all by the byte 24.5.
-// Bound by the memory's rate.)
+// Bound by the memory's rate; values' codes are read from LDS by the byte, more than half of its cycles
+// are conflicts.)
 template <typename V, bool ALIGNED>
 __global__ __launch_bounds__(256) void kv8_read_kernel(const Kv8Params p, V* __restrict__ k, V* __restrict__ v) {
   __shared__ long base[16];

@@ -14,10 +14,11 @@
 // The key axis is split over workgroups where columns are few; the last of them to finish adds the parts, in their order.
 //
 // Measured: 48 rows of 64 query heads on 8 of 128 channels over up to 16384 keys 151 us, 4.85 TB/s, which bounds it (without LDS
-// and with the next step's codes on their way, two wavefronts a SIMD are enough); one row over 131071 keys 58 us, of which six
-// are the split and the adding; 9 x 448 rows of 16 heads of 64 channels over up to 1500 keys 27.6 us, bound by vector
-// instructions (three quarters of the cycles), unpacking for 16 columns above all.  Tiles of two times 16 columns a wavefront
-// need more registers and were slower nearly everywhere (20 rows of 128 requests over 400 keys 23.4 and 27.0 us).
+// and with the next step's codes on their way, two wavefronts a SIMD are enough), in a window of 1024 23.3; one row over 131071
+// keys 58 us, of which six are the split and the adding, in a window of 4096 11.9; 9 x 448 rows of 16 heads of 64 channels over up
+// to 1500 keys 28.4 us, bound by vector instructions (three quarters of the cycles), unpacking for 16 columns above all.  Tiles of two
+// times 16 columns a wavefront need more registers and were slower nearly everywhere (20 rows of 128 requests over 400 keys 23.4
+// and 27.0 us).
 #include "q8_kv8_attend.h"
 #pragma clang fp contract(fast)
 
@@ -108,7 +109,9 @@ __global__ __launch_bounds__(64 * WAVES, G <= 4 ? 2 : 1) void kv8_attend_kernel(
     issue_values();
   }
 
-  // ---- its queries as the right operand, scaled to [1, 2) by a power of two and turned so that scores grow with the products
+  // ---- its queries as the right operand, scaled to [1, 2) by a power of two and turned so that scores grow with the products: binary16,
+  // so that the matrix instruction takes them.  fp16 and bf16 values down to 2^-14 and 2^-17 of their row's largest are exact,
+  // others off by 2^-25 of it at most.
   h8 qf[G];
   float scale;
   {

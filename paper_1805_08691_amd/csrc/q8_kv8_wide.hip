@@ -9,11 +9,12 @@
 // Lane (r, h) of S has 16 keys of sixteens h and 2 + h for column r, so that a factor is one number of a lane, and probabilities
 // are operands as they come.
 //
-// Measured: 2048 tokens of each of three requests over up to 8192 keys, 32 query heads on 4 of 128 channels, 353 us, 0.84 PFLOP/s;
-// matrix instructions in 40 %, vector instructions in 50 % of the cycles of two wavefronts a SIMD, at 1.83 GHz.  The order below,
-// exponentials between key products and unpacking between value products, took it from 383 to 354.  Eight wavefronts that share
-// keys, products of 16 x 16, and two groups that multiply in turn were no faster; 64 columns a wavefront, which halve what is read
-// from LDS, need 493 registers and lose it in moves between their halves (504).
+// Measured: 2048 tokens of each of three requests over up to 8192 keys, 32 query heads on 4 of 128 channels, 356 us, 0.83 PFLOP/s
+// (in a window of 1024 116); matrix instructions in 39 %, vector instructions in 53 % of the cycles, at 1.85 GHz, of 1.6 wavefronts a
+// SIMD where two have room: workgroups of whole tiles, of which there are barely two for each place, end at different times.  The order
+// below, exponentials between key products and unpacking between value products, took it from 383 to 354; a reference of each column
+// of its own costs 1 % of that.  Eight wavefronts that share keys, products of 16 x 16, and two groups that multiply in turn were no
+// faster; 64 columns a wavefront, which halve what is read from LDS, need 493 registers and lose it in moves between their halves (504).
 #include "q8_kv8_attend.h"
 
 namespace {
@@ -58,7 +59,7 @@ __global__ __launch_bounds__(256, G <= 4 ? 2 : 1) void kv8_wide_kernel(const Att
   const Codes codes;
   Part a;
   Tile t;
-  // (whole tiles: the last of a request see most keys, so they go first)
+  // (whole tiles: the last of a request see most keys, so they go before its others; requests are not ordered by their lengths)
   const int id = p.parts ? (int)blockIdx.x : (p.tiles - 1 - (int)blockIdx.x / p.H) * p.H + (int)blockIdx.x % p.H;
   if (!find_part<kWideCols, kWideParts, true>(p, id, shared, &a, &t)) return;
   const int head = a.head, start = t.lo + a.step0 * kStep, steps = a.step1 - a.step0;

@@ -4,8 +4,10 @@
 // Which pages are in use is one bit a page, set from the rows that are kept; every number that a page or a request gets is
 // its rank among bits or flags, in ascending order, so that results do not depend on which block came first.
 //
-// Measured (us): 32 requests of up to 63 pages 6.1 and the copies 2.4, 1000 requests 14.7; 4000 requests of up to 256 pages
-// 20, in five launches of which the rows take 6.4 and the free pages 7.5.  All of them wait for their few dependent trips to memory.
+// Measured (us): 32 requests of up to 63 pages 6.1 and the copies 2.4, 1000 of up to 16 14.5; 4000 requests of up to 256 pages
+// 19.4, in five launches of which the rows take 6.4 and the free pages 7.2.  All of them wait for their few dependent trips to memory.
+// Every block of the last launch reads all rows' flags and all blocks' counts, so that beyond some ten thousand rows it grows
+// with their product: 2^18 rows and 2^20 pages 290, 2^20 and 2^24 2200, 2^22 and 2^24 24500.
 #include "q8_kv4.h"
 #pragma clang fp contract(off)
 
@@ -487,7 +489,7 @@ struct Space {
 };
 
 // More new rows than this have their parents' first ones found by a launch of its own.  (us with and without it, tables of up to 256
-// places: 1200 rows 18.6 and 16.4, 2400 20.6 and 20.5, 4000 23.5 and 24.9.)
+// places: 1200 rows 18.4 and 17.9, 2000 18.6 and 18.7, 2400 21.0 and 20.8, 3000 21.2 and 21.7, 4000 21.2 and 24.4, 9000 30 and 44.)
 constexpr int kSearched = 2400;
 
 template <bool SELECT>
